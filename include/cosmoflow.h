@@ -511,6 +511,48 @@ cf_status cf_fc_head(int32_t m, int32_t nlayers, const int32_t *dims, int32_t dt
                      void *const *dz, void *const *dx, float *const *dw, float *const *db, float *loss, void *ws,
                      size_t ws_bytes, void *stream);
 
+/* ------------------------------------------------------------------------
+ * Layer normalisation.  The paper removes batch normalisation because every
+ * device holds a batch of one (Section III-A); normalising each row of values
+ * by its own statistics does not depend on the batch.  A row is c consecutive
+ * values: the channels of one NDHWC voxel (rows = n*d*h*w), or one sample's
+ * flattened activation (rows = n).
+ *   mean_r = sum_i x[r][i] / c
+ *   rstd_r = (sum_i (x[r][i] - mean_r)^2 / c + eps)^(-1/2)
+ *   y[r][i] = (x[r][i] - mean_r) * rstd_r * gamma[i] + beta[i]
+ * and, with g = dy * gamma and xh = (x - mean) * rstd,
+ *   dx[r][i] = rstd_r * (g[r][i] - sum_i g / c - xh[r][i] * sum_i (g xh) / c)
+ *   dgamma[i] = sum_r dy[r][i] xh[r][i],   dbeta[i] = sum_r dy[r][i].
+ * x, y, dy, dx are in dtype; gamma, beta, mean, rstd, dgamma, dbeta are fp32.
+ * Statistics and sums are fp32 (the variance from the distances to the mean,
+ * not from a difference of moments).  A NaN or an infinity stays in its row
+ * (and, backward, in its column's gradients) as the formulas have it.
+ * Sizes: rows >= 0, 1 <= c <= 2^30, rows * c < 2^40.  rows == 0 is a no-op of
+ * the forward pass; the backward pass writes dgamma = dbeta = 0.  eps finite
+ * and >= 0.  All pointers 16-byte aligned; y may be x and dx may be dy or x
+ * exactly (in place), otherwise outputs must not overlap inputs or each other
+ * (CF_ERR_ALIAS).  Deterministic: every sum has an order fixed by the sizes.
+ * ------------------------------------------------------------------------ */
+
+/* Bytes of device workspace cf_layernorm_fwd needs (0 for rows that fit a
+ * workgroup and for invalid sizes; ws may then be NULL). */
+size_t cf_layernorm_fwd_workspace_size(int64_t rows, int32_t c, int32_t dtype);
+
+/* y, and mean and rstd [rows], which the backward pass reads. */
+cf_status cf_layernorm_fwd(int64_t rows, int32_t c, int32_t dtype, const void *x, const float *gamma,
+                           const float *beta, float eps, void *y, float *mean, float *rstd, void *ws,
+                           size_t ws_bytes, void *stream);
+
+/* Bytes of device workspace cf_layernorm_bwd needs (partial sums of dgamma
+ * and dbeta; 0 for invalid sizes). */
+size_t cf_layernorm_bwd_workspace_size(int64_t rows, int32_t c, int32_t dtype);
+
+/* dx [rows][c], dgamma [c] and dbeta [c] (overwritten, not accumulated) from
+ * dy, the forward pass's input x and its mean and rstd. */
+cf_status cf_layernorm_bwd(int64_t rows, int32_t c, int32_t dtype, const void *dy, const void *x,
+                           const float *gamma, const float *mean, const float *rstd, void *dx, float *dgamma,
+                           float *dbeta, void *ws, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -42,6 +42,7 @@ EXPORTS = [
     "cf_conv3d_bwd_weight_noalloc", "cf_avgpool3d_lrelu_bwd_workspace_size", "cf_avgpool3d_lrelu_bwd",
     "cf_avgpool3d_lrelu_bwd_deferred", "cf_conv3d_bwd_fused", "cf_conv3d_bwd_fused_deferred",
     "cf_conv3d_bwd", "cf_conv3d_bwd_deferred",
+    "cf_layernorm_fwd_workspace_size", "cf_layernorm_fwd", "cf_layernorm_bwd_workspace_size", "cf_layernorm_bwd",
 ]
 
 
@@ -137,6 +138,10 @@ def lib():
         "cf_conv3d_bwd_weight_fused_deferred": ([D, vp, vp, vp, f32, ctypes.c_uint32, vp, vp, vp, vp, sz,
                                                  ctypes.POINTER(cf_reduction), ctypes.POINTER(i32), vp],
                                                 ctypes.c_int),
+        "cf_layernorm_fwd_workspace_size": ([i64, i32, i32], sz),
+        "cf_layernorm_fwd": ([i64, i32, i32, vp, vp, vp, f32, vp, vp, vp, vp, sz, vp], ctypes.c_int),
+        "cf_layernorm_bwd_workspace_size": ([i64, i32, i32], sz),
+        "cf_layernorm_bwd": ([i64, i32, i32] + [vp] * 9 + [sz, vp], ctypes.c_int),
         "cf_adam_larc_workspace_size": ([i32, ctypes.POINTER(i64)], sz),
         "cf_adam_larc_step": ([i32, ctypes.POINTER(i64), i64, ctypes.POINTER(cf_adam_larc_hparams), vp, vp, vp, vp,
                                vp, vp, sz, vp], ctypes.c_int),
@@ -478,3 +483,27 @@ def cf_fc_head(m, dims, dtype, x, w, b, alpha, target, y, dz, dx, dw, db, loss, 
 
 def cf_mse_loss(m, n, dtype, p, t, loss, dp, stream=None):
     _check(lib().cf_mse_loss(m, n, dtype_code(dtype), _ptr(p), _ptr(t), _ptr(loss), _ptr(dp), _stream(stream)))
+
+
+# ---- layer normalisation ---------------------------------------------------------
+
+def cf_layernorm_fwd_workspace_size(rows, c, dtype) -> int:
+    return int(lib().cf_layernorm_fwd_workspace_size(rows, c, dtype_code(dtype)))
+
+
+def cf_layernorm_fwd(rows, c, dtype, x, gamma, beta, eps, y, mean, rstd, ws=None, ws_bytes=None, stream=None):
+    if ws_bytes is None:
+        ws_bytes = 0 if ws is None or isinstance(ws, int) else ws.numel() * ws.element_size()
+    _check(lib().cf_layernorm_fwd(rows, c, dtype_code(dtype), _ptr(x), _ptr(gamma), _ptr(beta), float(eps), _ptr(y),
+                                  _ptr(mean), _ptr(rstd), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def cf_layernorm_bwd_workspace_size(rows, c, dtype) -> int:
+    return int(lib().cf_layernorm_bwd_workspace_size(rows, c, dtype_code(dtype)))
+
+
+def cf_layernorm_bwd(rows, c, dtype, dy, x, gamma, mean, rstd, dx, dgamma, dbeta, ws, ws_bytes=None, stream=None):
+    if ws_bytes is None:
+        ws_bytes = 0 if ws is None or isinstance(ws, int) else ws.numel() * ws.element_size()
+    _check(lib().cf_layernorm_bwd(rows, c, dtype_code(dtype), _ptr(dy), _ptr(x), _ptr(gamma), _ptr(mean), _ptr(rstd),
+                                  _ptr(dx), _ptr(dgamma), _ptr(dbeta), _ptr(ws), ws_bytes, _stream(stream)))

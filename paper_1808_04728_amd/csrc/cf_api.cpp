@@ -975,3 +975,101 @@ cf_status cf_mse_loss(int32_t m, int32_t n, int32_t dtype, const void *p, const 
   return finish(cf::launch_mse_loss(cnt, kdt(dtype), p, t, loss, dp, (float)(1.0 / (double)cnt), st), st,
                 "cf_mse_loss");
 }
+
+// ---- layer normalisation -------------------------------------------------------
+
+namespace {
+cf_status norm_check(int64_t rows, int32_t c, int32_t dtype, const char *who) {
+  if (rows < 0) return fail(CF_ERR_INVALID_ARG, std::string(who) + ": rows must be >= 0");
+  if (c <= 0) return fail(CF_ERR_INVALID_ARG, std::string(who) + ": c must be > 0");
+  if (c > (1 << 30)) return fail(CF_ERR_UNSUPPORTED, std::string(who) + ": more than 2^30 values a row");
+  if (rows >= (1LL << 40) / c) return fail(CF_ERR_UNSUPPORTED, std::string(who) + ": rows * c too large");
+  if (dtype != CF_F32 && dtype != CF_BF16) return fail(CF_ERR_INVALID_ARG, "unknown dtype");
+  return CF_OK;
+}
+
+typedef std::pair<const void *, size_t> Span;
+
+// an output may be one of `same` exactly; otherwise no output overlaps an input or another output
+cf_status norm_alias(std::initializer_list<Span> in, std::initializer_list<Span> out, const void *first_out,
+                     std::initializer_list<const void *> same, const char *who) {
+  for (const Span *o = out.begin(); o != out.end(); ++o) {
+    for (const Span &i : in) {
+      bool exact = false;
+      for (const void *p : same) exact = exact || (o->first == first_out && o->first == i.first && p == i.first);
+      if (!exact && overlap(o->first, o->second, i.first, i.second))
+        return fail(CF_ERR_ALIAS, std::string(who) + ": an output or the workspace overlaps an input");
+    }
+    for (const Span *q = o + 1; q != out.end(); ++q)
+      if (overlap(o->first, o->second, q->first, q->second))
+        return fail(CF_ERR_ALIAS, std::string(who) + ": two outputs overlap");
+  }
+  return CF_OK;
+}
+}  // namespace
+
+extern "C" {
+
+size_t cf_layernorm_fwd_workspace_size(int64_t rows, int32_t c, int32_t dtype) {
+  const std::string keep = g_last_error;
+  const bool bad = norm_check(rows, c, dtype, "layernorm") != CF_OK;
+  g_last_error = keep;
+  return bad || rows == 0 ? 0 : cf::layernorm_fwd_workspace(rows, c, kdt(dtype));
+}
+
+cf_status cf_layernorm_fwd(int64_t rows, int32_t c, int32_t dtype, const void *x, const float *gamma,
+                           const float *beta, float eps, void *y, float *mean, float *rstd, void *ws,
+                           size_t ws_bytes, void *stream) {
+  cf_status r = norm_check(rows, c, dtype, "layernorm_fwd");
+  if (r != CF_OK) return r;
+  if (!std::isfinite(eps) || eps < 0.f) return fail(CF_ERR_INVALID_ARG, "layernorm_fwd: eps must be finite and >= 0");
+  if (rows == 0) return ok();
+  if ((r = check_ptrs({x, gamma, beta, y, mean, rstd})) != CF_OK) return r;
+  const size_t need = cf::layernorm_fwd_workspace(rows, c, kdt(dtype));
+  if (need && (!ws || ws_bytes < need))
+    return fail(CF_ERR_WORKSPACE, "layernorm_fwd: workspace smaller than cf_layernorm_fwd_workspace_size()");
+  if (need && !aligned16(ws)) return fail(CF_ERR_ALIGNMENT, "workspace not 16-byte aligned");
+  const size_t nx = (size_t)rows * c * elem_size(dtype), nc = (size_t)c * 4, nr = (size_t)rows * 4;
+  if ((r = norm_alias({{x, nx}, {gamma, nc}, {beta, nc}}, {{y, nx}, {mean, nr}, {rstd, nr}, {ws, need}}, y, {x},
+                      "layernorm_fwd")) != CF_OK)
+    return r;
+  hipStream_t st = (hipStream_t)stream;
+  return finish(cf::launch_layernorm_fwd(rows, c, kdt(dtype), x, gamma, beta, eps, y, mean, rstd, ws, st), st,
+                "cf_layernorm_fwd");
+}
+
+size_t cf_layernorm_bwd_workspace_size(int64_t rows, int32_t c, int32_t dtype) {
+  const std::string keep = g_last_error;
+  const bool bad = norm_check(rows, c, dtype, "layernorm") != CF_OK;
+  g_last_error = keep;
+  return bad || rows == 0 ? 0 : cf::layernorm_bwd_workspace(rows, c, kdt(dtype));
+}
+
+cf_status cf_layernorm_bwd(int64_t rows, int32_t c, int32_t dtype, const void *dy, const void *x,
+                           const float *gamma, const float *mean, const float *rstd, void *dx, float *dgamma,
+                           float *dbeta, void *ws, size_t ws_bytes, void *stream) {
+  cf_status r = norm_check(rows, c, dtype, "layernorm_bwd");
+  if (r != CF_OK) return r;
+  hipStream_t st = (hipStream_t)stream;
+  const size_t nc = (size_t)c * 4;
+  if (rows == 0) {
+    if ((r = check_ptrs({dgamma, dbeta})) != CF_OK) return r;
+    if (overlap(dgamma, nc, dbeta, nc)) return fail(CF_ERR_ALIAS, "layernorm_bwd: two outputs overlap");
+    hipError_t e = cf::launch_fill_zero(dgamma, c, st);
+    if (e == hipSuccess) e = cf::launch_fill_zero(dbeta, c, st);
+    return finish(e, st, "cf_layernorm_bwd");
+  }
+  if ((r = check_ptrs({dy, x, gamma, mean, rstd, dx, dgamma, dbeta})) != CF_OK) return r;
+  const size_t need = cf::layernorm_bwd_workspace(rows, c, kdt(dtype));
+  if (!ws || ws_bytes < need)
+    return fail(CF_ERR_WORKSPACE, "layernorm_bwd: workspace smaller than cf_layernorm_bwd_workspace_size()");
+  if (!aligned16(ws)) return fail(CF_ERR_ALIGNMENT, "workspace not 16-byte aligned");
+  const size_t nx = (size_t)rows * c * elem_size(dtype), nr = (size_t)rows * 4;
+  if ((r = norm_alias({{dy, nx}, {x, nx}, {gamma, nc}, {mean, nr}, {rstd, nr}},
+                      {{dx, nx}, {dgamma, nc}, {dbeta, nc}, {ws, need}}, dx, {dy, x}, "layernorm_bwd")) != CF_OK)
+    return r;
+  return finish(cf::launch_layernorm_bwd(rows, c, kdt(dtype), dy, x, gamma, mean, rstd, dx, dgamma, dbeta, ws, st), st,
+                "cf_layernorm_bwd");
+}
+
+}  // extern "C"

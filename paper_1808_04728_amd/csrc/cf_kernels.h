@@ -237,6 +237,16 @@ int plan_opt_groups(int n, const long long *off, OptGroups *G);
 hipError_t launch_adam_larc(const OptGroups &G, int chunks, const OptHparams &hp, long long t, float *v,
                             const float *g, float *m, float *s, uint16_t *v16, double *part, hipStream_t st);
 
+// Layer normalisation (norm.hip) of `rows` rows of c values, c <= 2^30; the
+// workspaces hold chunk statistics and rows of partial column sums.
+size_t layernorm_fwd_workspace(long long rows, int c, int dtype);
+size_t layernorm_bwd_workspace(long long rows, int c, int dtype);
+hipError_t launch_layernorm_fwd(long long rows, int c, int dtype, const void *x, const float *gamma, const float *beta,
+                                float eps, void *y, float *mean, float *rstd, void *ws, hipStream_t st);
+hipError_t launch_layernorm_bwd(long long rows, int c, int dtype, const void *dy, const void *x, const float *gamma,
+                                const float *mean, const float *rstd, void *dx, float *dgamma, float *dbeta, void *ws,
+                                hipStream_t st);
+
 // Fully-connected layers (fc.hip): rows x[M][K], W[K][N], z[M][N].
 size_t fc_fwd_workspace(int M, int K, int N);
 hipError_t launch_fc_fwd(int M, int K, int N, int dtype, const void *x, const void *w, void *y, void *ws,

@@ -1,0 +1,785 @@
+// norm.hip -- layer normalisation of rows of c values, forward and backward.
+//
+//   mean = sum x / c,  rstd = (sum (x - mean)^2 / c + eps)^(-1/2)
+//   y = (x - mean) rstd gamma + beta
+//   g = dy gamma,  xh = (x - mean) rstd
+//   dx = rstd (g - sum(g) / c - xh sum(g xh) / c),  dgamma = sum_r dy xh,  dbeta = sum_r dy
+//
+// Both passes are bound by HBM (7 and 12 operations a value), so a value is
+// read once: a team of threads holds its row in registers (16-byte vectors as
+// they were loaded) between the sums over the row and the stores.  The variance
+// is the second pass over those registers, not a difference of moments.
+// Statistics, sums and the arithmetic are fp32 for both types; a bf16 output is
+// rounded once.
+//
+// A team is the smallest power of two of lanes that holds a row with one vector
+// each (64 / team rows a wave, so a row of 16 channels costs two lanes and one
+// exchange), then a wave with more vectors a lane, then a workgroup.  Rows that
+// no workgroup holds, and a few long rows that would leave most compute units
+// idle, are cut into chunks: a first launch leaves each chunk's statistics, the
+// second combines them in a fixed order and reads the chunk again.
+//
+// Rows whose length is no multiple of a vector start at any element: their
+// vectors are loaded and stored at the elements' own alignment, the last one
+// element by element, so nothing outside a row is touched.
+
+#include "cf_common.h"
+#include "cf_kernels.h"
+
+namespace cf {
+namespace {
+
+// 16 bytes at the alignment of one element
+typedef uint32_t u32x4f_t __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x4h_t __attribute__((ext_vector_type(4), aligned(2)));
+template <int DT> struct Loose;
+template <> struct Loose<DT_F32> { using V = u32x4f_t; };
+template <> struct Loose<DT_BF16> { using V = u32x4h_t; };
+
+// the product rounded on its own: with one value a row, g - sum(g) / c is exactly 0
+__device__ __forceinline__ float mul_rounded(float a, float b) {
+#pragma clang fp contract(off)
+  return a * b;
+}
+
+template <int DT> __device__ __forceinline__ void unpack(const u32x4_t &v, float (&f)[Store<DT>::VEC]) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const uint32_t w = v[q];
+    if constexpr (DT == DT_F32) {
+      f[q] = __uint_as_float(w);
+    } else {
+      f[2 * q] = __uint_as_float(w << 16);
+      f[2 * q + 1] = __uint_as_float(w & 0xffff0000u);
+    }
+  }
+}
+
+template <int DT> __device__ __forceinline__ u32x4_t pack(const float (&f)[Store<DT>::VEC]) {
+  if constexpr (DT == DT_F32) {
+    return u32x4_t{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+  } else {
+    return pack_bf16x8(f);
+  }
+}
+
+// vector at element e of a row of c values (zero past its end)
+template <int DT, bool RAG> __device__ __forceinline__ u32x4_t load_vec(const typename Store<DT>::T *row, int e, int c,
+                                                                        bool nt) {
+  constexpr int V = Store<DT>::VEC;
+  if constexpr (!RAG) {
+    if (e >= c) return u32x4_t{0u, 0u, 0u, 0u};
+    const u32x4_t *p = reinterpret_cast<const u32x4_t *>(row + e);
+    return nt ? __builtin_nontemporal_load(p) : *p;
+  } else {
+    if (e + V <= c) return *reinterpret_cast<const typename Loose<DT>::V *>(row + e);
+    u32x4_t v = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int i = 0; i < V - 1; ++i) {
+      if (e + i < c) {
+        if constexpr (DT == DT_F32) v[i] = __float_as_uint(row[e + i]);
+        else v[i >> 1] |= (uint32_t)row[e + i] << (16 * (i & 1));
+      }
+    }
+    return v;
+  }
+}
+
+template <int DT, bool RAG>
+__device__ __forceinline__ void store_vec(typename Store<DT>::T *row, int e, int c, const u32x4_t &v, bool nt) {
+  constexpr int V = Store<DT>::VEC;
+  if constexpr (!RAG) {
+    if (e >= c) return;
+    u32x4_t *p = reinterpret_cast<u32x4_t *>(row + e);
+    if (nt) __builtin_nontemporal_store(v, p);
+    else *p = v;
+  } else {
+    if (e + V <= c) {
+      *reinterpret_cast<typename Loose<DT>::V *>(row + e) = v;
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < V - 1; ++i) {
+      if (e + i < c) {
+        if constexpr (DT == DT_F32) row[e + i] = __uint_as_float(v[i]);
+        else row[e + i] = (uint16_t)(v[i >> 1] >> (16 * (i & 1)));
+      }
+    }
+  }
+}
+
+// V values of an fp32 vector (gamma, beta, gradients' partials) from element e on, zero past c
+template <int V, bool RAG> __device__ __forceinline__ void load_f32(const float *p, int e, int c, float (&f)[V]) {
+#pragma unroll
+  for (int q = 0; q < V; q += 4) {
+    if (e + q + 4 <= c) {
+      const float4 a = *reinterpret_cast<const float4 *>(p + e + q);
+      f[q] = a.x; f[q + 1] = a.y; f[q + 2] = a.z; f[q + 3] = a.w;
+    } else {
+#pragma unroll
+      for (int i = q; i < q + 4; ++i) f[i] = RAG && e + i < c ? p[e + i] : 0.f;
+    }
+  }
+}
+
+template <int V, bool RAG> __device__ __forceinline__ void store_f32(float *p, int e, int c, const float (&f)[V]) {
+#pragma unroll
+  for (int q = 0; q < V; q += 4) {
+    // (a row of partials starts on a vector only when c is a multiple of one)
+    if (!RAG && e + q + 4 <= c) {
+      *reinterpret_cast<float4 *>(p + e + q) = make_float4(f[q], f[q + 1], f[q + 2], f[q + 3]);
+    } else {
+#pragma unroll
+      for (int i = q; i < q + 4; ++i)
+        if (e + i < c) p[e + i] = f[i];
+    }
+  }
+}
+
+template <int T> __device__ __forceinline__ float team_sum(float s) {
+#pragma unroll
+  for (int o = T / 2; o >= 1; o >>= 1) s += __shfl_xor(s, o, 64);
+  return s;
+}
+
+// sum over a workgroup of W waves in wave order; `slot` alternates between two
+// halves of red so that one barrier a sum is enough
+template <int W> __device__ __forceinline__ float block_sum(float s, float *red, int slot) {
+  s = team_sum<64>(s);
+  if ((threadIdx.x & 63) == 0) red[slot * W + (threadIdx.x >> 6)] = s;
+  __syncthreads();
+  float t = red[slot * W];
+#pragma unroll
+  for (int w = 1; w < W; ++w) t += red[slot * W + w];
+  return t;
+}
+
+// ---- forward ------------------------------------------------------------------
+
+struct FwdArgs {
+  long long rows;
+  int c;
+  float eps, inv_c;
+  int nt;
+  const void *x;
+  const float *gamma, *beta;
+  void *y;
+  float *mean, *rstd;
+};
+
+// squared distance from the mean of a vector's values inside the row
+template <int DT, bool RAG>
+__device__ __forceinline__ float sq_dist(const u32x4_t &v, int e, int c, float mean) {
+  constexpr int V = Store<DT>::VEC;
+  float f[V], q = 0.f;
+  unpack<DT>(v, f);
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const float d = f[i] - mean;
+    q += (RAG ? e + i < c : e < c) ? d * d : 0.f;
+  }
+  return q;
+}
+
+template <int DT> __device__ __forceinline__ float vec_sum(const u32x4_t &v) {
+  constexpr int V = Store<DT>::VEC;
+  float f[V];
+  unpack<DT>(v, f);
+#pragma unroll
+  for (int w = V / 2; w >= 1; w >>= 1)
+#pragma unroll
+    for (int i = 0; i < w; ++i) f[i] += f[i + w];
+  return f[0];
+}
+
+template <int DT>
+__device__ __forceinline__ u32x4_t normalised(const u32x4_t &v, float mean, float rstd,
+                                              const float (&ga)[Store<DT>::VEC], const float (&be)[Store<DT>::VEC]) {
+  constexpr int V = Store<DT>::VEC;
+  float f[V];
+  unpack<DT>(v, f);
+#pragma unroll
+  for (int i = 0; i < V; ++i) f[i] = (f[i] - mean) * rstd * ga[i] + be[i];
+  return pack<DT>(f);
+}
+
+// teams of T lanes, NV vectors a lane, U rows a team (their loads all in flight)
+template <int DT, int T, int NV, int U, bool RAG>
+__global__ __launch_bounds__(256) void norm_fwd_wave(FwdArgs a) {
+  constexpr int V = Store<DT>::VEC;
+  using S = typename Store<DT>::T;
+  const int t = threadIdx.x % T;
+  const long long r0 = ((long long)blockIdx.x * (256 / T) + threadIdx.x / T) * U;
+  u32x4_t v[U][NV];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const S *row = (const S *)a.x + (r0 + u) * a.c;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      v[u][i] = r0 + u < a.rows ? load_vec<DT, RAG>(row, (t + T * i) * V, a.c, a.nt) : u32x4_t{0u, 0u, 0u, 0u};
+  }
+  float mean[U], rstd[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) s += vec_sum<DT>(v[u][i]);
+    mean[u] = team_sum<T>(s) * a.inv_c;
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    float q = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) q += sq_dist<DT, RAG>(v[u][i], (t + T * i) * V, a.c, mean[u]);
+    rstd[u] = 1.0f / sqrtf(team_sum<T>(q) * a.inv_c + a.eps);
+    if (t == 0 && r0 + u < a.rows) {
+      a.mean[r0 + u] = mean[u];
+      a.rstd[r0 + u] = rstd[u];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    float ga[V], be[V];
+    load_f32<V, RAG>(a.gamma, (t + T * i) * V, a.c, ga);
+    load_f32<V, RAG>(a.beta, (t + T * i) * V, a.c, be);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (r0 + u < a.rows)
+        store_vec<DT, RAG>((S *)a.y + (r0 + u) * a.c, (t + T * i) * V, a.c, normalised<DT>(v[u][i], mean[u], rstd[u], ga, be),
+                           a.nt);
+  }
+}
+
+// a workgroup a row
+template <int DT, int TH, int NV, bool RAG> __global__ __launch_bounds__(TH) void norm_fwd_block(FwdArgs a) {
+  constexpr int V = Store<DT>::VEC, W = TH / 64;
+  using S = typename Store<DT>::T;
+  __shared__ float red[2 * W];
+  const long long r = blockIdx.x;
+  const int t = threadIdx.x;
+  const S *row = (const S *)a.x + r * a.c;
+  u32x4_t v[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) v[i] = load_vec<DT, RAG>(row, (t + TH * i) * V, a.c, a.nt);
+  float s = 0.f, q = 0.f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) s += vec_sum<DT>(v[i]);
+  const float mean = block_sum<W>(s, red, 0) * a.inv_c;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) q += sq_dist<DT, RAG>(v[i], (t + TH * i) * V, a.c, mean);
+  const float rstd = 1.0f / sqrtf(block_sum<W>(q, red, 1) * a.inv_c + a.eps);
+  if (t == 0) {
+    a.mean[r] = mean;
+    a.rstd[r] = rstd;
+  }
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int e = (t + TH * i) * V;
+    if (e < a.c) {
+      float ga[V], be[V];
+      load_f32<V, RAG>(a.gamma, e, a.c, ga);
+      load_f32<V, RAG>(a.beta, e, a.c, be);
+      store_vec<DT, RAG>((S *)a.y + r * a.c, e, a.c, normalised<DT>(v[i], mean, rstd, ga, be), a.nt);
+    }
+  }
+}
+
+// rows in chunks: grid (chunk, row).  part[row][chunk] = (mean, sum of squares about it)
+template <int DT, int NV, bool RAG>
+__global__ __launch_bounds__(256) void norm_fwd_chunk_stats(FwdArgs a, int chunk, float2 *part) {
+  constexpr int V = Store<DT>::VEC;
+  using S = typename Store<DT>::T;
+  __shared__ float red[8];
+  const long long r = blockIdx.y + (long long)gridDim.y * blockIdx.z;
+  if (r >= a.rows) return;
+  const int beg = blockIdx.x * chunk, n = min(chunk, a.c - beg);
+  const S *row = (const S *)a.x + r * a.c + beg;
+  float mean = 0.f, m2 = 0.f;
+  int have = 0;
+  for (int o = 0; o < n; o += 256 * V * NV) {  // pieces that the registers hold, combined one after the other
+    const int k = min(n - o, 256 * V * NV);
+    u32x4_t v[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) v[i] = load_vec<DT, RAG>(row + o, ((int)threadIdx.x + 256 * i) * V, k, false);
+    float s = 0.f, q = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) s += vec_sum<DT>(v[i]);
+    const float pm = block_sum<4>(s, red, 0) / (float)k;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) q += sq_dist<DT, RAG>(v[i], ((int)threadIdx.x + 256 * i) * V, k, pm);
+    const float pq = block_sum<4>(q, red, 1);
+    const float d = pm - mean, w = (float)k / (float)(have + k);
+    m2 += pq + d * d * (float)have * w;
+    mean += d * w;
+    have += k;
+  }
+  if (threadIdx.x == 0) part[r * gridDim.x + blockIdx.x] = make_float2(mean, m2);
+}
+
+template <int DT, bool RAG>
+__global__ __launch_bounds__(256) void norm_fwd_chunk_apply(FwdArgs a, int chunk, const float2 *part) {
+  constexpr int V = Store<DT>::VEC;
+  using S = typename Store<DT>::T;
+  __shared__ float red[8];
+  const long long r = blockIdx.y + (long long)gridDim.y * blockIdx.z;
+  if (r >= a.rows) return;
+  const int beg = blockIdx.x * chunk, n = min(chunk, a.c - beg), nch = gridDim.x;
+  const float2 *pr = part + r * nch;
+  float s = 0.f, q = 0.f;
+  for (int i = threadIdx.x; i < nch; i += 256) s += pr[i].x * (float)min(chunk, a.c - i * chunk);
+  const float mean = block_sum<4>(s, red, 0) * a.inv_c;
+  for (int i = threadIdx.x; i < nch; i += 256) {
+    const float2 p = pr[i];
+    const float d = p.x - mean;
+    q += p.y + d * d * (float)min(chunk, a.c - i * chunk);
+  }
+  const float rstd = 1.0f / sqrtf(block_sum<4>(q, red, 1) * a.inv_c + a.eps);
+  if (beg == 0 && threadIdx.x == 0) {
+    a.mean[r] = mean;
+    a.rstd[r] = rstd;
+  }
+  const S *row = (const S *)a.x + r * a.c + beg;
+  S *out = (S *)a.y + r * a.c + beg;
+  for (int e = threadIdx.x * V; e < n; e += 256 * V) {
+    float ga[V], be[V];
+    const u32x4_t v = load_vec<DT, RAG>(row, e, n, a.nt);
+    load_f32<V, RAG>(a.gamma + beg, e, n, ga);
+    load_f32<V, RAG>(a.beta + beg, e, n, be);
+    store_vec<DT, RAG>(out, e, n, normalised<DT>(v, mean, rstd, ga, be), a.nt);
+  }
+}
+
+// ---- backward -----------------------------------------------------------------
+
+struct BwdArgs {
+  long long rows;
+  int c;
+  float inv_c;
+  int nt;
+  const void *dy, *x;
+  const float *gamma, *mean, *rstd;
+  void *dx;
+  float *pg, *pb;  // [workgroup][c] partial sums of dgamma and dbeta
+};
+
+// adds a vector's share of the two sums over the row and of dgamma, dbeta
+template <int DT>
+__device__ __forceinline__ void bwd_sums(const u32x4_t &xv, const u32x4_t &dv, float mean, float rstd,
+                                         const float (&ga)[Store<DT>::VEC], float &sg, float &sgx,
+                                         float (&dg)[Store<DT>::VEC], float (&db)[Store<DT>::VEC]) {
+  constexpr int V = Store<DT>::VEC;
+  float x[V], d[V];
+  unpack<DT>(xv, x);
+  unpack<DT>(dv, d);
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const float xh = (x[i] - mean) * rstd, g = mul_rounded(d[i], ga[i]);
+    sg += g;
+    sgx += g * xh;
+    dg[i] += d[i] * xh;
+    db[i] += d[i];
+  }
+}
+
+template <int DT>
+__device__ __forceinline__ u32x4_t bwd_dx(const u32x4_t &xv, const u32x4_t &dv, float mean, float rstd,
+                                          const float (&ga)[Store<DT>::VEC], float mg, float mgx) {
+  constexpr int V = Store<DT>::VEC;
+  float x[V], d[V];
+  unpack<DT>(xv, x);
+  unpack<DT>(dv, d);
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const float xh = (x[i] - mean) * rstd, g = mul_rounded(d[i], ga[i]);
+    x[i] = rstd * ((g - mg) - xh * mgx);
+  }
+  return pack<DT>(x);
+}
+
+// teams of T lanes; every team walks rows and keeps its columns' sums
+template <int DT, int T, int NV, int U, bool RAG>
+__global__ __launch_bounds__(256) void norm_bwd_wave(BwdArgs a) {
+  constexpr int V = Store<DT>::VEC;
+  using S = typename Store<DT>::T;
+  __shared__ float red[4][T * V];
+  const int t = threadIdx.x % T;
+  float ga[NV][V], dg[NV][V], db[NV][V];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    load_f32<V, RAG>(a.gamma, (t + T * i) * V, a.c, ga[i]);
+#pragma unroll
+    for (int j = 0; j < V; ++j) dg[i][j] = db[i][j] = 0.f;
+  }
+  constexpr int RB = 256 / T * U;  // rows a workgroup takes at a time
+  for (long long rb = (long long)blockIdx.x * RB; rb < a.rows; rb += (long long)gridDim.x * RB) {
+    u32x4_t xv[U][NV], dv[U][NV];
+    float mean[U], rstd[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const long long r = rb + u * (256 / T) + threadIdx.x / T;
+      const bool in = r < a.rows;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int e = (t + T * i) * V;
+        xv[u][i] = in ? load_vec<DT, RAG>((const S *)a.x + r * a.c, e, a.c, a.nt) : u32x4_t{0u, 0u, 0u, 0u};
+        dv[u][i] = in ? load_vec<DT, RAG>((const S *)a.dy + r * a.c, e, a.c, a.nt) : u32x4_t{0u, 0u, 0u, 0u};
+      }
+      mean[u] = in ? a.mean[r] : 0.f;
+      rstd[u] = in ? a.rstd[r] : 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const long long r = rb + u * (256 / T) + threadIdx.x / T;
+      float sg = 0.f, sgx = 0.f;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) bwd_sums<DT>(xv[u][i], dv[u][i], mean[u], rstd[u], ga[i], sg, sgx, dg[i], db[i]);
+      const float mg = team_sum<T>(sg) * a.inv_c, mgx = team_sum<T>(sgx) * a.inv_c;
+      if (r < a.rows) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+          store_vec<DT, RAG>((S *)a.dx + r * a.c, (t + T * i) * V, a.c,
+                             bwd_dx<DT>(xv[u][i], dv[u][i], mean[u], rstd[u], ga[i], mg, mgx), a.nt);
+      }
+    }
+  }
+  // the workgroup's teams: those of a wave by exchanges, the four waves in order
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      float *s = k ? db[i] : dg[i];
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        float z = s[j];
+#pragma unroll
+        for (int o = T; o < 64; o <<= 1) z += __shfl_xor(z, o, 64);
+        if (lane < T) red[wave][lane * V + j] = z;
+      }
+      __syncthreads();
+      for (int j = threadIdx.x; j < T * V; j += 256) {
+        const int col = i * T * V + j;
+        if (col < a.c)
+          (k ? a.pb : a.pg)[(long long)blockIdx.x * a.c + col] = (red[0][j] + red[1][j]) + (red[2][j] + red[3][j]);
+      }
+      __syncthreads();
+    }
+  }
+}
+
+// a workgroup a row at a time
+template <int DT, int TH, int NV, bool RAG> __global__ __launch_bounds__(TH) void norm_bwd_block(BwdArgs a) {
+  constexpr int V = Store<DT>::VEC, W = TH / 64;
+  using S = typename Store<DT>::T;
+  __shared__ float red[4 * W];
+  const int t = threadIdx.x;
+  float ga[NV][V], dg[NV][V], db[NV][V];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    load_f32<V, RAG>(a.gamma, (t + TH * i) * V, a.c, ga[i]);
+#pragma unroll
+    for (int j = 0; j < V; ++j) dg[i][j] = db[i][j] = 0.f;
+  }
+  int half = 0;
+  for (long long r = blockIdx.x; r < a.rows; r += gridDim.x, half ^= 1) {
+    u32x4_t xv[NV], dv[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      xv[i] = load_vec<DT, RAG>((const S *)a.x + r * a.c, (t + TH * i) * V, a.c, a.nt);
+      dv[i] = load_vec<DT, RAG>((const S *)a.dy + r * a.c, (t + TH * i) * V, a.c, a.nt);
+    }
+    const float mean = a.mean[r], rstd = a.rstd[r];
+    float sg = 0.f, sgx = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) bwd_sums<DT>(xv[i], dv[i], mean, rstd, ga[i], sg, sgx, dg[i], db[i]);
+    sg = team_sum<64>(sg);
+    sgx = team_sum<64>(sgx);
+    // the halves of red alternate: one barrier a row
+    if ((t & 63) == 0) {
+      red[half * 2 * W + (t >> 6)] = sg;
+      red[half * 2 * W + W + (t >> 6)] = sgx;
+    }
+    __syncthreads();
+    float mg = 0.f, mgx = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      mg += red[half * 2 * W + w];
+      mgx += red[half * 2 * W + W + w];
+    }
+    mg *= a.inv_c;
+    mgx *= a.inv_c;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      store_vec<DT, RAG>((S *)a.dx + r * a.c, (t + TH * i) * V, a.c, bwd_dx<DT>(xv[i], dv[i], mean, rstd, ga[i], mg, mgx),
+                         a.nt);
+  }
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int e = (t + TH * i) * V;
+    if (e < a.c) {
+      store_f32<V, RAG>(a.pg + (long long)blockIdx.x * a.c, e, a.c, dg[i]);
+      store_f32<V, RAG>(a.pb + (long long)blockIdx.x * a.c, e, a.c, db[i]);
+    }
+  }
+}
+
+// rows in chunks: part[row][chunk] = (sum g, sum g xh)
+template <int DT, bool RAG>
+__global__ __launch_bounds__(256) void norm_bwd_chunk_sums(BwdArgs a, int chunk, float2 *part) {
+  constexpr int V = Store<DT>::VEC;
+  using S = typename Store<DT>::T;
+  __shared__ float red[8];
+  const long long r = blockIdx.y + (long long)gridDim.y * blockIdx.z;
+  if (r >= a.rows) return;
+  const int beg = blockIdx.x * chunk, n = min(chunk, a.c - beg);
+  const S *x = (const S *)a.x + r * a.c + beg, *dy = (const S *)a.dy + r * a.c + beg;
+  const float mean = a.mean[r], rstd = a.rstd[r];
+  float sg = 0.f, sgx = 0.f, unused0[V] = {}, unused1[V] = {};
+  for (int e = threadIdx.x * V; e < n; e += 256 * V) {
+    float ga[V];
+    const u32x4_t xv = load_vec<DT, RAG>(x, e, n, false), dv = load_vec<DT, RAG>(dy, e, n, false);
+    load_f32<V, RAG>(a.gamma + beg, e, n, ga);
+    bwd_sums<DT>(xv, dv, mean, rstd, ga, sg, sgx, unused0, unused1);
+  }
+  sg = block_sum<4>(sg, red, 0);
+  sgx = block_sum<4>(sgx, red, 1);
+  if (threadIdx.x == 0) part[r * gridDim.x + blockIdx.x] = make_float2(sg, sgx);
+}
+
+// one vector column a thread over a block of `per` rows: dx, and the block's share of
+// dgamma and dbeta.  grid (256-vector column strip, row block); nch chunks a row in part
+constexpr int kColRows = 16;  // rows whose sums are combined at a time
+template <int DT, bool RAG>
+__global__ __launch_bounds__(256) void norm_bwd_columns(BwdArgs a, int per, int nch, const float2 *part) {
+  constexpr int V = Store<DT>::VEC;
+  using S = typename Store<DT>::T;
+  __shared__ float2 rs[kColRows];
+  const long long e = ((long long)blockIdx.x * 256 + threadIdx.x) * V;
+  float ga[V] = {}, dg[V] = {}, db[V] = {};
+  if (e < a.c) load_f32<V, RAG>(a.gamma, (int)e, a.c, ga);
+  const long long rend = min(((long long)blockIdx.y + 1) * per, a.rows);
+  for (long long r0 = (long long)blockIdx.y * per; r0 < rend; r0 += kColRows) {
+    const int nr = (int)min((long long)kColRows, rend - r0);
+    for (int i = threadIdx.x >> 6; i < nr; i += 4) {  // a wave a row
+      float sg = 0.f, sgx = 0.f;
+      for (int k = threadIdx.x & 63; k < nch; k += 64) {
+        const float2 p = part[(r0 + i) * nch + k];
+        sg += p.x;
+        sgx += p.y;
+      }
+      sg = team_sum<64>(sg);
+      sgx = team_sum<64>(sgx);
+      if ((threadIdx.x & 63) == 0) rs[i] = make_float2(sg * a.inv_c, sgx * a.inv_c);
+    }
+    __syncthreads();
+    if (e < a.c) {
+      for (int i = 0; i < nr; ++i) {
+        const long long at = (r0 + i) * a.c;
+        const u32x4_t xv = load_vec<DT, RAG>((const S *)a.x + at, (int)e, a.c, a.nt);
+        const u32x4_t dv = load_vec<DT, RAG>((const S *)a.dy + at, (int)e, a.c, a.nt);
+        const float mean = a.mean[r0 + i], rstd = a.rstd[r0 + i];
+        float s0 = 0.f, s1 = 0.f;
+        bwd_sums<DT>(xv, dv, mean, rstd, ga, s0, s1, dg, db);
+        store_vec<DT, RAG>((S *)a.dx + at, (int)e, a.c, bwd_dx<DT>(xv, dv, mean, rstd, ga, rs[i].x, rs[i].y), a.nt);
+      }
+    }
+    __syncthreads();
+  }
+  if (e < a.c) {
+    store_f32<V, RAG>(a.pg + (long long)blockIdx.y * a.c, (int)e, a.c, dg);
+    store_f32<V, RAG>(a.pb + (long long)blockIdx.y * a.c, (int)e, a.c, db);
+  }
+}
+
+// ---- plans --------------------------------------------------------------------
+
+int vec_of(int dtype) { return dtype == DT_BF16 ? Store<DT_BF16>::VEC : Store<DT_F32>::VEC; }
+
+// elements of a chunk (a multiple of the 256 vectors of one load round) and chunks
+// a row, for rows cut over workgroups: about four workgroups a compute unit and
+// at most 1024 chunks
+void plan_chunks(long long rows, int c, int V, int *chunk, int *nch) {
+  const long long unit = 256LL * V, units = (c + unit - 1) / unit;
+  const long long want = (4LL * kNumCUs + rows - 1) / rows;
+  long long per = (units + want - 1) / want;
+  while ((units + per - 1) / per > 1024) ++per;
+  *chunk = (int)(per * unit < (1LL << 31) - unit ? per * unit : c);
+  *nch = (int)((c + (long long)*chunk - 1) / *chunk);
+}
+
+// whether the forward pass cuts rows into chunks: always past what a workgroup of
+// 1024 threads holds in registers
+bool fwd_chunked(long long rows, int c, int dtype) { return c > 1024 * 16 * vec_of(dtype); }
+
+// backward: past 1024 threads' registers
+bool bwd_chunked(long long rows, int c, int dtype) { return c > 16384; }
+
+// rows of a block of the column pass: a multiple of kColRows that leaves about four
+// workgroups a compute unit
+int column_rows(long long rows, int c, int V) {
+  const long long strips = (c + 256LL * V - 1) / (256LL * V), want = (4LL * kNumCUs + strips - 1) / strips;
+  const long long per = (rows + want - 1) / want;
+  return (int)((per + kColRows - 1) / kColRows * kColRows);
+}
+
+// workgroups of the backward pass that keep column sums (rows of partials)
+int bwd_groups(long long rows, int c, int dtype) {
+  const int V = vec_of(dtype);
+  const long long nv = ((long long)c + V - 1) / V;
+  if (bwd_chunked(rows, c, dtype)) {
+    const int per = column_rows(rows, c, V);
+    return (int)((rows + per - 1) / per);
+  }
+  long long per, cap;
+  if (nv <= 64) {
+    int T = 1;
+    while (T < nv) T *= 2;
+    per = 256 / T * 2;
+    cap = 8 * kNumCUs;
+  } else if (c <= 1024) {
+    per = 4;
+    cap = 4 * kNumCUs;
+  } else {
+    per = 1;
+    cap = (c <= 4096 ? 4 : 1) * kNumCUs;
+  }
+  const long long need = (rows + per - 1) / per;
+  return (int)(need < cap ? need : cap);
+}
+
+template <int DT, bool RAG> hipError_t fwd(const FwdArgs &a, void *ws, hipStream_t st) {
+  constexpr int V = Store<DT>::VEC;
+  const long long nv = ((long long)a.c + V - 1) / V;
+#define CF_FWD_WAVE(T, NV, U)                                                                                       \
+  {                                                                                                                 \
+    const long long per = 256 / (T) * (U);                                                                          \
+    hipLaunchKernelGGL((norm_fwd_wave<DT, T, NV, U, RAG>), dim3((unsigned)((a.rows + per - 1) / per)), dim3(256), 0, \
+                       st, a);                                                                                      \
+    return hipGetLastError();                                                                                       \
+  }
+  if (nv <= 1) CF_FWD_WAVE(1, 1, 4)
+  if (nv <= 2) CF_FWD_WAVE(2, 1, 4)
+  if (nv <= 4) CF_FWD_WAVE(4, 1, 4)
+  if (nv <= 8) CF_FWD_WAVE(8, 1, 4)
+  if (nv <= 16) CF_FWD_WAVE(16, 1, 4)
+  if (nv <= 32) CF_FWD_WAVE(32, 1, 4)
+  if (nv <= 64) CF_FWD_WAVE(64, 1, 4)
+  if (nv <= 128) CF_FWD_WAVE(64, 2, 2)
+  if (nv <= 256) CF_FWD_WAVE(64, 4, 1)
+  if (nv <= 512) CF_FWD_WAVE(64, 8, 1)
+#undef CF_FWD_WAVE
+  if (!fwd_chunked(a.rows, a.c, DT)) {
+#define CF_FWD_BLOCK(TH, NV)                                                                                    \
+  {                                                                                                             \
+    hipLaunchKernelGGL((norm_fwd_block<DT, TH, NV, RAG>), dim3((unsigned)a.rows), dim3(TH), 0, st, a);          \
+    return hipGetLastError();                                                                                   \
+  }
+    if (nv <= 1024) CF_FWD_BLOCK(256, 4)
+    if (nv <= 2048) CF_FWD_BLOCK(256, 8)
+    if (nv <= 4096) CF_FWD_BLOCK(1024, 4)
+    if (nv <= 8192) CF_FWD_BLOCK(1024, 8)
+    CF_FWD_BLOCK(1024, 16)
+#undef CF_FWD_BLOCK
+  }
+  int chunk, nch;
+  plan_chunks(a.rows, a.c, V, &chunk, &nch);
+  const unsigned gy = (unsigned)(a.rows < 32768 ? a.rows : 32768), gz = (unsigned)((a.rows + gy - 1) / gy);
+  hipLaunchKernelGGL((norm_fwd_chunk_stats<DT, 4, RAG>), dim3(nch, gy, gz), dim3(256), 0, st, a, chunk, (float2 *)ws);
+  hipLaunchKernelGGL((norm_fwd_chunk_apply<DT, RAG>), dim3(nch, gy, gz), dim3(256), 0, st, a, chunk,
+                     (const float2 *)ws);
+  return hipGetLastError();
+}
+
+template <int DT, bool RAG> hipError_t bwd(const BwdArgs &a, int groups, void *rowpart, hipStream_t st) {
+  constexpr int V = Store<DT>::VEC;
+  const long long nv = ((long long)a.c + V - 1) / V;
+  if (bwd_chunked(a.rows, a.c, DT)) {
+    int chunk, nch;
+    plan_chunks(a.rows, a.c, V, &chunk, &nch);
+    const unsigned gy = (unsigned)(a.rows < 32768 ? a.rows : 32768), gz = (unsigned)((a.rows + gy - 1) / gy);
+    hipLaunchKernelGGL((norm_bwd_chunk_sums<DT, RAG>), dim3(nch, gy, gz), dim3(256), 0, st, a, chunk, (float2 *)rowpart);
+    hipLaunchKernelGGL((norm_bwd_columns<DT, RAG>), dim3((unsigned)((nv + 255) / 256), groups), dim3(256), 0, st, a,
+                       column_rows(a.rows, a.c, V), nch, (const float2 *)rowpart);
+    return hipGetLastError();
+  }
+#define CF_BWD_WAVE(T, NV, U)                                                                        \
+  {                                                                                                  \
+    hipLaunchKernelGGL((norm_bwd_wave<DT, T, NV, U, RAG>), dim3(groups), dim3(256), 0, st, a);       \
+    return hipGetLastError();                                                                        \
+  }
+#define CF_BWD_BLOCK(TH, NV)                                                                         \
+  {                                                                                                  \
+    hipLaunchKernelGGL((norm_bwd_block<DT, TH, NV, RAG>), dim3(groups), dim3(TH), 0, st, a);         \
+    return hipGetLastError();                                                                        \
+  }
+  if (nv <= 1) CF_BWD_WAVE(1, 1, 2)
+  if (nv <= 2) CF_BWD_WAVE(2, 1, 2)
+  if (nv <= 4) CF_BWD_WAVE(4, 1, 2)
+  if (nv <= 8) CF_BWD_WAVE(8, 1, 2)
+  if (nv <= 16) CF_BWD_WAVE(16, 1, 2)
+  if (nv <= 32) CF_BWD_WAVE(32, 1, 2)
+  if (nv <= 64) CF_BWD_WAVE(64, 1, 2)
+  constexpr int F = DT == DT_F32 ? 2 : 1;  // vectors of a type per 64 x 8 x ... values
+  if (a.c <= 1024) {
+    if (nv <= 128) CF_BWD_WAVE(64, 2, 1)
+    CF_BWD_WAVE(64, 4, 1)
+  }
+  if (a.c <= 2048) CF_BWD_BLOCK(256, F)
+  if (a.c <= 4096) CF_BWD_BLOCK(256, 2 * F)
+  if (a.c <= 8192) CF_BWD_BLOCK(1024, F)
+  CF_BWD_BLOCK(1024, 2 * F)
+#undef CF_BWD_WAVE
+#undef CF_BWD_BLOCK
+}
+
+size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
+
+}  // namespace
+
+size_t layernorm_fwd_workspace(long long rows, int c, int dtype) {
+  if (!fwd_chunked(rows, c, dtype)) return 0;
+  int chunk, nch;
+  plan_chunks(rows, c, vec_of(dtype), &chunk, &nch);
+  return up16((size_t)rows * nch * sizeof(float2));
+}
+
+size_t layernorm_bwd_workspace(long long rows, int c, int dtype) {
+  const size_t part = up16((size_t)bwd_groups(rows, c, dtype) * c * sizeof(float));
+  size_t n = 2 * part;
+  if (bwd_chunked(rows, c, dtype)) {
+    int chunk, nch;
+    plan_chunks(rows, c, vec_of(dtype), &chunk, &nch);
+    n += up16((size_t)rows * nch * sizeof(float2));
+  }
+  return n;
+}
+
+hipError_t launch_layernorm_fwd(long long rows, int c, int dtype, const void *x, const float *gamma, const float *beta,
+                                float eps, void *y, float *mean, float *rstd, void *ws, hipStream_t st) {
+  const long long bytes = rows * c * (dtype == DT_BF16 ? 2 : 4);
+  const FwdArgs a{rows, c, eps, 1.0f / (float)c, bytes >= kStreamBytes, x, gamma, beta, y, mean, rstd};
+  const bool rag = c % vec_of(dtype) != 0;
+  if (dtype == DT_BF16) return rag ? fwd<DT_BF16, true>(a, ws, st) : fwd<DT_BF16, false>(a, ws, st);
+  return rag ? fwd<DT_F32, true>(a, ws, st) : fwd<DT_F32, false>(a, ws, st);
+}
+
+hipError_t launch_layernorm_bwd(long long rows, int c, int dtype, const void *dy, const void *x, const float *gamma,
+                                const float *mean, const float *rstd, void *dx, float *dgamma, float *dbeta, void *ws,
+                                hipStream_t st) {
+  const long long bytes = rows * c * (dtype == DT_BF16 ? 2 : 4);
+  const int groups = bwd_groups(rows, c, dtype);
+  const size_t part = up16((size_t)groups * c * sizeof(float));
+  // one row of partials is the result itself
+  float *pg = groups == 1 ? dgamma : (float *)ws, *pb = groups == 1 ? dbeta : (float *)((char *)ws + part);
+  const BwdArgs a{rows, c, 1.0f / (float)c, bytes >= kStreamBytes, dy, x, gamma, mean, rstd, dx, pg, pb};
+  void *rowpart = (char *)ws + 2 * part;
+  const bool rag = c % vec_of(dtype) != 0;
+  const hipError_t e = dtype == DT_BF16
+                           ? (rag ? bwd<DT_BF16, true>(a, groups, rowpart, st) : bwd<DT_BF16, false>(a, groups, rowpart, st))
+                           : (rag ? bwd<DT_F32, true>(a, groups, rowpart, st) : bwd<DT_F32, false>(a, groups, rowpart, st));
+  if (e != hipSuccess || groups == 1) return e;
+  const SumJob jobs[2] = {{pg, dgamma, groups, c}, {pb, dbeta, groups, c}};
+  return launch_sum_batch(jobs, 2, st);
+}
+
+}  // namespace cf
