@@ -553,6 +553,93 @@ cf_status cf_layernorm_bwd(int64_t rows, int32_t c, int32_t dtype, const void *d
                            const float *gamma, const float *mean, const float *rstd, void *dx, float *dgamma,
                            float *dbeta, void *ws, size_t ws_bytes, void *stream);
 
+/* ------------------------------------------------------------------------
+ * Orthogonalised updates of weight matrices: an alternative to Adam + LARC
+ * for the parameters that are matrices.  A convolution's weights
+ * W[kd][kh][kw][c_in][c_out] are the matrix of kd*kh*kw*c_in rows and c_out
+ * columns, a fully-connected layer's W[k][n] that of k rows and n columns;
+ * biases and the scales and offsets of normalisation stay with
+ * cf_adam_larc_step.
+ *
+ * Newton-Schulz.  For a matrix G (rows x cols),
+ *   X_0 = G / (||G||_F + eps),   X_{i+1} = a X_i + (b H + c H^2) X_i,
+ *   H = X_i X_i'   (for rows > cols the same with X_i from the right:
+ *   X_{i+1} = a X_i + X_i (b H + c H^2), H = X_i' X_i),
+ * `steps` times: every singular value s of X_0 goes through the polynomial
+ * a s + b s^3 + c s^5, the singular vectors stay.  The usual (3.4445, -4.7750,
+ * 2.0315) and five steps bring the singular values from about 1e-2 on to
+ * between 0.7 and 1.2.
+ *
+ * Precision: products have the precision of fp32 (two fp16 values a factor,
+ * fp32 accumulators on the matrix cores); the Frobenius norm is summed in
+ * fp64.  Coefficients with which the iteration can leave the range of those
+ * factors for some singular value in [0, 1] are refused (CF_ERR_UNSUPPORTED).
+ * A matrix with a NaN or an infinity becomes all NaN; other matrices of the
+ * call are not affected.  A zero matrix gives zeros (eps > 0).  Deterministic.
+ * ------------------------------------------------------------------------ */
+
+/* A matrix in flat arrays: rows x cols values, row by row, from element
+ * `offset` on (a multiple of 8). */
+typedef struct cf_matrix {
+  int64_t offset;
+  int32_t rows, cols;
+} cf_matrix;
+
+typedef struct cf_ns_hparams {
+  double a, b, c; /* polynomial, finite */
+  double eps;     /* >= 0 */
+  int32_t steps;  /* 1 to CF_NS_MAX_STEPS */
+} cf_ns_hparams;
+
+#define CF_NS_MAX_STEPS 32
+
+/* Bytes of device workspace cf_newton_schulz needs (0 when every matrix is
+ * empty or the arguments are invalid). */
+size_t cf_newton_schulz_workspace_size(int32_t nmat, const cf_matrix *mats, int32_t dtype);
+
+/* o = the matrices of g after hp->steps steps.  mats: HOST array of nmat
+ * matrices in ascending order of offset that do not overlap (CF_ERR_ALIAS);
+ * a matrix without rows or columns is skipped.  g and o: flat device arrays in
+ * dtype; o may be g exactly, otherwise they must not overlap.  Elements of o
+ * outside the matrices are not touched.  Sizes: shorter side up to 16384,
+ * longer up to 2^24 (CF_ERR_UNSUPPORTED).  Matrices of one call run in the
+ * same launches, 24 at a time. */
+cf_status cf_newton_schulz(int32_t nmat, const cf_matrix *mats, int32_t dtype, const cf_ns_hparams *hp,
+                           const void *g, void *o, void *ws, size_t ws_bytes, void *stream);
+
+/* Scale of a matrix's orthogonalised update. */
+typedef enum cf_muon_scale {
+  CF_MUON_SCALE_SHAPE = 0, /* sqrt(max(1, cols / rows)): outputs over inputs */
+  CF_MUON_SCALE_RMS = 1    /* 0.2 sqrt(max(rows, cols)): the size of an Adam update */
+} cf_muon_scale;
+
+typedef struct cf_muon_hparams {
+  double eta0, eta_min; /* global rate, linear in t as in cf_adam_larc_hparams */
+  int64_t t_decay;      /* > 0 */
+  double mu;            /* momentum, in [0, 1) */
+  double weight_decay;  /* >= 0 */
+  cf_ns_hparams ns;
+  int32_t nesterov; /* 0 or 1 */
+  int32_t scale;    /* a cf_muon_scale */
+} cf_muon_hparams;
+
+/* Bytes of device workspace cf_muon_step needs (0 as above). */
+size_t cf_muon_workspace_size(int32_t nmat, const cf_matrix *mats);
+
+/* One update of every matrix of the flat fp32 device arrays v (parameters,
+ * updated in place), g (gradient, read only) and m (momentum, updated in
+ * place; zero before the first update), at step t (the updates already
+ * applied):
+ *   m = mu m + (1 - mu) g
+ *   u = (1 - mu) g + mu m  with nesterov, else m
+ *   v = v - eta_t (scale * newton_schulz(u) + weight_decay * v)
+ * eta_t and v16 (NULL, or the bf16 copy of the updated parameters at the same
+ * offsets) as in cf_adam_larc_step.  v, g, m, v16 and ws must not overlap.
+ * The momentum and the update are fp32, rounded at each operation's end.
+ * Elements outside the matrices are not touched. */
+cf_status cf_muon_step(int32_t nmat, const cf_matrix *mats, int64_t t, const cf_muon_hparams *hp, float *v,
+                       const float *g, float *m, void *v16, void *ws, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -43,6 +43,7 @@ EXPORTS = [
     "cf_avgpool3d_lrelu_bwd_deferred", "cf_conv3d_bwd_fused", "cf_conv3d_bwd_fused_deferred",
     "cf_conv3d_bwd", "cf_conv3d_bwd_deferred",
     "cf_layernorm_fwd_workspace_size", "cf_layernorm_fwd", "cf_layernorm_bwd_workspace_size", "cf_layernorm_bwd",
+    "cf_newton_schulz_workspace_size", "cf_newton_schulz", "cf_muon_workspace_size", "cf_muon_step",
 ]
 
 
@@ -82,6 +83,44 @@ def make_hparams(t_decay, **kw) -> cf_adam_larc_hparams:
     h.update(kw)
     return cf_adam_larc_hparams(h["eta0"], h["eta_min"], int(t_decay), h["beta1"], h["beta2"], h["eps_hat"],
                                 h["larc_coef"], h["larc_fallback"], h["larc_clip"])
+
+
+class cf_matrix(ctypes.Structure):
+    _fields_ = [("offset", ctypes.c_int64), ("rows", ctypes.c_int32), ("cols", ctypes.c_int32)]
+
+
+class cf_ns_hparams(ctypes.Structure):
+    _fields_ = [("a", ctypes.c_double), ("b", ctypes.c_double), ("c", ctypes.c_double), ("eps", ctypes.c_double),
+                ("steps", ctypes.c_int32)]
+
+
+class cf_muon_hparams(ctypes.Structure):
+    _fields_ = [("eta0", ctypes.c_double), ("eta_min", ctypes.c_double), ("t_decay", ctypes.c_int64),
+                ("mu", ctypes.c_double), ("weight_decay", ctypes.c_double), ("ns", cf_ns_hparams),
+                ("nesterov", ctypes.c_int32), ("scale", ctypes.c_int32)]
+
+
+CF_NS_MAX_STEPS = 32
+CF_MUON_SCALE_SHAPE, CF_MUON_SCALE_RMS = 0, 1
+#: the usual quintic: singular values from 1e-2 on end between 0.7 and 1.2 after five steps
+NS_COEF = (3.4445, -4.7750, 2.0315)
+
+
+def make_ns_hparams(steps=5, coef=NS_COEF, eps=1e-7) -> cf_ns_hparams:
+    return cf_ns_hparams(*(float(x) for x in coef), float(eps), int(steps))
+
+
+def make_muon_hparams(t_decay, eta0=0.02, eta_min=0.001, mu=0.95, weight_decay=0.0, steps=5, coef=NS_COEF, eps=1e-7,
+                      nesterov=True, scale=CF_MUON_SCALE_SHAPE) -> cf_muon_hparams:
+    return cf_muon_hparams(eta0, eta_min, int(t_decay), mu, weight_decay, make_ns_hparams(steps, coef, eps), int(nesterov),
+                           int(scale))
+
+
+def make_matrices(offsets, rows, cols):
+    """Host array of cf_matrix: matrix l is rows[l] x cols[l] values from offsets[l] on."""
+    if not len(offsets) == len(rows) == len(cols):
+        raise ValueError("make_matrices: offsets, rows and cols differ in length")
+    return (cf_matrix * len(offsets))(*[cf_matrix(int(o), int(r), int(c)) for o, r, c in zip(offsets, rows, cols)])
 
 
 _lib = None
@@ -142,6 +181,12 @@ def lib():
         "cf_layernorm_fwd": ([i64, i32, i32, vp, vp, vp, f32, vp, vp, vp, vp, sz, vp], ctypes.c_int),
         "cf_layernorm_bwd_workspace_size": ([i64, i32, i32], sz),
         "cf_layernorm_bwd": ([i64, i32, i32] + [vp] * 9 + [sz, vp], ctypes.c_int),
+        "cf_newton_schulz_workspace_size": ([i32, ctypes.POINTER(cf_matrix), i32], sz),
+        "cf_newton_schulz": ([i32, ctypes.POINTER(cf_matrix), i32, ctypes.POINTER(cf_ns_hparams), vp, vp, vp, sz, vp],
+                             ctypes.c_int),
+        "cf_muon_workspace_size": ([i32, ctypes.POINTER(cf_matrix)], sz),
+        "cf_muon_step": ([i32, ctypes.POINTER(cf_matrix), i64, ctypes.POINTER(cf_muon_hparams), vp, vp, vp, vp, vp, sz, vp],
+                         ctypes.c_int),
         "cf_adam_larc_workspace_size": ([i32, ctypes.POINTER(i64)], sz),
         "cf_adam_larc_step": ([i32, ctypes.POINTER(i64), i64, ctypes.POINTER(cf_adam_larc_hparams), vp, vp, vp, vp,
                                vp, vp, sz, vp], ctypes.c_int),
@@ -507,3 +552,30 @@ def cf_layernorm_bwd(rows, c, dtype, dy, x, gamma, mean, rstd, dx, dgamma, dbeta
         ws_bytes = 0 if ws is None or isinstance(ws, int) else ws.numel() * ws.element_size()
     _check(lib().cf_layernorm_bwd(rows, c, dtype_code(dtype), _ptr(dy), _ptr(x), _ptr(gamma), _ptr(mean), _ptr(rstd),
                                   _ptr(dx), _ptr(dgamma), _ptr(dbeta), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+# ---- orthogonalised updates --------------------------------------------------------
+
+def cf_newton_schulz_workspace_size(mats, dtype) -> int:
+    """mats: an array of cf_matrix (see make_matrices)."""
+    return int(lib().cf_newton_schulz_workspace_size(len(mats), mats, dtype_code(dtype)))
+
+
+def cf_newton_schulz(mats, dtype, hp, g, o, ws, ws_bytes=None, stream=None):
+    """hp: a cf_ns_hparams (see make_ns_hparams)."""
+    if ws_bytes is None:
+        ws_bytes = 0 if ws is None or isinstance(ws, int) else ws.numel() * ws.element_size()
+    _check(lib().cf_newton_schulz(len(mats), mats, dtype_code(dtype), ctypes.byref(hp), _ptr(g), _ptr(o), _ptr(ws), ws_bytes,
+                                  _stream(stream)))
+
+
+def cf_muon_workspace_size(mats) -> int:
+    return int(lib().cf_muon_workspace_size(len(mats), mats))
+
+
+def cf_muon_step(mats, t, hp, v, g, m, v16, ws, ws_bytes=None, stream=None):
+    """hp: a cf_muon_hparams (see make_muon_hparams)."""
+    if ws_bytes is None:
+        ws_bytes = 0 if ws is None or isinstance(ws, int) else ws.numel() * ws.element_size()
+    _check(lib().cf_muon_step(len(mats), mats, int(t), ctypes.byref(hp), _ptr(v), _ptr(g), _ptr(m), _ptr(v16), _ptr(ws),
+                              ws_bytes, _stream(stream)))

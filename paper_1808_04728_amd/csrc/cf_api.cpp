@@ -1073,3 +1073,164 @@ cf_status cf_layernorm_bwd(int64_t rows, int32_t c, int32_t dtype, const void *d
 }
 
 }  // extern "C"
+
+// ---- orthogonalised updates -----------------------------------------------------
+
+namespace {
+constexpr int32_t kMaxMats = 1 << 16;
+
+// validates the matrices; end = elements from the arrays' start to the last matrix's end
+cf_status mats_check(int32_t nmat, const cf_matrix *mats, int64_t *end, const char *who) {
+  *end = 0;
+  if (nmat < 0) return fail(CF_ERR_INVALID_ARG, std::string(who) + ": nmat must be >= 0");
+  if (nmat > kMaxMats) return fail(CF_ERR_UNSUPPORTED, std::string(who) + ": more than 65536 matrices");
+  if (nmat > 0 && !mats) return fail(CF_ERR_INVALID_ARG, std::string(who) + ": mats is NULL");
+  for (int32_t l = 0; l < nmat; ++l) {
+    const cf_matrix &M = mats[l];
+    if (M.offset < 0 || M.rows < 0 || M.cols < 0)
+      return fail(CF_ERR_INVALID_ARG, std::string(who) + ": negative offset, rows or cols");
+    if (M.offset % 8 != 0) return fail(CF_ERR_ALIGNMENT, std::string(who) + ": a matrix's offset is not a multiple of 8");
+    if (M.rows == 0 || M.cols == 0) continue;
+    const int32_t lo = M.rows < M.cols ? M.rows : M.cols, hi = M.rows < M.cols ? M.cols : M.rows;
+    if (lo > 16384 || hi > (1 << 24))
+      return fail(CF_ERR_UNSUPPORTED, std::string(who) + ": a side longer than 16384 (shorter) or 2^24 (longer)");
+    if (M.offset >= (1LL << 40)) return fail(CF_ERR_INVALID_ARG, std::string(who) + ": offset too large");
+    if (M.offset < *end) return fail(CF_ERR_ALIAS, std::string(who) + ": matrices overlap or are not in ascending order");
+    *end = M.offset + (int64_t)M.rows * M.cols;
+  }
+  return CF_OK;
+}
+
+cf_status ns_check(const cf_ns_hparams &hp, cf::NsSteps *S, const char *who) {
+  for (double x : {hp.a, hp.b, hp.c, hp.eps})
+    if (!std::isfinite(x)) return fail(CF_ERR_INVALID_ARG, std::string(who) + ": coefficients and eps must be finite");
+  if (hp.eps < 0.0) return fail(CF_ERR_INVALID_ARG, std::string(who) + ": eps must be >= 0");
+  if (hp.steps < 1 || hp.steps > CF_NS_MAX_STEPS)
+    return fail(CF_ERR_INVALID_ARG, std::string(who) + ": steps must be 1 to CF_NS_MAX_STEPS");
+  static_assert(cf::kNsMaxSteps == CF_NS_MAX_STEPS, "stage table size");
+  S->eps = hp.eps;
+  if (!cf::ns_scales(hp.a, hp.b, hp.c, hp.steps, S))
+    return fail(CF_ERR_UNSUPPORTED, std::string(who) + ": the iteration can grow past its factors' range with these coefficients");
+  return CF_OK;
+}
+
+// calls f(table, workspace bytes) for the non-empty matrices, a table at a time
+template <class F> cf_status mats_tables(int32_t nmat, const cf_matrix *mats, bool momentum, F f) {
+  int32_t l = 0;
+  while (l < nmat) {
+    long long off[cf::kNsTable];
+    int rows[cf::kNsTable], cols[cf::kNsTable], n = 0;
+    for (; l < nmat && n < cf::kNsTable; ++l) {
+      if (mats[l].rows == 0 || mats[l].cols == 0) continue;
+      off[n] = mats[l].offset;
+      rows[n] = mats[l].rows;
+      cols[n++] = mats[l].cols;
+    }
+    if (n == 0) break;
+    cf::NsTable T;
+    const size_t need = cf::ns_plan(n, off, rows, cols, momentum, &T);
+    const cf_status r = f(T, rows, cols, need);
+    if (r != CF_OK) return r;
+  }
+  return CF_OK;
+}
+
+size_t mats_workspace(int32_t nmat, const cf_matrix *mats, bool momentum) {
+  size_t most = 0;
+  mats_tables(nmat, mats, momentum, [&](cf::NsTable &, const int *, const int *, size_t need) {
+    most = need > most ? need : most;
+    return CF_OK;
+  });
+  return most;
+}
+}  // namespace
+
+extern "C" {
+
+size_t cf_newton_schulz_workspace_size(int32_t nmat, const cf_matrix *mats, int32_t dtype) {
+  const std::string keep = g_last_error;
+  int64_t end;
+  const bool bad = mats_check(nmat, mats, &end, "newton_schulz") != CF_OK || (dtype != CF_F32 && dtype != CF_BF16);
+  g_last_error = keep;
+  return bad ? 0 : mats_workspace(nmat, mats, false);
+}
+
+cf_status cf_newton_schulz(int32_t nmat, const cf_matrix *mats, int32_t dtype, const cf_ns_hparams *hp,
+                           const void *g, void *o, void *ws, size_t ws_bytes, void *stream) {
+  int64_t end;
+  cf_status r = mats_check(nmat, mats, &end, "newton_schulz");
+  if (r != CF_OK) return r;
+  if (dtype != CF_F32 && dtype != CF_BF16) return fail(CF_ERR_INVALID_ARG, "unknown dtype");
+  if (!hp) return fail(CF_ERR_INVALID_ARG, "newton_schulz: hp is NULL");
+  cf::NsSteps S;
+  if ((r = ns_check(*hp, &S, "newton_schulz")) != CF_OK) return r;
+  if (end == 0) return ok();
+  if ((r = check_ptrs({g, o})) != CF_OK) return r;
+  const size_t need = mats_workspace(nmat, mats, false), nb = (size_t)end * elem_size(dtype);
+  if (!ws || ws_bytes < need)
+    return fail(CF_ERR_WORKSPACE, "newton_schulz: workspace smaller than cf_newton_schulz_workspace_size()");
+  if (!aligned16(ws)) return fail(CF_ERR_ALIGNMENT, "workspace not 16-byte aligned");
+  if ((g != o && overlap(g, nb, o, nb)) || overlap(ws, need, g, nb) || overlap(ws, need, o, nb))
+    return fail(CF_ERR_ALIAS, "newton_schulz: g, o and the workspace must not overlap (o may be g)");
+  hipStream_t st = (hipStream_t)stream;
+  return mats_tables(nmat, mats, false, [&](cf::NsTable &T, const int *, const int *, size_t) {
+    return finish(cf::launch_newton_schulz(T, S, kdt(dtype), g, nullptr, nullptr, nullptr, o, nullptr, ws, st), st,
+                  "cf_newton_schulz");
+  });
+}
+
+size_t cf_muon_workspace_size(int32_t nmat, const cf_matrix *mats) {
+  const std::string keep = g_last_error;
+  int64_t end;
+  const bool bad = mats_check(nmat, mats, &end, "muon") != CF_OK;
+  g_last_error = keep;
+  return bad ? 0 : mats_workspace(nmat, mats, true);
+}
+
+cf_status cf_muon_step(int32_t nmat, const cf_matrix *mats, int64_t t, const cf_muon_hparams *hp, float *v,
+                       const float *g, float *m, void *v16, void *ws, size_t ws_bytes, void *stream) {
+  int64_t end;
+  cf_status r = mats_check(nmat, mats, &end, "muon");
+  if (r != CF_OK) return r;
+  if (!hp) return fail(CF_ERR_INVALID_ARG, "muon: hp is NULL");
+  if (t < 0) return fail(CF_ERR_INVALID_ARG, "muon: t must be >= 0");
+  if (hp->t_decay <= 0) return fail(CF_ERR_INVALID_ARG, "muon: t_decay must be > 0");
+  for (double x : {hp->eta0, hp->eta_min, hp->mu, hp->weight_decay})
+    if (!std::isfinite(x)) return fail(CF_ERR_INVALID_ARG, "muon: hyperparameters must be finite");
+  if (hp->mu < 0.0 || hp->mu >= 1.0) return fail(CF_ERR_INVALID_ARG, "muon: mu must lie in [0, 1)");
+  if (hp->weight_decay < 0.0) return fail(CF_ERR_INVALID_ARG, "muon: weight_decay must be >= 0");
+  if (hp->nesterov != 0 && hp->nesterov != 1) return fail(CF_ERR_INVALID_ARG, "muon: nesterov must be 0 or 1");
+  if (hp->scale != CF_MUON_SCALE_SHAPE && hp->scale != CF_MUON_SCALE_RMS)
+    return fail(CF_ERR_INVALID_ARG, "muon: unknown scale");
+  cf::NsSteps S;
+  if ((r = ns_check(hp->ns, &S, "muon")) != CF_OK) return r;
+  if (end == 0) return ok();
+  if ((r = check_ptrs({v, g, m})) != CF_OK) return r;
+  if (v16 && !aligned16(v16)) return fail(CF_ERR_ALIGNMENT, "muon: v16 not 16-byte aligned");
+  const size_t need = mats_workspace(nmat, mats, true);
+  if (!ws || ws_bytes < need) return fail(CF_ERR_WORKSPACE, "muon: workspace smaller than cf_muon_workspace_size()");
+  if (!aligned16(ws)) return fail(CF_ERR_ALIGNMENT, "workspace not 16-byte aligned");
+  const size_t nb = (size_t)end * 4;
+  const void *bufs[] = {v, g, m, v16, ws};
+  const size_t lens[] = {nb, nb, nb, nb / 2, need};
+  for (int a = 0; a < 5; ++a)
+    for (int b = a + 1; b < 5; ++b)
+      if (overlap(bufs[a], lens[a], bufs[b], lens[b]))
+        return fail(CF_ERR_ALIAS, "muon: v, g, m, v16 and the workspace must not overlap");
+  const double tc = (double)(t < hp->t_decay ? t : hp->t_decay);
+  const cf::NsMomentum mom{hp->mu, 1.0 - hp->mu, hp->nesterov};
+  const cf::NsUpdate up{(float)((hp->eta0 - hp->eta_min) * (1.0 - tc / (double)hp->t_decay) + hp->eta_min),
+                        (float)hp->weight_decay};
+  hipStream_t st = (hipStream_t)stream;
+  return mats_tables(nmat, mats, true, [&](cf::NsTable &T, const int *rows, const int *cols, size_t) {
+    for (int l = 0; l < T.count; ++l) {
+      const double R = rows[l], C = cols[l];
+      T.mat[l].gain = (float)(hp->scale == CF_MUON_SCALE_RMS ? 0.2 * std::sqrt(R > C ? R : C)
+                                                             : std::sqrt(C > R ? C / R : 1.0));
+    }
+    return finish(cf::launch_newton_schulz(T, S, cf::DT_F32, g, &mom, m, &up, v, (uint16_t *)v16, ws, st), st,
+                  "cf_muon_step");
+  });
+}
+
+}  // extern "C"

@@ -247,6 +247,62 @@ hipError_t launch_layernorm_bwd(long long rows, int c, int dtype, const void *dy
                                 const float *mean, const float *rstd, void *dx, float *dgamma, float *dbeta, void *ws,
                                 hipStream_t st);
 
+// Newton-Schulz orthogonalisation and the update with it (muon.hip).  A table holds
+// the matrices of one set of launches and is passed by value as a kernel argument.
+constexpr int kNsTable = 24;    // matrices a table holds
+constexpr int kNsChunk = 4096;  // elements of a chunk of the norm pass, shifted left per matrix
+struct NsMat {
+  long long off;  // first element in the flat arrays
+  int m, n;       // shorter and longer side; tall: the longer side is the rows
+  int mp, np;     // both padded to the matrix instructions' k
+  int tall;
+  int shift, chunks;  // of the norm pass
+  int slices;         // of the long side in the Gram product
+  float gain;         // of the update
+  // byte offsets in the workspace: chunk sums, u (-1: none), X [m][n], X' [n][m] twice,
+  // the m x m matrices, the Gram matrix's slices
+  long long ws_norm, ws_u, ws_xn, ws_xt, ws_xt2, ws_sq, ws_part;
+};
+struct NsTable {
+  int count;
+  int first[kNsTable + 1];  // first workgroup of each matrix in the launch
+  NsMat mat[kNsTable];
+};
+struct NsMomentum {
+  double mu, one_mu;
+  int nesterov;
+};
+struct NsUpdate {
+  float eta, decay;
+};
+// one product: workspace slots of its factors and result, scales of their fp16 pairs
+struct NsProduct {
+  int a, b, out, update;
+  float unscale, unscale_h, scale;
+  float ca, cb, cc;
+  float eta, decay;
+};
+// one or two steps from one Gram matrix: scales of X, of H and Q of each step, of Q H
+// and of the product of both Q
+struct NsStage {
+  int steps;
+  float sx, sh[2], sq[2], st, sp;
+};
+constexpr int kNsMaxSteps = 32;
+struct NsSteps {
+  double a, b, c, eps;
+  int stages;
+  NsStage stage[(kNsMaxSteps + 1) / 2];
+};
+// scales that keep every factor in range, from bounds of the polynomial on the singular
+// values' range; false if the iteration can leave it
+bool ns_scales(double a, double b, double c, int steps, NsSteps *S);
+// fills the table (count <= kNsTable; gain is the caller's), returns the bytes of workspace
+size_t ns_plan(int count, const long long *off, const int *rows, const int *cols, bool momentum, NsTable *T);
+// out: the orthogonalised matrices (dtype), or with up the fp32 parameters, updated in place
+hipError_t launch_newton_schulz(const NsTable &T, const NsSteps &S, int dtype, const void *g, const NsMomentum *mom,
+                                float *m, const NsUpdate *up, void *out, uint16_t *v16, void *ws, hipStream_t st);
+
 // Fully-connected layers (fc.hip): rows x[M][K], W[K][N], z[M][N].
 size_t fc_fwd_workspace(int M, int K, int N);
 hipError_t launch_fc_fwd(int M, int K, int N, int dtype, const void *x, const void *w, void *y, void *ws,
