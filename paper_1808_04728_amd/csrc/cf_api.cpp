@@ -1115,7 +1115,7 @@ cf_status ns_check(const cf_ns_hparams &hp, cf::NsSteps *S, const char *who) {
 }
 
 // calls f(table, workspace bytes) for the non-empty matrices, a table at a time
-template <class F> cf_status mats_tables(int32_t nmat, const cf_matrix *mats, bool momentum, F f) {
+template <class F> cf_status mats_tables(int32_t nmat, const cf_matrix *mats, int32_t dtype, bool momentum, F f) {
   int32_t l = 0;
   while (l < nmat) {
     long long off[cf::kNsTable];
@@ -1128,16 +1128,16 @@ template <class F> cf_status mats_tables(int32_t nmat, const cf_matrix *mats, bo
     }
     if (n == 0) break;
     cf::NsTable T;
-    const size_t need = cf::ns_plan(n, off, rows, cols, momentum, &T);
+    const size_t need = cf::ns_plan(n, off, rows, cols, kdt(dtype), momentum, &T);
     const cf_status r = f(T, rows, cols, need);
     if (r != CF_OK) return r;
   }
   return CF_OK;
 }
 
-size_t mats_workspace(int32_t nmat, const cf_matrix *mats, bool momentum) {
+size_t mats_workspace(int32_t nmat, const cf_matrix *mats, int32_t dtype, bool momentum) {
   size_t most = 0;
-  mats_tables(nmat, mats, momentum, [&](cf::NsTable &, const int *, const int *, size_t need) {
+  mats_tables(nmat, mats, dtype, momentum, [&](cf::NsTable &, const int *, const int *, size_t need) {
     most = need > most ? need : most;
     return CF_OK;
   });
@@ -1152,7 +1152,7 @@ size_t cf_newton_schulz_workspace_size(int32_t nmat, const cf_matrix *mats, int3
   int64_t end;
   const bool bad = mats_check(nmat, mats, &end, "newton_schulz") != CF_OK || (dtype != CF_F32 && dtype != CF_BF16);
   g_last_error = keep;
-  return bad ? 0 : mats_workspace(nmat, mats, false);
+  return bad ? 0 : mats_workspace(nmat, mats, dtype, false);
 }
 
 cf_status cf_newton_schulz(int32_t nmat, const cf_matrix *mats, int32_t dtype, const cf_ns_hparams *hp,
@@ -1166,14 +1166,14 @@ cf_status cf_newton_schulz(int32_t nmat, const cf_matrix *mats, int32_t dtype, c
   if ((r = ns_check(*hp, &S, "newton_schulz")) != CF_OK) return r;
   if (end == 0) return ok();
   if ((r = check_ptrs({g, o})) != CF_OK) return r;
-  const size_t need = mats_workspace(nmat, mats, false), nb = (size_t)end * elem_size(dtype);
+  const size_t need = mats_workspace(nmat, mats, dtype, false), nb = (size_t)end * elem_size(dtype);
   if (!ws || ws_bytes < need)
     return fail(CF_ERR_WORKSPACE, "newton_schulz: workspace smaller than cf_newton_schulz_workspace_size()");
   if (!aligned16(ws)) return fail(CF_ERR_ALIGNMENT, "workspace not 16-byte aligned");
   if ((g != o && overlap(g, nb, o, nb)) || overlap(ws, need, g, nb) || overlap(ws, need, o, nb))
     return fail(CF_ERR_ALIAS, "newton_schulz: g, o and the workspace must not overlap (o may be g)");
   hipStream_t st = (hipStream_t)stream;
-  return mats_tables(nmat, mats, false, [&](cf::NsTable &T, const int *, const int *, size_t) {
+  return mats_tables(nmat, mats, dtype, false, [&](cf::NsTable &T, const int *, const int *, size_t) {
     return finish(cf::launch_newton_schulz(T, S, kdt(dtype), g, nullptr, nullptr, nullptr, o, nullptr, ws, st), st,
                   "cf_newton_schulz");
   });
@@ -1184,7 +1184,7 @@ size_t cf_muon_workspace_size(int32_t nmat, const cf_matrix *mats) {
   int64_t end;
   const bool bad = mats_check(nmat, mats, &end, "muon") != CF_OK;
   g_last_error = keep;
-  return bad ? 0 : mats_workspace(nmat, mats, true);
+  return bad ? 0 : mats_workspace(nmat, mats, CF_F32, true);
 }
 
 cf_status cf_muon_step(int32_t nmat, const cf_matrix *mats, int64_t t, const cf_muon_hparams *hp, float *v,
@@ -1207,7 +1207,7 @@ cf_status cf_muon_step(int32_t nmat, const cf_matrix *mats, int64_t t, const cf_
   if (end == 0) return ok();
   if ((r = check_ptrs({v, g, m})) != CF_OK) return r;
   if (v16 && !aligned16(v16)) return fail(CF_ERR_ALIGNMENT, "muon: v16 not 16-byte aligned");
-  const size_t need = mats_workspace(nmat, mats, true);
+  const size_t need = mats_workspace(nmat, mats, CF_F32, true);
   if (!ws || ws_bytes < need) return fail(CF_ERR_WORKSPACE, "muon: workspace smaller than cf_muon_workspace_size()");
   if (!aligned16(ws)) return fail(CF_ERR_ALIGNMENT, "workspace not 16-byte aligned");
   const size_t nb = (size_t)end * 4;
@@ -1222,7 +1222,7 @@ cf_status cf_muon_step(int32_t nmat, const cf_matrix *mats, int64_t t, const cf_
   const cf::NsUpdate up{(float)((hp->eta0 - hp->eta_min) * (1.0 - tc / (double)hp->t_decay) + hp->eta_min),
                         (float)hp->weight_decay};
   hipStream_t st = (hipStream_t)stream;
-  return mats_tables(nmat, mats, true, [&](cf::NsTable &T, const int *rows, const int *cols, size_t) {
+  return mats_tables(nmat, mats, CF_F32, true, [&](cf::NsTable &T, const int *rows, const int *cols, size_t) {
     for (int l = 0; l < T.count; ++l) {
       const double R = rows[l], C = cols[l];
       T.mat[l].gain = (float)(hp->scale == CF_MUON_SCALE_RMS ? 0.2 * std::sqrt(R > C ? R : C)

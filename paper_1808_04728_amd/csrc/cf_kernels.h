@@ -256,13 +256,17 @@ struct NsMat {
   int m, n;       // shorter and longer side; tall: the longer side is the rows
   int mp, np;     // both padded to the matrix instructions' k
   int tall;
+  int mt;             // m padded to 16, 32, 64 or 128 where the skinny kernels run it, else 0
   int shift, chunks;  // of the norm pass
-  int slices;         // of the long side in the Gram product
+  int prow;           // skinny: rows of the long side in a chunk
+  int slices;         // of the long side in the Gram product (skinny: workgroups)
   float gain;         // of the update
   // byte offsets in the workspace: chunk sums, u (-1: none), X [m][n], X' [n][m] twice,
-  // the m x m matrices, the Gram matrix's slices
-  long long ws_norm, ws_u, ws_xn, ws_xt, ws_xt2, ws_sq, ws_part;
+  // the m x m matrices, the Gram matrix's slices.  Skinny: u and X are fp32 [n][mt], the
+  // one m x m matrix is P, ws_sum holds the slices' sum.
+  long long ws_norm, ws_u, ws_xn, ws_xt, ws_xt2, ws_sq, ws_part, ws_sum;
 };
+constexpr int kNsFewSlices = 2;  // so many slices the polynomial kernel adds itself
 struct NsTable {
   int count;
   int first[kNsTable + 1];  // first workgroup of each matrix in the launch
@@ -298,7 +302,10 @@ struct NsSteps {
 // values' range; false if the iteration can leave it
 bool ns_scales(double a, double b, double c, int steps, NsSteps *S);
 // fills the table (count <= kNsTable; gain is the caller's), returns the bytes of workspace
-size_t ns_plan(int count, const long long *off, const int *rows, const int *cols, bool momentum, NsTable *T);
+size_t ns_plan(int count, const long long *off, const int *rows, const int *cols, int dtype, bool momentum, NsTable *T);
+// the table's matrices of up to 128 columns or rows (muon_skinny.hip)
+hipError_t launch_ns_skinny(const NsTable &T, const NsSteps &S, int dtype, const void *g, const NsMomentum *mom, float *m,
+                            const NsUpdate *up, void *out, uint16_t *v16, void *ws, hipStream_t st);
 // out: the orthogonalised matrices (dtype), or with up the fp32 parameters, updated in place
 hipError_t launch_newton_schulz(const NsTable &T, const NsSteps &S, int dtype, const void *g, const NsMomentum *mom,
                                 float *m, const NsUpdate *up, void *out, uint16_t *v16, void *ws, hipStream_t st);

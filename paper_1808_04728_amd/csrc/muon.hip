@@ -22,43 +22,13 @@
 
 #include <type_traits>
 
-#include "cf_common.h"
-#include "cf_kernels.h"
+#include "muon_common.h"
 
 namespace cf {
 namespace {
 
-typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x4_t __attribute__((ext_vector_type(4)));
-
 constexpr int kTile = 64;
 constexpr int kStep = 32;  // k of one matrix instruction; both sides are padded to it
-
-__device__ __forceinline__ int find_mat(const NsTable &T, int b) {
-  int l = 0;
-  while (l + 1 < T.count && T.first[l + 1] <= b) ++l;
-  return l;
-}
-
-// Sum of a double over 256 threads in a fixed order.
-__device__ __forceinline__ double block_sum(double a, double *red) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) a += __shfl_xor(a, o, 64);
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = a;
-  __syncthreads();
-  return (red[0] + red[1]) + (red[2] + red[3]);
-}
-
-struct Half2 {
-  _Float16 hi, lo;
-};
-// x = hi + lo to 2^-23 of x
-__device__ __forceinline__ Half2 split(float x) {
-  Half2 r;
-  r.hi = (_Float16)x;
-  r.lo = (_Float16)(x - (float)r.hi);
-  return r;
-}
 
 // ---- momentum and norm --------------------------------------------------------
 
@@ -68,7 +38,7 @@ __device__ __forceinline__ Half2 split(float x) {
 template <int DT, bool MOM>
 __global__ __launch_bounds__(256) void ns_prep_kernel(NsTable T, NsMomentum mom, const void *g, float *m, char *ws) {
   __shared__ double red[4];
-  const int l = find_mat(T, blockIdx.x);
+  const int l = ns_find(T, blockIdx.x);
   const NsMat &M = T.mat[l];
   const long long count = (long long)M.m * M.n, span = (long long)kNsChunk << M.shift;
   const int chunk = blockIdx.x - T.first[l];
@@ -90,26 +60,15 @@ __global__ __launch_bounds__(256) void ns_prep_kernel(NsTable T, NsMomentum mom,
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if (i < k) {
-          const float gi = (float)mom.one_mu * x[i];
-          const float mi = (float)mom.mu * m[M.off + e + i] + gi;
-          m[M.off + e + i] = mi;
-          x[i] = mom.nesterov ? (float)mom.mu * mi + gi : mi;
+          x[i] = ns_momentum(mom, x[i], m[M.off + e + i]);
           u[e + i] = x[i];
         }
       }
     }
     s += (double)x[0] * x[0] + (double)x[1] * x[1] + (double)x[2] * x[2] + (double)x[3] * x[3];
   }
-  s = block_sum(s, red);
+  s = ns_block_sum(s, red);
   if (threadIdx.x == 0) ((double *)(ws + M.ws_norm))[chunk] = s;
-}
-
-// 1 / (||u|| + eps) from the chunks' sums, by every workgroup in the same order
-__device__ __forceinline__ double inv_norm(const NsMat &M, const char *ws, double eps, double *red) {
-  const double *p = (const double *)(ws + M.ws_norm);
-  double s = 0.0;
-  for (int i = threadIdx.x; i < M.chunks; i += 256) s += p[i];
-  return 1.0 / (sqrt(block_sum(s, red)) + eps);
 }
 
 // X = u / (||u|| + eps) in both layouts, xn [mp][np] and xt [np][mp] (hi and lo, zero
@@ -118,9 +77,9 @@ template <int DT>
 __global__ __launch_bounds__(256) void ns_split_kernel(NsTable T, double eps, float scale, const void *src, char *ws) {
   __shared__ double red[4];
   __shared__ float tile[64][65];
-  const int l = find_mat(T, blockIdx.x);
+  const int l = ns_find(T, blockIdx.x);
   const NsMat &M = T.mat[l];
-  const double inv = inv_norm(M, ws, eps, red);
+  const double inv = ns_inv_norm(M, ws, eps, red);
   const int tm = (M.mp + 63) / 64, b = blockIdx.x - T.first[l];
   const int n0 = b / tm * 64, m0 = b % tm * 64;
   const int c = threadIdx.x & 63, r0 = threadIdx.x >> 6;
@@ -143,13 +102,13 @@ __global__ __launch_bounds__(256) void ns_split_kernel(NsTable T, double eps, fl
   const int nrows = M.tall ? M.np : M.mp, ncols = M.tall ? M.mp : M.np;  // natural array, padded
   for (int r = r0; r < 64; r += 4) {
     if (rr + r < nrows && cc + c < ncols) {
-      const Half2 h = split(tile[r][c]);
+      const Half2 h = ns_split(tile[r][c]);
       const long long e = (long long)(rr + r) * ncols + cc + c;
       nat[e] = h.hi;
       nat[plane + e] = h.lo;
     }
     if (cc + r < ncols && rr + c < nrows) {
-      const Half2 h = split(tile[c][r]);
+      const Half2 h = ns_split(tile[c][r]);
       const long long e = (long long)(cc + r) * nrows + rr + c;
       tr[e] = h.hi;
       tr[plane + e] = h.lo;
@@ -207,7 +166,7 @@ __device__ __forceinline__ void tile_product(const _Float16 *A, long long pa, in
 //   FINAL  the output: o = xt P, or the parameter update with it
 template <int MODE, int DT>
 __global__ __launch_bounds__(256) void ns_product_kernel(NsTable T, NsProduct p, void *out, uint16_t *v16, char *ws) {
-  const int l = find_mat(T, blockIdx.x);
+  const int l = ns_find(T, blockIdx.x);
   const NsMat &M = T.mat[l];
   const int b = blockIdx.x - T.first[l];
   const int tm = (M.mp + kTile - 1) / kTile;
@@ -268,7 +227,7 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsTable T, NsProduct p,
             x = p.cc * x + p.cb * h;
             if (i + q == j && j < M.m) x += p.ca;
           }
-          const Half2 s = split(x * p.scale);
+          const Half2 s = ns_split(x * p.scale);
           o[e] = s.hi;
           o[sq + e] = s.lo;
         }
@@ -277,7 +236,7 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsTable T, NsProduct p,
         f16x4_t hi, lo;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const Half2 s = split(acc[ti][tj][q] * p.unscale * p.scale);
+          const Half2 s = ns_split(acc[ti][tj][q] * p.unscale * p.scale);
           xt[(long long)(i + q) * M.mp + j] = s.hi;
           xt[plane + (long long)(i + q) * M.mp + j] = s.lo;
           hi[q] = s.hi;
@@ -307,7 +266,7 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsTable T, NsProduct p,
 
 // H = sum of the slices' Gram matrices, in slice order
 __global__ __launch_bounds__(256) void ns_gram_sum_kernel(NsTable T, int slot, float scale, char *ws) {
-  const int l = find_mat(T, blockIdx.x);
+  const int l = ns_find(T, blockIdx.x);
   const NsMat &M = T.mat[l];
   const long long sq = (long long)M.mp * M.mp;
   const long long e = (long long)(blockIdx.x - T.first[l]) * 256 + threadIdx.x;
@@ -315,7 +274,7 @@ __global__ __launch_bounds__(256) void ns_gram_sum_kernel(NsTable T, int slot, f
   const float *part = (const float *)(ws + M.ws_part) + e;
   float s = 0.f;
   for (int i = 0; i < M.slices; ++i) s += part[i * sq];
-  const Half2 h = split(s * scale);
+  const Half2 h = ns_split(s * scale);
   _Float16 *o = (_Float16 *)(ws + M.ws_sq) + 2 * sq * slot;
   o[e] = h.hi;
   o[sq + e] = h.lo;
@@ -328,12 +287,12 @@ __global__ __launch_bounds__(256) void ns_gram_sum_kernel(NsTable T, int slot, f
 namespace {
 long long up(long long n, long long a) { return (n + a - 1) / a * a; }
 
-// first workgroup of every matrix of the launch; returns their number
+// first workgroup of every matrix that the general kernels run; returns their number
 template <class F> int number(NsTable *T, F blocks) {
   int at = 0;
   for (int l = 0; l < T->count; ++l) {
     T->first[l] = at;
-    at += (int)blocks(T->mat[l]);
+    if (!T->mat[l].mt) at += (int)blocks(T->mat[l]);
   }
   T->first[T->count] = at;
   return at;
@@ -347,14 +306,16 @@ bool ns_scales(double a, double b, double c, int steps, NsSteps *S) {
   S->b = b;
   S->c = c;
   S->stages = (steps + 1) / 2;
-  // the largest power of two that keeps values up to `bound` (and 5% of rounding) below 2^15
+  // the largest power of two that keeps values up to `bound` and twice that below 2^16:
+  // room for rounding and for what lies between the points at which the bounds are taken
   auto scale = [](double bound) {
     int e = 0;
     (void)frexp(32768.0 / (1.05 * (bound > 0.125 ? bound : 0.125)), &e);
     return (float)ldexp(1.0, e - 1 < 14 ? e - 1 : 14);
   };
-  constexpr int N = 8192;
-  double sigma = 1.0;  // bound of the singular values
+  auto most = [](double x, double y) { return x > y ? x : y; };
+  constexpr int N = 64;  // (every call pays for them: 8192 points took 100 us)
+  double sigma = 1.0;    // bound of the singular values
   for (int s = 0; s < S->stages; ++s) {
     NsStage &G = S->stage[s];
     G = NsStage{};
@@ -362,14 +323,14 @@ bool ns_scales(double a, double b, double c, int steps, NsSteps *S) {
     G.sx = scale(sigma);
     double hb[2] = {sigma * sigma, 0.0}, qb[2] = {0.0, 0.0}, tb = 0.0, pb = 0.0, next = 0.0;
     for (int i = 0; i <= N; ++i) {
-      const double x = sigma * i / N, h = x * x, q = a + b * h + c * h * h;
-      const double y = x * q, h1 = y * y, q1 = G.steps == 2 ? a + b * h1 + c * h1 * h1 : 1.0;
-      qb[0] = fmax(qb[0], fabs(q));
-      tb = fmax(tb, fabs(q * h));
-      hb[1] = fmax(hb[1], h1);
-      qb[1] = fmax(qb[1], fabs(q1));
-      pb = fmax(pb, fabs(q * q1));
-      next = fmax(next, fabs(y * q1));
+      const double x = sigma * i / N, h = x * x, q = fabs(a + b * h + c * h * h);
+      const double y = x * q, h1 = y * y, q1 = G.steps == 2 ? fabs(a + b * h1 + c * h1 * h1) : 1.0;
+      qb[0] = most(q, qb[0]);
+      tb = most(q * h, tb);
+      hb[1] = most(h1, hb[1]);
+      qb[1] = most(q1, qb[1]);
+      pb = most(q * q1, pb);
+      next = most(y * q1, next);
     }
     if (!(qb[0] < 1024.0 && qb[1] < 1024.0 && pb < 16384.0 && tb < 1024.0 && hb[1] < 1024.0 && next < 32.0)) return false;
     for (int k = 0; k < 2; ++k) {
@@ -378,12 +339,12 @@ bool ns_scales(double a, double b, double c, int steps, NsSteps *S) {
     }
     G.st = scale(tb);
     G.sp = scale(pb);
-    sigma = fmax(next, 0.125);
+    sigma = most(next, 0.125);
   }
   return true;
 }
 
-size_t ns_plan(int count, const long long *off, const int *rows, const int *cols, bool momentum, NsTable *T) {
+size_t ns_plan(int count, const long long *off, const int *rows, const int *cols, int dtype, bool momentum, NsTable *T) {
   long long at = 0;
   auto take = [&](long long bytes) {
     const long long p = at;
@@ -397,9 +358,32 @@ size_t ns_plan(int count, const long long *off, const int *rows, const int *cols
     M.tall = rows[l] >= cols[l];
     M.m = M.tall ? cols[l] : rows[l];
     M.n = M.tall ? rows[l] : cols[l];
+    const long long el = (long long)M.m * M.n;
+    M.mt = 0;
+    if (M.m <= 128) {
+      int mt = 16;
+      while (mt < M.m) mt *= 2;
+      M.mt = mt;
+      // chunks of about 8192 elements, at most 512
+      M.prow = (int)up(8192 / mt, 64);
+      while (((long long)M.n + M.prow - 1) / M.prow > 512) M.prow *= 2;
+      M.chunks = (M.n + M.prow - 1) / M.prow;
+      // workgroups of four waves: a wave takes 32 rows at a time
+      const long long wgs = ((long long)M.n + 127) / 128;
+      M.slices = (int)(wgs < kNumCUs ? wgs : kNumCUs);
+      const int tt = mt / 16;
+      const bool direct = !momentum && dtype == DT_F32 && M.tall && M.m == mt;
+      M.ws_norm = take(8LL * M.chunks);
+      const long long x = take(4LL * M.n * mt);
+      M.ws_u = direct ? -1 : x;
+      M.ws_xn = x;
+      M.ws_sq = take((long long)mt * ((tt + 1) / 2) * 128);
+      M.ws_part = take(1024LL * (tt * (tt + 1) / 2) * M.slices);
+      M.ws_sum = take(1024LL * (tt * (tt + 1) / 2));
+      continue;
+    }
     M.mp = (int)up(M.m, kStep);
     M.np = (int)up(M.n, kStep);
-    const long long el = (long long)M.m * M.n;
     M.shift = 0;
     while ((el + ((long long)kNsChunk << M.shift) - 1) / ((long long)kNsChunk << M.shift) > 512) ++M.shift;
     M.chunks = (int)((el + ((long long)kNsChunk << M.shift) - 1) / ((long long)kNsChunk << M.shift));
@@ -422,10 +406,12 @@ size_t ns_plan(int count, const long long *off, const int *rows, const int *cols
 
 hipError_t launch_newton_schulz(const NsTable &T0, const NsSteps &S, int dtype, const void *g, const NsMomentum *mom,
                                 float *m, const NsUpdate *up_, void *out, uint16_t *v16, void *ws_, hipStream_t st) {
-  if (T0.count == 0) return hipSuccess;
+  const hipError_t skinny = launch_ns_skinny(T0, S, dtype, g, mom, m, up_, out, v16, ws_, st);
+  if (skinny != hipSuccess) return skinny;
   NsTable T = T0;
   char *ws = (char *)ws_;
   int nb = number(&T, [](const NsMat &M) { return M.chunks; });
+  if (nb == 0) return hipSuccess;
   if (mom)
     hipLaunchKernelGGL((ns_prep_kernel<DT_F32, true>), dim3(nb), dim3(256), 0, st, T, *mom, g, m, ws);
   else if (dtype == DT_BF16)

@@ -1,0 +1,848 @@
+// muon_skinny.hip -- the Newton-Schulz products (see muon.hip) of matrices whose
+// shorter side m is at most 128: every weight matrix of the network.
+//
+// The long side is touched once a pair of steps.  A wave takes 32 of its rows at a
+// time from memory to registers, multiplies them by P and adds their share of the
+// next Gram matrix without leaving the registers:
+//   D = X P     the result of a matrix instruction has a column of D in a lane and
+//               four rows of it in the lane's registers;
+//   H += D' D   reads, for both factors, a lane with a column and eight rows: two
+//               results of the first product as they are.  Which rows these are does
+//               not matter as long as both factors agree.
+// The Gram matrix's upper tiles stay in accumulators; a workgroup's four waves add
+// theirs through LDS, the workgroups' sums are added in a fixed order.
+//
+// The m x m polynomials run in one workgroup a matrix.  Its waves own columns: for
+// a symmetric M and any product C = M B, a wave's columns of B are its own, so a
+// chain of products needs only M in LDS and no exchange between them.
+//
+// Columns are handled in slots: slot 16 (4 u + c) + r is column 64 u + 4 r + c, so that
+// a lane's four tiles c hold four consecutive columns and rows load and store in
+// 16-byte vectors.  The polynomials do not care; P is written with rows in slot order
+// and columns in their own, which is how the product with X reads it.
+//
+// Up to 32 columns factors are fp32 (the fp32 matrix rate covers them), above they
+// are fp16 pairs as in muon.hip.
+
+#include "muon_common.h"
+
+namespace cf {
+namespace {
+
+template <int MT> struct Geo {
+  static constexpr int TT = MT / 16;              // 16-column tiles
+  static constexpr int VW = TT < 4 ? TT : 4;      // columns of a vector
+  static constexpr int U = TT / VW;               // 64-column groups
+  static constexpr int KB = (TT + 1) / 2;         // 32-deep products over the columns
+  static constexpr bool F32 = MT <= 32;           // factor format
+  static constexpr int TRI = TT * (TT + 1) / 2;   // tiles of the upper triangle
+  static constexpr int LROW = KB * 128 + 16;      // bytes of a matrix row in LDS
+  static constexpr int MAT = MT * LROW;           // bytes of a matrix in LDS
+  static constexpr int RED = 4 * TRI * 1024;      // bytes of four waves' Gram tiles
+};
+
+// eight values of a factor, k = (g, 0..7) of a 32-deep product
+template <bool F32> struct Frag;
+template <> struct Frag<true> {
+  float v[8];
+};
+template <> struct Frag<false> {
+  f16x8_t hi, lo;
+};
+
+template <bool F32> __device__ __forceinline__ Frag<F32> make_frag(const float (&x)[8]) {
+  Frag<F32> f;
+  if constexpr (F32) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f.v[j] = x[j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const Half2 s = ns_split(x[j]);
+      f.hi[j] = s.hi;
+      f.lo[j] = s.lo;
+    }
+  }
+  return f;
+}
+
+template <bool F32> __device__ __forceinline__ float frag_value(const Frag<F32> &f, int j) {
+  if constexpr (F32) return f.v[j];
+  else return (float)f.hi[j] + (float)f.lo[j];
+}
+
+// acc += A B over the 32 k of the fragments
+template <bool F32> __device__ __forceinline__ void mma(f32x4_t &acc, const Frag<F32> &a, const Frag<F32> &b) {
+  if constexpr (F32) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[j], b.v[j], acc, 0, 0, 0);
+  } else {
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.hi, b.lo, acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.lo, b.hi, acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.hi, b.hi, acc, 0, 0, 0);
+  }
+}
+
+// a fragment is 32 bytes in memory: eight floats, or eight hi then eight lo
+template <bool F32> __device__ __forceinline__ Frag<F32> load_frag(const char *p) {
+  Frag<F32> f;
+  const u32x4_t a = *reinterpret_cast<const u32x4_t *>(p), b = *reinterpret_cast<const u32x4_t *>(p + 16);
+  if constexpr (F32) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      f.v[j] = __uint_as_float(a[j]);
+      f.v[4 + j] = __uint_as_float(b[j]);
+    }
+  } else {
+    f.hi = __builtin_bit_cast(f16x8_t, a);
+    f.lo = __builtin_bit_cast(f16x8_t, b);
+  }
+  return f;
+}
+
+template <bool F32> __device__ __forceinline__ void store_frag(char *p, const Frag<F32> &f) {
+  if constexpr (F32) {
+    *reinterpret_cast<float4 *>(p) = make_float4(f.v[0], f.v[1], f.v[2], f.v[3]);
+    *reinterpret_cast<float4 *>(p + 16) = make_float4(f.v[4], f.v[5], f.v[6], f.v[7]);
+  } else {
+    *reinterpret_cast<f16x8_t *>(p) = f.hi;
+    *reinterpret_cast<f16x8_t *>(p + 16) = f.lo;
+  }
+}
+
+// element j of the fragment at p
+template <bool F32> __device__ __forceinline__ void store_element(char *p, int j, float x) {
+  if constexpr (F32) {
+    *reinterpret_cast<float *>(p + 4 * j) = x;
+  } else {
+    const Half2 s = ns_split(x);
+    *reinterpret_cast<_Float16 *>(p + 2 * j) = s.hi;
+    *reinterpret_cast<_Float16 *>(p + 16 + 2 * j) = s.lo;
+  }
+}
+
+template <int VW> __device__ __forceinline__ void load_cols(const float *p, float (&x)[VW]) {
+  if constexpr (VW == 4) {
+    const float4 a = *reinterpret_cast<const float4 *>(p);
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+  } else if constexpr (VW == 2) {
+    const float2 a = *reinterpret_cast<const float2 *>(p);
+    x[0] = a.x; x[1] = a.y;
+  } else {
+    x[0] = *p;
+  }
+}
+
+template <int VW> __device__ __forceinline__ void store_cols(float *p, const float (&x)[VW]) {
+  if constexpr (VW == 4) *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
+  else if constexpr (VW == 2) *reinterpret_cast<float2 *>(p) = make_float2(x[0], x[1]);
+  else *p = x[0];
+}
+
+// x * s1 * s2: 1 / norm can be past fp32's range where their product with x is not
+struct Scale2 {
+  float s1, s2;
+};
+__device__ __forceinline__ Scale2 scale_of(double inv, float sx) {
+  int e = 0;
+  (void)frexp(inv, &e);
+  e = min(max(e, -126), 126);
+  Scale2 s;
+  s.s1 = ldexpf(1.0f, e);
+  s.s2 = (float)(inv * (double)sx * ldexp(1.0, -e));
+  return s;
+}
+
+// ---- Gram matrix of 32 rows ----------------------------------------------------
+
+template <int MT> struct Acc {
+  f32x4_t t[Geo<MT>::TRI];
+};
+
+template <int MT> __device__ __forceinline__ void gram_add(Acc<MT> &acc, const Frag<Geo<MT>::F32> (&f)[Geo<MT>::TT]) {
+  constexpr int TT = Geo<MT>::TT;
+  int k = 0;
+#pragma unroll
+  for (int i = 0; i < TT; ++i)
+#pragma unroll
+    for (int j = i; j < TT; ++j) mma<Geo<MT>::F32>(acc.t[k++], f[i], f[j]);
+}
+
+// Rows n0 .. n0 + 31 of X [n][MT] as the Gram product's factors: a lane has rows
+// 8 g .. 8 g + 7 of its columns.
+template <int MT> struct GramRows {
+  using G = Geo<MT>;
+  float v[8][G::U][G::VW];
+  __device__ __forceinline__ void load(const float *X, int n, int n0) {
+    const int r = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int u = 0; u < G::U; ++u)
+        load_cols<G::VW>(X + (long long)min(n0 + 8 * g + j, n - 1) * MT + 64 * u + G::VW * r, v[j][u]);
+  }
+  __device__ __forceinline__ void factors(Frag<G::F32> (&f)[G::TT], int n, int n0, const Scale2 &sc) const {
+    const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int t = 0; t < G::TT; ++t) {
+      float x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = n0 + 8 * g + j < n ? v[j][t / G::VW][t % G::VW] * sc.s1 * sc.s2 : 0.f;
+      f[t] = make_frag<G::F32>(x);
+    }
+  }
+};
+
+// the four waves' accumulators added in wave order, to out [TRI][64 lanes][4]
+template <int MT> __device__ __forceinline__ void gram_out(const Acc<MT> &acc, char *lds, float unscale, float *out) {
+  using G = Geo<MT>;
+  float4 *red = reinterpret_cast<float4 *>(lds);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __syncthreads();  // whatever the LDS held has been read
+#pragma unroll
+  for (int t = 0; t < G::TRI; ++t)
+    red[(wave * G::TRI + t) * 64 + lane] = make_float4(acc.t[t][0], acc.t[t][1], acc.t[t][2], acc.t[t][3]);
+  __syncthreads();
+  for (int i = threadIdx.x; i < G::TRI * 64; i += 256) {
+    const float4 a = red[i], b = red[G::TRI * 64 + i], c = red[2 * G::TRI * 64 + i], d = red[3 * G::TRI * 64 + i];
+    reinterpret_cast<float4 *>(out)[i] = make_float4(((a.x + b.x) + (c.x + d.x)) * unscale, ((a.y + b.y) + (c.y + d.y)) * unscale,
+                                                     ((a.z + b.z) + (c.z + d.z)) * unscale, ((a.w + b.w) + (c.w + d.w)) * unscale);
+  }
+}
+
+// ---- X P of 32 rows ------------------------------------------------------------
+
+// Rows n0 .. n0 + 31 of X as the left factors of X P: a lane has row 16 s + r, columns
+// 32 kb + 8 g .. + 7.  (16 columns fill half a product: lanes g >= 2 are zero.)
+template <int MT> struct ApplyRows {
+  using G = Geo<MT>;
+  float4 v[2][G::KB][2];
+  __device__ __forceinline__ void load(const float *X, int n, int n0) {
+    const int r = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const float *p = X + (long long)min(n0 + 16 * s + r, n - 1) * MT + (MT >= 32 ? 8 * g : 8 * (g & 1));
+#pragma unroll
+      for (int kb = 0; kb < G::KB; ++kb) {
+        v[s][kb][0] = *reinterpret_cast<const float4 *>(p + 32 * kb);
+        v[s][kb][1] = *reinterpret_cast<const float4 *>(p + 32 * kb + 4);
+      }
+    }
+  }
+  __device__ __forceinline__ void factors(Frag<G::F32> (&a)[2][G::KB], int n, int n0, const Scale2 &sc) const {
+    const int r = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const bool in = n0 + 16 * s + r < n && (MT >= 32 || g < 2);
+#pragma unroll
+      for (int kb = 0; kb < G::KB; ++kb) {
+        const float4 v0 = v[s][kb][0], v1 = v[s][kb][1];
+        float x[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = in ? x[j] * sc.s1 * sc.s2 : 0.f;
+        a[s][kb] = make_frag<G::F32>(x);
+      }
+    }
+  }
+};
+
+// d[s][t] = rows 16 s + 4 g + 0..3 of slot 16 t + r of X P, P in LDS
+template <int MT>
+__device__ __forceinline__ void apply_product(f32x4_t (&d)[2][Geo<MT>::TT], const Frag<Geo<MT>::F32> (&a)[2][Geo<MT>::KB],
+                                              const char *P) {
+  using G = Geo<MT>;
+  const int r = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+  for (int s = 0; s < 2; ++s)
+#pragma unroll
+    for (int t = 0; t < G::TT; ++t) d[s][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int kb = 0; kb < G::KB; ++kb) {
+#pragma unroll
+    for (int t = 0; t < G::TT; ++t) {
+      const Frag<G::F32> b = load_frag<G::F32>(P + (16 * t + r) * G::LROW + kb * 128 + g * 32);
+#pragma unroll
+      for (int s = 0; s < 2; ++s) mma<G::F32>(d[s][t], a[s][kb], b);
+    }
+    // (without this the loads of all of P move to the front and the registers spill)
+    if (G::KB > 1) __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
+// P from the workspace to LDS
+template <int MT> __device__ __forceinline__ void load_p(const char *src, char *lds) {
+  using G = Geo<MT>;
+  constexpr int C = G::KB * 8;  // 16-byte pieces of a row
+  constexpr int N = (MT * C + 255) / 256;
+  u32x4_t v[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const int i = threadIdx.x + 256 * k;
+    if (MT * C % 256 == 0 || i < MT * C) v[k] = reinterpret_cast<const u32x4_t *>(src)[i];
+  }
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const int i = threadIdx.x + 256 * k;
+    if (MT * C % 256 == 0 || i < MT * C) *reinterpret_cast<u32x4_t *>(lds + i / C * G::LROW + i % C * 16) = v[k];
+  }
+  __syncthreads();
+}
+
+// X <- X P for the waves' rows, in place or from another buffer, and their Gram matrix.
+// `x` holds the wave's first rows (asked for before P was); the next are asked for as
+// soon as these are factors.
+template <int MT>
+__device__ __forceinline__ void apply_gram_steps(Acc<MT> &acc, ApplyRows<MT> &x, const float *src, float *dst, int n, int first,
+                                                 int stride, const Scale2 &sc, float unscale, const char *P) {
+  using G = Geo<MT>;
+  const int r = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+  for (int n0 = first * 32; n0 < n; n0 += stride * 32) {
+    f32x4_t d[2][G::TT];
+    Frag<G::F32> a[2][G::KB], f[G::TT];
+    x.factors(a, n, n0, sc);
+    if (n0 + stride * 32 < n) x.load(src, n, n0 + stride * 32);
+    apply_product<MT>(d, a, P);
+#pragma unroll
+    for (int t = 0; t < G::TT; ++t) {
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        d[j >> 2][t][j & 3] *= unscale;
+        v[j] = d[j >> 2][t][j & 3];
+      }
+      f[t] = make_frag<G::F32>(v);
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int row = n0 + 16 * s + 4 * g + q;
+        if (row < n) {
+#pragma unroll
+          for (int u = 0; u < G::U; ++u) {
+            float v[G::VW];
+#pragma unroll
+            for (int c = 0; c < G::VW; ++c) v[c] = d[s][u * G::VW + c][q];
+            store_cols<G::VW>(dst + (long long)row * MT + 64 * u + G::VW * r, v);
+          }
+        }
+      }
+    gram_add<MT>(acc, f);
+  }
+}
+
+// ---- the output -----------------------------------------------------------------
+
+struct Out {
+  void *o;
+  uint16_t *v16;
+  int update;
+  float eta, decay, gain;
+};
+
+__device__ __forceinline__ float update_one(const Out &o, float v, float x) { return v - o.eta * (o.gain * x + o.decay * v); }
+
+// W consecutive elements from e on
+template <int DT, int W> __device__ __forceinline__ void emit(const Out &o, long long e, const float (&x)[W], bool vec) {
+  if (o.update) {
+    float *v = (float *)o.o + e;
+    if (W == 4 && vec) {
+      float4 a = *reinterpret_cast<float4 *>(v);
+      a.x = update_one(o, a.x, x[0]);
+      a.y = update_one(o, a.y, x[1]);
+      a.z = update_one(o, a.z, x[W > 2 ? 2 : 0]);
+      a.w = update_one(o, a.w, x[W > 3 ? 3 : 0]);
+      *reinterpret_cast<float4 *>(v) = a;
+      if (o.v16) *reinterpret_cast<uint2 *>(o.v16 + e) = make_uint2(f2bf2(a.x, a.y), f2bf2(a.z, a.w));
+    } else {
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        const float a = update_one(o, v[i], x[i]);
+        v[i] = a;
+        if (o.v16) o.v16[e + i] = f2bf(a);
+      }
+    }
+  } else if (W == 4 && vec) {
+    if constexpr (DT == DT_F32)
+      *reinterpret_cast<float4 *>((float *)o.o + e) = make_float4(x[0], x[1], x[W > 2 ? 2 : 0], x[W > 3 ? 3 : 0]);
+    else
+      *reinterpret_cast<uint2 *>((uint16_t *)o.o + e) =
+          make_uint2(f2bf2(x[0], x[1]), f2bf2(x[W > 2 ? 2 : 0], x[W > 3 ? 3 : 0]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < W; ++i) ((typename Store<DT>::T *)o.o)[e + i] = from_f32<DT>(x[i]);
+  }
+}
+
+template <int MT, int DT>
+__device__ __forceinline__ void final_steps(const NsMat &M, const Out &o, ApplyRows<MT> &x, const float *src, int first,
+                                            int stride, const Scale2 &sc, float unscale, const char *P) {
+  using G = Geo<MT>;
+  const int r = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+  for (int n0 = first * 32; n0 < M.n; n0 += stride * 32) {
+    f32x4_t d[2][G::TT];
+    Frag<G::F32> a[2][G::KB];
+    x.factors(a, M.n, n0, sc);
+    if (n0 + stride * 32 < M.n) x.load(src, M.n, n0 + stride * 32);
+    apply_product<MT>(d, a, P);
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int u = 0; u < G::U; ++u) {
+        const int row = n0 + 16 * s + 4 * g, col = 64 * u + G::VW * r;
+        if (M.tall) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            float v[G::VW];
+#pragma unroll
+            for (int c = 0; c < G::VW; ++c) v[c] = d[s][u * G::VW + c][q] * unscale;
+            if (row + q >= M.n) continue;
+            const long long e = M.off + (long long)(row + q) * M.m + col;
+            if (col + G::VW <= M.m) {
+              emit<DT, G::VW>(o, e, v, M.m % 4 == 0);
+            } else {
+#pragma unroll
+              for (int c = 0; c < G::VW; ++c)
+                if (col + c < M.m) emit<DT, 1>(o, e + c, {v[c]}, false);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int c = 0; c < G::VW; ++c) {
+            float v[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] = d[s][u * G::VW + c][q] * unscale;
+            if (col + c >= M.m) continue;
+            const long long e = M.off + (long long)(col + c) * M.n + row;
+            if (row + 4 <= M.n) {
+              emit<DT, 4>(o, e, v, M.n % 4 == 0);
+            } else {
+#pragma unroll
+              for (int q = 0; q < 4; ++q)
+                if (row + q < M.n) emit<DT, 1>(o, e + q, {v[q]}, false);
+            }
+          }
+        }
+      }
+  }
+}
+
+// ---- the m x m polynomials --------------------------------------------------------
+
+// P of one or two steps from the Gram matrix (upper tiles, the sum of `parts` arrays
+// in order), rows in slot order, to dst [MT][KB * 128 bytes].  lds: two matrices.
+template <int MT>
+__device__ __forceinline__ void polynomial(const float *gram, int parts, const NsStage &st, float ca, float cb, float cc,
+                                           char *lds, char *dst) {
+  using G = Geo<MT>;
+  constexpr bool F = G::F32;
+  constexpr int NC = G::TT > 4 ? G::TT / 4 : 1;  // tile columns of a wave
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, g = lane >> 4;
+  const float sh0 = F ? 1.f : st.sh[0], sq0 = F ? 1.f : st.sq[0], sh1 = F ? 1.f : st.sh[1], sq1 = F ? 1.f : st.sq[1];
+  const float stt = F ? 1.f : st.st, sp = F ? 1.f : st.sp;
+  char *H = lds, *Q = lds + G::MAT;
+  for (int i = tid; i < G::TRI * 64; i += 256) {
+    float4 s = reinterpret_cast<const float4 *>(gram)[i];
+    for (int p = 1; p < parts; ++p) {
+      const float4 a = reinterpret_cast<const float4 *>(gram)[(long long)p * G::TRI * 64 + i];
+      s.x += a.x; s.y += a.y; s.z += a.z; s.w += a.w;
+    }
+    const float x[4] = {s.x * sh0, s.y * sh0, s.z * sh0, s.w * sh0};
+    int tj = i >> 6, ti = 0;
+    while (tj >= G::TT - ti) {
+      tj -= G::TT - ti;
+      ++ti;
+    }
+    tj += ti;
+    const int rr = i & 15, gg = (i & 63) >> 4;  // elements (16 ti + 4 gg + q, 16 tj + rr)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      store_element<F>(H + (16 * tj + rr) * G::LROW + (ti >> 1) * 128 + gg * 32, 4 * (ti & 1) + q, x[q]);
+      if (ti != tj)
+        store_element<F>(H + (16 * ti + 4 * gg + q) * G::LROW + (tj >> 1) * 128 + (rr >> 2) * 32, 4 * (tj & 1) + (rr & 3), x[q]);
+      if (G::TT == 1) store_element<F>(H + rr * G::LROW + gg * 32, 4 + q, 0.f);
+    }
+  }
+  __syncthreads();
+  const bool active = wave * NC < G::TT;
+  // element (tile row i, q) of the wave's column c as a factor's element
+  Frag<F> h[NC][G::KB], q0[NC][G::KB], x[NC][G::KB];
+  f32x4_t d[NC][G::TT];
+  auto product = [&](const char *A, const Frag<F>(&b)[NC][G::KB]) {  // d = A b
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int t = 0; t < G::TT; ++t) d[c][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int kb = 0; kb < G::KB; ++kb)
+#pragma unroll
+      for (int t = 0; t < G::TT; ++t) {
+        const Frag<F> a = load_frag<F>(A + (16 * t + r) * G::LROW + kb * 128 + g * 32);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) mma<F>(d[c][t], a, b[c][kb]);
+      }
+  };
+  auto factor = [&](Frag<F>(&f)[NC][G::KB], float scale) {  // f = d * scale
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int kb = 0; kb < G::KB; ++kb) {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int t = 2 * kb + (j >> 2);
+          v[j] = t < G::TT ? d[c][t < G::TT ? t : 0][j & 3] * scale : 0.f;
+        }
+        f[c][kb] = make_frag<F>(v);
+      }
+  };
+  auto put = [&](char *A, const Frag<F>(&f)[NC][G::KB]) {  // the wave's columns as rows of a symmetric matrix
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int kb = 0; kb < G::KB; ++kb) store_frag<F>(A + (16 * (wave * NC + c) + r) * G::LROW + kb * 128 + g * 32, f[c][kb]);
+  };
+  auto poly = [&](const Frag<F>(&hf)[NC][G::KB], float sh) {  // d = ca I + cb h + cc d (d: the square)
+    const float uh = 1.f / sh, us = uh * uh;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int t = 0; t < G::TT; ++t)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          float v = cb * (frag_value<F>(hf[c][t >> 1], 4 * (t & 1) + q) * uh) + cc * (d[c][t][q] * us);
+          if (t == wave * NC + c && 4 * g + q == r) v += ca;
+          d[c][t][q] = v;
+        }
+  };
+  float out = 1.f;  // scale of d when P is written
+  if (active) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int kb = 0; kb < G::KB; ++kb) h[c][kb] = load_frag<F>(H + (16 * (wave * NC + c) + r) * G::LROW + kb * 128 + g * 32);
+    product(H, h);
+    poly(h, sh0);
+    out = sq0;
+  }
+  if (st.steps == 2) {
+    if (active) {
+      factor(q0, sq0);
+      put(Q, q0);
+    }
+    __syncthreads();
+    if (active) {
+      product(Q, h);  // T = Q H
+      factor(x, stt / (sq0 * sh0));
+      product(Q, x);  // H' = Q T
+      factor(h, sh1 / (sq0 * stt));
+      put(H, h);
+    }
+    __syncthreads();
+    if (active) {
+      product(H, h);
+      poly(h, sh1);
+      factor(x, sq1);
+      product(Q, x);  // P = Q Q'
+      out = sp / (sq0 * sq1);
+    }
+  }
+  if (active) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      char *row = dst + (long long)(16 * (wave * NC + c) + r) * (G::KB * 128);
+#pragma unroll
+      for (int t = 0; t < G::TT; ++t)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int col = 64 * (t / G::VW) + G::VW * (4 * g + q) + t % G::VW;
+          store_element<F>(row + col / 8 * 32, col % 8, d[c][t][q] * out);
+          if (G::TT == 1) store_element<F>(row + (16 + 4 * g) / 8 * 32, (4 * g + q) % 8, 0.f);
+        }
+    }
+  }
+}
+
+// ---- kernels ----------------------------------------------------------------------
+
+// calls f.template run<MT>() for the matrix's width, MT <= MAX
+#define CF_NS_WIDTH(MAX, mt, CALL)                        \
+  {                                                       \
+    if (MAX >= 128 && (mt) == 128) CALL(128)              \
+    else if (MAX >= 64 && (mt) == 64) CALL(64)            \
+    else if ((mt) == 32) CALL(32)                         \
+    else CALL(16)                                         \
+  }
+
+template <int MAX> constexpr int lds_bytes() {
+  using G = Geo<MAX>;
+  return 2 * G::MAT > G::RED ? 2 * G::MAT : G::RED;
+}
+
+__device__ __forceinline__ const float *ns_source(const NsMat &M, const char *ws, const void *g) {
+  return M.ws_u >= 0 ? (const float *)(ws + M.ws_u) : (const float *)g + M.off;
+}
+
+// Rows [r0, r1) of the long side: momentum, the update into u [n][mt] (zero padding
+// columns) unless the matrix is read where it is, and the sum of its squares.
+template <int DT, bool MOM>
+__device__ __forceinline__ double prep_rows(const NsMat &M, const NsMomentum &mom, const void *g, float *m, float *u, int r0,
+                                            int r1, float *tile) {
+  using S = typename Store<DT>::T;
+  const S *gp = (const S *)g + M.off;
+  double s = 0.0;
+  if (M.tall) {
+    const long long beg = (long long)r0 * M.m, end = (long long)r1 * M.m;
+    if (M.m == M.mt) {  // the layouts agree
+      for (long long e = beg + 4 * threadIdx.x; e < end; e += 4 * 256) {
+        float x[4];
+        if constexpr (DT == DT_F32) {
+          load_cols<4>((const float *)gp + e, x);
+        } else {
+          const uint2 a = *reinterpret_cast<const uint2 *>(gp + e);
+          x[0] = __uint_as_float(a.x << 16);
+          x[1] = __uint_as_float(a.x & 0xffff0000u);
+          x[2] = __uint_as_float(a.y << 16);
+          x[3] = __uint_as_float(a.y & 0xffff0000u);
+        }
+        if constexpr (MOM) {
+          float mv[4];
+          load_cols<4>(m + M.off + e, mv);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[i] = ns_momentum(mom, x[i], mv[i]);
+          store_cols<4>(m + M.off + e, mv);
+        }
+        if (M.ws_u >= 0) store_cols<4>(u + e, x);
+        s += ((double)x[0] * x[0] + (double)x[1] * x[1]) + ((double)x[2] * x[2] + (double)x[3] * x[3]);
+      }
+    } else {
+      for (long long k = (long long)r0 * M.mt + threadIdx.x; k < (long long)r1 * M.mt; k += 256) {
+        const long long row = k / M.mt;
+        const int col = (int)(k % M.mt);
+        float x = 0.f;
+        if (col < M.m) {
+          const long long e = row * M.m + col;
+          x = to_f32<DT>(gp[e]);
+          if constexpr (MOM) x = ns_momentum(mom, x, m[M.off + e]);
+        }
+        u[k] = x;
+        s += (double)x * x;
+      }
+    }
+    return s;
+  }
+  // wide: 64 columns at a time through a tile, rows of u are columns of the matrix
+  const int c = threadIdx.x & 63;
+  for (int n0 = r0; n0 < r1; n0 += 64) {
+    for (int i = threadIdx.x >> 6; i < M.mt; i += 4) {
+      float x = 0.f;
+      if (i < M.m && n0 + c < r1) {
+        const long long e = (long long)i * M.n + n0 + c;
+        x = to_f32<DT>(gp[e]);
+        if constexpr (MOM) x = ns_momentum(mom, x, m[M.off + e]);
+      }
+      tile[i * 65 + c] = x;
+      s += (double)x * x;
+    }
+    __syncthreads();
+    for (int k = threadIdx.x; k < 64 * M.mt; k += 256) {
+      const int row = k / M.mt, col = k % M.mt;
+      if (n0 + row < r1) u[(long long)(n0 + row) * M.mt + col] = tile[col * 65 + row];
+    }
+    __syncthreads();
+  }
+  return s;
+}
+
+template <int DT, bool MOM>
+__global__ __launch_bounds__(256) void skinny_prep_kernel(NsTable T, NsMomentum mom, const void *g, float *m, char *ws) {
+  __shared__ double red[4];
+  __shared__ float tile[128 * 65];
+  const int l = ns_find(T, blockIdx.x);
+  const NsMat &M = T.mat[l];
+  const int chunk = blockIdx.x - T.first[l], r0 = chunk * M.prow, r1 = min(r0 + M.prow, M.n);
+  const double s = ns_block_sum(prep_rows<DT, MOM>(M, mom, g, m, (float *)(ws + M.ws_u), r0, r1, tile), red);
+  if (threadIdx.x == 0) ((double *)(ws + M.ws_norm))[chunk] = s;
+}
+
+// Gram matrix of X = u / (||u|| + eps)
+template <int MAX> __global__ __launch_bounds__(256) void skinny_gram_kernel(NsTable T, NsStage st, double eps, const void *g, char *ws) {
+  __shared__ __attribute__((aligned(16))) char lds[lds_bytes<MAX>()];
+  __shared__ double red[4];
+  const int l = ns_find(T, blockIdx.x);
+  const NsMat &M = T.mat[l];
+  const int b = blockIdx.x - T.first[l];
+  const float *X = ns_source(M, ws, g);
+  const int first = b * 4 + (threadIdx.x >> 6), stride = M.slices * 4;
+#define CALL(MT)                                                                                              \
+  {                                                                                                           \
+    GramRows<MT> x;                                                                                           \
+    x.load(X, M.n, first * 32);                                                                               \
+    const float sx = Geo<MT>::F32 ? 1.f : st.sx;                                                              \
+    const Scale2 sc = scale_of(ns_inv_norm(M, ws, eps, red), sx);                                             \
+    Acc<MT> acc{};                                                                                            \
+    for (int n0 = first * 32; n0 < M.n; n0 += stride * 32) {                                                  \
+      Frag<Geo<MT>::F32> f[Geo<MT>::TT];                                                                      \
+      x.factors(f, M.n, n0, sc);                                                                              \
+      if (n0 + stride * 32 < M.n) x.load(X, M.n, n0 + stride * 32);                                           \
+      gram_add<MT>(acc, f);                                                                                   \
+    }                                                                                                         \
+    gram_out<MT>(acc, lds, 1.f / (sx * sx), (float *)(ws + M.ws_part) + (long long)b * (Geo<MT>::TRI * 256));  \
+  }
+  CF_NS_WIDTH(MAX, M.mt, CALL)
+#undef CALL
+}
+
+// sums of many workgroups' Gram matrices: 64 columns of float4 by 4 phases a workgroup
+__global__ __launch_bounds__(256) void skinny_sum_kernel(NsTable T, char *ws) {
+  __shared__ float4 red[256];
+  const int l = ns_find(T, blockIdx.x);
+  const NsMat &M = T.mat[l];
+  const int tt = M.mt / 16, cols = tt * (tt + 1) / 2 * 64;  // float4 of a Gram matrix
+  const int c = (blockIdx.x - T.first[l]) * 16 + (threadIdx.x & 15), ph = threadIdx.x >> 4;
+  const float4 *part = (const float4 *)(ws + M.ws_part);
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int i = ph; i < M.slices; i += 16) {
+    const float4 a = part[(long long)i * cols + c];
+    s.x += a.x; s.y += a.y; s.z += a.z; s.w += a.w;
+  }
+  red[threadIdx.x] = s;
+  __syncthreads();
+  for (int st = 8; st > 0; st >>= 1) {
+    if (ph < st) {
+      const float4 a = red[threadIdx.x + st * 16];
+      float4 b = red[threadIdx.x];
+      b.x += a.x; b.y += a.y; b.z += a.z; b.w += a.w;
+      red[threadIdx.x] = b;
+    }
+    __syncthreads();
+  }
+  if (ph == 0) ((float4 *)(ws + M.ws_sum))[c] = red[threadIdx.x];
+}
+
+template <int MAX> __global__ __launch_bounds__(256) void skinny_poly_kernel(NsTable T, NsStage st, float a, float b, float c, char *ws) {
+  __shared__ __attribute__((aligned(16))) char lds[2 * Geo<MAX>::MAT];
+  const int l = ns_find(T, blockIdx.x);
+  const NsMat &M = T.mat[l];
+  const bool summed = M.slices > kNsFewSlices;
+  const float *gram = (const float *)(ws + (summed ? M.ws_sum : M.ws_part));
+#define CALL(MT) polynomial<MT>(gram, summed ? 1 : M.slices, st, a, b, c, lds, ws + M.ws_sq);
+  CF_NS_WIDTH(MAX, M.mt, CALL)
+#undef CALL
+}
+
+// X <- X P (from the matrix itself in the first stage) and the Gram matrix of the result
+template <int MAX>
+__global__ __launch_bounds__(256) void skinny_apply_kernel(NsTable T, NsStage st, float next_sx, int first_stage, double eps,
+                                                           const void *g, char *ws) {
+  __shared__ __attribute__((aligned(16))) char lds[lds_bytes<MAX>()];
+  __shared__ double red[4];
+  const int l = ns_find(T, blockIdx.x);
+  const NsMat &M = T.mat[l];
+  const int b = blockIdx.x - T.first[l];
+  float *X = (float *)(ws + M.ws_xn);
+  const float *src = first_stage ? ns_source(M, ws, g) : X;
+  const int first = b * 4 + (threadIdx.x >> 6), stride = M.slices * 4;
+#define CALL(MT)                                                                                               \
+  {                                                                                                            \
+    ApplyRows<MT> x;                                                                                           \
+    x.load(src, M.n, first * 32);                                                                              \
+    constexpr bool F = Geo<MT>::F32;                                                                           \
+    const float sx = F ? 1.f : st.sx, sp = F ? 1.f : st.steps == 2 ? st.sp : st.sq[0], sn = F ? 1.f : next_sx; \
+    const Scale2 sc = first_stage ? scale_of(ns_inv_norm(M, ws, eps, red), sx) : Scale2{1.f, 1.f};             \
+    load_p<MT>(ws + M.ws_sq, lds);                                                                             \
+    Acc<MT> acc{};                                                                                             \
+    apply_gram_steps<MT>(acc, x, src, X, M.n, first, stride, sc, sn / (sx * sp), lds);                         \
+    gram_out<MT>(acc, lds, 1.f / (sn * sn), (float *)(ws + M.ws_part) + (long long)b * (Geo<MT>::TRI * 256));   \
+  }
+  CF_NS_WIDTH(MAX, M.mt, CALL)
+#undef CALL
+}
+
+template <int MAX, int DT>
+__global__ __launch_bounds__(256, 2) void skinny_final_kernel(NsTable T, NsStage st, int first_stage, double eps, const void *g,
+                                                           Out o, char *ws) {
+  __shared__ __attribute__((aligned(16))) char lds[Geo<MAX>::MAT];
+  __shared__ double red[4];
+  const int l = ns_find(T, blockIdx.x);
+  const NsMat &M = T.mat[l];
+  const int b = blockIdx.x - T.first[l];
+  const float *src = first_stage ? ns_source(M, ws, g) : (const float *)(ws + M.ws_xn);
+  const int first = b * 4 + (threadIdx.x >> 6), stride = M.slices * 4;
+  o.gain = M.gain;
+#define CALL(MT)                                                                                                   \
+  {                                                                                                                \
+    ApplyRows<MT> x;                                                                                               \
+    x.load(src, M.n, first * 32);                                                                                  \
+    constexpr bool F = Geo<MT>::F32;                                                                               \
+    const float sx = F ? 1.f : st.sx, sp = F ? 1.f : st.steps == 2 ? st.sp : st.sq[0];                              \
+    const Scale2 sc = first_stage ? scale_of(ns_inv_norm(M, ws, eps, red), sx) : Scale2{1.f, 1.f};                 \
+    load_p<MT>(ws + M.ws_sq, lds);                                                                                 \
+    final_steps<MT, DT>(M, o, x, src, first, stride, sc, 1.f / (sx * sp), lds);                                    \
+  }
+  CF_NS_WIDTH(MAX, M.mt, CALL)
+#undef CALL
+}
+
+template <int MAX>
+hipError_t run(const NsTable &T0, const NsSteps &S, int dtype, const void *g, const NsMomentum *mom, float *m,
+               const NsUpdate *up, void *out, uint16_t *v16, char *ws, hipStream_t st) {
+  NsTable T = T0;
+  auto number = [&](auto blocks) {
+    int at = 0;
+    for (int l = 0; l < T.count; ++l) {
+      T.first[l] = at;
+      if (T.mat[l].mt) at += blocks(T.mat[l]);
+    }
+    T.first[T.count] = at;
+    return at;
+  };
+  int nb = number([](const NsMat &M) { return M.chunks; });
+  if (mom)
+    hipLaunchKernelGGL((skinny_prep_kernel<DT_F32, true>), dim3(nb), dim3(256), 0, st, T, *mom, g, m, ws);
+  else if (dtype == DT_BF16)
+    hipLaunchKernelGGL((skinny_prep_kernel<DT_BF16, false>), dim3(nb), dim3(256), 0, st, T, NsMomentum{}, g, m, ws);
+  else
+    hipLaunchKernelGGL((skinny_prep_kernel<DT_F32, false>), dim3(nb), dim3(256), 0, st, T, NsMomentum{}, g, m, ws);
+  const int slabs = number([](const NsMat &M) { return M.slices; });
+  hipLaunchKernelGGL((skinny_gram_kernel<MAX>), dim3(slabs), dim3(256), 0, st, T, S.stage[0], S.eps, g, ws);
+  for (int s = 0; s < S.stages; ++s) {
+    nb = number([](const NsMat &M) {
+      const int tt = M.mt / 16;
+      return M.slices > kNsFewSlices ? tt * (tt + 1) / 2 * 4 : 0;
+    });
+    if (nb) hipLaunchKernelGGL(skinny_sum_kernel, dim3(nb), dim3(256), 0, st, T, ws);
+    nb = number([](const NsMat &) { return 1; });
+    hipLaunchKernelGGL((skinny_poly_kernel<MAX>), dim3(nb), dim3(256), 0, st, T, S.stage[s], (float)S.a, (float)S.b,
+                       (float)S.c, ws);
+    number([](const NsMat &M) { return M.slices; });
+    if (s + 1 < S.stages) {
+      hipLaunchKernelGGL((skinny_apply_kernel<MAX>), dim3(slabs), dim3(256), 0, st, T, S.stage[s], S.stage[s + 1].sx, s == 0,
+                         S.eps, g, ws);
+    } else {
+      const Out o{out, v16, up != nullptr, up ? up->eta : 0.f, up ? up->decay : 0.f, 0.f};
+      if (dtype == DT_BF16)
+        hipLaunchKernelGGL((skinny_final_kernel<MAX, DT_BF16>), dim3(slabs), dim3(256), 0, st, T, S.stage[s], s == 0, S.eps, g,
+                           o, ws);
+      else
+        hipLaunchKernelGGL((skinny_final_kernel<MAX, DT_F32>), dim3(slabs), dim3(256), 0, st, T, S.stage[s], s == 0, S.eps, g, o,
+                           ws);
+    }
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_ns_skinny(const NsTable &T, const NsSteps &S, int dtype, const void *g, const NsMomentum *mom, float *m,
+                            const NsUpdate *up, void *out, uint16_t *v16, void *ws, hipStream_t st) {
+  int most = 0;
+  for (int l = 0; l < T.count; ++l) most = T.mat[l].mt > most ? T.mat[l].mt : most;
+  if (most == 0) return hipSuccess;
+  if (most > 64) return run<128>(T, S, dtype, g, mom, m, up, out, v16, (char *)ws, st);
+  if (most > 32) return run<64>(T, S, dtype, g, mom, m, up, out, v16, (char *)ws, st);
+  return run<32>(T, S, dtype, g, mom, m, up, out, v16, (char *)ws, st);
+}
+
+}  // namespace cf
