@@ -45,6 +45,25 @@ __device__ __forceinline__ Half2 ns_split(float x) {
   return r;
 }
 
+// The same of eight values at two instructions a value: hi by pairs, the remainder
+// x - hi as a mixed-precision fma, which reads hi's halves in place.
+__device__ __forceinline__ void ns_split8(const float (&x)[8], f16x8_t &hi, f16x8_t &lo) {
+  typedef float f32x2_t __attribute__((ext_vector_type(2)));
+  typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) {
+    const f16x2_t h = __builtin_convertvector((f32x2_t{x[i], x[i + 1]}), f16x2_t);
+    float a, b;
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(a) : "v"(h), "v"(x[i]));
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(b) : "v"(h), "v"(x[i + 1]));
+    const f16x2_t l = __builtin_convertvector((f32x2_t{a, b}), f16x2_t);
+    hi[i] = h[0];
+    hi[i + 1] = h[1];
+    lo[i] = l[0];
+    lo[i + 1] = l[1];
+  }
+}
+
 // one element of the momentum update: new momentum in m, returns the update u
 __device__ __forceinline__ float ns_momentum(const NsMomentum &mom, float g, float &m) {
   const float gi = (float)mom.one_mu * g;

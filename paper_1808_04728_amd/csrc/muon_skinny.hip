@@ -56,12 +56,7 @@ template <bool F32> __device__ __forceinline__ Frag<F32> make_frag(const float (
 #pragma unroll
     for (int j = 0; j < 8; ++j) f.v[j] = x[j];
   } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const Half2 s = ns_split(x[j]);
-      f.hi[j] = s.hi;
-      f.lo[j] = s.lo;
-    }
+    ns_split8(x, f.hi, f.lo);
   }
   return f;
 }
@@ -110,14 +105,22 @@ template <bool F32> __device__ __forceinline__ void store_frag(char *p, const Fr
   }
 }
 
-// element j of the fragment at p
-template <bool F32> __device__ __forceinline__ void store_element(char *p, int j, float x) {
+// elements j .. j + N - 1 of the fragment at p (j a multiple of N)
+template <bool F32, int N> __device__ __forceinline__ void store_elements(char *p, int j, const float (&x)[N]) {
   if constexpr (F32) {
-    *reinterpret_cast<float *>(p + 4 * j) = x;
+#pragma unroll
+    for (int i = 0; i < N; ++i) reinterpret_cast<float *>(p + 4 * j)[i] = x[i];
   } else {
-    const Half2 s = ns_split(x);
-    *reinterpret_cast<_Float16 *>(p + 2 * j) = s.hi;
-    *reinterpret_cast<_Float16 *>(p + 16 + 2 * j) = s.lo;
+    typedef _Float16 vec_t __attribute__((ext_vector_type(N)));
+    vec_t hi, lo;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const Half2 s = ns_split(x[i]);
+      hi[i] = s.hi;
+      lo[i] = s.lo;
+    }
+    *reinterpret_cast<vec_t *>(p + 2 * j) = hi;
+    *reinterpret_cast<vec_t *>(p + 16 + 2 * j) = lo;
   }
 }
 
@@ -139,20 +142,22 @@ template <int VW> __device__ __forceinline__ void store_cols(float *p, const flo
   else *p = x[0];
 }
 
-// x * s1 * s2: 1 / norm can be past fp32's range where their product with x is not
-struct Scale2 {
+// x s1 s2.  s1 is 1 unless 1 / norm is past where fp32's range ends but its product
+// with x is not; without `on` x is taken as it is.
+struct Scale {
+  bool on;
   float s1, s2;
 };
-__device__ __forceinline__ Scale2 scale_of(double inv, float sx) {
+__device__ __forceinline__ Scale scale_of(double inv, float sx) {
   int e = 0;
   (void)frexp(inv, &e);
-  e = min(max(e, -126), 126);
-  Scale2 s;
+  Scale s;
+  s.on = true;
+  e = e > 100 || e < -100 ? min(max(e, -126), 126) : 0;
   s.s1 = ldexpf(1.0f, e);
   s.s2 = (float)(inv * (double)sx * ldexp(1.0, -e));
   return s;
 }
-
 // ---- Gram matrix of 32 rows ----------------------------------------------------
 
 template <int MT> struct Acc {
@@ -181,15 +186,25 @@ template <int MT> struct GramRows {
       for (int u = 0; u < G::U; ++u)
         load_cols<G::VW>(X + (long long)min(n0 + 8 * g + j, n - 1) * MT + 64 * u + G::VW * r, v[j][u]);
   }
-  __device__ __forceinline__ void factors(Frag<G::F32> (&f)[G::TT], int n, int n0, const Scale2 &sc) const {
+  __device__ __forceinline__ void factors(Frag<G::F32> (&f)[G::TT], int n, int n0, const Scale &sc) {
     const int g = (threadIdx.x & 63) >> 4;
+    if (sc.s1 != 1.f) each([&](float &x, int) { x *= sc.s1; });
+    if (n0 + 32 > n) each([&](float &x, int j) { x = n0 + 8 * g + j < n ? x : 0.f; });
 #pragma unroll
     for (int t = 0; t < G::TT; ++t) {
       float x[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = n0 + 8 * g + j < n ? v[j][t / G::VW][t % G::VW] * sc.s1 * sc.s2 : 0.f;
+      for (int j = 0; j < 8; ++j) x[j] = v[j][t / G::VW][t % G::VW] * sc.s2;
       f[t] = make_frag<G::F32>(x);
     }
+  }
+  template <class F> __device__ __forceinline__ void each(F f) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int u = 0; u < G::U; ++u)
+#pragma unroll
+        for (int c = 0; c < G::VW; ++c) f(v[j][u][c], j);
   }
 };
 
@@ -216,7 +231,7 @@ template <int MT> __device__ __forceinline__ void gram_out(const Acc<MT> &acc, c
 // 32 kb + 8 g .. + 7.  (16 columns fill half a product: lanes g >= 2 are zero.)
 template <int MT> struct ApplyRows {
   using G = Geo<MT>;
-  float4 v[2][G::KB][2];
+  float v[2][G::KB][8];
   __device__ __forceinline__ void load(const float *X, int n, int n0) {
     const int r = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
 #pragma unroll
@@ -224,25 +239,36 @@ template <int MT> struct ApplyRows {
       const float *p = X + (long long)min(n0 + 16 * s + r, n - 1) * MT + (MT >= 32 ? 8 * g : 8 * (g & 1));
 #pragma unroll
       for (int kb = 0; kb < G::KB; ++kb) {
-        v[s][kb][0] = *reinterpret_cast<const float4 *>(p + 32 * kb);
-        v[s][kb][1] = *reinterpret_cast<const float4 *>(p + 32 * kb + 4);
+        float a[4], b[4];
+        load_cols<4>(p + 32 * kb, a);
+        load_cols<4>(p + 32 * kb + 4, b);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          v[s][kb][j] = a[j];
+          v[s][kb][4 + j] = b[j];
+        }
       }
     }
   }
-  __device__ __forceinline__ void factors(Frag<G::F32> (&a)[2][G::KB], int n, int n0, const Scale2 &sc) const {
+  __device__ __forceinline__ void factors(Frag<G::F32> (&a)[2][G::KB], int n, int n0, const Scale &sc) {
     const int r = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const bool in = n0 + 16 * s + r < n && (MT >= 32 || g < 2);
-#pragma unroll
-      for (int kb = 0; kb < G::KB; ++kb) {
-        const float4 v0 = v[s][kb][0], v1 = v[s][kb][1];
-        float x[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = in ? x[j] * sc.s1 * sc.s2 : 0.f;
-        a[s][kb] = make_frag<G::F32>(x);
-      }
+    if (sc.on) {
+      if (sc.s1 != 1.f) each([&](float &x, int) { x *= sc.s1; });
+      each([&](float &x, int) { x *= sc.s2; });
     }
+    if (n0 + 32 > n || MT < 32) each([&](float &x, int s) { x = n0 + 16 * s + r < n && (MT >= 32 || g < 2) ? x : 0.f; });
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int kb = 0; kb < G::KB; ++kb) a[s][kb] = make_frag<G::F32>(v[s][kb]);
+  }
+  template <class F> __device__ __forceinline__ void each(F f) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int kb = 0; kb < G::KB; ++kb)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f(v[s][kb][j], s);
   }
 };
 
@@ -293,7 +319,7 @@ template <int MT> __device__ __forceinline__ void load_p(const char *src, char *
 // soon as these are factors.
 template <int MT>
 __device__ __forceinline__ void apply_gram_steps(Acc<MT> &acc, ApplyRows<MT> &x, const float *src, float *dst, int n, int first,
-                                                 int stride, const Scale2 &sc, float unscale, const char *P) {
+                                                 int stride, const Scale &sc, float unscale, const char *P) {
   using G = Geo<MT>;
   const int r = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
   for (int n0 = first * 32; n0 < n; n0 += stride * 32) {
@@ -376,15 +402,15 @@ template <int DT, int W> __device__ __forceinline__ void emit(const Out &o, long
 
 template <int MT, int DT>
 __device__ __forceinline__ void final_steps(const NsMat &M, const Out &o, ApplyRows<MT> &x, const float *src, int first,
-                                            int stride, const Scale2 &sc, float unscale, const char *P) {
+                                            int stride, const Scale &sc, float unscale, const char *P) {
   using G = Geo<MT>;
   const int r = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
   for (int n0 = first * 32; n0 < M.n; n0 += stride * 32) {
     f32x4_t d[2][G::TT];
     Frag<G::F32> a[2][G::KB];
     x.factors(a, M.n, n0, sc);
-    if (n0 + stride * 32 < M.n) x.load(src, M.n, n0 + stride * 32);
     apply_product<MT>(d, a, P);
+    if (n0 + stride * 32 < M.n) x.load(src, M.n, n0 + stride * 32);
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -441,26 +467,40 @@ __device__ __forceinline__ void polynomial(const float *gram, int parts, const N
   const float sh0 = F ? 1.f : st.sh[0], sq0 = F ? 1.f : st.sq[0], sh1 = F ? 1.f : st.sh[1], sq1 = F ? 1.f : st.sq[1];
   const float stt = F ? 1.f : st.st, sp = F ? 1.f : st.sp;
   char *H = lds, *Q = lds + G::MAT;
-  for (int i = tid; i < G::TRI * 64; i += 256) {
-    float4 s = reinterpret_cast<const float4 *>(gram)[i];
-    for (int p = 1; p < parts; ++p) {
-      const float4 a = reinterpret_cast<const float4 *>(gram)[(long long)p * G::TRI * 64 + i];
-      s.x += a.x; s.y += a.y; s.z += a.z; s.w += a.w;
-    }
-    const float x[4] = {s.x * sh0, s.y * sh0, s.z * sh0, s.w * sh0};
-    int tj = i >> 6, ti = 0;
-    while (tj >= G::TT - ti) {
-      tj -= G::TT - ti;
-      ++ti;
-    }
-    tj += ti;
-    const int rr = i & 15, gg = (i & 63) >> 4;  // elements (16 ti + 4 gg + q, 16 tj + rr)
+  {
+    constexpr int N = (G::TRI + 3) / 4;  // tiles of a wave
+    const int w = __builtin_amdgcn_readfirstlane(wave);
+    float4 s[N];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      store_element<F>(H + (16 * tj + rr) * G::LROW + (ti >> 1) * 128 + gg * 32, 4 * (ti & 1) + q, x[q]);
-      if (ti != tj)
-        store_element<F>(H + (16 * ti + 4 * gg + q) * G::LROW + (tj >> 1) * 128 + (rr >> 2) * 32, 4 * (tj & 1) + (rr & 3), x[q]);
-      if (G::TT == 1) store_element<F>(H + rr * G::LROW + gg * 32, 4 + q, 0.f);
+    for (int k = 0; k < N; ++k)
+      if (w + 4 * k < G::TRI) s[k] = reinterpret_cast<const float4 *>(gram)[(w + 4 * k) * 64 + lane];
+    for (int p = 1; p < parts; ++p) {
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+        if (w + 4 * k < G::TRI) {
+          const float4 a = reinterpret_cast<const float4 *>(gram)[((long long)p * G::TRI + w + 4 * k) * 64 + lane];
+          s[k].x += a.x; s[k].y += a.y; s[k].z += a.z; s[k].w += a.w;
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      if (w + 4 * k >= G::TRI) continue;
+      int tj = w + 4 * k, ti = 0;
+      while (tj >= G::TT - ti) {
+        tj -= G::TT - ti;
+        ++ti;
+      }
+      tj += ti;
+      // elements (16 ti + 4 g + q, 16 tj + r): as row 16 tj + r, and mirrored
+      const float x[4] = {s[k].x * sh0, s[k].y * sh0, s[k].z * sh0, s[k].w * sh0};
+      store_elements<F, 4>(H + (16 * tj + r) * G::LROW + (ti >> 1) * 128 + g * 32, 4 * (ti & 1), x);
+      if (ti != tj) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          store_elements<F, 1>(H + (16 * ti + 4 * g + q) * G::LROW + (tj >> 1) * 128 + (r >> 2) * 32, 4 * (tj & 1) + (r & 3),
+                               {x[q]});
+      }
+      if (G::TT == 1) store_elements<F, 4>(H + r * G::LROW + g * 32, 4, {0.f, 0.f, 0.f, 0.f});
     }
   }
   __syncthreads();
@@ -552,12 +592,15 @@ __device__ __forceinline__ void polynomial(const float *gram, int parts, const N
     for (int c = 0; c < NC; ++c) {
       char *row = dst + (long long)(16 * (wave * NC + c) + r) * (G::KB * 128);
 #pragma unroll
-      for (int t = 0; t < G::TT; ++t)
+      for (int u = 0; u < G::U; ++u)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const int col = 64 * (t / G::VW) + G::VW * (4 * g + q) + t % G::VW;
-          store_element<F>(row + col / 8 * 32, col % 8, d[c][t][q] * out);
-          if (G::TT == 1) store_element<F>(row + (16 + 4 * g) / 8 * 32, (4 * g + q) % 8, 0.f);
+          const int col = 64 * u + G::VW * (4 * g + q);
+          float v[G::VW];
+#pragma unroll
+          for (int k = 0; k < G::VW; ++k) v[k] = d[c][u * G::VW + k][q] * out;
+          store_elements<F, G::VW>(row + col / 8 * 32, col % 8, v);
+          if (G::TT == 1) store_elements<F, 1>(row + (16 + 4 * g) / 8 * 32, (4 * g + q) % 8, {0.f});
         }
     }
   }
@@ -679,7 +722,7 @@ template <int MAX> __global__ __launch_bounds__(256) void skinny_gram_kernel(NsT
     GramRows<MT> x;                                                                                           \
     x.load(X, M.n, first * 32);                                                                               \
     const float sx = Geo<MT>::F32 ? 1.f : st.sx;                                                              \
-    const Scale2 sc = scale_of(ns_inv_norm(M, ws, eps, red), sx);                                             \
+    const Scale sc = scale_of(ns_inv_norm(M, ws, eps, red), sx);                                             \
     Acc<MT> acc{};                                                                                            \
     for (int n0 = first * 32; n0 < M.n; n0 += stride * 32) {                                                  \
       Frag<Geo<MT>::F32> f[Geo<MT>::TT];                                                                      \
@@ -750,7 +793,7 @@ __global__ __launch_bounds__(256) void skinny_apply_kernel(NsTable T, NsStage st
     x.load(src, M.n, first * 32);                                                                              \
     constexpr bool F = Geo<MT>::F32;                                                                           \
     const float sx = F ? 1.f : st.sx, sp = F ? 1.f : st.steps == 2 ? st.sp : st.sq[0], sn = F ? 1.f : next_sx; \
-    const Scale2 sc = first_stage ? scale_of(ns_inv_norm(M, ws, eps, red), sx) : Scale2{1.f, 1.f};             \
+    const Scale sc = first_stage ? scale_of(ns_inv_norm(M, ws, eps, red), sx) : Scale{false, 1.f, 1.f};             \
     load_p<MT>(ws + M.ws_sq, lds);                                                                             \
     Acc<MT> acc{};                                                                                             \
     apply_gram_steps<MT>(acc, x, src, X, M.n, first, stride, sc, sn / (sx * sp), lds);                         \
@@ -759,6 +802,9 @@ __global__ __launch_bounds__(256) void skinny_apply_kernel(NsTable T, NsStage st
   CF_NS_WIDTH(MAX, M.mt, CALL)
 #undef CALL
 }
+
+// workgroups of the last product: two fit a compute unit
+__host__ __device__ inline int final_groups(const NsMat &M) { return min((M.n + 127) / 128, 2 * kNumCUs); }
 
 template <int MAX, int DT>
 __global__ __launch_bounds__(256, 2) void skinny_final_kernel(NsTable T, NsStage st, int first_stage, double eps, const void *g,
@@ -769,7 +815,7 @@ __global__ __launch_bounds__(256, 2) void skinny_final_kernel(NsTable T, NsStage
   const NsMat &M = T.mat[l];
   const int b = blockIdx.x - T.first[l];
   const float *src = first_stage ? ns_source(M, ws, g) : (const float *)(ws + M.ws_xn);
-  const int first = b * 4 + (threadIdx.x >> 6), stride = M.slices * 4;
+  const int first = b * 4 + (threadIdx.x >> 6), stride = final_groups(M) * 4;
   o.gain = M.gain;
 #define CALL(MT)                                                                                                   \
   {                                                                                                                \
@@ -777,7 +823,7 @@ __global__ __launch_bounds__(256, 2) void skinny_final_kernel(NsTable T, NsStage
     x.load(src, M.n, first * 32);                                                                                  \
     constexpr bool F = Geo<MT>::F32;                                                                               \
     const float sx = F ? 1.f : st.sx, sp = F ? 1.f : st.steps == 2 ? st.sp : st.sq[0];                              \
-    const Scale2 sc = first_stage ? scale_of(ns_inv_norm(M, ws, eps, red), sx) : Scale2{1.f, 1.f};                 \
+    const Scale sc = first_stage ? scale_of(ns_inv_norm(M, ws, eps, red), sx) : Scale{false, 1.f, 1.f};                 \
     load_p<MT>(ws + M.ws_sq, lds);                                                                                 \
     final_steps<MT, DT>(M, o, x, src, first, stride, sc, 1.f / (sx * sp), lds);                                    \
   }
@@ -821,12 +867,13 @@ hipError_t run(const NsTable &T0, const NsSteps &S, int dtype, const void *g, co
       hipLaunchKernelGGL((skinny_apply_kernel<MAX>), dim3(slabs), dim3(256), 0, st, T, S.stage[s], S.stage[s + 1].sx, s == 0,
                          S.eps, g, ws);
     } else {
+      nb = number([](const NsMat &M) { return final_groups(M); });
       const Out o{out, v16, up != nullptr, up ? up->eta : 0.f, up ? up->decay : 0.f, 0.f};
       if (dtype == DT_BF16)
-        hipLaunchKernelGGL((skinny_final_kernel<MAX, DT_BF16>), dim3(slabs), dim3(256), 0, st, T, S.stage[s], s == 0, S.eps, g,
+        hipLaunchKernelGGL((skinny_final_kernel<MAX, DT_BF16>), dim3(nb), dim3(256), 0, st, T, S.stage[s], s == 0, S.eps, g,
                            o, ws);
       else
-        hipLaunchKernelGGL((skinny_final_kernel<MAX, DT_F32>), dim3(slabs), dim3(256), 0, st, T, S.stage[s], s == 0, S.eps, g, o,
+        hipLaunchKernelGGL((skinny_final_kernel<MAX, DT_F32>), dim3(nb), dim3(256), 0, st, T, S.stage[s], s == 0, S.eps, g, o,
                            ws);
     }
   }
