@@ -368,36 +368,45 @@ struct Out {
 
 __device__ __forceinline__ float update_one(const Out &o, float v, float x) { return v - o.eta * (o.gain * x + o.decay * v); }
 
-// W consecutive elements from e on
-template <int DT, int W> __device__ __forceinline__ void emit(const Out &o, long long e, const float (&x)[W], bool vec) {
+// element e
+template <int DT> __device__ __forceinline__ void emit1(const Out &o, long long e, float x) {
   if (o.update) {
     float *v = (float *)o.o + e;
-    if (W == 4 && vec) {
-      float4 a = *reinterpret_cast<float4 *>(v);
-      a.x = update_one(o, a.x, x[0]);
-      a.y = update_one(o, a.y, x[1]);
-      a.z = update_one(o, a.z, x[W > 2 ? 2 : 0]);
-      a.w = update_one(o, a.w, x[W > 3 ? 3 : 0]);
-      *reinterpret_cast<float4 *>(v) = a;
-      if (o.v16) *reinterpret_cast<uint2 *>(o.v16 + e) = make_uint2(f2bf2(a.x, a.y), f2bf2(a.z, a.w));
-    } else {
-#pragma unroll
-      for (int i = 0; i < W; ++i) {
-        const float a = update_one(o, v[i], x[i]);
-        v[i] = a;
-        if (o.v16) o.v16[e + i] = f2bf(a);
-      }
-    }
-  } else if (W == 4 && vec) {
-    if constexpr (DT == DT_F32)
-      *reinterpret_cast<float4 *>((float *)o.o + e) = make_float4(x[0], x[1], x[W > 2 ? 2 : 0], x[W > 3 ? 3 : 0]);
-    else
-      *reinterpret_cast<uint2 *>((uint16_t *)o.o + e) =
-          make_uint2(f2bf2(x[0], x[1]), f2bf2(x[W > 2 ? 2 : 0], x[W > 3 ? 3 : 0]));
+    const float a = update_one(o, *v, x);
+    *v = a;
+    if (o.v16) o.v16[e] = f2bf(a);
   } else {
-#pragma unroll
-    for (int i = 0; i < W; ++i) ((typename Store<DT>::T *)o.o)[e + i] = from_f32<DT>(x[i]);
+    ((typename Store<DT>::T *)o.o)[e] = from_f32<DT>(x);
   }
+}
+
+// elements e .. e + 3, e a multiple of 4
+template <int DT> __device__ __forceinline__ void emit4(const Out &o, long long e, const float (&x)[4]) {
+  if (o.update) {
+    float a[4];
+    load_cols<4>((float *)o.o + e, a);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = update_one(o, a[i], x[i]);
+    store_cols<4>((float *)o.o + e, a);
+    if (o.v16) *reinterpret_cast<uint2 *>(o.v16 + e) = make_uint2(f2bf2(a[0], a[1]), f2bf2(a[2], a[3]));
+  } else if constexpr (DT == DT_F32) {
+    store_cols<4>((float *)o.o + e, x);
+  } else {
+    *reinterpret_cast<uint2 *>((uint16_t *)o.o + e) = make_uint2(f2bf2(x[0], x[1]), f2bf2(x[2], x[3]));
+  }
+}
+
+// the first k of W consecutive elements from e on
+template <int DT, int W> __device__ __forceinline__ void emit(const Out &o, long long e, const float (&x)[W], int k, bool vec) {
+  if constexpr (W == 4) {
+    if (vec && k >= 4) {
+      emit4<DT>(o, e, x);
+      return;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < W; ++i)
+    if (i < k) emit1<DT>(o, e + i, x[i]);
 }
 
 template <int MT, int DT>
@@ -422,15 +431,8 @@ __device__ __forceinline__ void final_steps(const NsMat &M, const Out &o, ApplyR
             float v[G::VW];
 #pragma unroll
             for (int c = 0; c < G::VW; ++c) v[c] = d[s][u * G::VW + c][q] * unscale;
-            if (row + q >= M.n) continue;
-            const long long e = M.off + (long long)(row + q) * M.m + col;
-            if (col + G::VW <= M.m) {
-              emit<DT, G::VW>(o, e, v, M.m % 4 == 0);
-            } else {
-#pragma unroll
-              for (int c = 0; c < G::VW; ++c)
-                if (col + c < M.m) emit<DT, 1>(o, e + c, {v[c]}, false);
-            }
+            if (row + q < M.n)
+              emit<DT, G::VW>(o, M.off + (long long)(row + q) * M.m + col, v, M.m - col, M.m % 4 == 0);
           }
         } else {
 #pragma unroll
@@ -438,15 +440,7 @@ __device__ __forceinline__ void final_steps(const NsMat &M, const Out &o, ApplyR
             float v[4];
 #pragma unroll
             for (int q = 0; q < 4; ++q) v[q] = d[s][u * G::VW + c][q] * unscale;
-            if (col + c >= M.m) continue;
-            const long long e = M.off + (long long)(col + c) * M.n + row;
-            if (row + 4 <= M.n) {
-              emit<DT, 4>(o, e, v, M.n % 4 == 0);
-            } else {
-#pragma unroll
-              for (int q = 0; q < 4; ++q)
-                if (row + q < M.n) emit<DT, 1>(o, e + q, {v[q]}, false);
-            }
+            if (col + c < M.m) emit<DT, 4>(o, M.off + (long long)(col + c) * M.n + row, v, M.n - row, M.n % 4 == 0);
           }
         }
       }
@@ -505,24 +499,27 @@ __device__ __forceinline__ void polynomial(const float *gram, int parts, const N
   }
   __syncthreads();
   const bool active = wave * NC < G::TT;
-  // element (tile row i, q) of the wave's column c as a factor's element
-  Frag<F> h[NC][G::KB], q0[NC][G::KB], x[NC][G::KB];
-  f32x4_t d[NC][G::TT];
-  auto product = [&](const char *A, const Frag<F>(&b)[NC][G::KB]) {  // d = A b
+  const int mine = (16 * wave * NC + r) * G::LROW + g * 32;  // the wave's first column, as a row
+  f32x4_t d[NC][G::TT];  // element (16 t + 4 g + q, own column c)
+  auto product = [&](const char *A, const char *B) {  // d = A B, B's columns as its rows
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
       for (int t = 0; t < G::TT; ++t) d[c][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int kb = 0; kb < G::KB; ++kb) {
+      Frag<F> b[NC];
 #pragma unroll
-    for (int kb = 0; kb < G::KB; ++kb)
+      for (int c = 0; c < NC; ++c) b[c] = load_frag<F>(B + mine + 16 * c * G::LROW + kb * 128);
 #pragma unroll
       for (int t = 0; t < G::TT; ++t) {
         const Frag<F> a = load_frag<F>(A + (16 * t + r) * G::LROW + kb * 128 + g * 32);
 #pragma unroll
-        for (int c = 0; c < NC; ++c) mma<F>(d[c][t], a, b[c][kb]);
+        for (int c = 0; c < NC; ++c) mma<F>(d[c][t], a, b[c]);
       }
+    }
   };
-  auto factor = [&](Frag<F>(&f)[NC][G::KB], float scale) {  // f = d * scale
+  auto put = [&](char *A, float scale) {  // A's own rows = d * scale
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
@@ -533,59 +530,54 @@ __device__ __forceinline__ void polynomial(const float *gram, int parts, const N
           const int t = 2 * kb + (j >> 2);
           v[j] = t < G::TT ? d[c][t < G::TT ? t : 0][j & 3] * scale : 0.f;
         }
-        f[c][kb] = make_frag<F>(v);
+        store_frag<F>(A + mine + 16 * c * G::LROW + kb * 128, make_frag<F>(v));
       }
   };
-  auto put = [&](char *A, const Frag<F>(&f)[NC][G::KB]) {  // the wave's columns as rows of a symmetric matrix
+  auto poly = [&](float sh) {  // d = ca I + cb H + cc d, d the square of sh H
+    const float uh = cb / sh, us = cc / (sh * sh);
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
-      for (int kb = 0; kb < G::KB; ++kb) store_frag<F>(A + (16 * (wave * NC + c) + r) * G::LROW + kb * 128 + g * 32, f[c][kb]);
-  };
-  auto poly = [&](const Frag<F>(&hf)[NC][G::KB], float sh) {  // d = ca I + cb h + cc d (d: the square)
-    const float uh = 1.f / sh, us = uh * uh;
+      for (int kb = 0; kb < G::KB; ++kb) {
+        const Frag<F> h = load_frag<F>(H + mine + 16 * c * G::LROW + kb * 128);
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-      for (int t = 0; t < G::TT; ++t)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          float v = cb * (frag_value<F>(hf[c][t >> 1], 4 * (t & 1) + q) * uh) + cc * (d[c][t][q] * us);
-          if (t == wave * NC + c && 4 * g + q == r) v += ca;
-          d[c][t][q] = v;
+        for (int j = 0; j < 8; ++j) {
+          const int t = 2 * kb + (j >> 2), q = j & 3;
+          if (t >= G::TT) continue;
+          float x = uh * frag_value<F>(h, j) + us * d[c][t < G::TT ? t : 0][q];
+          if (t == wave * NC + c && 4 * g + q == r) x += ca;
+          d[c][t < G::TT ? t : 0][q] = x;
         }
+      }
   };
-  float out = 1.f;  // scale of d when P is written
+  // A matrix in LDS is read by every wave on the left of a product, between barriers,
+  // and a wave's own rows by that wave alone on the right: it overwrites them freely
+  // once no wave reads the matrix on the left.
+  float out = sq0;  // scale of d when P is written
   if (active) {
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-      for (int kb = 0; kb < G::KB; ++kb) h[c][kb] = load_frag<F>(H + (16 * (wave * NC + c) + r) * G::LROW + kb * 128 + g * 32);
-    product(H, h);
-    poly(h, sh0);
-    out = sq0;
+    product(H, H);
+    poly(sh0);
   }
   if (st.steps == 2) {
+    if (active) put(Q, sq0);
+    __syncthreads();
     if (active) {
-      factor(q0, sq0);
-      put(Q, q0);
+      product(Q, H);  // T = Q H
+      put(H, stt / (sq0 * sh0));
+      product(Q, H);  // H' = Q T
+      put(H, sh1 / (sq0 * stt));
     }
     __syncthreads();
     if (active) {
-      product(Q, h);  // T = Q H
-      factor(x, stt / (sq0 * sh0));
-      product(Q, x);  // H' = Q T
-      factor(h, sh1 / (sq0 * stt));
-      put(H, h);
+      product(H, H);
+      poly(sh1);
     }
     __syncthreads();
     if (active) {
-      product(H, h);
-      poly(h, sh1);
-      factor(x, sq1);
-      product(Q, x);  // P = Q Q'
-      out = sp / (sq0 * sq1);
+      put(H, sq1);
+      product(Q, H);  // P = Q Q'
     }
+    out = sp / (sq0 * sq1);
   }
   if (active) {
 #pragma unroll
