@@ -27,8 +27,26 @@
 namespace cf {
 namespace {
 
-constexpr int kTile = 64;
 constexpr int kStep = 32;  // k of one matrix instruction; both sides are padded to it
+
+// A matrix of fp16 pairs: a row is a sequence of 128-byte blocks of 32 columns, 32 hi
+// values and 32 lo values, so that a tile's row of one k-step is one cache line.
+__device__ __forceinline__ long long pair_row(int ld) { return (long long)ld * 4; }  // bytes; ld columns
+__device__ __forceinline__ int pair_col(int c) { return (c >> 5) * 128 + (c & 31) * 2; }
+
+// W consecutive columns (W divides 32) from column c on of the row at p
+template <int W> __device__ __forceinline__ void store_pairs(char *p, int c, const float (&x)[W]) {
+  typedef _Float16 vec_t __attribute__((ext_vector_type(W)));
+  vec_t hi, lo;
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+    const Half2 h = ns_split(x[i]);
+    hi[i] = h.hi;
+    lo[i] = h.lo;
+  }
+  *reinterpret_cast<vec_t *>(p + pair_col(c)) = hi;
+  *reinterpret_cast<vec_t *>(p + pair_col(c) + 64) = lo;
+}
 
 // ---- momentum and norm --------------------------------------------------------
 
@@ -97,21 +115,21 @@ __global__ __launch_bounds__(256) void ns_split_kernel(NsTable T, double eps, fl
     tile[r][c] = x;
   }
   __syncthreads();
-  _Float16 *nat = (_Float16 *)(ws + (M.tall ? M.ws_xt : M.ws_xn)), *tr = (_Float16 *)(ws + (M.tall ? M.ws_xn : M.ws_xt));
-  const long long plane = (long long)M.mp * M.np;
+  char *nat = ws + (M.tall ? M.ws_xt : M.ws_xn), *tr = ws + (M.tall ? M.ws_xn : M.ws_xt);
   const int nrows = M.tall ? M.np : M.mp, ncols = M.tall ? M.mp : M.np;  // natural array, padded
-  for (int r = r0; r < 64; r += 4) {
-    if (rr + r < nrows && cc + c < ncols) {
-      const Half2 h = ns_split(tile[r][c]);
-      const long long e = (long long)(rr + r) * ncols + cc + c;
-      nat[e] = h.hi;
-      nat[plane + e] = h.lo;
+  const int row = threadIdx.x >> 2, seg = (threadIdx.x & 3) * 16;
+#pragma unroll
+  for (int h = 0; h < 16; h += 8) {
+    float x[8];
+    if (rr + row < nrows && cc + seg < ncols) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = tile[row][seg + h + i];
+      store_pairs<8>(nat + (rr + row) * pair_row(ncols), cc + seg + h, x);
     }
-    if (cc + r < ncols && rr + c < nrows) {
-      const Half2 h = ns_split(tile[c][r]);
-      const long long e = (long long)(cc + r) * nrows + rr + c;
-      tr[e] = h.hi;
-      tr[plane + e] = h.lo;
+    if (cc + row < ncols && rr + seg < nrows) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = tile[seg + h + i][row];
+      store_pairs<8>(tr + (cc + row) * pair_row(nrows), rr + seg + h, x);
     }
   }
 }
@@ -120,164 +138,271 @@ __global__ __launch_bounds__(256) void ns_split_kernel(NsTable T, double eps, fl
 
 enum : int { NS_GRAM = 0, NS_POLY = 1, NS_PROD = 2, NS_APPLY = 3, NS_FINAL = 4 };
 
-// acc = A B' over k in [k0, k1): 64 x 64 tile at rows i0 of A, j0 of B, a wave 32 x 32
-// (2 x 2 instructions).  A, B: [rows][ld] hi, lo one plane apart; rows past the
-// arrays read their last row, the results are not stored.
-__device__ __forceinline__ void tile_product(const _Float16 *A, long long pa, int ra, const _Float16 *B, long long pb,
-                                             int rb, int ld, int i0, int j0, int k0, int k1, f32x4_t (&acc)[2][2]) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int r = lane & 15, ko = lane >> 4 << 3;
-  const _Float16 *ap[2], *bp[2];
+typedef __attribute__((address_space(3))) void lds_void_t;
+typedef const __attribute__((address_space(1))) void global_void_t;
+
+// A square tile of B columns: WR x WC waves of TR x TC matrix instructions each, NS
+// k-steps of both factors in LDS.
+template <int B_> struct Tile;
+template <> struct Tile<64> {
+  static constexpr int B = 64, WR = 2, WC = 2, NS = 4;
+};
+template <> struct Tile<128> {
+  static constexpr int B = 128, WR = 2, WC = 2, NS = 2;
+};
+template <> struct Tile<256> {
+  static constexpr int B = 256, WR = 2, WC = 4, NS = 2;
+};
+template <class G> struct TileGeo {
+  static constexpr int NT = 64 * G::WR * G::WC;
+  static constexpr int TR = G::B / G::WR / 16, TC = G::B / G::WC / 16;
+  static constexpr int STAGE = 2 * G::B * 128;  // bytes of one k-step
+  static constexpr int LD = G::B * 8 / NT;      // 16-byte loads a thread and factor
+};
+
+// Both factors' rows of one k-step into LDS, 16 bytes a lane straight from memory.  LDS
+// rows are 128 bytes; piece c of row r is at piece c ^ ((r >> 1) & 7), which spreads the
+// sixteen rows of a fragment over all banks.
+template <class G> struct Loader {
+  using T = TileGeo<G>;
+  const char *a, *b;  // first row of the tile, this k-step
+  uint32_t ao[T::LD], bo[T::LD];
+  __device__ __forceinline__ Loader(const char *A, int ra, int i0, const char *B, int rb, int j0, int ld, int k0) {
+    a = A + i0 * pair_row(ld) + (long long)k0 * 4;
+    b = B + j0 * pair_row(ld) + (long long)k0 * 4;
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    ap[t] = A + (long long)min(i0 + (wave >> 1) * 32 + t * 16 + r, ra - 1) * ld + ko;
-    bp[t] = B + (long long)min(j0 + (wave & 1) * 32 + t * 16 + r, rb - 1) * ld + ko;
+    for (int i = 0; i < T::LD; ++i) {
+      const int id = i * T::NT + threadIdx.x, row = id >> 3, c = (id & 7) ^ ((row >> 1) & 7);
+      ao[i] = (uint32_t)(min(row, ra - 1 - i0) * pair_row(ld)) + c * 16;
+      bo[i] = (uint32_t)(min(row, rb - 1 - j0) * pair_row(ld)) + c * 16;
+    }
   }
+  // the next k-step into `stage`
+  __device__ __forceinline__ void issue(char *stage) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < T::LD; ++i)
+      __builtin_amdgcn_global_load_lds((global_void_t *)(a + ao[i]), (lds_void_t *)(stage + (i * T::NT + wave * 64) * 16), 16,
+                                       0, 0);
 #pragma unroll
-    for (int j = 0; j < 2; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  for (int k = k0; k < k1; k += kStep) {
-    f16x8_t ah[2], al[2], bh[2], bl[2];
+    for (int i = 0; i < T::LD; ++i)
+      __builtin_amdgcn_global_load_lds((global_void_t *)(b + bo[i]),
+                                       (lds_void_t *)(stage + G::B * 128 + (i * T::NT + wave * 64) * 16), 16, 0, 0);
+    a += 128;
+    b += 128;
+  }
+};
+
+// waits until at most N of the wave's loads are in flight
+template <int N> __device__ __forceinline__ void wait_loads() {
+  __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | ((N >> 4) << 14));
+}
+
+template <class G> using TileAcc = f32x4_t[TileGeo<G>::TR][TileGeo<G>::TC];
+
+// acc = A B' over k-steps [k0, k1) / 32: rows i0.. of A, j0.. of B.  Rows past the
+// arrays (ra, rb of them) read their last row; their results are not stored.
+template <class G>
+__device__ __forceinline__ void tile_product(TileAcc<G> &acc, char *lds, const char *A, int ra, int i0, const char *B, int rb,
+                                             int j0, int ld, int k0, int k1) {
+  using T = TileGeo<G>;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      ah[t] = *reinterpret_cast<const f16x8_t *>(ap[t] + k);
-      al[t] = *reinterpret_cast<const f16x8_t *>(ap[t] + pa + k);
-      bh[t] = *reinterpret_cast<const f16x8_t *>(bp[t] + k);
-      bl[t] = *reinterpret_cast<const f16x8_t *>(bp[t] + pb + k);
+  for (int i = 0; i < T::TR; ++i)
+#pragma unroll
+    for (int j = 0; j < T::TC; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  const int steps = (k1 - k0) / kStep;
+  Loader<G> load(A, ra, i0, B, rb, j0, ld, k0);
+#pragma unroll
+  for (int s = 0; s < G::NS - 1; ++s)
+    if (s < steps) load.issue(lds + s * T::STAGE);
+  // this lane's pieces of a fragment: (row r, hi g) and (row r, lo g)
+  const int sw = (r >> 1) & 7;
+  const int fh = r * 128 + ((g ^ sw) << 4), fl = r * 128 + (((4 + g) ^ sw) << 4);
+  const int arow = (wave / G::WC) * T::TR * 2048, brow = G::B * 128 + (wave % G::WC) * T::TC * 2048;
+  int slot = 0;
+  for (int s = 0; s < steps; ++s) {
+    // the k-step's loads have landed (the later ones may be in flight), for every wave;
+    // and every wave is done with the slot that the next loads overwrite
+    if (s + G::NS - 1 <= steps) wait_loads<(G::NS - 2) * 2 * T::LD>();
+    else wait_loads<0>();
+    asm volatile("s_barrier" ::: "memory");
+    if (s + G::NS - 1 < steps) load.issue(lds + (slot + G::NS - 1) % G::NS * T::STAGE);
+    const char *st = lds + slot * T::STAGE;
+    f16x8_t bh[T::TC], bl[T::TC];
+#pragma unroll
+    for (int j = 0; j < T::TC; ++j) {
+      bh[j] = *reinterpret_cast<const f16x8_t *>(st + brow + j * 2048 + fh);
+      bl[j] = *reinterpret_cast<const f16x8_t *>(st + brow + j * 2048 + fl);
     }
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < T::TR; ++i) {
+      const f16x8_t ah = *reinterpret_cast<const f16x8_t *>(st + arow + i * 2048 + fh);
+      const f16x8_t al = *reinterpret_cast<const f16x8_t *>(st + arow + i * 2048 + fl);
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[i], bl[j], acc[i][j], 0, 0, 0);
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al[i], bh[j], acc[i][j], 0, 0, 0);
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[i], bh[j], acc[i][j], 0, 0, 0);
-      }
+      for (int j = 0; j < T::TC; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bl[j], acc[i][j], 0, 0, 0);
+#pragma unroll
+      for (int j = 0; j < T::TC; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al, bh[j], acc[i][j], 0, 0, 0);
+#pragma unroll
+      for (int j = 0; j < T::TC; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bh[j], acc[i][j], 0, 0, 0);
+    }
+    slot = slot + 1 == G::NS ? 0 : slot + 1;
   }
+}
+
+// tile b of the upper triangle of t x t tiles, row by row
+__device__ __forceinline__ void triangle_tile(int b, int t, int *ti, int *tj) {
+  // row i starts at i t - i (i - 1) / 2
+  const float f = t + 0.5f;
+  int i = (int)(f - sqrtf(f * f - 2.f * b));
+  i = max(0, min(i, t - 1));
+  while (i > 0 && i * t - i * (i - 1) / 2 > b) --i;
+  while ((i + 1) * t - (i + 1) * i / 2 <= b) ++i;
+  *ti = i;
+  *tj = i + b - (i * t - i * (i - 1) / 2);
 }
 
 // One product of every matrix of the launch.  A, B and the output are named by their
 // slots in the group's workspace:
-//   GRAM   part[slice][mp][mp] = X X' over the slice's columns (fp32)
+//   GRAM   part[slice] = X X' over the slice's columns (fp32, tiles of the upper triangle)
 //   POLY   out = a I + b A + c A A'          (A = B = H)
 //   PROD   out = A B'                        (all m x m, symmetric)
 //   APPLY  xt' = xt P, xn' its transpose
 //   FINAL  the output: o = xt P, or the parameter update with it
-template <int MODE, int DT>
-__global__ __launch_bounds__(256) void ns_product_kernel(NsTable T, NsProduct p, void *out, uint16_t *v16, char *ws) {
+// The m x m products commute and are symmetric: tiles of the upper triangle, stored
+// both ways.
+template <int MODE, int TB, int DT>
+__global__ __launch_bounds__(TileGeo<Tile<TB>>::NT, TB == 256 ? 1 : 2) void ns_product_kernel(NsTable T, NsProduct p, void *out,
+                                                                                             uint16_t *v16, char *ws) {
+  using G = Tile<TB>;
+  using TG = TileGeo<G>;
+  __shared__ __attribute__((aligned(16))) char lds[G::NS * TG::STAGE];
   const int l = ns_find(T, blockIdx.x);
   const NsMat &M = T.mat[l];
   const int b = blockIdx.x - T.first[l];
-  const int tm = (M.mp + kTile - 1) / kTile;
+  const int tm = (M.mp + TB - 1) / TB;
   constexpr bool kLong = MODE == NS_APPLY || MODE == NS_FINAL;
-  int i0, j0, k0 = 0, k1 = M.mp, ra = M.mp;
-  const _Float16 *A, *B;
-  long long pa, ld;
-  const long long sq = (long long)M.mp * M.mp, plane = (long long)M.mp * M.np;
-  int slice = 0;
-  if constexpr (MODE == NS_GRAM) {
-    slice = b / (tm * tm);
-    i0 = b / tm % tm * kTile;
-    j0 = b % tm * kTile;
-    const int steps = M.np / kStep, per = (steps + M.slices - 1) / M.slices;
-    k0 = min(slice * per, steps) * kStep;
-    k1 = min((slice + 1) * per, steps) * kStep;
-    A = B = (const _Float16 *)(ws + M.ws_xn);
-    pa = plane;
-    ld = M.np;
-  } else if constexpr (kLong) {
-    i0 = b / tm * kTile;
-    j0 = b % tm * kTile;
-    A = (const _Float16 *)(ws + (p.a ? M.ws_xt2 : M.ws_xt));
-    B = (const _Float16 *)(ws + M.ws_sq) + 2 * sq * p.b;
-    pa = plane;
+  int ti, tj, k0 = 0, k1 = M.mp, ra = M.mp, ld = M.mp, slice = 0;
+  const char *A, *B;
+  const long long sq = (long long)M.mp * M.mp * 4;
+  if constexpr (kLong) {
+    ti = b / tm;
+    tj = b % tm;
+    A = ws + (p.a ? M.ws_xt2 : M.ws_xt);
+    B = ws + M.ws_sq + sq * p.b;
     ra = M.np;
-    ld = M.mp;
   } else {
-    i0 = b / tm * kTile;
-    j0 = b % tm * kTile;
-    A = (const _Float16 *)(ws + M.ws_sq) + 2 * sq * p.a;
-    B = (const _Float16 *)(ws + M.ws_sq) + 2 * sq * p.b;
-    pa = sq;
-    ld = M.mp;
+    const int tri = tm * (tm + 1) / 2;
+    slice = MODE == NS_GRAM ? b / tri : 0;
+    triangle_tile(b - slice * tri, tm, &ti, &tj);
+    if constexpr (MODE == NS_GRAM) {
+      const int steps = M.np / kStep, per = (steps + M.slices - 1) / M.slices;
+      k0 = min(slice * per, steps) * kStep;
+      k1 = min((slice + 1) * per, steps) * kStep;
+      A = B = ws + M.ws_xn;
+      ld = M.np;
+    } else {
+      A = ws + M.ws_sq + sq * p.a;
+      B = ws + M.ws_sq + sq * p.b;
+    }
   }
-  f32x4_t acc[2][2];
-  tile_product(A, pa, ra, B, MODE == NS_GRAM ? plane : sq, M.mp, (int)ld, i0, j0, k0, k1, acc);
+  TileAcc<G> acc;
+  tile_product<G>(acc, lds, A, ra, ti * TB, B, M.mp, tj * TB, ld, k0, k1);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if constexpr (MODE == NS_GRAM) {
+    // accumulators as they are: [tile][wave tile][lane]
+    float4 *part = (float4 *)(ws + M.ws_part) + ((long long)b * TG::NT / 64 * TG::TR * TG::TC) * 64;
 #pragma unroll
-  for (int ti = 0; ti < 2; ++ti)
+    for (int i = 0; i < TG::TR; ++i)
 #pragma unroll
-    for (int tj = 0; tj < 2; ++tj) {
-      const int i = i0 + (wave >> 1) * 32 + ti * 16 + (lane >> 4) * 4;  // rows i .. i + 3
-      const int j = j0 + (wave & 1) * 32 + tj * 16 + (lane & 15);
+      for (int j = 0; j < TG::TC; ++j)
+        part[((wave * TG::TR + i) * TG::TC + j) * 64 + lane] = make_float4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
+    return;
+  }
+#pragma unroll
+  for (int ii = 0; ii < TG::TR; ++ii)
+#pragma unroll
+    for (int jj = 0; jj < TG::TC; ++jj) {
+      const int i = ti * TB + ((wave / G::WC) * TG::TR + ii) * 16 + (lane >> 4) * 4;  // rows i .. i + 3
+      const int j = tj * TB + ((wave % G::WC) * TG::TC + jj) * 16 + (lane & 15);
       if (j >= M.mp || i >= (kLong ? M.np : M.mp)) continue;
-      if constexpr (MODE == NS_GRAM) {
-        float *part = (float *)(ws + M.ws_part) + slice * sq;
+      float x[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) part[(long long)(i + q) * M.mp + j] = acc[ti][tj][q] * p.unscale;
-      } else if constexpr (MODE == NS_POLY || MODE == NS_PROD) {
-        _Float16 *o = (_Float16 *)(ws + M.ws_sq) + 2 * sq * p.out;
+      for (int q = 0; q < 4; ++q) x[q] = acc[ii][jj][q] * p.unscale;
+      if constexpr (MODE == NS_POLY || MODE == NS_PROD) {
+        char *o = ws + M.ws_sq + sq * p.out;
+        if constexpr (MODE == NS_POLY) {
+          // H is symmetric: four consecutive columns of its row j
+          const char *h = A + j * pair_row(M.mp) + pair_col(i);
+          const f16x4_t hh = *reinterpret_cast<const f16x4_t *>(h), hl = *reinterpret_cast<const f16x4_t *>(h + 64);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const long long e = (long long)(i + q) * M.mp + j;
-          float x = acc[ti][tj][q] * p.unscale;
-          if constexpr (MODE == NS_POLY) {
-            const float h = ((float)A[e] + (float)A[sq + e]) * p.unscale_h;
-            x = p.cc * x + p.cb * h;
-            if (i + q == j && j < M.m) x += p.ca;
+          for (int q = 0; q < 4; ++q) {
+            x[q] = p.cc * x[q] + p.cb * (((float)hh[q] + (float)hl[q]) * p.unscale_h);
+            if (i + q == j && j < M.m) x[q] += p.ca;
           }
-          const Half2 s = ns_split(x * p.scale);
-          o[e] = s.hi;
-          o[sq + e] = s.lo;
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) x[q] *= p.scale;
+        store_pairs<4>(o + j * pair_row(M.mp), i, x);
+        if (ti != tj) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) store_pairs<1>(o + (i + q) * pair_row(M.mp), j, {x[q]});
         }
       } else if constexpr (MODE == NS_APPLY) {
-        _Float16 *xt = (_Float16 *)(ws + (p.a ? M.ws_xt : M.ws_xt2)), *xn = (_Float16 *)(ws + M.ws_xn);
-        f16x4_t hi, lo;
+        char *xt = ws + (p.a ? M.ws_xt : M.ws_xt2), *xn = ws + M.ws_xn;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const Half2 s = ns_split(acc[ti][tj][q] * p.unscale * p.scale);
-          xt[(long long)(i + q) * M.mp + j] = s.hi;
-          xt[plane + (long long)(i + q) * M.mp + j] = s.lo;
-          hi[q] = s.hi;
-          lo[q] = s.lo;
-        }
-        *reinterpret_cast<f16x4_t *>(xn + (long long)j * M.np + i) = hi;
-        *reinterpret_cast<f16x4_t *>(xn + plane + (long long)j * M.np + i) = lo;
+        for (int q = 0; q < 4; ++q) x[q] *= p.scale;
+        store_pairs<4>(xn + j * pair_row(M.np), i, x);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) store_pairs<1>(xt + (i + q) * pair_row(M.mp), j, {x[q]});
       } else {
         if (j >= M.m) continue;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           if (i + q >= M.n) continue;
           const long long e = M.off + (M.tall ? (long long)(i + q) * M.m + j : (long long)j * M.n + i + q);
-          const float x = acc[ti][tj][q] * p.unscale;
           if (p.update) {
             float *v = (float *)out;
-            const float w = v[e] - p.eta * (M.gain * x + p.decay * v[e]);
+            const float w = v[e] - p.eta * (M.gain * x[q] + p.decay * v[e]);
             v[e] = w;
             if (v16) v16[e] = f2bf(w);
           } else {
-            ((typename Store<DT>::T *)out)[e] = from_f32<DT>(x);
+            ((typename Store<DT>::T *)out)[e] = from_f32<DT>(x[q]);
           }
         }
       }
     }
 }
 
-// H = sum of the slices' Gram matrices, in slice order
-__global__ __launch_bounds__(256) void ns_gram_sum_kernel(NsTable T, int slot, float scale, char *ws) {
+// H = sum of the slices' Gram matrices, in slice order; one matrix-instruction tile a wave
+template <int TB> __global__ __launch_bounds__(256) void ns_gram_sum_kernel(NsTable T, int slot, float scale, char *ws) {
+  using G = Tile<TB>;
+  using TG = TileGeo<G>;
+  constexpr int PER = TB / 16 * (TB / 16);  // instruction tiles of a tile
   const int l = ns_find(T, blockIdx.x);
   const NsMat &M = T.mat[l];
-  const long long sq = (long long)M.mp * M.mp;
-  const long long e = (long long)(blockIdx.x - T.first[l]) * 256 + threadIdx.x;
-  if (e >= sq) return;
-  const float *part = (const float *)(ws + M.ws_part) + e;
-  float s = 0.f;
-  for (int i = 0; i < M.slices; ++i) s += part[i * sq];
-  const Half2 h = ns_split(s * scale);
-  _Float16 *o = (_Float16 *)(ws + M.ws_sq) + 2 * sq * slot;
-  o[e] = h.hi;
-  o[sq + e] = h.lo;
+  const int tm = (M.mp + TB - 1) / TB, tri = tm * (tm + 1) / 2;
+  const int lane = threadIdx.x & 63, w = (blockIdx.x - T.first[l]) * 4 + (threadIdx.x >> 6);
+  const int b = w / PER, k = w % PER, wave = k / (TG::TR * TG::TC);
+  int ti, tj;
+  triangle_tile(b, tm, &ti, &tj);
+  const int i = ti * TB + ((wave / G::WC) * TG::TR + k / TG::TC % TG::TR) * 16 + (lane >> 4) * 4;
+  const int j = tj * TB + ((wave % G::WC) * TG::TC + k % TG::TC) * 16 + (lane & 15);
+  if (j >= M.mp || i >= M.mp) return;
+  const float4 *part = (const float4 *)(ws + M.ws_part) + ((long long)b * PER + k) * 64 + lane;
+  float4 s = part[0];
+#pragma unroll 4
+  for (int n = 1; n < M.slices; ++n) {
+    const float4 a = part[(long long)n * tri * PER * 64];
+    s.x += a.x; s.y += a.y; s.z += a.z; s.w += a.w;
+  }
+  const float x[4] = {s.x * scale, s.y * scale, s.z * scale, s.w * scale};
+  char *o = ws + M.ws_sq + (long long)M.mp * M.mp * 4 * slot;
+  store_pairs<4>(o + j * pair_row(M.mp), i, x);
+  if (ti != tj) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) store_pairs<1>(o + (i + q) * pair_row(M.mp), j, {x[q]});
+  }
 }
 
 }  // namespace
@@ -298,6 +423,7 @@ template <class F> int number(NsTable *T, F blocks) {
   return at;
 }
 
+// the m x m matrices of a group
 enum : int { SQ_H = 0, SQ_Q = 1, SQ_T = 2, SQ_Q1 = 3, SQ_P = 4, SQ_COUNT = 5 };
 }  // namespace
 
@@ -387,11 +513,6 @@ size_t ns_plan(int count, const long long *off, const int *rows, const int *cols
     M.shift = 0;
     while ((el + ((long long)kNsChunk << M.shift) - 1) / ((long long)kNsChunk << M.shift) > 512) ++M.shift;
     M.chunks = (int)((el + ((long long)kNsChunk << M.shift) - 1) / ((long long)kNsChunk << M.shift));
-    const int tm = (M.mp + kTile - 1) / kTile, ksteps = M.np / kStep;
-    // slices of the long side: about four workgroups a compute unit, eight k-steps at least
-    int slices = (4 * kNumCUs + tm * tm - 1) / (tm * tm);
-    if (slices > (ksteps + 7) / 8) slices = (ksteps + 7) / 8;
-    M.slices = slices;
     const long long plane = (long long)M.mp * M.np, sq = (long long)M.mp * M.mp;
     M.ws_norm = take(8LL * M.chunks);
     M.ws_u = momentum ? take(4 * el) : -1;
@@ -399,7 +520,17 @@ size_t ns_plan(int count, const long long *off, const int *rows, const int *cols
     M.ws_xt = take(4 * plane);
     M.ws_xt2 = take(4 * plane);
     M.ws_sq = take(4 * sq * SQ_COUNT);
-    M.ws_part = take(4 * sq * slices);
+    auto tiles = [](long long rows, long long tb) { return (rows + tb - 1) / tb; };
+    auto triangle = [&](long long tb) { return tiles(M.mp, tb) * (tiles(M.mp, tb) + 1) / 2; };
+    M.tile_sq = triangle(256) >= 128 ? 256 : triangle(128) >= 256 ? 128 : 64;
+    auto rect = [&](long long tb) { return tiles(M.mp, tb) * tiles(M.np, tb); };
+    M.tile_long = rect(256) >= 192 ? 256 : rect(128) >= 192 ? 128 : 64;
+    // slices of the long side: about two workgroups a compute unit, eight k-steps at least
+    const long long tri = triangle(M.tile_sq), ksteps = M.np / kStep;
+    long long slices = (2 * kNumCUs + tri - 1) / tri;
+    if (slices > ksteps / 8) slices = ksteps / 8 > 0 ? ksteps / 8 : 1;
+    M.slices = (int)slices;
+    M.ws_part = take(4LL * tri * M.tile_sq * M.tile_sq * slices);
   }
   return (size_t)at;
 }
@@ -424,59 +555,82 @@ hipError_t launch_newton_schulz(const NsTable &T0, const NsSteps &S, int dtype, 
     hipLaunchKernelGGL((ns_split_kernel<DT_BF16>), dim3(nb), dim3(256), 0, st, T, S.eps, sx0, g, ws);
   else
     hipLaunchKernelGGL((ns_split_kernel<DT_F32>), dim3(nb), dim3(256), 0, st, T, S.eps, sx0, g, ws);
-  auto tiles = [](const NsMat &M) {
-    const long long t = (M.mp + kTile - 1) / kTile;
-    return t * t;
+  // f(tile) for each tile size that a matrix of the table uses in this product
+  auto each_tile = [&](bool is_long, auto f) {
+    auto used = [&](int tb) {
+      for (int l = 0; l < T.count; ++l)
+        if (!T.mat[l].mt && (is_long ? T.mat[l].tile_long : T.mat[l].tile_sq) == tb) return true;
+      return false;
+    };
+    if (used(256)) f(std::integral_constant<int, 256>{});
+    if (used(128)) f(std::integral_constant<int, 128>{});
+    if (used(64)) f(std::integral_constant<int, 64>{});
   };
+  auto product = [&](auto mode, auto dt, NsProduct p) {
+    constexpr int MODE = decltype(mode)::value, DT = decltype(dt)::value;
+    constexpr bool kLong = MODE == NS_APPLY || MODE == NS_FINAL;
+    each_tile(kLong, [&](auto tile) {
+      constexpr int TB = decltype(tile)::value;
+      const int blocks = number(&T, [](const NsMat &M) {
+        if ((kLong ? M.tile_long : M.tile_sq) != TB) return 0LL;
+        const long long t = (M.mp + TB - 1) / TB;
+        return kLong ? t * ((M.np + TB - 1) / TB) : t * (t + 1) / 2 * (MODE == NS_GRAM ? M.slices : 1);
+      });
+      hipLaunchKernelGGL((ns_product_kernel<MODE, TB, DT>), dim3(blocks), dim3(TileGeo<Tile<TB>>::NT), 0, st, T, p, out, v16, ws);
+    });
+  };
+  using Gram = std::integral_constant<int, NS_GRAM>;
+  using Poly = std::integral_constant<int, NS_POLY>;
+  using Prod = std::integral_constant<int, NS_PROD>;
+  using Apply = std::integral_constant<int, NS_APPLY>;
+  using Final = std::integral_constant<int, NS_FINAL>;
+  using F32 = std::integral_constant<int, DT_F32>;
+  using BF16 = std::integral_constant<int, DT_BF16>;
   const float a = (float)S.a, b = (float)S.b, c = (float)S.c;
   for (int s = 0; s < S.stages; ++s) {
     const NsStage &G = S.stage[s];
-    const bool last = s + 1 == S.stages;
-    auto product = [&](auto mode, int pa, int pb, int po, float unscale, float unscale_h, float scale) {
+    auto square = [&](auto mode, int pa, int pb, int po, float unscale, float unscale_h, float scale) {
       NsProduct p{};
       p.a = pa; p.b = pb; p.out = po;
       p.unscale = unscale; p.unscale_h = unscale_h; p.scale = scale;
       p.ca = a; p.cb = b; p.cc = c;
-      hipLaunchKernelGGL((ns_product_kernel<decltype(mode)::value, DT_F32>), dim3(nb), dim3(256), 0, st, T, p, nullptr,
-                         nullptr, ws);
+      product(mode, F32{}, p);
     };
-    using Gram = std::integral_constant<int, NS_GRAM>;
-    using Poly = std::integral_constant<int, NS_POLY>;
-    using Prod = std::integral_constant<int, NS_PROD>;
-    using Apply = std::integral_constant<int, NS_APPLY>;
-    nb = number(&T, [&](const NsMat &M) { return tiles(M) * M.slices; });
-    product(Gram{}, 0, 0, 0, 1.f / (G.sx * G.sx), 0.f, 0.f);
-    nb = number(&T, [](const NsMat &M) { return ((long long)M.mp * M.mp + 255) / 256; });
-    hipLaunchKernelGGL(ns_gram_sum_kernel, dim3(nb), dim3(256), 0, st, T, (int)SQ_H, G.sh[0], ws);
-    nb = number(&T, tiles);
-    product(Poly{}, SQ_H, SQ_H, SQ_Q, 1.f / (G.sh[0] * G.sh[0]), 1.f / G.sh[0], G.sq[0]);
+    square(Gram{}, 0, 0, 0, 1.f, 0.f, 0.f);
+    each_tile(false, [&](auto tile) {
+      constexpr int TB = decltype(tile)::value;
+      nb = number(&T, [](const NsMat &M) {
+        const long long t = (M.mp + TB - 1) / TB;
+        return M.tile_sq == TB ? t * (t + 1) / 2 * (TB / 16 * (TB / 16) / 4) : 0LL;
+      });
+      hipLaunchKernelGGL((ns_gram_sum_kernel<TB>), dim3(nb), dim3(256), 0, st, T, (int)SQ_H, G.sh[0] / (G.sx * G.sx), ws);
+    });
+    square(Poly{}, SQ_H, SQ_H, SQ_Q, 1.f / (G.sh[0] * G.sh[0]), 1.f / G.sh[0], G.sq[0]);
     int slot = SQ_Q;
     float sp = G.sq[0];
     if (G.steps == 2) {
-      product(Prod{}, SQ_Q, SQ_H, SQ_T, 1.f / (G.sq[0] * G.sh[0]), 0.f, G.st);
-      product(Prod{}, SQ_T, SQ_Q, SQ_H, 1.f / (G.st * G.sq[0]), 0.f, G.sh[1]);
-      product(Poly{}, SQ_H, SQ_H, SQ_Q1, 1.f / (G.sh[1] * G.sh[1]), 1.f / G.sh[1], G.sq[1]);
-      product(Prod{}, SQ_Q1, SQ_Q, SQ_P, 1.f / (G.sq[1] * G.sq[0]), 0.f, G.sp);
+      square(Prod{}, SQ_Q, SQ_H, SQ_T, 1.f / (G.sq[0] * G.sh[0]), 0.f, G.st);
+      square(Prod{}, SQ_T, SQ_Q, SQ_H, 1.f / (G.st * G.sq[0]), 0.f, G.sh[1]);
+      square(Poly{}, SQ_H, SQ_H, SQ_Q1, 1.f / (G.sh[1] * G.sh[1]), 1.f / G.sh[1], G.sq[1]);
+      square(Prod{}, SQ_Q1, SQ_Q, SQ_P, 1.f / (G.sq[1] * G.sq[0]), 0.f, G.sp);
       slot = SQ_P;
       sp = G.sp;
     }
-    nb = number(&T, [](const NsMat &M) { return up(M.mp, kTile) / kTile * (up(M.np, kTile) / kTile); });
-    if (!last) {
-      product(Apply{}, s & 1, slot, 0, 1.f / (G.sx * sp), 0.f, S.stage[s + 1].sx);
+    NsProduct p{};
+    p.a = s & 1;
+    p.b = slot;
+    p.unscale = 1.f / (G.sx * sp);
+    if (s + 1 < S.stages) {
+      p.scale = S.stage[s + 1].sx;
+      product(Apply{}, F32{}, p);
     } else {
-      NsProduct p{};
-      p.a = s & 1;
-      p.b = slot;
-      p.unscale = 1.f / (G.sx * sp);
       if (up_) {
         p.update = 1;
         p.eta = up_->eta;
         p.decay = up_->decay;
       }
-      if (dtype == DT_BF16)
-        hipLaunchKernelGGL((ns_product_kernel<NS_FINAL, DT_BF16>), dim3(nb), dim3(256), 0, st, T, p, out, v16, ws);
-      else
-        hipLaunchKernelGGL((ns_product_kernel<NS_FINAL, DT_F32>), dim3(nb), dim3(256), 0, st, T, p, out, v16, ws);
+      if (dtype == DT_BF16) product(Final{}, BF16{}, p);
+      else product(Final{}, F32{}, p);
     }
   }
   return hipGetLastError();
