@@ -259,7 +259,7 @@ struct NsMat {
   int mt;             // m padded to 16, 32, 64 or 128 where the skinny kernels run it, else 0
   int shift, chunks;  // of the norm pass
   int prow;           // skinny: rows of the long side in a chunk
-  int tile_sq, tile_long;  // sides of the general kernels' tiles: m x m products, n x m ones
+  int tile_sq, tile_long, tile_gram;  // sides of the general kernels' tiles: m x m products, n x m, X X'
   int slices;         // of the long side in the Gram product (skinny: workgroups)
   float gain;         // of the update
   // byte offsets in the workspace: chunk sums, u (-1: none), X [m][n], X' [n][m] twice,

@@ -34,18 +34,12 @@ constexpr int kStep = 32;  // k of one matrix instruction; both sides are padded
 __device__ __forceinline__ long long pair_row(int ld) { return (long long)ld * 4; }  // bytes; ld columns
 __device__ __forceinline__ int pair_col(int c) { return (c >> 5) * 128 + (c & 31) * 2; }
 
-// W consecutive columns (W divides 32) from column c on of the row at p
-template <int W> __device__ __forceinline__ void store_pairs(char *p, int c, const float (&x)[W]) {
-  typedef _Float16 vec_t __attribute__((ext_vector_type(W)));
-  vec_t hi, lo;
-#pragma unroll
-  for (int i = 0; i < W; ++i) {
-    const Half2 h = ns_split(x[i]);
-    hi[i] = h.hi;
-    lo[i] = h.lo;
-  }
-  *reinterpret_cast<vec_t *>(p + pair_col(c)) = hi;
-  *reinterpret_cast<vec_t *>(p + pair_col(c) + 64) = lo;
+// columns c .. c + 7 (c a multiple of 8) of the row at p
+__device__ __forceinline__ void store_pairs(char *p, int c, const float (&x)[8]) {
+  f16x8_t hi, lo;
+  ns_split8(x, hi, lo);
+  *reinterpret_cast<f16x8_t *>(p + pair_col(c)) = hi;
+  *reinterpret_cast<f16x8_t *>(p + pair_col(c) + 64) = lo;
 }
 
 // ---- momentum and norm --------------------------------------------------------
@@ -97,23 +91,24 @@ __global__ __launch_bounds__(256) void ns_split_kernel(NsTable T, double eps, fl
   __shared__ float tile[64][65];
   const int l = ns_find(T, blockIdx.x);
   const NsMat &M = T.mat[l];
-  const double inv = ns_inv_norm(M, ws, eps, red);
   const int tm = (M.mp + 63) / 64, b = blockIdx.x - T.first[l];
   const int n0 = b / tm * 64, m0 = b % tm * 64;
   const int c = threadIdx.x & 63, r0 = threadIdx.x >> 6;
   // natural order: tall matrices have the long side as rows
   const int cols = M.tall ? M.m : M.n, rlim = M.tall ? M.n : M.m;
   const int rr = M.tall ? n0 : m0, cc = M.tall ? m0 : n0;
-  for (int r = r0; r < 64; r += 4) {
-    float x = 0.f;
-    if (rr + r < rlim && cc + c < cols) {
-      const long long e = (long long)(rr + r) * cols + cc + c;
-      const float g = M.ws_u >= 0 ? ((const float *)(ws + M.ws_u))[e]
-                                  : to_f32<DT>(((const typename Store<DT>::T *)src)[M.off + e]);
-      x = (float)(g * inv) * scale;
-    }
-    tile[r][c] = x;
+  float x[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int r = r0 + 4 * i;
+    const long long e = (long long)(rr + r) * cols + cc + c;
+    x[i] = 0.f;
+    if (rr + r < rlim && cc + c < cols)
+      x[i] = M.ws_u >= 0 ? ((const float *)(ws + M.ws_u))[e] : to_f32<DT>(((const typename Store<DT>::T *)src)[M.off + e]);
   }
+  const Scale sc = scale_of(ns_inv_norm(M, ws, eps, red), scale);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) tile[r0 + 4 * i][c] = x[i] * sc.s1 * sc.s2;
   __syncthreads();
   char *nat = ws + (M.tall ? M.ws_xt : M.ws_xn), *tr = ws + (M.tall ? M.ws_xn : M.ws_xt);
   const int nrows = M.tall ? M.np : M.mp, ncols = M.tall ? M.mp : M.np;  // natural array, padded
@@ -124,12 +119,12 @@ __global__ __launch_bounds__(256) void ns_split_kernel(NsTable T, double eps, fl
     if (rr + row < nrows && cc + seg < ncols) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = tile[row][seg + h + i];
-      store_pairs<8>(nat + (rr + row) * pair_row(ncols), cc + seg + h, x);
+      store_pairs(nat + (rr + row) * pair_row(ncols), cc + seg + h, x);
     }
     if (cc + row < ncols && rr + seg < nrows) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = tile[seg + h + i][row];
-      store_pairs<8>(tr + (cc + row) * pair_row(nrows), rr + seg + h, x);
+      store_pairs(tr + (cc + row) * pair_row(nrows), rr + seg + h, x);
     }
   }
 }
@@ -142,22 +137,39 @@ typedef __attribute__((address_space(3))) void lds_void_t;
 typedef const __attribute__((address_space(1))) void global_void_t;
 
 // A square tile of B columns: WR x WC waves of TR x TC matrix instructions each, NS
-// k-steps of both factors in LDS.
+// k-steps of both factors in LDS.  Small tiles have KG such groups of waves, each with
+// its own k-steps (group k the steps k, k + KG, ...) and loads; one group alone waits for
+// LDS and the barrier most of a step (64: 0.32 us a step, of which the matrix
+// instructions are 0.08).
 template <int B_> struct Tile;
 template <> struct Tile<64> {
-  static constexpr int B = 64, WR = 2, WC = 2, NS = 4;
+  static constexpr int B = 64, WR = 2, WC = 2, NS = 4, KG = 2;
 };
 template <> struct Tile<128> {
-  static constexpr int B = 128, WR = 2, WC = 2, NS = 2;
+  static constexpr int B = 128, WR = 2, WC = 2, NS = 2, KG = 2;
+};
+template <> struct Tile<192> {
+  static constexpr int B = 192, WR = 2, WC = 4, NS = 3, KG = 1;
 };
 template <> struct Tile<256> {
-  static constexpr int B = 256, WR = 2, WC = 4, NS = 2;
+  static constexpr int B = 256, WR = 2, WC = 4, NS = 2, KG = 1;
 };
+constexpr int pow2_of(int n) { return n & -n; }
+// In a wave's part of the tile, instruction tile (ii, jj) has rows 4 g + q and columns r at
+// row (4 g + q) TR + ii and column r TC + jj: a lane holds 4 TR consecutive rows of TC
+// consecutive columns.  (The factors' rows are put into LDS in that order.)
 template <class G> struct TileGeo {
-  static constexpr int NT = 64 * G::WR * G::WC;
+  static constexpr int NG = 64 * G::WR * G::WC, NT = NG * G::KG;  // threads of a group, of the workgroup
   static constexpr int TR = G::B / G::WR / 16, TC = G::B / G::WC / 16;
   static constexpr int STAGE = 2 * G::B * 128;  // bytes of one k-step
-  static constexpr int LD = G::B * 8 / NT;      // 16-byte loads a thread and factor
+  static constexpr int LDS = G::NS * G::KG * STAGE;
+  static constexpr int LD = G::B * 8 / NG;  // 16-byte loads a thread and factor
+  static constexpr int VJ = pow2_of(TC);
+  static constexpr int OROW = 16 * TR * 4 + 16;  // bytes of an output row of a wave in LDS
+  static_assert(4 * TR % 8 == 0 && TC <= 4, "rows are stored by eights, columns by at most four");
+  static_assert(16 * OROW * G::WR * G::WC <= LDS, "every wave's output rows in LDS");
+  // tile row of LDS row s, for a factor whose waves have T instruction tiles
+  static __device__ __forceinline__ int tile_row(int s, int T) { return s / (16 * T) * (16 * T) + s % 16 * T + s / 16 % T; }
 };
 
 // Both factors' rows of one k-step into LDS, 16 bytes a lane straight from memory.  LDS
@@ -172,24 +184,24 @@ template <class G> struct Loader {
     b = B + j0 * pair_row(ld) + (long long)k0 * 4;
 #pragma unroll
     for (int i = 0; i < T::LD; ++i) {
-      const int id = i * T::NT + threadIdx.x, row = id >> 3, c = (id & 7) ^ ((row >> 1) & 7);
-      ao[i] = (uint32_t)(min(row, ra - 1 - i0) * pair_row(ld)) + c * 16;
-      bo[i] = (uint32_t)(min(row, rb - 1 - j0) * pair_row(ld)) + c * 16;
+      const int id = i * T::NG + threadIdx.x % T::NG, row = id >> 3, c = (id & 7) ^ ((row >> 1) & 7);
+      ao[i] = (uint32_t)(min(T::tile_row(row, T::TR), ra - 1 - i0) * pair_row(ld)) + c * 16;
+      bo[i] = (uint32_t)(min(T::tile_row(row, T::TC), rb - 1 - j0) * pair_row(ld)) + c * 16;
     }
   }
-  // the next k-step into `stage`
+  // the group's next k-step into `stage`
   __device__ __forceinline__ void issue(char *stage) {
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x % T::NG >> 6);
 #pragma unroll
     for (int i = 0; i < T::LD; ++i)
-      __builtin_amdgcn_global_load_lds((global_void_t *)(a + ao[i]), (lds_void_t *)(stage + (i * T::NT + wave * 64) * 16), 16,
+      __builtin_amdgcn_global_load_lds((global_void_t *)(a + ao[i]), (lds_void_t *)(stage + (i * T::NG + wave * 64) * 16), 16,
                                        0, 0);
 #pragma unroll
     for (int i = 0; i < T::LD; ++i)
       __builtin_amdgcn_global_load_lds((global_void_t *)(b + bo[i]),
-                                       (lds_void_t *)(stage + G::B * 128 + (i * T::NT + wave * 64) * 16), 16, 0, 0);
-    a += 128;
-    b += 128;
+                                       (lds_void_t *)(stage + G::B * 128 + (i * T::NG + wave * 64) * 16), 16, 0, 0);
+    a += 128 * G::KG;
+    b += 128 * G::KG;
   }
 };
 
@@ -200,35 +212,56 @@ template <int N> __device__ __forceinline__ void wait_loads() {
 
 template <class G> using TileAcc = f32x4_t[TileGeo<G>::TR][TileGeo<G>::TC];
 
-// acc = A B' over k-steps [k0, k1) / 32: rows i0.. of A, j0.. of B.  Rows past the
-// arrays (ra, rb of them) read their last row; their results are not stored.
+// acc = A B' over the columns [k0, k1) (multiples of 32): rows i0.. of A, j0.. of B; the
+// first group's waves have it.  Rows past the arrays (ra, rb of them) read their last
+// row; their results are not stored.
 template <class G>
 __device__ __forceinline__ void tile_product(TileAcc<G> &acc, char *lds, const char *A, int ra, int i0, const char *B, int rb,
                                              int j0, int ld, int k0, int k1) {
   using T = TileGeo<G>;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x % T::NG >> 6, r = lane & 15, g = lane >> 4;
+  const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / T::NG);
 #pragma unroll
   for (int i = 0; i < T::TR; ++i)
 #pragma unroll
     for (int j = 0; j < T::TC; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  const int steps = (k1 - k0) / kStep;
-  Loader<G> load(A, ra, i0, B, rb, j0, ld, k0);
+  const int all = (k1 - k0) / kStep, steps = (all - group + G::KG - 1) / G::KG, turns = (all + G::KG - 1) / G::KG;
+  char *ring = lds + group * G::NS * T::STAGE;
+  Loader<G> load(A, ra, i0, B, rb, j0, ld, k0 + group * kStep);
 #pragma unroll
   for (int s = 0; s < G::NS - 1; ++s)
-    if (s < steps) load.issue(lds + s * T::STAGE);
+    if (s < steps) load.issue(ring + s * T::STAGE);
   // this lane's pieces of a fragment: (row r, hi g) and (row r, lo g)
   const int sw = (r >> 1) & 7;
   const int fh = r * 128 + ((g ^ sw) << 4), fl = r * 128 + (((4 + g) ^ sw) << 4);
   const int arow = (wave / G::WC) * T::TR * 2048, brow = G::B * 128 + (wave % G::WC) * T::TC * 2048;
-  int slot = 0;
-  for (int s = 0; s < steps; ++s) {
-    // the k-step's loads have landed (the later ones may be in flight), for every wave;
-    // and every wave is done with the slot that the next loads overwrite
-    if (s + G::NS - 1 <= steps) wait_loads<(G::NS - 2) * 2 * T::LD>();
-    else wait_loads<0>();
+  // Two halves of the waves, the later one a phase behind the other: while the matrix
+  // instructions of one run, the fragments of the other come from LDS.  A barrier ends
+  // every phase.  (Waves w and w + 4 share a SIMD.)
+  static_assert(T::NT == 512, "two waves a SIMD");
+  const bool late = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) >= 4;
+  auto barrier = [] {
+    __builtin_amdgcn_sched_barrier(0);
     asm volatile("s_barrier" ::: "memory");
-    if (s + G::NS - 1 < steps) load.issue(lds + (slot + G::NS - 1) % G::NS * T::STAGE);
-    const char *st = lds + slot * T::STAGE;
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto wait_lds = [] { __builtin_amdgcn_s_waitcnt(0xc07f); };  // lgkmcnt(0)
+  // the wave's loads of the k-step s + 1 have landed (later ones may be in flight)
+  auto wait_next = [&](int s) {
+    if (s + G::NS <= steps) wait_loads<(G::NS - 2) * 2 * T::LD>();
+    else wait_loads<0>();
+  };
+  constexpr int PH = G::KG == 1 ? 2 : 1, HR = T::TR / PH;  // phases of a k-step, rows of instruction tiles in one
+  static_assert(T::TR % PH == 0, "phases of equal rows");
+  wait_next(-1);
+  barrier();
+  if (late) barrier();
+  int slot = 0;
+  for (int s = 0; s < turns; ++s) {
+    // every wave has read all of the slot that the next loads overwrite: the reads of
+    // both halves were over before the last barrier
+    if (s + G::NS - 1 < steps) load.issue(ring + (slot + G::NS - 1) % G::NS * T::STAGE);
+    const char *st = ring + slot * T::STAGE;
     f16x8_t bh[T::TC], bl[T::TC];
 #pragma unroll
     for (int j = 0; j < T::TC; ++j) {
@@ -236,17 +269,59 @@ __device__ __forceinline__ void tile_product(TileAcc<G> &acc, char *lds, const c
       bl[j] = *reinterpret_cast<const f16x8_t *>(st + brow + j * 2048 + fl);
     }
 #pragma unroll
-    for (int i = 0; i < T::TR; ++i) {
-      const f16x8_t ah = *reinterpret_cast<const f16x8_t *>(st + arow + i * 2048 + fh);
-      const f16x8_t al = *reinterpret_cast<const f16x8_t *>(st + arow + i * 2048 + fl);
+    for (int half = 0; half < PH; ++half) {
+      f16x8_t ah[HR], al[HR];
 #pragma unroll
-      for (int j = 0; j < T::TC; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bl[j], acc[i][j], 0, 0, 0);
+      for (int i = 0; i < HR; ++i) {
+        ah[i] = *reinterpret_cast<const f16x8_t *>(st + arow + (half * HR + i) * 2048 + fh);
+        al[i] = *reinterpret_cast<const f16x8_t *>(st + arow + (half * HR + i) * 2048 + fl);
+      }
+      wait_lds();
+      // (one group: the early half reads the next k-step, all waves' loads of it, right
+      // after the barrier that ends the later half's last load phase)
+      if (G::KG == 1 && half == PH - 1) wait_next(s);
+      barrier();
+      if (G::KG == 1 || s < steps) {  // (a group without a last step only keeps the barriers)
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-      for (int j = 0; j < T::TC; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al, bh[j], acc[i][j], 0, 0, 0);
+        for (int i = 0; i < HR; ++i)
 #pragma unroll
-      for (int j = 0; j < T::TC; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bh[j], acc[i][j], 0, 0, 0);
+          for (int j = 0; j < T::TC; ++j)
+            acc[half * HR + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[i], bl[j], acc[half * HR + i][j], 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < HR; ++i)
+#pragma unroll
+          for (int j = 0; j < T::TC; ++j)
+            acc[half * HR + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al[i], bh[j], acc[half * HR + i][j], 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < HR; ++i)
+#pragma unroll
+          for (int j = 0; j < T::TC; ++j)
+            acc[half * HR + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[i], bh[j], acc[half * HR + i][j], 0, 0, 0);
+        __builtin_amdgcn_s_setprio(0);
+      }
+      if (G::KG > 1) wait_next(s);  // (two groups: each reads its own loads)
+      barrier();
     }
     slot = slot + 1 == G::NS ? 0 : slot + 1;
+  }
+  if (!late) barrier();
+  __syncthreads();  // the output goes through the LDS
+  if constexpr (G::KG > 1) {
+    static_assert(G::KG == 2 && G::B * G::B * 4 <= T::LDS, "the second group's accumulators in LDS");
+    f32x4_t *part = reinterpret_cast<f32x4_t *>(lds);
+#pragma unroll
+    for (int i = 0; i < T::TR; ++i)
+#pragma unroll
+      for (int j = 0; j < T::TC; ++j)
+        if (group == 1) part[((wave * T::TR + i) * T::TC + j) * 64 + lane] = acc[i][j];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < T::TR; ++i)
+#pragma unroll
+      for (int j = 0; j < T::TC; ++j)
+        if (group == 0) acc[i][j] += part[((wave * T::TR + i) * T::TC + j) * 64 + lane];
+    __syncthreads();
   }
 }
 
@@ -262,6 +337,85 @@ __device__ __forceinline__ void triangle_tile(int b, int t, int *ti, int *tj) {
   *tj = i + b - (i * t - i * (i - 1) / 2);
 }
 
+// where a lane's part of the tile begins
+template <class G> struct Origin {
+  int i, j;
+  __device__ __forceinline__ Origin(int ti, int tj) {
+    using T = TileGeo<G>;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;  // (of the first group)
+    i = ti * G::B + wave / G::WC * T::TR * 16 + (lane >> 4) * 4 * T::TR;
+    j = tj * G::B + wave % G::WC * T::TC * 16 + (lane & 15) * T::TC;
+  }
+};
+
+// value of the lane's row di (0 .. 4 TR - 1) and column jj
+template <class G> __device__ __forceinline__ float acc_at(const TileAcc<G> &acc, int di, int jj) {
+  return acc[di % TileGeo<G>::TR][jj][di / TileGeo<G>::TR];
+}
+
+// The tile times `scale` as pairs: by columns into `cols` (row j has the tile's column j,
+// `ldc` columns) and, unless null, by rows into `rows` (`ldr` columns).  Rows past ilim and
+// columns past jlim (multiples of 32) are not stored.  By rows sixteen lanes store 64
+// bytes in a piece as they are; by columns a lane has a whole line, and sixteen rows at
+// a time pass through the wave's part of the LDS so that eight lanes store a line
+// together (each its own line took 25 of a 256 tile's 42 us at 256 columns).
+template <class G>
+__device__ __forceinline__ void store_tile(const TileAcc<G> &acc, char *lds, int ti, int tj, float scale, char *cols, int ldc,
+                                           char *rows, int ldr, int ilim, int jlim) {
+  using T = TileGeo<G>;
+  const Origin<G> at(ti, tj);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+  const int iw = ti * G::B + wave / G::WC * T::TR * 16, jw = tj * G::B + wave % G::WC * T::TC * 16;  // the wave's part
+  char *mine = lds + wave * 16 * T::OROW;
+  f16x8_t hi[T::TR / 2][T::TC], lo[T::TR / 2][T::TC];
+#pragma unroll
+  for (int jj = 0; jj < T::TC; ++jj) {
+#pragma unroll
+    for (int e = 0; e < T::TR / 2; ++e) {
+      float x[8];
+#pragma unroll
+      for (int d = 0; d < 8; ++d) x[d] = acc_at<G>(acc, 8 * e + d, jj) * scale;
+      ns_split8(x, hi[e][jj], lo[e][jj]);
+      char *p = mine + r * T::OROW + pair_col(g * 4 * T::TR + 8 * e);
+      *reinterpret_cast<f16x8_t *>(p) = hi[e][jj];
+      *reinterpret_cast<f16x8_t *>(p + 64) = lo[e][jj];
+    }
+    // (the LDS accesses of one wave are in order)
+    constexpr int C = T::TR * 4;  // 16-byte pieces of a row
+#pragma unroll
+    for (int k = 0; k < T::TR; ++k) {
+      const int id = k * 64 + lane, row = id / C, c = id % C;
+      const u32x4_t v = *reinterpret_cast<const u32x4_t *>(mine + row * T::OROW + c * 16);
+      const int j = jw + row * T::TC + jj;
+      if (j < jlim && iw + (c >> 3) * 32 < ilim)
+        *reinterpret_cast<u32x4_t *>(cols + j * pair_row(ldc) + (iw >> 5) * 128 + c * 16) = v;
+    }
+  }
+  if (!rows) return;
+  typedef _Float16 vec_t __attribute__((ext_vector_type(T::VJ)));
+  char *rp = rows + at.i * pair_row(ldr);
+#pragma unroll
+  for (int e = 0; e < T::TR / 2; ++e) {
+    if (at.i + 8 * e >= ilim) break;
+#pragma unroll
+    for (int d = 0; d < 8; ++d)
+#pragma unroll
+      for (int j0 = 0; j0 < T::TC; j0 += T::VJ) {
+        vec_t h, l;
+#pragma unroll
+        for (int k = 0; k < T::VJ; ++k) {
+          h[k] = hi[e][j0 + k][d];
+          l[k] = lo[e][j0 + k][d];
+        }
+        if (at.j + j0 < jlim) {
+          char *p = rp + (8 * e + d) * pair_row(ldr) + pair_col(at.j + j0);
+          *reinterpret_cast<vec_t *>(p) = h;
+          *reinterpret_cast<vec_t *>(p + 64) = l;
+        }
+      }
+  }
+}
+
 // One product of every matrix of the launch.  A, B and the output are named by their
 // slots in the group's workspace:
 //   GRAM   part[slice] = X X' over the slice's columns (fp32, tiles of the upper triangle)
@@ -272,11 +426,11 @@ __device__ __forceinline__ void triangle_tile(int b, int t, int *ti, int *tj) {
 // The m x m products commute and are symmetric: tiles of the upper triangle, stored
 // both ways.
 template <int MODE, int TB, int DT>
-__global__ __launch_bounds__(TileGeo<Tile<TB>>::NT, TB == 256 ? 1 : 2) void ns_product_kernel(NsTable T, NsProduct p, void *out,
-                                                                                             uint16_t *v16, char *ws) {
+__global__ __launch_bounds__(TileGeo<Tile<TB>>::NT, 1) void ns_product_kernel(NsTable T, NsProduct p, void *out, uint16_t *v16,
+                                                                              char *ws) {
   using G = Tile<TB>;
   using TG = TileGeo<G>;
-  __shared__ __attribute__((aligned(16))) char lds[G::NS * TG::STAGE];
+  __shared__ __attribute__((aligned(16))) char lds[TG::LDS];
   const int l = ns_find(T, blockIdx.x);
   const NsMat &M = T.mat[l];
   const int b = blockIdx.x - T.first[l];
@@ -308,101 +462,102 @@ __global__ __launch_bounds__(TileGeo<Tile<TB>>::NT, TB == 256 ? 1 : 2) void ns_p
   }
   TileAcc<G> acc;
   tile_product<G>(acc, lds, A, ra, ti * TB, B, M.mp, tj * TB, ld, k0, k1);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if constexpr (MODE == NS_GRAM) {
-    // accumulators as they are: [tile][wave tile][lane]
-    float4 *part = (float4 *)(ws + M.ws_part) + ((long long)b * TG::NT / 64 * TG::TR * TG::TC) * 64;
+  if (threadIdx.x >= TG::NG) return;
+  char *o = ws + M.ws_sq + sq * p.out;
+  if (MODE == NS_GRAM && M.slices == 1) {
+    store_tile<G>(acc, lds, ti, tj, p.unscale * p.scale, o, M.mp, ti != tj ? o : nullptr, M.mp, M.mp, M.mp);
+  } else if constexpr (MODE == NS_GRAM) {
+    // accumulators as they are: [slice][tile][wave tile][lane]
+    float4 *part = (float4 *)(ws + M.ws_part) + (long long)b * (TB * TB / 4) + (threadIdx.x >> 6) * TG::TR * TG::TC * 64 +
+                   (threadIdx.x & 63);
 #pragma unroll
     for (int i = 0; i < TG::TR; ++i)
 #pragma unroll
       for (int j = 0; j < TG::TC; ++j)
-        part[((wave * TG::TR + i) * TG::TC + j) * 64 + lane] = make_float4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
-    return;
-  }
+        part[(i * TG::TC + j) * 64] = make_float4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
+  } else if constexpr (MODE == NS_POLY || MODE == NS_PROD) {
+    float scale = p.unscale * p.scale;
+    if constexpr (MODE == NS_POLY) {
+      // H is symmetric: eight consecutive columns of its row j
+      const Origin<G> at(ti, tj);
 #pragma unroll
-  for (int ii = 0; ii < TG::TR; ++ii)
+      for (int jj = 0; jj < TG::TC; ++jj)
 #pragma unroll
-    for (int jj = 0; jj < TG::TC; ++jj) {
-      const int i = ti * TB + ((wave / G::WC) * TG::TR + ii) * 16 + (lane >> 4) * 4;  // rows i .. i + 3
-      const int j = tj * TB + ((wave % G::WC) * TG::TC + jj) * 16 + (lane & 15);
-      if (j >= M.mp || i >= (kLong ? M.np : M.mp)) continue;
-      float x[4];
+        for (int e = 0; e < 4 * TG::TR; e += 8) {
+          if (at.j + jj >= M.mp || at.i + e >= M.mp) continue;
+          const char *h = A + (at.j + jj) * pair_row(M.mp) + pair_col(at.i + e);
+          const f16x8_t hh = *reinterpret_cast<const f16x8_t *>(h), hl = *reinterpret_cast<const f16x8_t *>(h + 64);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) x[q] = acc[ii][jj][q] * p.unscale;
-      if constexpr (MODE == NS_POLY || MODE == NS_PROD) {
-        char *o = ws + M.ws_sq + sq * p.out;
-        if constexpr (MODE == NS_POLY) {
-          // H is symmetric: four consecutive columns of its row j
-          const char *h = A + j * pair_row(M.mp) + pair_col(i);
-          const f16x4_t hh = *reinterpret_cast<const f16x4_t *>(h), hl = *reinterpret_cast<const f16x4_t *>(h + 64);
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            x[q] = p.cc * x[q] + p.cb * (((float)hh[q] + (float)hl[q]) * p.unscale_h);
-            if (i + q == j && j < M.m) x[q] += p.ca;
+          for (int d = 0; d < 8; ++d) {
+            const int ii = (e + d) % TG::TR, q = (e + d) / TG::TR;
+            float x = p.cc * (acc[ii][jj][q] * p.unscale) + p.cb * (((float)hh[d] + (float)hl[d]) * p.unscale_h);
+            if (at.i + e + d == at.j + jj && at.j + jj < M.m) x += p.ca;
+            acc[ii][jj][q] = x;
           }
         }
-#pragma unroll
-        for (int q = 0; q < 4; ++q) x[q] *= p.scale;
-        store_pairs<4>(o + j * pair_row(M.mp), i, x);
-        if (ti != tj) {
-#pragma unroll
-          for (int q = 0; q < 4; ++q) store_pairs<1>(o + (i + q) * pair_row(M.mp), j, {x[q]});
-        }
-      } else if constexpr (MODE == NS_APPLY) {
-        char *xt = ws + (p.a ? M.ws_xt : M.ws_xt2), *xn = ws + M.ws_xn;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) x[q] *= p.scale;
-        store_pairs<4>(xn + j * pair_row(M.np), i, x);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) store_pairs<1>(xt + (i + q) * pair_row(M.mp), j, {x[q]});
-      } else {
-        if (j >= M.m) continue;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          if (i + q >= M.n) continue;
-          const long long e = M.off + (M.tall ? (long long)(i + q) * M.m + j : (long long)j * M.n + i + q);
-          if (p.update) {
-            float *v = (float *)out;
-            const float w = v[e] - p.eta * (M.gain * x[q] + p.decay * v[e]);
-            v[e] = w;
-            if (v16) v16[e] = f2bf(w);
-          } else {
-            ((typename Store<DT>::T *)out)[e] = from_f32<DT>(x[q]);
-          }
-        }
-      }
+      scale = p.scale;
     }
+    store_tile<G>(acc, lds, ti, tj, scale, o, M.mp, ti != tj ? o : nullptr, M.mp, M.mp, M.mp);
+  } else if constexpr (MODE == NS_APPLY) {
+    store_tile<G>(acc, lds, ti, tj, p.unscale * p.scale, ws + M.ws_xn, M.np, ws + (p.a ? M.ws_xt : M.ws_xt2), M.mp, M.np, M.mp);
+  } else {
+    const Origin<G> at(ti, tj);
+    const Out dst{out, v16, p.update, p.eta, p.decay, M.gain};
+    if (M.tall) {
+#pragma unroll
+      for (int e = 0; e < 4 * TG::TR; ++e)
+#pragma unroll
+        for (int j0 = 0; j0 < TG::TC; j0 += TG::VJ) {
+          float x[TG::VJ];
+#pragma unroll
+          for (int k = 0; k < TG::VJ; ++k) x[k] = acc_at<G>(acc, e, j0 + k) * p.unscale;
+          if (at.i + e < M.n)
+            emit<DT, TG::VJ>(dst, M.off + (long long)(at.i + e) * M.m + at.j + j0, x, M.m - at.j - j0, M.m % 4 == 0);
+        }
+    } else {
+#pragma unroll
+      for (int jj = 0; jj < TG::TC; ++jj)
+#pragma unroll
+        for (int e = 0; e < 4 * TG::TR; e += 4) {
+          float x[4];
+#pragma unroll
+          for (int d = 0; d < 4; ++d) x[d] = acc_at<G>(acc, e + d, jj) * p.unscale;
+          if (at.j + jj < M.m)
+            emit<DT, 4>(dst, M.off + (long long)(at.j + jj) * M.n + at.i + e, x, M.n - at.i - e, M.n % 4 == 0);
+        }
+    }
+  }
 }
 
-// H = sum of the slices' Gram matrices, in slice order; one matrix-instruction tile a wave
-template <int TB> __global__ __launch_bounds__(256) void ns_gram_sum_kernel(NsTable T, int slot, float scale, char *ws) {
+// H = sum of the slices' Gram matrices, in slice order
+template <int TB>
+__global__ __launch_bounds__(TileGeo<Tile<TB>>::NG) void ns_gram_sum_kernel(NsTable T, int slot, float scale, char *ws) {
   using G = Tile<TB>;
   using TG = TileGeo<G>;
-  constexpr int PER = TB / 16 * (TB / 16);  // instruction tiles of a tile
+  __shared__ __attribute__((aligned(16))) char lds[16 * TG::OROW * G::WR * G::WC];
   const int l = ns_find(T, blockIdx.x);
   const NsMat &M = T.mat[l];
-  const int tm = (M.mp + TB - 1) / TB, tri = tm * (tm + 1) / 2;
-  const int lane = threadIdx.x & 63, w = (blockIdx.x - T.first[l]) * 4 + (threadIdx.x >> 6);
-  const int b = w / PER, k = w % PER, wave = k / (TG::TR * TG::TC);
+  const int tm = (M.mp + TB - 1) / TB, tri = tm * (tm + 1) / 2, b = blockIdx.x - T.first[l];
   int ti, tj;
   triangle_tile(b, tm, &ti, &tj);
-  const int i = ti * TB + ((wave / G::WC) * TG::TR + k / TG::TC % TG::TR) * 16 + (lane >> 4) * 4;
-  const int j = tj * TB + ((wave % G::WC) * TG::TC + k % TG::TC) * 16 + (lane & 15);
-  if (j >= M.mp || i >= M.mp) return;
-  const float4 *part = (const float4 *)(ws + M.ws_part) + ((long long)b * PER + k) * 64 + lane;
-  float4 s = part[0];
-#pragma unroll 4
-  for (int n = 1; n < M.slices; ++n) {
-    const float4 a = part[(long long)n * tri * PER * 64];
-    s.x += a.x; s.y += a.y; s.z += a.z; s.w += a.w;
-  }
-  const float x[4] = {s.x * scale, s.y * scale, s.z * scale, s.w * scale};
-  char *o = ws + M.ws_sq + (long long)M.mp * M.mp * 4 * slot;
-  store_pairs<4>(o + j * pair_row(M.mp), i, x);
-  if (ti != tj) {
+  const float4 *part = (const float4 *)(ws + M.ws_part) + (long long)b * (TB * TB / 4) + (threadIdx.x >> 6) * TG::TR * TG::TC * 64 +
+                       (threadIdx.x & 63);
+  TileAcc<G> acc;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) store_pairs<1>(o + (i + q) * pair_row(M.mp), j, {x[q]});
+  for (int i = 0; i < TG::TR; ++i)
+#pragma unroll
+    for (int j = 0; j < TG::TC; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  for (int n = 0; n < M.slices; ++n) {
+#pragma unroll
+    for (int i = 0; i < TG::TR; ++i)
+#pragma unroll
+      for (int j = 0; j < TG::TC; ++j) {
+        const float4 a = part[(long long)n * tri * (TB * TB / 4) + (i * TG::TC + j) * 64];
+        acc[i][j] += f32x4_t{a.x, a.y, a.z, a.w};
+      }
   }
+  char *o = ws + M.ws_sq + (long long)M.mp * M.mp * 4 * slot;
+  store_tile<G>(acc, lds, ti, tj, scale, o, M.mp, ti != tj ? o : nullptr, M.mp, M.mp, M.mp);
 }
 
 }  // namespace
@@ -470,6 +625,26 @@ bool ns_scales(double a, double b, double c, int steps, NsSteps *S) {
   return true;
 }
 
+namespace {
+// Time of a product of `tiles` tiles over `ksteps` k-steps, in us: rounds of a tile a
+// compute unit, each a launch's and tile's fixed share and its k-steps, which take 1.4
+// times as long on a full machine as on an empty one.  Measured on square matrices (tiles
+// of the triangle; m x m products of 64 / 128 / 192 / 256 in us): 512 8.2 / 13.6 / 28 / 34,
+// 1024 12.6 / 19.9 / 44 / 56, 1536 33 / 28 / 60 / 79, 2048 64 / 39 / 79 / 105,
+// 3200 - / 120 / 126 / 168, 4096 - / 242 / 187 / 223.
+struct TileCost {
+  int tile;
+  double fixed, step;
+};
+constexpr TileCost kTileCost[] = {{64, 4.4, 0.25}, {128, 6.5, 0.42}, {192, 11.5, 1.0}, {256, 21.5, 1.45}};
+double tile_time(const TileCost &c, long long tiles, long long ksteps) {
+  const long long full = tiles / kNumCUs, rest = tiles % kNumCUs;
+  double t = full * (c.fixed + 1.4 * c.step * ksteps);
+  if (rest) t += c.fixed + (1.0 + 0.4 * rest / kNumCUs) * c.step * ksteps;
+  return t;
+}
+}  // namespace
+
 size_t ns_plan(int count, const long long *off, const int *rows, const int *cols, int dtype, bool momentum, NsTable *T) {
   long long at = 0;
   auto take = [&](long long bytes) {
@@ -522,15 +697,21 @@ size_t ns_plan(int count, const long long *off, const int *rows, const int *cols
     M.ws_sq = take(4 * sq * SQ_COUNT);
     auto tiles = [](long long rows, long long tb) { return (rows + tb - 1) / tb; };
     auto triangle = [&](long long tb) { return tiles(M.mp, tb) * (tiles(M.mp, tb) + 1) / 2; };
-    M.tile_sq = triangle(256) >= 128 ? 256 : triangle(128) >= 256 ? 128 : 64;
-    auto rect = [&](long long tb) { return tiles(M.mp, tb) * tiles(M.np, tb); };
-    M.tile_long = rect(256) >= 192 ? 256 : rect(128) >= 192 ? 128 : 64;
-    // slices of the long side: about two workgroups a compute unit, eight k-steps at least
-    const long long tri = triangle(M.tile_sq), ksteps = M.np / kStep;
-    long long slices = (2 * kNumCUs + tri - 1) / tri;
-    if (slices > ksteps / 8) slices = ksteps / 8 > 0 ? ksteps / 8 : 1;
-    M.slices = (int)slices;
-    M.ws_part = take(4LL * tri * M.tile_sq * M.tile_sq * slices);
+    double best_sq = 1e30, best_long = 1e30, best_gram = 1e30;
+    const long long ksteps = M.np / kStep;
+    for (const TileCost &c : kTileCost) {
+      const double sq = tile_time(c, triangle(c.tile), M.mp / kStep);
+      if (sq < best_sq) best_sq = sq, M.tile_sq = c.tile;
+      const double lng = tile_time(c, tiles(M.mp, c.tile) * tiles(M.np, c.tile), M.mp / kStep);
+      if (lng < best_long) best_long = lng, M.tile_long = c.tile;
+      // the Gram product also in slices of the long side, whose sums another launch adds
+      for (long long s = 1; s <= 64 && (s == 1 || s * 8 <= ksteps); ++s) {
+        const double bytes = 8.0 * s * triangle(c.tile) * c.tile * c.tile;  // written and read
+        const double gram = tile_time(c, triangle(c.tile) * s, (ksteps + s - 1) / s) + (s > 1 ? 5.0 + bytes / 4e6 : 0.0);
+        if (gram < best_gram) best_gram = gram, M.tile_gram = c.tile, M.slices = (int)s;
+      }
+    }
+    M.ws_part = M.slices > 1 ? take(4LL * triangle(M.tile_gram) * M.tile_gram * M.tile_gram * M.slices) : 0;
   }
   return (size_t)at;
 }
@@ -556,23 +737,25 @@ hipError_t launch_newton_schulz(const NsTable &T0, const NsSteps &S, int dtype, 
   else
     hipLaunchKernelGGL((ns_split_kernel<DT_F32>), dim3(nb), dim3(256), 0, st, T, S.eps, sx0, g, ws);
   // f(tile) for each tile size that a matrix of the table uses in this product
-  auto each_tile = [&](bool is_long, auto f) {
+  auto each_tile = [&](int NsMat::*side, auto f) {
     auto used = [&](int tb) {
       for (int l = 0; l < T.count; ++l)
-        if (!T.mat[l].mt && (is_long ? T.mat[l].tile_long : T.mat[l].tile_sq) == tb) return true;
+        if (!T.mat[l].mt && T.mat[l].*side == tb) return true;
       return false;
     };
     if (used(256)) f(std::integral_constant<int, 256>{});
+    if (used(192)) f(std::integral_constant<int, 192>{});
     if (used(128)) f(std::integral_constant<int, 128>{});
     if (used(64)) f(std::integral_constant<int, 64>{});
   };
   auto product = [&](auto mode, auto dt, NsProduct p) {
     constexpr int MODE = decltype(mode)::value, DT = decltype(dt)::value;
     constexpr bool kLong = MODE == NS_APPLY || MODE == NS_FINAL;
-    each_tile(kLong, [&](auto tile) {
+    constexpr int NsMat::*side = kLong ? &NsMat::tile_long : MODE == NS_GRAM ? &NsMat::tile_gram : &NsMat::tile_sq;
+    each_tile(side, [&](auto tile) {
       constexpr int TB = decltype(tile)::value;
-      const int blocks = number(&T, [](const NsMat &M) {
-        if ((kLong ? M.tile_long : M.tile_sq) != TB) return 0LL;
+      const int blocks = number(&T, [=](const NsMat &M) {
+        if (M.*side != TB) return 0LL;
         const long long t = (M.mp + TB - 1) / TB;
         return kLong ? t * ((M.np + TB - 1) / TB) : t * (t + 1) / 2 * (MODE == NS_GRAM ? M.slices : 1);
       });
@@ -596,14 +779,16 @@ hipError_t launch_newton_schulz(const NsTable &T0, const NsSteps &S, int dtype, 
       p.ca = a; p.cb = b; p.cc = c;
       product(mode, F32{}, p);
     };
-    square(Gram{}, 0, 0, 0, 1.f, 0.f, 0.f);
-    each_tile(false, [&](auto tile) {
+    square(Gram{}, 0, 0, SQ_H, 1.f / (G.sx * G.sx), 0.f, G.sh[0]);
+    each_tile(&NsMat::tile_gram, [&](auto tile) {
       constexpr int TB = decltype(tile)::value;
       nb = number(&T, [](const NsMat &M) {
         const long long t = (M.mp + TB - 1) / TB;
-        return M.tile_sq == TB ? t * (t + 1) / 2 * (TB / 16 * (TB / 16) / 4) : 0LL;
+        return M.tile_gram == TB && M.slices > 1 ? t * (t + 1) / 2 : 0LL;
       });
-      hipLaunchKernelGGL((ns_gram_sum_kernel<TB>), dim3(nb), dim3(256), 0, st, T, (int)SQ_H, G.sh[0] / (G.sx * G.sx), ws);
+      if (nb)
+        hipLaunchKernelGGL((ns_gram_sum_kernel<TB>), dim3(nb), dim3(TileGeo<Tile<TB>>::NG), 0, st, T, (int)SQ_H,
+                           G.sh[0] / (G.sx * G.sx), ws);
     });
     square(Poly{}, SQ_H, SQ_H, SQ_Q, 1.f / (G.sh[0] * G.sh[0]), 1.f / G.sh[0], G.sq[0]);
     int slot = SQ_Q;

@@ -124,40 +124,6 @@ template <bool F32, int N> __device__ __forceinline__ void store_elements(char *
   }
 }
 
-template <int VW> __device__ __forceinline__ void load_cols(const float *p, float (&x)[VW]) {
-  if constexpr (VW == 4) {
-    const float4 a = *reinterpret_cast<const float4 *>(p);
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-  } else if constexpr (VW == 2) {
-    const float2 a = *reinterpret_cast<const float2 *>(p);
-    x[0] = a.x; x[1] = a.y;
-  } else {
-    x[0] = *p;
-  }
-}
-
-template <int VW> __device__ __forceinline__ void store_cols(float *p, const float (&x)[VW]) {
-  if constexpr (VW == 4) *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
-  else if constexpr (VW == 2) *reinterpret_cast<float2 *>(p) = make_float2(x[0], x[1]);
-  else *p = x[0];
-}
-
-// x s1 s2.  s1 is 1 unless 1 / norm is past where fp32's range ends but its product
-// with x is not; without `on` x is taken as it is.
-struct Scale {
-  bool on;
-  float s1, s2;
-};
-__device__ __forceinline__ Scale scale_of(double inv, float sx) {
-  int e = 0;
-  (void)frexp(inv, &e);
-  Scale s;
-  s.on = true;
-  e = e > 100 || e < -100 ? min(max(e, -126), 126) : 0;
-  s.s1 = ldexpf(1.0f, e);
-  s.s2 = (float)(inv * (double)sx * ldexp(1.0, -e));
-  return s;
-}
 // ---- Gram matrix of 32 rows ----------------------------------------------------
 
 template <int MT> struct Acc {
@@ -358,56 +324,6 @@ __device__ __forceinline__ void apply_gram_steps(Acc<MT> &acc, ApplyRows<MT> &x,
 }
 
 // ---- the output -----------------------------------------------------------------
-
-struct Out {
-  void *o;
-  uint16_t *v16;
-  int update;
-  float eta, decay, gain;
-};
-
-__device__ __forceinline__ float update_one(const Out &o, float v, float x) { return v - o.eta * (o.gain * x + o.decay * v); }
-
-// element e
-template <int DT> __device__ __forceinline__ void emit1(const Out &o, long long e, float x) {
-  if (o.update) {
-    float *v = (float *)o.o + e;
-    const float a = update_one(o, *v, x);
-    *v = a;
-    if (o.v16) o.v16[e] = f2bf(a);
-  } else {
-    ((typename Store<DT>::T *)o.o)[e] = from_f32<DT>(x);
-  }
-}
-
-// elements e .. e + 3, e a multiple of 4
-template <int DT> __device__ __forceinline__ void emit4(const Out &o, long long e, const float (&x)[4]) {
-  if (o.update) {
-    float a[4];
-    load_cols<4>((float *)o.o + e, a);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) a[i] = update_one(o, a[i], x[i]);
-    store_cols<4>((float *)o.o + e, a);
-    if (o.v16) *reinterpret_cast<uint2 *>(o.v16 + e) = make_uint2(f2bf2(a[0], a[1]), f2bf2(a[2], a[3]));
-  } else if constexpr (DT == DT_F32) {
-    store_cols<4>((float *)o.o + e, x);
-  } else {
-    *reinterpret_cast<uint2 *>((uint16_t *)o.o + e) = make_uint2(f2bf2(x[0], x[1]), f2bf2(x[2], x[3]));
-  }
-}
-
-// the first k of W consecutive elements from e on
-template <int DT, int W> __device__ __forceinline__ void emit(const Out &o, long long e, const float (&x)[W], int k, bool vec) {
-  if constexpr (W == 4) {
-    if (vec && k >= 4) {
-      emit4<DT>(o, e, x);
-      return;
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < W; ++i)
-    if (i < k) emit1<DT>(o, e + i, x[i]);
-}
 
 template <int MT, int DT>
 __device__ __forceinline__ void final_steps(const NsMat &M, const Out &o, ApplyRows<MT> &x, const float *src, int first,
