@@ -258,6 +258,7 @@ struct NsMat {
   int tall;
   int mt;             // m padded to 16, 32, 64 or 128 where the skinny kernels run it, else 0
   int shift, chunks;  // of the norm pass
+  int whole;          // skinny: one workgroup runs the whole iteration
   int prow;           // skinny: rows of the long side in a chunk
   int tile_sq, tile_long, tile_gram;  // sides of the general kernels' tiles: m x m products, n x m, X X'
   int slices;         // of the long side in the Gram product (skinny: workgroups)
@@ -271,6 +272,7 @@ constexpr int kNsFewSlices = 2;  // so many slices the polynomial kernel adds it
 struct NsTable {
   int count;
   int first[kNsTable + 1];  // first workgroup of each matrix in the launch
+  int wholes, whole[kNsTable];  // the matrices with `whole`
   NsMat mat[kNsTable];
 };
 struct NsMomentum {

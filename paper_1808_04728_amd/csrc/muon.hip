@@ -512,7 +512,7 @@ __global__ __launch_bounds__(TileGeo<Tile<TB>>::NT, 1) void ns_product_kernel(Ns
 #pragma unroll
           for (int k = 0; k < TG::VJ; ++k) x[k] = acc_at<G>(acc, e, j0 + k) * p.unscale;
           if (at.i + e < M.n)
-            emit<DT, TG::VJ>(dst, M.off + (long long)(at.i + e) * M.m + at.j + j0, x, M.m - at.j - j0, M.m % 4 == 0);
+            emit<DT, TG::VJ>(dst, M.off + (long long)(at.i + e) * M.m + at.j + j0, x, M.m - at.j - j0);
         }
     } else {
 #pragma unroll
@@ -523,7 +523,7 @@ __global__ __launch_bounds__(TileGeo<Tile<TB>>::NT, 1) void ns_product_kernel(Ns
 #pragma unroll
           for (int d = 0; d < 4; ++d) x[d] = acc_at<G>(acc, e + d, jj) * p.unscale;
           if (at.j + jj < M.m)
-            emit<DT, 4>(dst, M.off + (long long)(at.j + jj) * M.n + at.i + e, x, M.n - at.i - e, M.n % 4 == 0);
+            emit<DT, 4>(dst, M.off + (long long)(at.j + jj) * M.n + at.i + e, x, M.n - at.i - e);
         }
     }
   }
@@ -653,6 +653,7 @@ size_t ns_plan(int count, const long long *off, const int *rows, const int *cols
     return p;
   };
   T->count = count;
+  T->wholes = 0;
   for (int l = 0; l < count; ++l) {
     NsMat &M = T->mat[l];
     M.off = off[l];
@@ -665,6 +666,11 @@ size_t ns_plan(int count, const long long *off, const int *rows, const int *cols
       int mt = 16;
       while (mt < M.m) mt *= 2;
       M.mt = mt;
+      // One workgroup runs what takes it no longer than the large matrices' Gram launch,
+      // beside which it runs: 512 x 16 and 256 x 32 24 us, 64 x 64 23 (1024 x 32 66, 256 x 64 32;
+      // the other kernels' launches take about 35 for any small matrix).
+      M.whole = (long long)M.n * mt <= (mt <= 32 ? 8192 : 4096) && mt <= 64;
+      if (M.whole) T->whole[T->wholes++] = l;
       // chunks of about 8192 elements, at most 512
       M.prow = (int)up(8192 / mt, 64);
       while (((long long)M.n + M.prow - 1) / M.prow > 512) M.prow *= 2;

@@ -127,26 +127,36 @@ template <int DT> __device__ __forceinline__ void emit1(const Out &o, long long 
   }
 }
 
-// elements e .. e + 3, e a multiple of 4
+// four values at the alignment of one element
+typedef uint32_t u32x4f_t __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x2h_t __attribute__((ext_vector_type(2), aligned(2)));
+
+// elements e .. e + 3
 template <int DT> __device__ __forceinline__ void emit4(const Out &o, long long e, const float (&x)[4]) {
-  if (o.update) {
-    float a[4];
-    load_cols<4>((float *)o.o + e, a);
+  if (DT == DT_F32 || o.update) {
+    u32x4f_t *p = reinterpret_cast<u32x4f_t *>((float *)o.o + e);
+    u32x4f_t a;
+    if (o.update) {
+      a = *p;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) a[i] = update_one(o, a[i], x[i]);
-    store_cols<4>((float *)o.o + e, a);
-    if (o.v16) *reinterpret_cast<uint2 *>(o.v16 + e) = make_uint2(f2bf2(a[0], a[1]), f2bf2(a[2], a[3]));
-  } else if constexpr (DT == DT_F32) {
-    store_cols<4>((float *)o.o + e, x);
+      for (int i = 0; i < 4; ++i) a[i] = __float_as_uint(update_one(o, __uint_as_float(a[i]), x[i]));
+      if (o.v16)
+        *reinterpret_cast<u32x2h_t *>(o.v16 + e) = u32x2h_t{f2bf2(__uint_as_float(a[0]), __uint_as_float(a[1])),
+                                                            f2bf2(__uint_as_float(a[2]), __uint_as_float(a[3]))};
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[i] = __float_as_uint(x[i]);
+    }
+    *p = a;
   } else {
-    *reinterpret_cast<uint2 *>((uint16_t *)o.o + e) = make_uint2(f2bf2(x[0], x[1]), f2bf2(x[2], x[3]));
+    *reinterpret_cast<u32x2h_t *>((uint16_t *)o.o + e) = u32x2h_t{f2bf2(x[0], x[1]), f2bf2(x[2], x[3])};
   }
 }
 
 // the first k of W consecutive elements from e on
-template <int DT, int W> __device__ __forceinline__ void emit(const Out &o, long long e, const float (&x)[W], int k, bool vec) {
+template <int DT, int W> __device__ __forceinline__ void emit(const Out &o, long long e, const float (&x)[W], int k) {
   if constexpr (W == 4) {
-    if (vec && k >= 4) {
+    if (k >= 4) {
       emit4<DT>(o, e, x);
       return;
     }
