@@ -264,10 +264,11 @@ struct NsMat {
   int slices;         // of the long side in the Gram product (skinny: workgroups)
   float gain;         // of the update
   // byte offsets in the workspace: chunk sums, u (-1: none), X [m][n], X' [n][m] twice,
-  // the m x m matrices, the Gram matrix's slices.  Skinny: u and X are fp32 [n][mt], the
-  // one m x m matrix is P, ws_sum holds the slices' sum.
-  long long ws_norm, ws_u, ws_xn, ws_xt, ws_xt2, ws_sq, ws_part, ws_sum;
+  // the m x m matrices, the Gram matrix's slices.  Skinny: u and X are fp32 [n][mt], two
+  // buffers of slices take turns, ws_sum holds the slices' sum.
+  long long ws_norm, ws_u, ws_xn, ws_xt, ws_xt2, ws_sq, ws_part, ws_part2, ws_sum;
 };
+constexpr int kNsSlices = 171;   // most workgroups of a skinny matrix
 constexpr int kNsFewSlices = 2;  // so many slices the polynomial kernel adds itself
 struct NsTable {
   int count;

@@ -675,17 +675,18 @@ size_t ns_plan(int count, const long long *off, const int *rows, const int *cols
       M.prow = (int)up(8192 / mt, 64);
       while (((long long)M.n + M.prow - 1) / M.prow > 512) M.prow *= 2;
       M.chunks = (M.n + M.prow - 1) / M.prow;
-      // workgroups of four waves: a wave takes 32 rows at a time
-      const long long wgs = ((long long)M.n + 127) / 128;
-      M.slices = (int)(wgs < kNumCUs ? wgs : kNumCUs);
+      // Workgroups of the long side: 256 rows at a time (128 of 128 columns), on at most
+      // two thirds of the compute units so that a call's other matrices run beside.
+      const long long wgs = ((long long)M.n + (mt == 128 ? 127 : 255)) / (mt == 128 ? 128 : 256);
+      M.slices = (int)(wgs < kNsSlices ? wgs : kNsSlices);
       const int tt = mt / 16;
       const bool direct = !momentum && dtype == DT_F32 && M.tall && M.m == mt;
       M.ws_norm = take(8LL * M.chunks);
       const long long x = take(4LL * M.n * mt);
       M.ws_u = direct ? -1 : x;
       M.ws_xn = x;
-      M.ws_sq = take((long long)mt * ((tt + 1) / 2) * 128);
       M.ws_part = take(1024LL * (tt * (tt + 1) / 2) * M.slices);
+      M.ws_part2 = M.slices > kNsFewSlices ? M.ws_part : take(1024LL * (tt * (tt + 1) / 2) * M.slices);
       M.ws_sum = take(1024LL * (tt * (tt + 1) / 2));
       continue;
     }

@@ -17,21 +17,26 @@ __device__ __forceinline__ int ns_find(const NsTable &T, int b) {
   return l;
 }
 
-// Sum of a double over 256 threads in a fixed order.
-__device__ __forceinline__ double ns_block_sum(double a, double *red) {
+// Sum of a double over W waves in a fixed order.
+template <int W = 4> __device__ __forceinline__ double ns_block_sum(double a, double *red) {
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) a += __shfl_xor(a, o, 64);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = a;
   __syncthreads();
-  return (red[0] + red[1]) + (red[2] + red[3]);
+  double s = red[0];
+#pragma unroll
+  for (int w = 1; w < W; ++w) s += red[w];
+  return s;
 }
 
-// 1 / (||u|| + eps) from the chunks' sums, by every workgroup in the same order
-__device__ __forceinline__ double ns_inv_norm(const NsMat &M, const char *ws, double eps, double *red) {
+// 1 / (||u|| + eps) from the chunks' sums, by every workgroup in the same order: 256
+// threads' shares, whatever the number of threads
+template <int W = 4> __device__ __forceinline__ double ns_inv_norm(const NsMat &M, const char *ws, double eps, double *red) {
   const double *p = (const double *)(ws + M.ws_norm);
   double s = 0.0;
-  for (int i = threadIdx.x; i < M.chunks; i += 256) s += p[i];
-  return 1.0 / (sqrt(ns_block_sum(s, red)) + eps);
+  if (W == 4 || threadIdx.x < 256)
+    for (int i = threadIdx.x; i < M.chunks; i += 256) s += p[i];
+  return 1.0 / (sqrt(ns_block_sum<W>(s, red)) + eps);
 }
 
 struct Half2 {
@@ -45,13 +50,13 @@ __device__ __forceinline__ Half2 ns_split(float x) {
   return r;
 }
 
-// The same of eight values at two instructions a value: hi by pairs, the remainder
+// The same of N values (N even) at two instructions a value: hi by pairs, the remainder
 // x - hi as a mixed-precision fma, which reads hi's halves in place.
-__device__ __forceinline__ void ns_split8(const float (&x)[8], f16x8_t &hi, f16x8_t &lo) {
+template <int N, class V> __device__ __forceinline__ void ns_split_pairs(const float (&x)[N], V &hi, V &lo) {
   typedef float f32x2_t __attribute__((ext_vector_type(2)));
   typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 #pragma unroll
-  for (int i = 0; i < 8; i += 2) {
+  for (int i = 0; i < N; i += 2) {
     const f16x2_t h = __builtin_convertvector((f32x2_t{x[i], x[i + 1]}), f16x2_t);
     float a, b;
     asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(a) : "v"(h), "v"(x[i]));
@@ -63,6 +68,7 @@ __device__ __forceinline__ void ns_split8(const float (&x)[8], f16x8_t &hi, f16x
     lo[i + 1] = l[1];
   }
 }
+__device__ __forceinline__ void ns_split8(const float (&x)[8], f16x8_t &hi, f16x8_t &lo) { ns_split_pairs<8>(x, hi, lo); }
 
 // one element of the momentum update: new momentum in m, returns the update u
 __device__ __forceinline__ float ns_momentum(const NsMomentum &mom, float g, float &m) {

@@ -24,6 +24,8 @@
 // Up to 32 columns factors are fp32 (the fp32 matrix rate covers them), above they
 // are fp16 pairs as in muon.hip.
 
+#include <utility>
+
 #include "muon_common.h"
 
 namespace cf {
@@ -38,7 +40,7 @@ template <int MT> struct Geo {
   static constexpr int TRI = TT * (TT + 1) / 2;   // tiles of the upper triangle
   static constexpr int LROW = KB * 128 + 16;      // bytes of a matrix row in LDS
   static constexpr int MAT = MT * LROW;           // bytes of a matrix in LDS
-  static constexpr int RED = 4 * TRI * 1024;      // bytes of four waves' Gram tiles
+  static constexpr int SET = TRI * 1024;          // bytes of a Gram matrix's tiles
 };
 
 // eight values of a factor, k = (g, 0..7) of a 32-deep product
@@ -59,11 +61,6 @@ template <bool F32> __device__ __forceinline__ Frag<F32> make_frag(const float (
     ns_split8(x, f.hi, f.lo);
   }
   return f;
-}
-
-template <bool F32> __device__ __forceinline__ float frag_value(const Frag<F32> &f, int j) {
-  if constexpr (F32) return f.v[j];
-  else return (float)f.hi[j] + (float)f.lo[j];
 }
 
 // acc += A B over the 32 k of the fragments
@@ -113,14 +110,26 @@ template <bool F32, int N> __device__ __forceinline__ void store_elements(char *
   } else {
     typedef _Float16 vec_t __attribute__((ext_vector_type(N)));
     vec_t hi, lo;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const Half2 s = ns_split(x[i]);
-      hi[i] = s.hi;
-      lo[i] = s.lo;
+    if constexpr (N == 1) {
+      const Half2 s = ns_split(x[0]);
+      hi[0] = s.hi;
+      lo[0] = s.lo;
+    } else {
+      ns_split_pairs<N>(x, hi, lo);
     }
     *reinterpret_cast<vec_t *>(p + 2 * j) = hi;
     *reinterpret_cast<vec_t *>(p + 16 + 2 * j) = lo;
+  }
+}
+
+// four elements from j on of the fragment at p
+template <bool F32> __device__ __forceinline__ void load_elements(const char *p, int j, float (&x)[4]) {
+  if constexpr (F32) {
+    load_cols<4>(reinterpret_cast<const float *>(p + 4 * j), x);
+  } else {
+    const f16x4_t hi = *reinterpret_cast<const f16x4_t *>(p + 2 * j), lo = *reinterpret_cast<const f16x4_t *>(p + 16 + 2 * j);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) x[q] = (float)hi[q] + (float)lo[q];
   }
 }
 
@@ -174,21 +183,32 @@ template <int MT> struct GramRows {
   }
 };
 
-// the four waves' accumulators added in wave order, to out [TRI][64 lanes][4]
-template <int MT> __device__ __forceinline__ void gram_out(const Acc<MT> &acc, char *lds, float unscale, float *out) {
+// The sum of SETS Gram matrices in LDS, tile by tile, in order, to out [TRI][64 lanes][4]
+template <int MT, int SETS> __device__ __forceinline__ void gram_sum(const char *lds, float unscale, float *out) {
+  constexpr int N = Geo<MT>::TRI * 64;
+  const float4 *red = reinterpret_cast<const float4 *>(lds);
+  __syncthreads();
+  for (int i = threadIdx.x; i < N; i += blockDim.x) {
+    f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < SETS; ++k) {
+      const float4 a = red[k * N + i];
+      s += f32x4_t{a.x, a.y, a.z, a.w};
+    }
+    reinterpret_cast<float4 *>(out)[i] = make_float4(s[0] * unscale, s[1] * unscale, s[2] * unscale, s[3] * unscale);
+  }
+}
+
+// the waves' accumulators added in wave order
+template <int MT, int WAVES> __device__ __forceinline__ void gram_out(const Acc<MT> &acc, char *lds, float unscale, float *out) {
   using G = Geo<MT>;
-  float4 *red = reinterpret_cast<float4 *>(lds);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   __syncthreads();  // whatever the LDS held has been read
 #pragma unroll
   for (int t = 0; t < G::TRI; ++t)
-    red[(wave * G::TRI + t) * 64 + lane] = make_float4(acc.t[t][0], acc.t[t][1], acc.t[t][2], acc.t[t][3]);
-  __syncthreads();
-  for (int i = threadIdx.x; i < G::TRI * 64; i += 256) {
-    const float4 a = red[i], b = red[G::TRI * 64 + i], c = red[2 * G::TRI * 64 + i], d = red[3 * G::TRI * 64 + i];
-    reinterpret_cast<float4 *>(out)[i] = make_float4(((a.x + b.x) + (c.x + d.x)) * unscale, ((a.y + b.y) + (c.y + d.y)) * unscale,
-                                                     ((a.z + b.z) + (c.z + d.z)) * unscale, ((a.w + b.w) + (c.w + d.w)) * unscale);
-  }
+    reinterpret_cast<float4 *>(lds)[(wave * G::TRI + t) * 64 + lane] =
+        make_float4(acc.t[t][0], acc.t[t][1], acc.t[t][2], acc.t[t][3]);
+  gram_sum<MT, WAVES>(lds, unscale, out);
 }
 
 // ---- X P of 32 rows ------------------------------------------------------------
@@ -238,20 +258,20 @@ template <int MT> struct ApplyRows {
   }
 };
 
-// d[s][t] = rows 16 s + 4 g + 0..3 of slot 16 t + r of X P, P in LDS
-template <int MT>
-__device__ __forceinline__ void apply_product(f32x4_t (&d)[2][Geo<MT>::TT], const Frag<Geo<MT>::F32> (&a)[2][Geo<MT>::KB],
-                                              const char *P) {
+// d[s][t] = rows 16 s + 4 g + 0..3 of slot 16 t + r of X P, P in LDS from its first of
+// N tiles on
+template <int MT, int N>
+__device__ __forceinline__ void apply_product(f32x4_t (&d)[2][N], const Frag<Geo<MT>::F32> (&a)[2][Geo<MT>::KB], const char *P) {
   using G = Geo<MT>;
   const int r = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
 #pragma unroll
   for (int s = 0; s < 2; ++s)
 #pragma unroll
-    for (int t = 0; t < G::TT; ++t) d[s][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < N; ++t) d[s][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int kb = 0; kb < G::KB; ++kb) {
 #pragma unroll
-    for (int t = 0; t < G::TT; ++t) {
+    for (int t = 0; t < N; ++t) {
       const Frag<G::F32> b = load_frag<G::F32>(P + (16 * t + r) * G::LROW + kb * 128 + g * 32);
 #pragma unroll
       for (int s = 0; s < 2; ++s) mma<G::F32>(d[s][t], a[s][kb], b);
@@ -261,23 +281,42 @@ __device__ __forceinline__ void apply_product(f32x4_t (&d)[2][Geo<MT>::TT], cons
   }
 }
 
-// P from the workspace to LDS
-template <int MT> __device__ __forceinline__ void load_p(const char *src, char *lds) {
+// d scaled, and as Gram factors
+template <int MT, int N>
+__device__ __forceinline__ void scale_rows(f32x4_t (&d)[2][N], Frag<Geo<MT>::F32> (&f)[N], float unscale) {
   using G = Geo<MT>;
-  constexpr int C = G::KB * 8;  // 16-byte pieces of a row
-  constexpr int N = (MT * C + 255) / 256;
-  u32x4_t v[N];
 #pragma unroll
-  for (int k = 0; k < N; ++k) {
-    const int i = threadIdx.x + 256 * k;
-    if (MT * C % 256 == 0 || i < MT * C) v[k] = reinterpret_cast<const u32x4_t *>(src)[i];
-  }
+  for (int t = 0; t < N; ++t) {
+    float v[8];
 #pragma unroll
-  for (int k = 0; k < N; ++k) {
-    const int i = threadIdx.x + 256 * k;
-    if (MT * C % 256 == 0 || i < MT * C) *reinterpret_cast<u32x4_t *>(lds + i / C * G::LROW + i % C * 16) = v[k];
+    for (int j = 0; j < 8; ++j) {
+      d[j >> 2][t][j & 3] *= unscale;
+      v[j] = d[j >> 2][t][j & 3];
+    }
+    f[t] = make_frag<G::F32>(v);
   }
-  __syncthreads();
+}
+
+// d as rows n0 .. n0 + 31 of X, groups of VW tiles from column col0 on
+template <int MT, int N>
+__device__ __forceinline__ void store_rows(const f32x4_t (&d)[2][N], float *X, int n, int n0, int col0) {
+  using G = Geo<MT>;
+  const int r = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+  for (int s = 0; s < 2; ++s)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int row = n0 + 16 * s + 4 * g + q;
+      if (row < n) {
+#pragma unroll
+        for (int u = 0; u < N / G::VW; ++u) {
+          float v[G::VW];
+#pragma unroll
+          for (int c = 0; c < G::VW; ++c) v[c] = d[s][u * G::VW + c][q];
+          store_cols<G::VW>(X + (long long)row * MT + col0 + 64 * u + G::VW * r, v);
+        }
+      }
+    }
 }
 
 // X <- X P for the waves' rows, in place or from another buffer, and their Gram matrix.
@@ -287,43 +326,91 @@ template <int MT>
 __device__ __forceinline__ void apply_gram_steps(Acc<MT> &acc, ApplyRows<MT> &x, const float *src, float *dst, int n, int first,
                                                  int stride, const Scale &sc, float unscale, const char *P) {
   using G = Geo<MT>;
-  const int r = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
   for (int n0 = first * 32; n0 < n; n0 += stride * 32) {
     f32x4_t d[2][G::TT];
     Frag<G::F32> a[2][G::KB], f[G::TT];
     x.factors(a, n, n0, sc);
     if (n0 + stride * 32 < n) x.load(src, n, n0 + stride * 32);
-    apply_product<MT>(d, a, P);
-#pragma unroll
-    for (int t = 0; t < G::TT; ++t) {
-      float v[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        d[j >> 2][t][j & 3] *= unscale;
-        v[j] = d[j >> 2][t][j & 3];
-      }
-      f[t] = make_frag<G::F32>(v);
-    }
-#pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int row = n0 + 16 * s + 4 * g + q;
-        if (row < n) {
-#pragma unroll
-          for (int u = 0; u < G::U; ++u) {
-            float v[G::VW];
-#pragma unroll
-            for (int c = 0; c < G::VW; ++c) v[c] = d[s][u * G::VW + c][q];
-            store_cols<G::VW>(dst + (long long)row * MT + 64 * u + G::VW * r, v);
-          }
-        }
-      }
+    apply_product<MT, G::TT>(d, a, P);
+    scale_rows<MT, G::TT>(d, f, unscale);
+    store_rows<MT, G::TT>(d, dst, n, n0, 0);
     gram_add<MT>(acc, f);
   }
 }
 
-// ---- the output -----------------------------------------------------------------
+// The same of 128 columns by pairs of waves: all 36 Gram tiles and the factors fill one
+// wave's registers and leave a SIMD one wave.  Two waves have the same rows; each
+// multiplies them by half of P, hands its columns' factors to the other through LDS, and
+// adds 18 tiles.  Then two waves share a SIMD and cover each other's waits (65536 rows:
+// 25 us with one, 18 with two).
+struct PairAcc {
+  f32x4_t own[10], cross[8];  // tiles inside the wave's half, tiles of both
+};
+constexpr int kPairs = 4;
+constexpr int kPairLds = kPairs * 2 * 4 * 64 * 32;  // bytes: every wave's four factors
+
+__device__ __forceinline__ void apply_gram_pairs(PairAcc &acc, ApplyRows<128> &x, const float *src, float *dst, int n, int b,
+                                                 int slices, const Scale &sc, float unscale, const char *P, char *swap) {
+  using G = Geo<128>;
+  using F = Frag<false>;
+  const int lane = threadIdx.x & 63, pair = threadIdx.x >> 6 & 3, h = threadIdx.x >> 8;
+  char *mine = swap + (pair * 2 + h) * 4 * 2048 + lane * 32, *other = swap + (pair * 2 + 1 - h) * 4 * 2048 + lane * 32;
+  for (int base = b * kPairs; base * 32 < n; base += slices * kPairs) {  // (the same turns for every wave)
+    const int n0 = (base + pair) * 32;
+    F a[2][G::KB], f[4], o[4];
+    f32x4_t d[2][4];
+    x.factors(a, n, n0, sc);
+    apply_product<128, 4>(d, a, P + h * 64 * G::LROW);
+    if ((base + slices * kPairs) * 32 < n) x.load(src, n, n0 + slices * kPairs * 32);
+    scale_rows<128, 4>(d, f, unscale);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) store_frag<false>(mine + t * 2048, f[t]);
+    __syncthreads();
+    // (not before: in place, the other wave has read the rows by now)
+    store_rows<128, 4>(d, dst, n, n0, 64 * h);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) o[t] = load_frag<false>(other + t * 2048);
+    int k = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = i; j < 4; ++j) mma<false>(acc.own[k++], f[i], f[j]);
+    // tiles (i, 4 + j): the first wave i = 0, 1, the second i = 2, 3
+    if (h == 0) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) mma<false>(acc.cross[4 * i + j], f[i], o[j]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) mma<false>(acc.cross[4 * i + j], o[2 + i], f[j]);
+    }
+    __syncthreads();  // both have read before the next factors are written
+  }
+}
+
+// the pairs' tiles to their places, added in pair order
+__device__ __forceinline__ void pairs_out(const PairAcc &acc, char *lds, float unscale, float *out) {
+  using G = Geo<128>;
+  const int lane = threadIdx.x & 63, pair = threadIdx.x >> 6 & 3, h = threadIdx.x >> 8;
+  float4 *red = reinterpret_cast<float4 *>(lds) + pair * G::TRI * 64 + lane;
+  auto put = [&](int i, int j, const f32x4_t &v) {  // tile (i, j) of the upper triangle
+    red[(i * G::TT - i * (i - 1) / 2 + j - i) * 64] = make_float4(v[0], v[1], v[2], v[3]);
+  };
+  __syncthreads();  // P has been read
+  int k = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = i; j < 4; ++j) put(4 * h + i, 4 * h + j, acc.own[k++]);
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) put(2 * h + i, 4 + j, acc.cross[4 * i + j]);
+  gram_sum<128, kPairs>(lds, unscale, out);
+}
 
 template <int MT, int DT>
 __device__ __forceinline__ void final_steps(const NsMat &M, const Out &o, ApplyRows<MT> &x, const float *src, int first,
@@ -334,7 +421,7 @@ __device__ __forceinline__ void final_steps(const NsMat &M, const Out &o, ApplyR
     f32x4_t d[2][G::TT];
     Frag<G::F32> a[2][G::KB];
     x.factors(a, M.n, n0, sc);
-    apply_product<MT>(d, a, P);
+    apply_product<MT, G::TT>(d, a, P);
     if (n0 + stride * 32 < M.n) x.load(src, M.n, n0 + stride * 32);
 #pragma unroll
     for (int s = 0; s < 2; ++s)
@@ -366,37 +453,38 @@ __device__ __forceinline__ void final_steps(const NsMat &M, const Out &o, ApplyR
 // ---- the m x m polynomials --------------------------------------------------------
 
 // P of one or two steps from the Gram matrix (upper tiles, the sum of `parts` arrays
-// in order), rows in slot order, to the rows of KB * 128 bytes `pitch` apart at dst.
-// lds: two matrices.
-template <int MT>
+// in order), rows in slot order, to dst in LDS (lds itself or apart from it), by NW waves.
+// lds: two matrices.  A wave has NC tile columns, and with eight waves half of
+// their rows.
+template <int MT, int NW>
 __device__ __forceinline__ void polynomial(const float *gram, int parts, const NsStage &st, float ca, float cb, float cc,
-                                           char *lds, char *dst, int pitch) {
+                                           char *lds, char *dst) {
   using G = Geo<MT>;
   constexpr bool F = G::F32;
-  constexpr int NC = G::TT > 4 ? G::TT / 4 : 1;  // tile columns of a wave
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, g = lane >> 4;
+  constexpr int NC = G::TT > 4 ? G::TT / 4 : 1, RH = NW == 8 && G::TT > 1 ? 2 : 1, RT = G::TT / RH;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
   const float sh0 = F ? 1.f : st.sh[0], sq0 = F ? 1.f : st.sq[0], sh1 = F ? 1.f : st.sh[1], sq1 = F ? 1.f : st.sq[1];
   const float stt = F ? 1.f : st.st, sp = F ? 1.f : st.sp;
   char *H = lds, *Q = lds + G::MAT;
   {
-    constexpr int N = (G::TRI + 3) / 4;  // tiles of a wave
+    constexpr int N = (G::TRI + NW - 1) / NW;  // tiles of a wave
     const int w = __builtin_amdgcn_readfirstlane(wave);
     float4 s[N];
 #pragma unroll
     for (int k = 0; k < N; ++k)
-      if (w + 4 * k < G::TRI) s[k] = reinterpret_cast<const float4 *>(gram)[(w + 4 * k) * 64 + lane];
+      if (w + NW * k < G::TRI) s[k] = reinterpret_cast<const float4 *>(gram)[(w + NW * k) * 64 + lane];
     for (int p = 1; p < parts; ++p) {
 #pragma unroll
       for (int k = 0; k < N; ++k)
-        if (w + 4 * k < G::TRI) {
-          const float4 a = reinterpret_cast<const float4 *>(gram)[((long long)p * G::TRI + w + 4 * k) * 64 + lane];
+        if (w + NW * k < G::TRI) {
+          const float4 a = reinterpret_cast<const float4 *>(gram)[((long long)p * G::TRI + w + NW * k) * 64 + lane];
           s[k].x += a.x; s[k].y += a.y; s[k].z += a.z; s[k].w += a.w;
         }
     }
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-      if (w + 4 * k >= G::TRI) continue;
-      int tj = w + 4 * k, ti = 0;
+      if (w + NW * k >= G::TRI) continue;
+      int tj = w + NW * k, ti = 0;
       while (tj >= G::TT - ti) {
         tj -= G::TT - ti;
         ++ti;
@@ -404,115 +492,128 @@ __device__ __forceinline__ void polynomial(const float *gram, int parts, const N
       tj += ti;
       // elements (16 ti + 4 g + q, 16 tj + r): as row 16 tj + r, and mirrored
       const float x[4] = {s[k].x * sh0, s[k].y * sh0, s[k].z * sh0, s[k].w * sh0};
-      store_elements<F, 4>(H + (16 * tj + r) * G::LROW + (ti >> 1) * 128 + g * 32, 4 * (ti & 1), x);
-      if (ti != tj) {
+      char *row = H + (16 * tj + r) * G::LROW + (ti >> 1) * 128 + g * 32;
+      char *col = H + (16 * ti + 4 * g) * G::LROW + (tj >> 1) * 128 + (r >> 2) * 32;
+      const int jc = 4 * (tj & 1) + (r & 3);
+      if constexpr (F) {
+        store_elements<F, 4>(row, 4 * (ti & 1), x);
+        if (ti != tj) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          store_elements<F, 1>(H + (16 * ti + 4 * g + q) * G::LROW + (tj >> 1) * 128 + (r >> 2) * 32, 4 * (tj & 1) + (r & 3),
-                               {x[q]});
+          for (int q = 0; q < 4; ++q) store_elements<F, 1>(col + q * G::LROW, jc, {x[q]});
+        }
+      } else {
+        f16x4_t hi, lo;
+        ns_split_pairs<4>(x, hi, lo);
+        *reinterpret_cast<f16x4_t *>(row + 8 * (ti & 1)) = hi;
+        *reinterpret_cast<f16x4_t *>(row + 16 + 8 * (ti & 1)) = lo;
+        if (ti != tj) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            *reinterpret_cast<_Float16 *>(col + q * G::LROW + 2 * jc) = hi[q];
+            *reinterpret_cast<_Float16 *>(col + q * G::LROW + 16 + 2 * jc) = lo[q];
+          }
+        }
       }
-      if (G::TT == 1) store_elements<F, 4>(H + r * G::LROW + g * 32, 4, {0.f, 0.f, 0.f, 0.f});
+      if (G::TT == 1) {  // 16 columns are half a product's depth
+        store_elements<F, 4>(H + r * G::LROW + g * 32, 4, {0.f, 0.f, 0.f, 0.f});
+        store_elements<F, 4>(Q + r * G::LROW + g * 32, 4, {0.f, 0.f, 0.f, 0.f});
+      }
     }
   }
-  __syncthreads();
-  const bool active = wave * NC < G::TT;
-  const int mine = (16 * wave * NC + r) * G::LROW + g * 32;  // the wave's first column, as a row
-  f32x4_t d[NC][G::TT];  // element (16 t + 4 g + q, own column c)
+  const int t0 = wave / 4 * RT;                            // the wave's first tile row
+  const bool active = (wave & 3) * NC < G::TT && t0 < G::TT;
+  const int mine = (16 * (wave & 3) * NC + r) * G::LROW + g * 32;  // its first column, as a row
+  f32x4_t d[NC][RT];  // element (16 (t0 + t) + 4 g + q, own column c)
   auto product = [&](const char *A, const char *B) {  // d = A B, B's columns as its rows
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
-      for (int t = 0; t < G::TT; ++t) d[c][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      for (int t = 0; t < RT; ++t) d[c][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
     for (int kb = 0; kb < G::KB; ++kb) {
       Frag<F> b[NC];
 #pragma unroll
       for (int c = 0; c < NC; ++c) b[c] = load_frag<F>(B + mine + 16 * c * G::LROW + kb * 128);
 #pragma unroll
-      for (int t = 0; t < G::TT; ++t) {
-        const Frag<F> a = load_frag<F>(A + (16 * t + r) * G::LROW + kb * 128 + g * 32);
+      for (int t = 0; t < RT; ++t) {
+        const Frag<F> a = load_frag<F>(A + (16 * (t0 + t) + r) * G::LROW + kb * 128 + g * 32);
 #pragma unroll
         for (int c = 0; c < NC; ++c) mma<F>(d[c][t], a, b[c]);
       }
     }
   };
-  auto put = [&](char *A, float scale) {  // A's own rows = d * scale
+  auto put = [&](char *A, float scale) {  // the wave's part of a symmetric matrix = d * scale
+    if (!active) return;
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
-      for (int kb = 0; kb < G::KB; ++kb) {
-        float v[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int t = 2 * kb + (j >> 2);
-          v[j] = t < G::TT ? d[c][t < G::TT ? t : 0][j & 3] * scale : 0.f;
-        }
-        store_frag<F>(A + mine + 16 * c * G::LROW + kb * 128, make_frag<F>(v));
-      }
+      for (int t = 0; t < RT; ++t)
+        store_elements<F, 4>(A + mine + 16 * c * G::LROW + ((t0 + t) >> 1) * 128, 4 * ((t0 + t) & 1),
+                             {d[c][t][0] * scale, d[c][t][1] * scale, d[c][t][2] * scale, d[c][t][3] * scale});
   };
   auto poly = [&](float sh) {  // d = ca I + cb H + cc d, d the square of sh H
     const float uh = cb / sh, us = cc / (sh * sh);
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
-      for (int kb = 0; kb < G::KB; ++kb) {
-        const Frag<F> h = load_frag<F>(H + mine + 16 * c * G::LROW + kb * 128);
+      for (int t = 0; t < RT; ++t) {
+        float h[4];
+        load_elements<F>(H + mine + 16 * c * G::LROW + ((t0 + t) >> 1) * 128, 4 * ((t0 + t) & 1), h);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int t = 2 * kb + (j >> 2), q = j & 3;
-          if (t >= G::TT) continue;
-          float x = uh * frag_value<F>(h, j) + us * d[c][t < G::TT ? t : 0][q];
-          if (t == wave * NC + c && 4 * g + q == r) x += ca;
-          d[c][t < G::TT ? t : 0][q] = x;
+        for (int q = 0; q < 4; ++q) {
+          float x = uh * h[q] + us * d[c][t][q];
+          if (t0 + t == (wave & 3) * NC + c && 4 * g + q == r) x += ca;
+          d[c][t][q] = x;
         }
       }
   };
-  // A matrix in LDS is read by every wave on the left of a product, between barriers,
-  // and a wave's own rows by that wave alone on the right: it overwrites them freely
-  // once no wave reads the matrix on the left.
+  // a matrix in LDS is overwritten only when every wave has read it
   float out = sq0;  // scale of d when P is written
+  __syncthreads();
   if (active) {
     product(H, H);
     poly(sh0);
   }
   if (st.steps == 2) {
-    if (active) put(Q, sq0);
+    put(Q, sq0);
     __syncthreads();
-    if (active) {
-      product(Q, H);  // T = Q H
-      put(H, stt / (sq0 * sh0));
-      product(Q, H);  // H' = Q T
-      put(H, sh1 / (sq0 * stt));
-    }
+    if (active) product(Q, H);  // T = Q H
+    __syncthreads();
+    put(H, stt / (sq0 * sh0));
+    __syncthreads();
+    if (active) product(Q, H);  // H' = Q T
+    __syncthreads();
+    put(H, sh1 / (sq0 * stt));
     __syncthreads();
     if (active) {
       product(H, H);
       poly(sh1);
     }
     __syncthreads();
-    if (active) {
-      put(H, sq1);
-      product(Q, H);  // P = Q Q'
-    }
+    put(H, sq1);
+    __syncthreads();
+    if (active) product(Q, H);  // P = Q Q'
     out = sp / (sq0 * sq1);
   }
-  if (active) {
+  __syncthreads();  // (dst may be lds)
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      char *row = dst + (16 * (wave * NC + c) + r) * pitch;
+  for (int c = 0; c < NC && active; ++c) {
+    char *row = dst + (16 * ((wave & 3) * NC + c) + r) * G::LROW;
 #pragma unroll
-      for (int u = 0; u < G::U; ++u)
+    for (int t = 0; t < RT; t += RT < G::VW ? RT : G::VW)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int col = 64 * u + G::VW * (4 * g + q);
-          float v[G::VW];
+      for (int q = 0; q < 4; ++q) {
+        // columns of the tiles t0 + t ..: consecutive within a group of VW tiles
+        constexpr int W = RT < G::VW ? RT : G::VW;
+        const int col = 64 * ((t0 + t) / G::VW) + G::VW * (4 * g + q) + (t0 + t) % G::VW;
+        float v[W];
 #pragma unroll
-          for (int k = 0; k < G::VW; ++k) v[k] = d[c][u * G::VW + k][q] * out;
-          store_elements<F, G::VW>(row + col / 8 * 32, col % 8, v);
-          if (G::TT == 1) store_elements<F, 1>(row + (16 + 4 * g) / 8 * 32, (4 * g + q) % 8, {0.f});
-        }
-    }
+        for (int k = 0; k < W; ++k) v[k] = d[c][t + k][q] * out;
+        store_elements<F, W>(row + col / 8 * 32, col % 8, v);
+        if (G::TT == 1) store_elements<F, 1>(row + (16 + 4 * g) / 8 * 32, (4 * g + q) % 8, {0.f});
+      }
   }
+  __syncthreads();
 }
 
 // ---- kernels ----------------------------------------------------------------------
@@ -526,10 +627,7 @@ __device__ __forceinline__ void polynomial(const float *gram, int parts, const N
     else CALL(16)                                         \
   }
 
-template <int MAX> constexpr int lds_bytes() {
-  using G = Geo<MAX>;
-  return 2 * G::MAT > G::RED ? 2 * G::MAT : G::RED;
-}
+constexpr int most(int a, int b) { return a > b ? a : b; }
 
 __device__ __forceinline__ const float *ns_source(const NsMat &M, const char *ws, const void *g) {
   return M.ws_u >= 0 ? (const float *)(ws + M.ws_u) : (const float *)g + M.off;
@@ -626,7 +724,7 @@ template <int MAX> struct Whole {
   static constexpr int W = MAX < 64 ? MAX : 64;  // widest matrix
   using G = Geo<W>;
   static constexpr int TILE = W * 65 * 4;  // of prep_rows
-  static constexpr int FRONT = G::RED > TILE ? G::RED : TILE;
+  static constexpr int FRONT = most(4 * G::SET, TILE);
   static constexpr int BYTES = FRONT + 3 * G::MAT + G::TRI * 1024;
 };
 struct WholeArgs {
@@ -665,10 +763,9 @@ __device__ __forceinline__ void whole_matrix(const NsMat &M, const NsSteps &S, W
     for (int s = 0; s < stages; ++s) {                                                                        \
       NsStage st = S.stage[F ? 0 : s];                                                                        \
       if (F) st.steps = 1;                                                                                    \
-      gram_out<MT>(acc, lds, 1.f / (sx * sx), gram);                                                          \
+      gram_out<MT, 4>(acc, lds, 1.f / (sx * sx), gram);                                                         \
       __syncthreads();                                                                                        \
-      polynomial<MT>(gram, 1, st, (float)S.a, (float)S.b, (float)S.c, mats, P, Geo<MT>::LROW);                \
-      __syncthreads();                                                                                        \
+      polynomial<MT, 4>(gram, 1, st, (float)S.a, (float)S.b, (float)S.c, mats, P);                            \
       const float sp = F ? 1.f : st.steps == 2 ? st.sp : st.sq[0];                                            \
       ApplyRows<MT> x;                                                                                        \
       if (first * 32 < M.n) x.load(src, M.n, first * 32);                                                     \
@@ -700,8 +797,7 @@ __global__ __launch_bounds__(256) void skinny_whole_kernel(NsTable T, NsSteps S,
 // matrices as a whole beside it: they take no longer than the large ones here.
 template <int MAX, int DT, bool MOM>
 __global__ __launch_bounds__(256) void skinny_gram_kernel(NsTable T, NsSteps S, WholeArgs a, char *ws) {
-  constexpr int L = lds_bytes<MAX>(), W = Whole<MAX>::BYTES;
-  __shared__ __attribute__((aligned(16))) char lds[L > W ? L : W];
+  __shared__ __attribute__((aligned(16))) char lds[most(4 * Geo<MAX>::SET, Whole<MAX>::BYTES)];
   __shared__ double red[4];
   if ((int)blockIdx.x < T.wholes) {
     whole_matrix<MAX, DT, MOM>(T.mat[T.whole[blockIdx.x]], S, a, ws, lds, red);
@@ -726,7 +822,7 @@ __global__ __launch_bounds__(256) void skinny_gram_kernel(NsTable T, NsSteps S, 
       if (n0 + stride * 32 < M.n) x.load(X, M.n, n0 + stride * 32);                                           \
       gram_add<MT>(acc, f);                                                                                   \
     }                                                                                                         \
-    gram_out<MT>(acc, lds, 1.f / (sx * sx), (float *)(ws + M.ws_part) + (long long)b * (Geo<MT>::TRI * 256));  \
+    gram_out<MT, 4>(acc, lds, 1.f / (sx * sx), (float *)(ws + M.ws_part) + (long long)b * (Geo<MT>::TRI * 256));  \
   }
   CF_NS_WIDTH(MAX, M.mt, CALL)
 #undef CALL
@@ -760,58 +856,74 @@ __global__ __launch_bounds__(256) void skinny_sum_kernel(NsTable T, char *ws) {
   if (ph == 0) ((float4 *)(ws + M.ws_sum))[c] = red[threadIdx.x];
 }
 
-template <int MAX> __global__ __launch_bounds__(256) void skinny_poly_kernel(NsTable T, NsStage st, float a, float b, float c, char *ws) {
-  __shared__ __attribute__((aligned(16))) char lds[2 * Geo<MAX>::MAT];
-  const int l = ns_find(T, blockIdx.x);
-  const NsMat &M = T.mat[l];
+// the Gram matrix of all slices, in as many arrays as `parts` says
+__device__ __forceinline__ const float *gram_of(const NsMat &M, const char *ws, int *parts) {
   const bool summed = M.slices > kNsFewSlices;
-  const float *gram = (const float *)(ws + (summed ? M.ws_sum : M.ws_part));
-#define CALL(MT) polynomial<MT>(gram, summed ? 1 : M.slices, st, a, b, c, lds, ws + M.ws_sq, Geo<MT>::KB * 128);
-  CF_NS_WIDTH(MAX, M.mt, CALL)
-#undef CALL
+  *parts = summed ? 1 : M.slices;
+  return (const float *)(ws + (summed ? M.ws_sum : M.ws_part));
 }
 
-// X <- X P (from the matrix itself in the first stage) and the Gram matrix of the result
+// X <- X P (from the matrix itself in the first stage) and the Gram matrix of the result,
+// into the other of the two buffers of slices.  Every workgroup computes P for itself: a
+// launch of one workgroup a matrix for it and the way through memory take longer.
 template <int MAX>
-__global__ __launch_bounds__(256) void skinny_apply_kernel(NsTable T, NsStage st, float next_sx, int first_stage, double eps,
-                                                           const void *g, char *ws) {
-  __shared__ __attribute__((aligned(16))) char lds[lds_bytes<MAX>()];
-  __shared__ double red[4];
+__global__ __launch_bounds__(512) void skinny_apply_kernel(NsTable T, NsStage st, float ca, float cb, float cc, float next_sx,
+                                                           int first_stage, double eps, const void *g, char *ws) {
+  constexpr int SETS = MAX == 128 ? most(kPairs * Geo<128>::SET, Geo<128>::MAT + kPairLds) : 8 * Geo<MAX>::SET;
+  __shared__ __attribute__((aligned(16))) char lds[most(SETS, 2 * Geo<MAX>::MAT)];
+  __shared__ double red[8];
   const int l = ns_find(T, blockIdx.x);
   const NsMat &M = T.mat[l];
   const int b = blockIdx.x - T.first[l];
   float *X = (float *)(ws + M.ws_xn);
   const float *src = first_stage ? ns_source(M, ws, g) : X;
-  const int first = b * 4 + (threadIdx.x >> 6), stride = M.slices * 4;
+  const int first = b * 8 + (threadIdx.x >> 6), stride = M.slices * 8;
+  int parts;
+  const float *gram = gram_of(M, ws, &parts);
+  // (with few slices the sums' launch does not run, and others still read this buffer)
+  float *part = (float *)(ws + M.ws_part2);
+  if (MAX == 128 && M.mt == 128) {
+    const float sx = st.sx, sp = st.steps == 2 ? st.sp : st.sq[0];
+    const Scale sc = first_stage ? scale_of(ns_inv_norm<8>(M, ws, eps, red), sx) : Scale{false, 1.f, 1.f};
+    ApplyRows<128> x;
+    x.load(src, M.n, (b * kPairs + (threadIdx.x >> 6 & 3)) * 32);
+    polynomial<128, 8>(gram, parts, st, ca, cb, cc, lds, lds);
+    PairAcc acc{};
+    apply_gram_pairs(acc, x, src, X, M.n, b, M.slices, sc, next_sx / (sx * sp), lds, lds + Geo<128>::MAT);
+    pairs_out(acc, lds, 1.f / (next_sx * next_sx), part + (long long)b * (Geo<128>::TRI * 256));
+    return;
+  }
 #define CALL(MT)                                                                                               \
   {                                                                                                            \
-    ApplyRows<MT> x;                                                                                           \
-    x.load(src, M.n, first * 32);                                                                              \
     constexpr bool F = Geo<MT>::F32;                                                                           \
     const float sx = F ? 1.f : st.sx, sp = F ? 1.f : st.steps == 2 ? st.sp : st.sq[0], sn = F ? 1.f : next_sx; \
-    const Scale sc = first_stage ? scale_of(ns_inv_norm(M, ws, eps, red), sx) : Scale{false, 1.f, 1.f};             \
-    load_p<MT>(ws + M.ws_sq, lds);                                                                             \
+    ApplyRows<MT> x;                                                                                           \
+    x.load(src, M.n, first * 32);                                                                              \
+    const Scale sc = first_stage ? scale_of(ns_inv_norm<8>(M, ws, eps, red), sx) : Scale{false, 1.f, 1.f};     \
+    polynomial<MT, 8>(gram, parts, st, ca, cb, cc, lds, lds);                                                  \
     Acc<MT> acc{};                                                                                             \
     apply_gram_steps<MT>(acc, x, src, X, M.n, first, stride, sc, sn / (sx * sp), lds);                         \
-    gram_out<MT>(acc, lds, 1.f / (sn * sn), (float *)(ws + M.ws_part) + (long long)b * (Geo<MT>::TRI * 256));   \
+    gram_out<MT, 8>(acc, lds, 1.f / (sn * sn), part + (long long)b * (Geo<MT>::TRI * 256));                     \
   }
-  CF_NS_WIDTH(MAX, M.mt, CALL)
+  CF_NS_WIDTH((MAX < 64 ? MAX : 64), M.mt, CALL)
 #undef CALL
 }
 
-// workgroups of the last product: two fit a compute unit
-__host__ __device__ inline int final_groups(const NsMat &M) { return min((M.n + 127) / 128, 2 * kNumCUs); }
+// workgroups of the last product, eight waves of 32 rows at a time
+__host__ __device__ inline int final_groups(const NsMat &M) { return min((M.n + 255) / 256, kNsSlices); }
 
 template <int MAX, int DT>
-__global__ __launch_bounds__(256, 2) void skinny_final_kernel(NsTable T, NsStage st, int first_stage, double eps, const void *g,
-                                                           Out o, char *ws) {
-  __shared__ __attribute__((aligned(16))) char lds[Geo<MAX>::MAT];
-  __shared__ double red[4];
+__global__ __launch_bounds__(512) void skinny_final_kernel(NsTable T, NsStage st, float ca, float cb, float cc, int first_stage,
+                                                           double eps, const void *g, Out o, char *ws) {
+  __shared__ __attribute__((aligned(16))) char lds[2 * Geo<MAX>::MAT];
+  __shared__ double red[8];
   const int l = ns_find(T, blockIdx.x);
   const NsMat &M = T.mat[l];
   const int b = blockIdx.x - T.first[l];
   const float *src = first_stage ? ns_source(M, ws, g) : (const float *)(ws + M.ws_xn);
-  const int first = b * 4 + (threadIdx.x >> 6), stride = final_groups(M) * 4;
+  const int first = b * 8 + (threadIdx.x >> 6), stride = final_groups(M) * 8;
+  int parts;
+  const float *gram = gram_of(M, ws, &parts);
   o.gain = M.gain;
 #define CALL(MT)                                                                                                   \
   {                                                                                                                \
@@ -819,8 +931,8 @@ __global__ __launch_bounds__(256, 2) void skinny_final_kernel(NsTable T, NsStage
     x.load(src, M.n, first * 32);                                                                                  \
     constexpr bool F = Geo<MT>::F32;                                                                               \
     const float sx = F ? 1.f : st.sx, sp = F ? 1.f : st.steps == 2 ? st.sp : st.sq[0];                              \
-    const Scale sc = first_stage ? scale_of(ns_inv_norm(M, ws, eps, red), sx) : Scale{false, 1.f, 1.f};                 \
-    load_p<MT>(ws + M.ws_sq, lds);                                                                                 \
+    const Scale sc = first_stage ? scale_of(ns_inv_norm<8>(M, ws, eps, red), sx) : Scale{false, 1.f, 1.f};         \
+    polynomial<MT, 8>(gram, parts, st, ca, cb, cc, lds, lds);                                                      \
     final_steps<MT, DT>(M, o, x, src, first, stride, sc, 1.f / (sx * sp), lds);                                    \
   }
   CF_NS_WIDTH(MAX, M.mt, CALL)
@@ -854,16 +966,17 @@ hipError_t run(const NsTable &T0, const NsSteps &S, const WholeArgs &a, char *ws
       return M.slices > kNsFewSlices ? tt * (tt + 1) / 2 * 4 : 0;
     });
     if (nb) hipLaunchKernelGGL(skinny_sum_kernel, dim3(nb), dim3(256), 0, st, T, ws);
-    nb = number([](const NsMat &) { return 1; });
-    hipLaunchKernelGGL((skinny_poly_kernel<MAX>), dim3(nb), dim3(256), 0, st, T, S.stage[s], (float)S.a, (float)S.b,
-                       (float)S.c, ws);
-    number([](const NsMat &M) { return M.slices; });
+    const float ca = (float)S.a, cb = (float)S.b, cc = (float)S.c;
     if (s + 1 < S.stages) {
-      hipLaunchKernelGGL((skinny_apply_kernel<MAX>), dim3(slabs), dim3(256), 0, st, T, S.stage[s], S.stage[s + 1].sx, s == 0,
-                         S.eps, g, ws);
+      number([](const NsMat &M) { return M.slices; });
+      hipLaunchKernelGGL((skinny_apply_kernel<MAX>), dim3(slabs), dim3(512), 0, st, T, S.stage[s], ca, cb, cc, S.stage[s + 1].sx,
+                         s == 0, S.eps, g, ws);
+      // the slices just written are the next stage's
+      for (int l = 0; l < T.count; ++l) std::swap(T.mat[l].ws_part, T.mat[l].ws_part2);
     } else {
       nb = number([](const NsMat &M) { return final_groups(M); });
-      hipLaunchKernelGGL((skinny_final_kernel<MAX, DT>), dim3(nb), dim3(256), 0, st, T, S.stage[s], s == 0, S.eps, g, a.o, ws);
+      hipLaunchKernelGGL((skinny_final_kernel<MAX, DT>), dim3(nb), dim3(512), 0, st, T, S.stage[s], ca, cb, cc, s == 0, S.eps, g,
+                         a.o, ws);
     }
   }
   return hipGetLastError();
