@@ -529,7 +529,7 @@ __device__ __forceinline__ void polynomial(const float *gram, int parts, const N
     for (int c = 0; c < NC; ++c)
 #pragma unroll
       for (int t = 0; t < RT; ++t) d[c][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
+#pragma unroll
     for (int kb = 0; kb < G::KB; ++kb) {
       Frag<F> b[NC];
 #pragma unroll
