@@ -20,8 +20,16 @@
 // second combines them in a fixed order and reads the chunk again.
 //
 // Rows whose length is no multiple of a vector start at any element: their
-// vectors are loaded and stored at the elements' own alignment, the last one
-// element by element, so nothing outside a row is touched.
+// vectors are loaded and stored at the elements' own alignment, and the last one is
+// the row's last full vector, which repeats some of its neighbour's elements (they
+// count once in sums; stored twice they have the same value, and every load of a row
+// comes before its first store).  Element by element that vector took up to fourteen
+// instructions, more than the rest of a short row: 65536 bf16 rows of 255 went from 20.8
+// to BEFORE us.  Rows shorter than a vector, and the ends of chunks (where a
+// neighbour may have stored already, in place), do go in smaller pieces.  Nothing
+// outside a row is touched.
+
+#include <type_traits>
 
 #include "cf_common.h"
 #include "cf_kernels.h"
@@ -63,77 +71,189 @@ template <int DT> __device__ __forceinline__ u32x4_t pack(const float (&f)[Store
   }
 }
 
-// vector at element e of a row of c values (zero past its end)
-template <int DT, bool RAG> __device__ __forceinline__ u32x4_t load_vec(const typename Store<DT>::T *row, int e, int c,
-                                                                        bool nt) {
-  constexpr int V = Store<DT>::VEC;
-  if constexpr (!RAG) {
-    if (e >= c) return u32x4_t{0u, 0u, 0u, 0u};
-    const u32x4_t *p = reinterpret_cast<const u32x4_t *>(row + e);
-    return nt ? __builtin_nontemporal_load(p) : *p;
-  } else {
-    if (e + V <= c) return *reinterpret_cast<const typename Loose<DT>::V *>(row + e);
-    u32x4_t v = {0u, 0u, 0u, 0u};
-#pragma unroll
-    for (int i = 0; i < V - 1; ++i) {
-      if (e + i < c) {
-        if constexpr (DT == DT_F32) v[i] = __float_as_uint(row[e + i]);
-        else v[i >> 1] |= (uint32_t)row[e + i] << (16 * (i & 1));
-      }
+// How rows lie: FULL a multiple of a vector, RAGGED longer than one, SHORT below one.
+enum : int { FULL = 0, RAGGED = 1, SHORT = 2 };
+
+// A lane's vector j of a row: its first element, and how many of its elements belong to
+// the vector before (all of them for a vector past the row's end).
+template <int DT, int ROW> struct Place {
+  int e, skip;
+  __device__ __forceinline__ Place(int j, int c) {
+    constexpr int V = Store<DT>::VEC;
+    e = j * V;
+    if constexpr (ROW == RAGGED) e = min(e, c - V);
+    skip = j * V < c ? j * V - e : V;
+  }
+  __device__ __forceinline__ bool any() const { return skip < Store<DT>::VEC; }
+  // whether element i counts (c: the row's length)
+  __device__ __forceinline__ bool has(int i, int c) const {
+    if constexpr (ROW == SHORT) return i < c;
+    else if constexpr (ROW == RAGGED) return i >= skip;
+    else return any();
+  }
+};
+
+// the first c < V elements at p in pieces of 4, 2 and 1
+template <int DT> __device__ __forceinline__ u32x4_t load_short(const typename Store<DT>::T *p, int c) {
+  u32x4_t v = {0u, 0u, 0u, 0u};
+  if constexpr (DT == DT_F32) {
+    if (c & 2) {
+      v[0] = __float_as_uint(p[0]);
+      v[1] = __float_as_uint(p[1]);
     }
-    return v;
+    if (c & 1) v[c & 2] = __float_as_uint(p[c & 2]);
+  } else {
+    typedef uint32_t u32x2h_t __attribute__((ext_vector_type(2), aligned(2)));
+    typedef uint32_t u32h_t __attribute__((aligned(2)));
+    if (c & 4) {
+      const u32x2h_t a = *reinterpret_cast<const u32x2h_t *>(p);
+      v[0] = a[0];
+      v[1] = a[1];
+    }
+    const int at = c & 4;
+    uint32_t w = 0;
+    if (c & 2) w = *reinterpret_cast<const u32h_t *>(p + at);
+    uint32_t z = 0;
+    if (c & 1) z = p[c & 6];
+    const uint32_t lo = c & 2 ? w : z, hi = c & 2 ? z : 0u;
+    if (at) {
+      v[2] = lo;
+      v[3] = hi;
+    } else {
+      v[0] = lo;
+      v[1] = hi;
+    }
+  }
+  return v;
+}
+
+template <int DT> __device__ __forceinline__ void store_short(typename Store<DT>::T *p, int c, const u32x4_t &v) {
+  if constexpr (DT == DT_F32) {
+    if (c & 2) {
+      p[0] = __uint_as_float(v[0]);
+      p[1] = __uint_as_float(v[1]);
+    }
+    if (c & 1) p[c & 2] = __uint_as_float(c & 2 ? v[2] : v[0]);
+  } else {
+    typedef uint32_t u32x2h_t __attribute__((ext_vector_type(2), aligned(2)));
+    typedef uint32_t u32h_t __attribute__((aligned(2)));
+    if (c & 4) *reinterpret_cast<u32x2h_t *>(p) = u32x2h_t{v[0], v[1]};
+    const uint32_t lo = c & 4 ? v[2] : v[0], hi = c & 4 ? v[3] : v[1];
+    if (c & 2) *reinterpret_cast<u32h_t *>(p + (c & 4)) = lo;
+    if (c & 1) p[c & 6] = (uint16_t)(c & 2 ? hi : lo);
+  }
+}
+
+// a lane's vector of a row (zero where it has none)
+template <int DT, int ROW>
+__device__ __forceinline__ u32x4_t load_vec(const typename Store<DT>::T *row, const Place<DT, ROW> &at, int c, bool nt) {
+  if (!at.any()) return u32x4_t{0u, 0u, 0u, 0u};
+  if constexpr (ROW == FULL) {
+    const u32x4_t *p = reinterpret_cast<const u32x4_t *>(row + at.e);
+    return nt ? __builtin_nontemporal_load(p) : *p;
+  } else if constexpr (ROW == RAGGED) {
+    return *reinterpret_cast<const typename Loose<DT>::V *>(row + at.e);
+  } else {
+    return load_short<DT>(row, c);
+  }
+}
+
+template <int DT, int ROW>
+__device__ __forceinline__ void store_vec(typename Store<DT>::T *row, const Place<DT, ROW> &at, int c, const u32x4_t &v, bool nt) {
+  if (!at.any()) return;
+  if constexpr (ROW == FULL) {
+    u32x4_t *p = reinterpret_cast<u32x4_t *>(row + at.e);
+    if (nt) __builtin_nontemporal_store(v, p);
+    else *p = v;
+  } else if constexpr (ROW == RAGGED) {
+    *reinterpret_cast<typename Loose<DT>::V *>(row + at.e) = v;
+  } else {
+    store_short<DT>(row, c, v);
+  }
+}
+
+// vector at element e of a chunk of n values (zero past its end), the last one in pieces
+template <int DT, bool RAG> __device__ __forceinline__ u32x4_t load_part(const typename Store<DT>::T *p, int e, int n, bool nt) {
+  constexpr int V = Store<DT>::VEC;
+  if (e >= n) return u32x4_t{0u, 0u, 0u, 0u};
+  if constexpr (!RAG) {
+    const u32x4_t *q = reinterpret_cast<const u32x4_t *>(p + e);
+    return nt ? __builtin_nontemporal_load(q) : *q;
+  } else {
+    if (e + V <= n) return *reinterpret_cast<const typename Loose<DT>::V *>(p + e);
+    return load_short<DT>(p + e, n - e);
   }
 }
 
 template <int DT, bool RAG>
-__device__ __forceinline__ void store_vec(typename Store<DT>::T *row, int e, int c, const u32x4_t &v, bool nt) {
+__device__ __forceinline__ void store_part(typename Store<DT>::T *p, int e, int n, const u32x4_t &v, bool nt) {
   constexpr int V = Store<DT>::VEC;
+  if (e >= n) return;
   if constexpr (!RAG) {
-    if (e >= c) return;
-    u32x4_t *p = reinterpret_cast<u32x4_t *>(row + e);
-    if (nt) __builtin_nontemporal_store(v, p);
-    else *p = v;
+    u32x4_t *q = reinterpret_cast<u32x4_t *>(p + e);
+    if (nt) __builtin_nontemporal_store(v, q);
+    else *q = v;
   } else {
-    if (e + V <= c) {
-      *reinterpret_cast<typename Loose<DT>::V *>(row + e) = v;
-      return;
-    }
+    if (e + V <= n) *reinterpret_cast<typename Loose<DT>::V *>(p + e) = v;
+    else store_short<DT>(p + e, n - e, v);
+  }
+}
+
+// a lane's V values of an fp32 vector of c (gamma, beta), zero where it has none
+template <int DT, int ROW>
+__device__ __forceinline__ void load_f32(const float *p, const Place<DT, ROW> &at, int c, float (&f)[Store<DT>::VEC]) {
+  constexpr int V = Store<DT>::VEC;
 #pragma unroll
-    for (int i = 0; i < V - 1; ++i) {
-      if (e + i < c) {
-        if constexpr (DT == DT_F32) row[e + i] = __uint_as_float(v[i]);
-        else row[e + i] = (uint16_t)(v[i >> 1] >> (16 * (i & 1)));
-      }
+  for (int i = 0; i < V; ++i) f[i] = 0.f;
+  if (!at.any()) return;
+  if constexpr (ROW == SHORT) {
+#pragma unroll
+    for (int i = 0; i < V - 1; ++i)
+      if (i < c) f[i] = p[i];
+  } else {
+#pragma unroll
+    for (int q = 0; q < V; q += 4) {
+      const u32x4f_t a = *reinterpret_cast<const u32x4f_t *>(p + at.e + q);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f[q + i] = __uint_as_float(a[i]);
     }
   }
 }
 
-// V values of an fp32 vector (gamma, beta, gradients' partials) from element e on, zero past c
-template <int V, bool RAG> __device__ __forceinline__ void load_f32(const float *p, int e, int c, float (&f)[V]) {
+// the lane's own of V column sums, into a row of c
+template <int DT, int ROW>
+__device__ __forceinline__ void store_f32(float *p, const Place<DT, ROW> &at, int c, const float (&f)[Store<DT>::VEC]) {
+  constexpr int V = Store<DT>::VEC;
+  if (ROW != SHORT && at.skip == 0) {
+#pragma unroll
+    for (int q = 0; q < V; q += 4)
+      *reinterpret_cast<u32x4f_t *>(p + at.e + q) = u32x4f_t{__float_as_uint(f[q]), __float_as_uint(f[q + 1]),
+                                                             __float_as_uint(f[q + 2]), __float_as_uint(f[q + 3])};
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (at.any() && at.has(i, c)) p[at.e + i] = f[i];
+  }
+}
+
+// the same from element e of a chunk of n on
+template <int V> __device__ __forceinline__ void load_f32_part(const float *p, int e, int n, float (&f)[V]) {
 #pragma unroll
   for (int q = 0; q < V; q += 4) {
-    if (e + q + 4 <= c) {
+    if (e + q + 4 <= n) {
       const float4 a = *reinterpret_cast<const float4 *>(p + e + q);
       f[q] = a.x; f[q + 1] = a.y; f[q + 2] = a.z; f[q + 3] = a.w;
     } else {
 #pragma unroll
-      for (int i = q; i < q + 4; ++i) f[i] = RAG && e + i < c ? p[e + i] : 0.f;
+      for (int i = q; i < q + 4; ++i) f[i] = e + i < n ? p[e + i] : 0.f;
     }
   }
 }
 
-template <int V, bool RAG> __device__ __forceinline__ void store_f32(float *p, int e, int c, const float (&f)[V]) {
+template <int V> __device__ __forceinline__ void store_f32_part(float *p, int e, int n, const float (&f)[V]) {
 #pragma unroll
-  for (int q = 0; q < V; q += 4) {
-    // (a row of partials starts on a vector only when c is a multiple of one)
-    if (!RAG && e + q + 4 <= c) {
-      *reinterpret_cast<float4 *>(p + e + q) = make_float4(f[q], f[q + 1], f[q + 2], f[q + 3]);
-    } else {
-#pragma unroll
-      for (int i = q; i < q + 4; ++i)
-        if (e + i < c) p[e + i] = f[i];
-    }
-  }
+  for (int i = 0; i < V; ++i)
+    if (e + i < n) p[e + i] = f[i];
 }
 
 template <int T> __device__ __forceinline__ float team_sum(float s) {
@@ -167,29 +287,51 @@ struct FwdArgs {
   float *mean, *rstd;
 };
 
-// squared distance from the mean of a vector's values inside the row
-template <int DT, bool RAG>
-__device__ __forceinline__ float sq_dist(const u32x4_t &v, int e, int c, float mean) {
+// sum of f over the elements that count
+template <int DT, int ROW> __device__ __forceinline__ float vec_sum(const u32x4_t &v, const Place<DT, ROW> &at, int c) {
+  constexpr int V = Store<DT>::VEC;
+  float f[V];
+  unpack<DT>(v, f);
+  // (past a short row's end, and in vectors past the end, the elements are zero)
+  if constexpr (ROW == RAGGED) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) f[i] = at.has(i, c) ? f[i] : 0.f;
+  }
+#pragma unroll
+  for (int w = V / 2; w >= 1; w >>= 1)
+#pragma unroll
+    for (int i = 0; i < w; ++i) f[i] += f[i + w];
+  return f[0];
+}
+
+// their squared distance from the mean
+template <int DT, int ROW>
+__device__ __forceinline__ float sq_dist(const u32x4_t &v, const Place<DT, ROW> &at, int c, float mean) {
   constexpr int V = Store<DT>::VEC;
   float f[V], q = 0.f;
   unpack<DT>(v, f);
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     const float d = f[i] - mean;
-    q += (RAG ? e + i < c : e < c) ? d * d : 0.f;
+    q += at.has(i, c) ? d * d : 0.f;
   }
   return q;
 }
 
-template <int DT> __device__ __forceinline__ float vec_sum(const u32x4_t &v) {
+// the same of the vector at element e of a chunk of n
+template <int DT> __device__ __forceinline__ float sum_part(const u32x4_t &v) {
+  return vec_sum<DT, FULL>(v, Place<DT, FULL>(0, Store<DT>::VEC), Store<DT>::VEC);
+}
+template <int DT> __device__ __forceinline__ float sq_dist_part(const u32x4_t &v, int e, int n, float mean) {
   constexpr int V = Store<DT>::VEC;
-  float f[V];
+  float f[V], q = 0.f;
   unpack<DT>(v, f);
 #pragma unroll
-  for (int w = V / 2; w >= 1; w >>= 1)
-#pragma unroll
-    for (int i = 0; i < w; ++i) f[i] += f[i + w];
-  return f[0];
+  for (int i = 0; i < V; ++i) {
+    const float d = f[i] - mean;
+    q += e + i < n ? d * d : 0.f;
+  }
+  return q;
 }
 
 template <int DT>
@@ -204,7 +346,7 @@ __device__ __forceinline__ u32x4_t normalised(const u32x4_t &v, float mean, floa
 }
 
 // teams of T lanes, NV vectors a lane, U rows a team (their loads all in flight)
-template <int DT, int T, int NV, int U, bool RAG>
+template <int DT, int T, int NV, int U, int ROW>
 __global__ __launch_bounds__(256) void norm_fwd_wave(FwdArgs a) {
   constexpr int V = Store<DT>::VEC;
   using S = typename Store<DT>::T;
@@ -216,21 +358,21 @@ __global__ __launch_bounds__(256) void norm_fwd_wave(FwdArgs a) {
     const S *row = (const S *)a.x + (r0 + u) * a.c;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
-      v[u][i] = r0 + u < a.rows ? load_vec<DT, RAG>(row, (t + T * i) * V, a.c, a.nt) : u32x4_t{0u, 0u, 0u, 0u};
+      v[u][i] = r0 + u < a.rows ? load_vec<DT, ROW>(row, Place<DT, ROW>(t + T * i, a.c), a.c, a.nt) : u32x4_t{0u, 0u, 0u, 0u};
   }
   float mean[U], rstd[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     float s = 0.f;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) s += vec_sum<DT>(v[u][i]);
+    for (int i = 0; i < NV; ++i) s += vec_sum<DT, ROW>(v[u][i], Place<DT, ROW>(t + T * i, a.c), a.c);
     mean[u] = team_sum<T>(s) * a.inv_c;
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     float q = 0.f;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) q += sq_dist<DT, RAG>(v[u][i], (t + T * i) * V, a.c, mean[u]);
+    for (int i = 0; i < NV; ++i) q += sq_dist<DT, ROW>(v[u][i], Place<DT, ROW>(t + T * i, a.c), a.c, mean[u]);
     rstd[u] = 1.0f / sqrtf(team_sum<T>(q) * a.inv_c + a.eps);
     if (t == 0 && r0 + u < a.rows) {
       a.mean[r0 + u] = mean[u];
@@ -239,19 +381,19 @@ __global__ __launch_bounds__(256) void norm_fwd_wave(FwdArgs a) {
   }
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
+    const Place<DT, ROW> at(t + T * i, a.c);
     float ga[V], be[V];
-    load_f32<V, RAG>(a.gamma, (t + T * i) * V, a.c, ga);
-    load_f32<V, RAG>(a.beta, (t + T * i) * V, a.c, be);
+    load_f32<DT, ROW>(a.gamma, at, a.c, ga);
+    load_f32<DT, ROW>(a.beta, at, a.c, be);
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (r0 + u < a.rows)
-        store_vec<DT, RAG>((S *)a.y + (r0 + u) * a.c, (t + T * i) * V, a.c, normalised<DT>(v[u][i], mean[u], rstd[u], ga, be),
-                           a.nt);
+        store_vec<DT, ROW>((S *)a.y + (r0 + u) * a.c, at, a.c, normalised<DT>(v[u][i], mean[u], rstd[u], ga, be), a.nt);
   }
 }
 
 // a workgroup a row
-template <int DT, int TH, int NV, bool RAG> __global__ __launch_bounds__(TH) void norm_fwd_block(FwdArgs a) {
+template <int DT, int TH, int NV, int ROW> __global__ __launch_bounds__(TH) void norm_fwd_block(FwdArgs a) {
   constexpr int V = Store<DT>::VEC, W = TH / 64;
   using S = typename Store<DT>::T;
   __shared__ float red[2 * W];
@@ -260,13 +402,13 @@ template <int DT, int TH, int NV, bool RAG> __global__ __launch_bounds__(TH) voi
   const S *row = (const S *)a.x + r * a.c;
   u32x4_t v[NV];
 #pragma unroll
-  for (int i = 0; i < NV; ++i) v[i] = load_vec<DT, RAG>(row, (t + TH * i) * V, a.c, a.nt);
+  for (int i = 0; i < NV; ++i) v[i] = load_vec<DT, ROW>(row, Place<DT, ROW>(t + TH * i, a.c), a.c, a.nt);
   float s = 0.f, q = 0.f;
 #pragma unroll
-  for (int i = 0; i < NV; ++i) s += vec_sum<DT>(v[i]);
+  for (int i = 0; i < NV; ++i) s += vec_sum<DT, ROW>(v[i], Place<DT, ROW>(t + TH * i, a.c), a.c);
   const float mean = block_sum<W>(s, red, 0) * a.inv_c;
 #pragma unroll
-  for (int i = 0; i < NV; ++i) q += sq_dist<DT, RAG>(v[i], (t + TH * i) * V, a.c, mean);
+  for (int i = 0; i < NV; ++i) q += sq_dist<DT, ROW>(v[i], Place<DT, ROW>(t + TH * i, a.c), a.c, mean);
   const float rstd = 1.0f / sqrtf(block_sum<W>(q, red, 1) * a.inv_c + a.eps);
   if (t == 0) {
     a.mean[r] = mean;
@@ -274,12 +416,12 @@ template <int DT, int TH, int NV, bool RAG> __global__ __launch_bounds__(TH) voi
   }
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int e = (t + TH * i) * V;
-    if (e < a.c) {
+    const Place<DT, ROW> at(t + TH * i, a.c);
+    if (at.any()) {
       float ga[V], be[V];
-      load_f32<V, RAG>(a.gamma, e, a.c, ga);
-      load_f32<V, RAG>(a.beta, e, a.c, be);
-      store_vec<DT, RAG>((S *)a.y + r * a.c, e, a.c, normalised<DT>(v[i], mean, rstd, ga, be), a.nt);
+      load_f32<DT, ROW>(a.gamma, at, a.c, ga);
+      load_f32<DT, ROW>(a.beta, at, a.c, be);
+      store_vec<DT, ROW>((S *)a.y + r * a.c, at, a.c, normalised<DT>(v[i], mean, rstd, ga, be), a.nt);
     }
   }
 }
@@ -300,13 +442,13 @@ __global__ __launch_bounds__(256) void norm_fwd_chunk_stats(FwdArgs a, int chunk
     const int k = min(n - o, 256 * V * NV);
     u32x4_t v[NV];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) v[i] = load_vec<DT, RAG>(row + o, ((int)threadIdx.x + 256 * i) * V, k, false);
+    for (int i = 0; i < NV; ++i) v[i] = load_part<DT, RAG>(row + o, ((int)threadIdx.x + 256 * i) * V, k, false);
     float s = 0.f, q = 0.f;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) s += vec_sum<DT>(v[i]);
+    for (int i = 0; i < NV; ++i) s += sum_part<DT>(v[i]);
     const float pm = block_sum<4>(s, red, 0) / (float)k;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) q += sq_dist<DT, RAG>(v[i], ((int)threadIdx.x + 256 * i) * V, k, pm);
+    for (int i = 0; i < NV; ++i) q += sq_dist_part<DT>(v[i], ((int)threadIdx.x + 256 * i) * V, k, pm);
     const float pq = block_sum<4>(q, red, 1);
     const float d = pm - mean, w = (float)k / (float)(have + k);
     m2 += pq + d * d * (float)have * w;
@@ -342,10 +484,10 @@ __global__ __launch_bounds__(256) void norm_fwd_chunk_apply(FwdArgs a, int chunk
   S *out = (S *)a.y + r * a.c + beg;
   for (int e = threadIdx.x * V; e < n; e += 256 * V) {
     float ga[V], be[V];
-    const u32x4_t v = load_vec<DT, RAG>(row, e, n, a.nt);
-    load_f32<V, RAG>(a.gamma + beg, e, n, ga);
-    load_f32<V, RAG>(a.beta + beg, e, n, be);
-    store_vec<DT, RAG>(out, e, n, normalised<DT>(v, mean, rstd, ga, be), a.nt);
+    const u32x4_t v = load_part<DT, RAG>(row, e, n, a.nt);
+    load_f32_part<V>(a.gamma + beg, e, n, ga);
+    load_f32_part<V>(a.beta + beg, e, n, be);
+    store_part<DT, RAG>(out, e, n, normalised<DT>(v, mean, rstd, ga, be), a.nt);
   }
 }
 
@@ -362,10 +504,11 @@ struct BwdArgs {
   float *pg, *pb;  // [workgroup][c] partial sums of dgamma and dbeta
 };
 
-// adds a vector's share of the two sums over the row and of dgamma, dbeta
-template <int DT>
-__device__ __forceinline__ void bwd_sums(const u32x4_t &xv, const u32x4_t &dv, float mean, float rstd,
-                                         const float (&ga)[Store<DT>::VEC], float &sg, float &sgx,
+// adds a vector's share of the two sums over the row (of the elements that count; dy is
+// zero past the end) and of dgamma, dbeta
+template <int DT, int ROW>
+__device__ __forceinline__ void bwd_sums(const u32x4_t &xv, const u32x4_t &dv, const Place<DT, ROW> &at, int c, float mean,
+                                         float rstd, const float (&ga)[Store<DT>::VEC], float &sg, float &sgx,
                                          float (&dg)[Store<DT>::VEC], float (&db)[Store<DT>::VEC]) {
   constexpr int V = Store<DT>::VEC;
   float x[V], d[V];
@@ -373,11 +516,17 @@ __device__ __forceinline__ void bwd_sums(const u32x4_t &xv, const u32x4_t &dv, f
   unpack<DT>(dv, d);
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const float xh = (x[i] - mean) * rstd, g = mul_rounded(d[i], ga[i]);
-    sg += g;
-    sgx += g * xh;
+    const float xh = (x[i] - mean) * rstd;
+    float g = mul_rounded(d[i], ga[i]);
     dg[i] += d[i] * xh;
     db[i] += d[i];
+    if constexpr (ROW == RAGGED) {
+      sg += at.has(i, c) ? g : 0.f;
+      sgx += at.has(i, c) ? g * xh : 0.f;
+    } else {
+      sg += g;
+      sgx += g * xh;
+    }
   }
 }
 
@@ -397,7 +546,7 @@ __device__ __forceinline__ u32x4_t bwd_dx(const u32x4_t &xv, const u32x4_t &dv, 
 }
 
 // teams of T lanes; every team walks rows and keeps its columns' sums
-template <int DT, int T, int NV, int U, bool RAG>
+template <int DT, int T, int NV, int U, int ROW>
 __global__ __launch_bounds__(256) void norm_bwd_wave(BwdArgs a) {
   constexpr int V = Store<DT>::VEC;
   using S = typename Store<DT>::T;
@@ -406,7 +555,7 @@ __global__ __launch_bounds__(256) void norm_bwd_wave(BwdArgs a) {
   float ga[NV][V], dg[NV][V], db[NV][V];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    load_f32<V, RAG>(a.gamma, (t + T * i) * V, a.c, ga[i]);
+    load_f32<DT, ROW>(a.gamma, Place<DT, ROW>(t + T * i, a.c), a.c, ga[i]);
 #pragma unroll
     for (int j = 0; j < V; ++j) dg[i][j] = db[i][j] = 0.f;
   }
@@ -420,9 +569,9 @@ __global__ __launch_bounds__(256) void norm_bwd_wave(BwdArgs a) {
       const bool in = r < a.rows;
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        const int e = (t + T * i) * V;
-        xv[u][i] = in ? load_vec<DT, RAG>((const S *)a.x + r * a.c, e, a.c, a.nt) : u32x4_t{0u, 0u, 0u, 0u};
-        dv[u][i] = in ? load_vec<DT, RAG>((const S *)a.dy + r * a.c, e, a.c, a.nt) : u32x4_t{0u, 0u, 0u, 0u};
+        const Place<DT, ROW> at(t + T * i, a.c);
+        xv[u][i] = in ? load_vec<DT, ROW>((const S *)a.x + r * a.c, at, a.c, a.nt) : u32x4_t{0u, 0u, 0u, 0u};
+        dv[u][i] = in ? load_vec<DT, ROW>((const S *)a.dy + r * a.c, at, a.c, a.nt) : u32x4_t{0u, 0u, 0u, 0u};
       }
       mean[u] = in ? a.mean[r] : 0.f;
       rstd[u] = in ? a.rstd[r] : 0.f;
@@ -432,12 +581,13 @@ __global__ __launch_bounds__(256) void norm_bwd_wave(BwdArgs a) {
       const long long r = rb + u * (256 / T) + threadIdx.x / T;
       float sg = 0.f, sgx = 0.f;
 #pragma unroll
-      for (int i = 0; i < NV; ++i) bwd_sums<DT>(xv[u][i], dv[u][i], mean[u], rstd[u], ga[i], sg, sgx, dg[i], db[i]);
+      for (int i = 0; i < NV; ++i)
+        bwd_sums<DT, ROW>(xv[u][i], dv[u][i], Place<DT, ROW>(t + T * i, a.c), a.c, mean[u], rstd[u], ga[i], sg, sgx, dg[i], db[i]);
       const float mg = team_sum<T>(sg) * a.inv_c, mgx = team_sum<T>(sgx) * a.inv_c;
       if (r < a.rows) {
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-          store_vec<DT, RAG>((S *)a.dx + r * a.c, (t + T * i) * V, a.c,
+          store_vec<DT, ROW>((S *)a.dx + r * a.c, Place<DT, ROW>(t + T * i, a.c), a.c,
                              bwd_dx<DT>(xv[u][i], dv[u][i], mean[u], rstd[u], ga[i], mg, mgx), a.nt);
       }
     }
@@ -458,9 +608,9 @@ __global__ __launch_bounds__(256) void norm_bwd_wave(BwdArgs a) {
       }
       __syncthreads();
       for (int j = threadIdx.x; j < T * V; j += 256) {
-        const int col = i * T * V + j;
-        if (col < a.c)
-          (k ? a.pb : a.pg)[(long long)blockIdx.x * a.c + col] = (red[0][j] + red[1][j]) + (red[2][j] + red[3][j]);
+        const Place<DT, ROW> at(j / V + T * i, a.c);
+        if (at.any() && at.has(j % V, a.c))
+          (k ? a.pb : a.pg)[(long long)blockIdx.x * a.c + at.e + j % V] = (red[0][j] + red[1][j]) + (red[2][j] + red[3][j]);
       }
       __syncthreads();
     }
@@ -468,7 +618,7 @@ __global__ __launch_bounds__(256) void norm_bwd_wave(BwdArgs a) {
 }
 
 // a workgroup a row at a time
-template <int DT, int TH, int NV, bool RAG> __global__ __launch_bounds__(TH) void norm_bwd_block(BwdArgs a) {
+template <int DT, int TH, int NV, int ROW> __global__ __launch_bounds__(TH) void norm_bwd_block(BwdArgs a) {
   constexpr int V = Store<DT>::VEC, W = TH / 64;
   using S = typename Store<DT>::T;
   __shared__ float red[4 * W];
@@ -476,7 +626,7 @@ template <int DT, int TH, int NV, bool RAG> __global__ __launch_bounds__(TH) voi
   float ga[NV][V], dg[NV][V], db[NV][V];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    load_f32<V, RAG>(a.gamma, (t + TH * i) * V, a.c, ga[i]);
+    load_f32<DT, ROW>(a.gamma, Place<DT, ROW>(t + TH * i, a.c), a.c, ga[i]);
 #pragma unroll
     for (int j = 0; j < V; ++j) dg[i][j] = db[i][j] = 0.f;
   }
@@ -485,13 +635,15 @@ template <int DT, int TH, int NV, bool RAG> __global__ __launch_bounds__(TH) voi
     u32x4_t xv[NV], dv[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      xv[i] = load_vec<DT, RAG>((const S *)a.x + r * a.c, (t + TH * i) * V, a.c, a.nt);
-      dv[i] = load_vec<DT, RAG>((const S *)a.dy + r * a.c, (t + TH * i) * V, a.c, a.nt);
+      const Place<DT, ROW> at(t + TH * i, a.c);
+      xv[i] = load_vec<DT, ROW>((const S *)a.x + r * a.c, at, a.c, a.nt);
+      dv[i] = load_vec<DT, ROW>((const S *)a.dy + r * a.c, at, a.c, a.nt);
     }
     const float mean = a.mean[r], rstd = a.rstd[r];
     float sg = 0.f, sgx = 0.f;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) bwd_sums<DT>(xv[i], dv[i], mean, rstd, ga[i], sg, sgx, dg[i], db[i]);
+    for (int i = 0; i < NV; ++i)
+      bwd_sums<DT, ROW>(xv[i], dv[i], Place<DT, ROW>(t + TH * i, a.c), a.c, mean, rstd, ga[i], sg, sgx, dg[i], db[i]);
     sg = team_sum<64>(sg);
     sgx = team_sum<64>(sgx);
     // the halves of red alternate: one barrier a row
@@ -510,15 +662,15 @@ template <int DT, int TH, int NV, bool RAG> __global__ __launch_bounds__(TH) voi
     mgx *= a.inv_c;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
-      store_vec<DT, RAG>((S *)a.dx + r * a.c, (t + TH * i) * V, a.c, bwd_dx<DT>(xv[i], dv[i], mean, rstd, ga[i], mg, mgx),
-                         a.nt);
+      store_vec<DT, ROW>((S *)a.dx + r * a.c, Place<DT, ROW>(t + TH * i, a.c), a.c,
+                         bwd_dx<DT>(xv[i], dv[i], mean, rstd, ga[i], mg, mgx), a.nt);
   }
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int e = (t + TH * i) * V;
-    if (e < a.c) {
-      store_f32<V, RAG>(a.pg + (long long)blockIdx.x * a.c, e, a.c, dg[i]);
-      store_f32<V, RAG>(a.pb + (long long)blockIdx.x * a.c, e, a.c, db[i]);
+    const Place<DT, ROW> at(t + TH * i, a.c);
+    if (at.any()) {
+      store_f32<DT, ROW>(a.pg + (long long)blockIdx.x * a.c, at, a.c, dg[i]);
+      store_f32<DT, ROW>(a.pb + (long long)blockIdx.x * a.c, at, a.c, db[i]);
     }
   }
 }
@@ -537,9 +689,9 @@ __global__ __launch_bounds__(256) void norm_bwd_chunk_sums(BwdArgs a, int chunk,
   float sg = 0.f, sgx = 0.f, unused0[V] = {}, unused1[V] = {};
   for (int e = threadIdx.x * V; e < n; e += 256 * V) {
     float ga[V];
-    const u32x4_t xv = load_vec<DT, RAG>(x, e, n, false), dv = load_vec<DT, RAG>(dy, e, n, false);
-    load_f32<V, RAG>(a.gamma + beg, e, n, ga);
-    bwd_sums<DT>(xv, dv, mean, rstd, ga, sg, sgx, unused0, unused1);
+    const u32x4_t xv = load_part<DT, RAG>(x, e, n, false), dv = load_part<DT, RAG>(dy, e, n, false);
+    load_f32_part<V>(a.gamma + beg, e, n, ga);
+    bwd_sums<DT, FULL>(xv, dv, Place<DT, FULL>(0, V), V, mean, rstd, ga, sg, sgx, unused0, unused1);
   }
   sg = block_sum<4>(sg, red, 0);
   sgx = block_sum<4>(sgx, red, 1);
@@ -556,7 +708,7 @@ __global__ __launch_bounds__(256) void norm_bwd_columns(BwdArgs a, int per, int 
   __shared__ float2 rs[kColRows];
   const long long e = ((long long)blockIdx.x * 256 + threadIdx.x) * V;
   float ga[V] = {}, dg[V] = {}, db[V] = {};
-  if (e < a.c) load_f32<V, RAG>(a.gamma, (int)e, a.c, ga);
+  if (e < a.c) load_f32_part<V>(a.gamma, (int)e, a.c, ga);
   const long long rend = min(((long long)blockIdx.y + 1) * per, a.rows);
   for (long long r0 = (long long)blockIdx.y * per; r0 < rend; r0 += kColRows) {
     const int nr = (int)min((long long)kColRows, rend - r0);
@@ -575,25 +727,43 @@ __global__ __launch_bounds__(256) void norm_bwd_columns(BwdArgs a, int per, int 
     if (e < a.c) {
       for (int i = 0; i < nr; ++i) {
         const long long at = (r0 + i) * a.c;
-        const u32x4_t xv = load_vec<DT, RAG>((const S *)a.x + at, (int)e, a.c, a.nt);
-        const u32x4_t dv = load_vec<DT, RAG>((const S *)a.dy + at, (int)e, a.c, a.nt);
+        const u32x4_t xv = load_part<DT, RAG>((const S *)a.x + at, (int)e, a.c, a.nt);
+        const u32x4_t dv = load_part<DT, RAG>((const S *)a.dy + at, (int)e, a.c, a.nt);
         const float mean = a.mean[r0 + i], rstd = a.rstd[r0 + i];
         float s0 = 0.f, s1 = 0.f;
-        bwd_sums<DT>(xv, dv, mean, rstd, ga, s0, s1, dg, db);
-        store_vec<DT, RAG>((S *)a.dx + at, (int)e, a.c, bwd_dx<DT>(xv, dv, mean, rstd, ga, rs[i].x, rs[i].y), a.nt);
+        bwd_sums<DT, FULL>(xv, dv, Place<DT, FULL>(0, V), V, mean, rstd, ga, s0, s1, dg, db);
+        store_part<DT, RAG>((S *)a.dx + at, (int)e, a.c, bwd_dx<DT>(xv, dv, mean, rstd, ga, rs[i].x, rs[i].y), a.nt);
       }
     }
     __syncthreads();
   }
   if (e < a.c) {
-    store_f32<V, RAG>(a.pg + (long long)blockIdx.y * a.c, (int)e, a.c, dg);
-    store_f32<V, RAG>(a.pb + (long long)blockIdx.y * a.c, (int)e, a.c, db);
+    store_f32_part<V>(a.pg + (long long)blockIdx.y * a.c, (int)e, a.c, dg);
+    store_f32_part<V>(a.pb + (long long)blockIdx.y * a.c, (int)e, a.c, db);
   }
 }
 
 // ---- plans --------------------------------------------------------------------
 
 int vec_of(int dtype) { return dtype == DT_BF16 ? Store<DT_BF16>::VEC : Store<DT_F32>::VEC; }
+
+// Lanes of a team and vectors a lane for rows of nv <= 512 vectors: the fewest lanes of
+// those with one, two or three vectors that waste least (33 vectors: 16 lanes with
+// three rather than 64 with one).
+struct Team {
+  int lanes, vecs;
+};
+Team team_of(long long nv) {
+  if (nv > 256) return {64, 8};
+  if (nv > 192) return {64, 4};
+  if (nv > 128) return {64, 3};
+  if (nv > 96) return {64, 2};
+  for (int t = 1; t < 64; t *= 2) {
+    if (nv <= t) return {t, 1};
+    if (t >= 2 && nv > t * 2 && nv <= t * 3) return {t, 3};
+  }
+  return {64, 1};
+}
 
 // elements of a chunk (a multiple of the 256 vectors of one load round) and chunks
 // a row, for rows cut over workgroups: about four workgroups a compute unit and
@@ -607,12 +777,13 @@ void plan_chunks(long long rows, int c, int V, int *chunk, int *nch) {
   *nch = (int)((c + (long long)*chunk - 1) / *chunk);
 }
 
-// whether the forward pass cuts rows into chunks: always past what a workgroup of
-// 1024 threads holds in registers
-bool fwd_chunked(long long rows, int c, int dtype) { return c > 1024 * 16 * vec_of(dtype); }
+// Whether the forward pass cuts rows into chunks: past the 2^16 values that a workgroup of
+// 1024 threads holds in registers, and from 2^14 on when there are fewer rows than compute
+// units (8 rows of 65536 fp32 values 11.3 us with a workgroup a row).
+bool fwd_chunked(long long rows, int c) { return c > 65536 || (c > 16384 && rows < kNumCUs); }
 
-// backward: past 1024 threads' registers
-bool bwd_chunked(long long rows, int c, int dtype) { return c > 16384; }
+// Backward: past what 1024 threads hold of x, dy, gamma and the column sums.
+bool bwd_chunked(int c) { return c > 16384; }
 
 // rows of a block of the column pass: a multiple of kColRows that leaves about four
 // workgroups a compute unit
@@ -626,74 +797,96 @@ int column_rows(long long rows, int c, int V) {
 int bwd_groups(long long rows, int c, int dtype) {
   const int V = vec_of(dtype);
   const long long nv = ((long long)c + V - 1) / V;
-  if (bwd_chunked(rows, c, dtype)) {
+  if (bwd_chunked(c)) {
     const int per = column_rows(rows, c, V);
     return (int)((rows + per - 1) / per);
   }
-  long long per, cap;
-  if (nv <= 64) {
-    int T = 1;
-    while (T < nv) T *= 2;
-    per = 256 / T * 2;
+  // rows a workgroup takes at a time; a workgroup of at least four times that keeps the
+  // partial sums (8 bytes a column and workgroup) small beside the rows, but every
+  // compute unit should have one
+  long long per = 1, cap = kNumCUs;
+  if (c <= 1024) {
+    const Team t = team_of(nv);
+    per = 256 / t.lanes * (t.vecs == 1 ? 2 : 1);
     cap = 8 * kNumCUs;
-  } else if (c <= 1024) {
-    per = 4;
+  } else if (c <= 4096) {
     cap = 4 * kNumCUs;
-  } else {
-    per = 1;
-    cap = (c <= 4096 ? 4 : 1) * kNumCUs;
   }
   const long long need = (rows + per - 1) / per;
-  return (int)(need < cap ? need : cap);
+  long long groups = need / 4 > kNumCUs ? need / 4 : kNumCUs;
+  if (groups > cap) groups = cap;
+  return (int)(need < groups ? need : groups);
 }
 
-template <int DT, bool RAG> hipError_t fwd(const FwdArgs &a, void *ws, hipStream_t st) {
+template <int DT, int ROW> hipError_t fwd(const FwdArgs &a, void *ws, hipStream_t st) {
   constexpr int V = Store<DT>::VEC;
   const long long nv = ((long long)a.c + V - 1) / V;
+  if (fwd_chunked(a.rows, a.c)) {
+    constexpr bool RAG = ROW != FULL;
+    int chunk, nch;
+    plan_chunks(a.rows, a.c, V, &chunk, &nch);
+    const unsigned gy = (unsigned)(a.rows < 32768 ? a.rows : 32768), gz = (unsigned)((a.rows + gy - 1) / gy);
+    hipLaunchKernelGGL((norm_fwd_chunk_stats<DT, 4, RAG>), dim3(nch, gy, gz), dim3(256), 0, st, a, chunk, (float2 *)ws);
+    hipLaunchKernelGGL((norm_fwd_chunk_apply<DT, RAG>), dim3(nch, gy, gz), dim3(256), 0, st, a, chunk, (const float2 *)ws);
+    return hipGetLastError();
+  }
 #define CF_FWD_WAVE(T, NV, U)                                                                                       \
   {                                                                                                                 \
     const long long per = 256 / (T) * (U);                                                                          \
-    hipLaunchKernelGGL((norm_fwd_wave<DT, T, NV, U, RAG>), dim3((unsigned)((a.rows + per - 1) / per)), dim3(256), 0, \
+    hipLaunchKernelGGL((norm_fwd_wave<DT, T, NV, U, ROW>), dim3((unsigned)((a.rows + per - 1) / per)), dim3(256), 0, \
                        st, a);                                                                                      \
     return hipGetLastError();                                                                                       \
   }
-  if (nv <= 1) CF_FWD_WAVE(1, 1, 4)
-  if (nv <= 2) CF_FWD_WAVE(2, 1, 4)
-  if (nv <= 4) CF_FWD_WAVE(4, 1, 4)
-  if (nv <= 8) CF_FWD_WAVE(8, 1, 4)
-  if (nv <= 16) CF_FWD_WAVE(16, 1, 4)
-  if (nv <= 32) CF_FWD_WAVE(32, 1, 4)
-  if (nv <= 64) CF_FWD_WAVE(64, 1, 4)
-  if (nv <= 128) CF_FWD_WAVE(64, 2, 2)
-  if (nv <= 256) CF_FWD_WAVE(64, 4, 1)
-  if (nv <= 512) CF_FWD_WAVE(64, 8, 1)
-#undef CF_FWD_WAVE
-  if (!fwd_chunked(a.rows, a.c, DT)) {
 #define CF_FWD_BLOCK(TH, NV)                                                                                    \
   {                                                                                                             \
-    hipLaunchKernelGGL((norm_fwd_block<DT, TH, NV, RAG>), dim3((unsigned)a.rows), dim3(TH), 0, st, a);          \
+    hipLaunchKernelGGL((norm_fwd_block<DT, TH, NV, ROW>), dim3((unsigned)a.rows), dim3(TH), 0, st, a);          \
     return hipGetLastError();                                                                                   \
   }
+  if constexpr (ROW == SHORT) CF_FWD_WAVE(1, 1, 4)
+  else {
+    if (nv <= 512) {
+      const Team t = team_of(nv);
+      switch (t.lanes * 16 + t.vecs) {
+        case 1 * 16 + 1: CF_FWD_WAVE(1, 1, 4)
+        case 2 * 16 + 1: CF_FWD_WAVE(2, 1, 4)
+        case 2 * 16 + 3: CF_FWD_WAVE(2, 3, 2)
+        case 4 * 16 + 1: CF_FWD_WAVE(4, 1, 4)
+        case 4 * 16 + 3: CF_FWD_WAVE(4, 3, 2)
+        case 8 * 16 + 1: CF_FWD_WAVE(8, 1, 4)
+        case 8 * 16 + 3: CF_FWD_WAVE(8, 3, 2)
+        case 16 * 16 + 1: CF_FWD_WAVE(16, 1, 4)
+        case 16 * 16 + 3: CF_FWD_WAVE(16, 3, 2)
+        case 32 * 16 + 1: CF_FWD_WAVE(32, 1, 4)
+        case 32 * 16 + 3: CF_FWD_WAVE(32, 3, 2)
+        case 64 * 16 + 1: CF_FWD_WAVE(64, 1, 4)
+        case 64 * 16 + 2: CF_FWD_WAVE(64, 2, 2)
+        case 64 * 16 + 3: CF_FWD_WAVE(64, 3, 1)
+        case 64 * 16 + 4: CF_FWD_WAVE(64, 4, 1)
+        default: CF_FWD_WAVE(64, 8, 1)
+      }
+    }
+    if (nv <= 768) CF_FWD_BLOCK(256, 3)
     if (nv <= 1024) CF_FWD_BLOCK(256, 4)
+    if (nv <= 1536) CF_FWD_BLOCK(256, 6)
     if (nv <= 2048) CF_FWD_BLOCK(256, 8)
+    if (nv <= 3072) CF_FWD_BLOCK(1024, 3)
     if (nv <= 4096) CF_FWD_BLOCK(1024, 4)
-    if (nv <= 8192) CF_FWD_BLOCK(1024, 8)
-    CF_FWD_BLOCK(1024, 16)
-#undef CF_FWD_BLOCK
+    if constexpr (DT == DT_F32) {
+      if (nv <= 8192) CF_FWD_BLOCK(1024, 8)
+      CF_FWD_BLOCK(1024, 16)
+    } else {
+      CF_FWD_BLOCK(1024, 8)
+    }
   }
-  int chunk, nch;
-  plan_chunks(a.rows, a.c, V, &chunk, &nch);
-  const unsigned gy = (unsigned)(a.rows < 32768 ? a.rows : 32768), gz = (unsigned)((a.rows + gy - 1) / gy);
-  hipLaunchKernelGGL((norm_fwd_chunk_stats<DT, 4, RAG>), dim3(nch, gy, gz), dim3(256), 0, st, a, chunk, (float2 *)ws);
-  hipLaunchKernelGGL((norm_fwd_chunk_apply<DT, RAG>), dim3(nch, gy, gz), dim3(256), 0, st, a, chunk,
-                     (const float2 *)ws);
-  return hipGetLastError();
+#undef CF_FWD_WAVE
+#undef CF_FWD_BLOCK
 }
 
-template <int DT, bool RAG> hipError_t bwd(const BwdArgs &a, int groups, void *rowpart, hipStream_t st) {
+template <int DT, int ROW> hipError_t bwd(const BwdArgs &a, int groups, void *rowpart, hipStream_t st) {
   constexpr int V = Store<DT>::VEC;
   const long long nv = ((long long)a.c + V - 1) / V;
-  if (bwd_chunked(a.rows, a.c, DT)) {
+  if (bwd_chunked(a.c)) {
+    constexpr bool RAG = ROW != FULL;
     int chunk, nch;
     plan_chunks(a.rows, a.c, V, &chunk, &nch);
     const unsigned gy = (unsigned)(a.rows < 32768 ? a.rows : 32768), gz = (unsigned)((a.rows + gy - 1) / gy);
@@ -704,32 +897,61 @@ template <int DT, bool RAG> hipError_t bwd(const BwdArgs &a, int groups, void *r
   }
 #define CF_BWD_WAVE(T, NV, U)                                                                        \
   {                                                                                                  \
-    hipLaunchKernelGGL((norm_bwd_wave<DT, T, NV, U, RAG>), dim3(groups), dim3(256), 0, st, a);       \
+    hipLaunchKernelGGL((norm_bwd_wave<DT, T, NV, U, ROW>), dim3(groups), dim3(256), 0, st, a);       \
     return hipGetLastError();                                                                        \
   }
 #define CF_BWD_BLOCK(TH, NV)                                                                         \
   {                                                                                                  \
-    hipLaunchKernelGGL((norm_bwd_block<DT, TH, NV, RAG>), dim3(groups), dim3(TH), 0, st, a);         \
+    hipLaunchKernelGGL((norm_bwd_block<DT, TH, NV, ROW>), dim3(groups), dim3(TH), 0, st, a);         \
     return hipGetLastError();                                                                        \
   }
-  if (nv <= 1) CF_BWD_WAVE(1, 1, 2)
-  if (nv <= 2) CF_BWD_WAVE(2, 1, 2)
-  if (nv <= 4) CF_BWD_WAVE(4, 1, 2)
-  if (nv <= 8) CF_BWD_WAVE(8, 1, 2)
-  if (nv <= 16) CF_BWD_WAVE(16, 1, 2)
-  if (nv <= 32) CF_BWD_WAVE(32, 1, 2)
-  if (nv <= 64) CF_BWD_WAVE(64, 1, 2)
-  constexpr int F = DT == DT_F32 ? 2 : 1;  // vectors of a type per 64 x 8 x ... values
-  if (a.c <= 1024) {
-    if (nv <= 128) CF_BWD_WAVE(64, 2, 1)
-    CF_BWD_WAVE(64, 4, 1)
+  if constexpr (ROW == SHORT) CF_BWD_WAVE(1, 1, 2)
+  else {
+    if (a.c <= 1024) {
+      const Team t = team_of(nv);
+      switch (t.lanes * 16 + t.vecs) {
+        case 1 * 16 + 1: CF_BWD_WAVE(1, 1, 2)
+        case 2 * 16 + 1: CF_BWD_WAVE(2, 1, 2)
+        case 2 * 16 + 3: CF_BWD_WAVE(2, 3, 1)
+        case 4 * 16 + 1: CF_BWD_WAVE(4, 1, 2)
+        case 4 * 16 + 3: CF_BWD_WAVE(4, 3, 1)
+        case 8 * 16 + 1: CF_BWD_WAVE(8, 1, 2)
+        case 8 * 16 + 3: CF_BWD_WAVE(8, 3, 1)
+        case 16 * 16 + 1: CF_BWD_WAVE(16, 1, 2)
+        case 16 * 16 + 3: CF_BWD_WAVE(16, 3, 1)
+        case 32 * 16 + 1: CF_BWD_WAVE(32, 1, 2)
+        case 32 * 16 + 3: CF_BWD_WAVE(32, 3, 1)
+        case 64 * 16 + 1: CF_BWD_WAVE(64, 1, 2)
+        case 64 * 16 + 2: CF_BWD_WAVE(64, 2, 1)
+        case 64 * 16 + 3: CF_BWD_WAVE(64, 3, 1)
+        default: CF_BWD_WAVE(64, 4, 1)
+      }
+    }
+    // (up to 16384 values: four vectors of fp32, two of bf16 for each of 1024 threads)
+    if constexpr (DT == DT_F32) {
+      if (nv <= 512) CF_BWD_BLOCK(256, 2)
+      if (nv <= 768) CF_BWD_BLOCK(256, 3)
+      if (nv <= 1024) CF_BWD_BLOCK(256, 4)
+      if (nv <= 2048) CF_BWD_BLOCK(1024, 2)
+      if (nv <= 3072) CF_BWD_BLOCK(1024, 3)
+      CF_BWD_BLOCK(1024, 4)
+    } else {
+      if (nv <= 256) CF_BWD_BLOCK(256, 1)
+      if (nv <= 512) CF_BWD_BLOCK(256, 2)
+      if (nv <= 1024) CF_BWD_BLOCK(1024, 1)
+      CF_BWD_BLOCK(1024, 2)
+    }
   }
-  if (a.c <= 2048) CF_BWD_BLOCK(256, F)
-  if (a.c <= 4096) CF_BWD_BLOCK(256, 2 * F)
-  if (a.c <= 8192) CF_BWD_BLOCK(1024, F)
-  CF_BWD_BLOCK(1024, 2 * F)
 #undef CF_BWD_WAVE
 #undef CF_BWD_BLOCK
+}
+
+// how the rows lie picks the kernels
+template <int DT, class F> hipError_t by_row(int c, F f) {
+  constexpr int V = Store<DT>::VEC;
+  if (c % V == 0) return f(std::integral_constant<int, FULL>{});
+  if (c > V) return f(std::integral_constant<int, RAGGED>{});
+  return f(std::integral_constant<int, SHORT>{});
 }
 
 size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
@@ -737,7 +959,7 @@ size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
 }  // namespace
 
 size_t layernorm_fwd_workspace(long long rows, int c, int dtype) {
-  if (!fwd_chunked(rows, c, dtype)) return 0;
+  if (!fwd_chunked(rows, c)) return 0;
   int chunk, nch;
   plan_chunks(rows, c, vec_of(dtype), &chunk, &nch);
   return up16((size_t)rows * nch * sizeof(float2));
@@ -746,7 +968,7 @@ size_t layernorm_fwd_workspace(long long rows, int c, int dtype) {
 size_t layernorm_bwd_workspace(long long rows, int c, int dtype) {
   const size_t part = up16((size_t)bwd_groups(rows, c, dtype) * c * sizeof(float));
   size_t n = 2 * part;
-  if (bwd_chunked(rows, c, dtype)) {
+  if (bwd_chunked(c)) {
     int chunk, nch;
     plan_chunks(rows, c, vec_of(dtype), &chunk, &nch);
     n += up16((size_t)rows * nch * sizeof(float2));
@@ -758,9 +980,8 @@ hipError_t launch_layernorm_fwd(long long rows, int c, int dtype, const void *x,
                                 float eps, void *y, float *mean, float *rstd, void *ws, hipStream_t st) {
   const long long bytes = rows * c * (dtype == DT_BF16 ? 2 : 4);
   const FwdArgs a{rows, c, eps, 1.0f / (float)c, bytes >= kStreamBytes, x, gamma, beta, y, mean, rstd};
-  const bool rag = c % vec_of(dtype) != 0;
-  if (dtype == DT_BF16) return rag ? fwd<DT_BF16, true>(a, ws, st) : fwd<DT_BF16, false>(a, ws, st);
-  return rag ? fwd<DT_F32, true>(a, ws, st) : fwd<DT_F32, false>(a, ws, st);
+  if (dtype == DT_BF16) return by_row<DT_BF16>(c, [&](auto row) { return fwd<DT_BF16, decltype(row)::value>(a, ws, st); });
+  return by_row<DT_F32>(c, [&](auto row) { return fwd<DT_F32, decltype(row)::value>(a, ws, st); });
 }
 
 hipError_t launch_layernorm_bwd(long long rows, int c, int dtype, const void *dy, const void *x, const float *gamma,
@@ -773,10 +994,10 @@ hipError_t launch_layernorm_bwd(long long rows, int c, int dtype, const void *dy
   float *pg = groups == 1 ? dgamma : (float *)ws, *pb = groups == 1 ? dbeta : (float *)((char *)ws + part);
   const BwdArgs a{rows, c, 1.0f / (float)c, bytes >= kStreamBytes, dy, x, gamma, mean, rstd, dx, pg, pb};
   void *rowpart = (char *)ws + 2 * part;
-  const bool rag = c % vec_of(dtype) != 0;
-  const hipError_t e = dtype == DT_BF16
-                           ? (rag ? bwd<DT_BF16, true>(a, groups, rowpart, st) : bwd<DT_BF16, false>(a, groups, rowpart, st))
-                           : (rag ? bwd<DT_F32, true>(a, groups, rowpart, st) : bwd<DT_F32, false>(a, groups, rowpart, st));
+  const hipError_t e =
+      dtype == DT_BF16
+          ? by_row<DT_BF16>(c, [&](auto row) { return bwd<DT_BF16, decltype(row)::value>(a, groups, rowpart, st); })
+          : by_row<DT_F32>(c, [&](auto row) { return bwd<DT_F32, decltype(row)::value>(a, groups, rowpart, st); });
   if (e != hipSuccess || groups == 1) return e;
   const SumJob jobs[2] = {{pg, dgamma, groups, c}, {pb, dbeta, groups, c}};
   return launch_sum_batch(jobs, 2, st);

@@ -20,7 +20,8 @@ GUARD = 64
 
 SHAPES = [(1, 1), (5, 1), (3, 2), (7, 3), (1, 5), (64, 4), (33, 16), (1000, 16), (4099, 8), (257, 31), (130, 64), (77, 65),
           (9, 255), (6, 256), (5, 257), (11, 512), (4, 1000), (3, 1023), (3, 1025), (5, 2049), (3, 4100), (2, 8192), (9, 8195),
-          (2, 16384), (3, 16385), (1, 65536), (9, 65537), (1, 131073), (2, 300001), (40, 20000), (2049, 777), (300, 3000)]
+          (2, 16384), (3, 16385), (1, 65536), (9, 65537), (1, 131073), (2, 300001), (40, 20000), (2049, 777), (300, 3000),
+          (500, 7), (100, 21), (101, 43), (50, 90), (41, 180), (30, 370), (21, 700), (5, 1400), (700, 17), (3, 5100), (300, 17000)]
 
 
 def _t(dt):
