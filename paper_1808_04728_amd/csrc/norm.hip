@@ -25,7 +25,7 @@
 // count once in sums; stored twice they have the same value, and every load of a row
 // comes before its first store).  Element by element that vector took up to fourteen
 // instructions, more than the rest of a short row: 65536 bf16 rows of 255 went from 20.8
-// to BEFORE us.  Rows shorter than a vector, and the ends of chunks (where a
+// to 13.6 us.  Rows shorter than a vector, and the ends of chunks (where a
 // neighbour may have stored already, in place), do go in smaller pieces.  Nothing
 // outside a row is touched.
 
@@ -617,16 +617,19 @@ __global__ __launch_bounds__(256) void norm_bwd_wave(BwdArgs a) {
   }
 }
 
-// a workgroup a row at a time
+// a workgroup a row at a time; 1024 threads, of 128 registers each, read gamma again for
+// every row where it would not fit beside the sums (2000 fp32 rows of 12345 105 us with
+// it kept, 78 so)
 template <int DT, int TH, int NV, int ROW> __global__ __launch_bounds__(TH) void norm_bwd_block(BwdArgs a) {
   constexpr int V = Store<DT>::VEC, W = TH / 64;
+  constexpr bool kKeep = TH < 1024 || NV * V <= 12;
   using S = typename Store<DT>::T;
   __shared__ float red[4 * W];
   const int t = threadIdx.x;
-  float ga[NV][V], dg[NV][V], db[NV][V];
+  float ga[kKeep ? NV : 1][V], dg[NV][V], db[NV][V];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    load_f32<DT, ROW>(a.gamma, Place<DT, ROW>(t + TH * i, a.c), a.c, ga[i]);
+    if constexpr (kKeep) load_f32<DT, ROW>(a.gamma, Place<DT, ROW>(t + TH * i, a.c), a.c, ga[i]);
 #pragma unroll
     for (int j = 0; j < V; ++j) dg[i][j] = db[i][j] = 0.f;
   }
@@ -642,8 +645,11 @@ template <int DT, int TH, int NV, int ROW> __global__ __launch_bounds__(TH) void
     const float mean = a.mean[r], rstd = a.rstd[r];
     float sg = 0.f, sgx = 0.f;
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-      bwd_sums<DT, ROW>(xv[i], dv[i], Place<DT, ROW>(t + TH * i, a.c), a.c, mean, rstd, ga[i], sg, sgx, dg[i], db[i]);
+    for (int i = 0; i < NV; ++i) {
+      const Place<DT, ROW> at(t + TH * i, a.c);
+      if constexpr (!kKeep) load_f32<DT, ROW>(a.gamma, at, a.c, ga[0]);
+      bwd_sums<DT, ROW>(xv[i], dv[i], at, a.c, mean, rstd, ga[kKeep ? i : 0], sg, sgx, dg[i], db[i]);
+    }
     sg = team_sum<64>(sg);
     sgx = team_sum<64>(sgx);
     // the halves of red alternate: one barrier a row
@@ -661,9 +667,11 @@ template <int DT, int TH, int NV, int ROW> __global__ __launch_bounds__(TH) void
     mg *= a.inv_c;
     mgx *= a.inv_c;
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-      store_vec<DT, ROW>((S *)a.dx + r * a.c, Place<DT, ROW>(t + TH * i, a.c), a.c,
-                         bwd_dx<DT>(xv[i], dv[i], mean, rstd, ga[i], mg, mgx), a.nt);
+    for (int i = 0; i < NV; ++i) {
+      const Place<DT, ROW> at(t + TH * i, a.c);
+      if constexpr (!kKeep) load_f32<DT, ROW>(a.gamma, at, a.c, ga[0]);
+      store_vec<DT, ROW>((S *)a.dx + r * a.c, at, a.c, bwd_dx<DT>(xv[i], dv[i], mean, rstd, ga[kKeep ? i : 0], mg, mgx), a.nt);
+    }
   }
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -749,7 +757,8 @@ int vec_of(int dtype) { return dtype == DT_BF16 ? Store<DT_BF16>::VEC : Store<DT
 
 // Lanes of a team and vectors a lane for rows of nv <= 512 vectors: the fewest lanes of
 // those with one, two or three vectors that waste least (33 vectors: 16 lanes with
-// three rather than 64 with one).
+// three rather than 64 with one; two lanes' three vectors are too short a piece of memory:
+// 2^20 fp32 rows of 17 58.7 us forward, 32.8 with eight lanes).
 struct Team {
   int lanes, vecs;
 };
@@ -760,7 +769,7 @@ Team team_of(long long nv) {
   if (nv > 96) return {64, 2};
   for (int t = 1; t < 64; t *= 2) {
     if (nv <= t) return {t, 1};
-    if (t >= 2 && nv > t * 2 && nv <= t * 3) return {t, 3};
+    if (t >= 4 && nv > t * 2 && nv <= t * 3) return {t, 3};
   }
   return {64, 1};
 }
@@ -782,7 +791,7 @@ void plan_chunks(long long rows, int c, int V, int *chunk, int *nch) {
 // units (8 rows of 65536 fp32 values 11.3 us with a workgroup a row).
 bool fwd_chunked(long long rows, int c) { return c > 65536 || (c > 16384 && rows < kNumCUs); }
 
-// Backward: past what 1024 threads hold of x, dy, gamma and the column sums.
+// Backward: past what 1024 threads hold of x, dy and the column sums.
 bool bwd_chunked(int c) { return c > 16384; }
 
 // rows of a block of the column pass: a multiple of kColRows that leaves about four
@@ -801,7 +810,7 @@ int bwd_groups(long long rows, int c, int dtype) {
     const int per = column_rows(rows, c, V);
     return (int)((rows + per - 1) / per);
   }
-  // rows a workgroup takes at a time; a workgroup of at least four times that keeps the
+  // rows a workgroup takes at a time; a workgroup of at least twice that keeps the
   // partial sums (8 bytes a column and workgroup) small beside the rows, but every
   // compute unit should have one
   long long per = 1, cap = kNumCUs;
@@ -813,7 +822,7 @@ int bwd_groups(long long rows, int c, int dtype) {
     cap = 4 * kNumCUs;
   }
   const long long need = (rows + per - 1) / per;
-  long long groups = need / 4 > kNumCUs ? need / 4 : kNumCUs;
+  long long groups = need / 2 > kNumCUs ? need / 2 : kNumCUs;
   if (groups > cap) groups = cap;
   return (int)(need < groups ? need : groups);
 }
@@ -849,7 +858,6 @@ template <int DT, int ROW> hipError_t fwd(const FwdArgs &a, void *ws, hipStream_
       switch (t.lanes * 16 + t.vecs) {
         case 1 * 16 + 1: CF_FWD_WAVE(1, 1, 4)
         case 2 * 16 + 1: CF_FWD_WAVE(2, 1, 4)
-        case 2 * 16 + 3: CF_FWD_WAVE(2, 3, 2)
         case 4 * 16 + 1: CF_FWD_WAVE(4, 1, 4)
         case 4 * 16 + 3: CF_FWD_WAVE(4, 3, 2)
         case 8 * 16 + 1: CF_FWD_WAVE(8, 1, 4)
@@ -912,7 +920,6 @@ template <int DT, int ROW> hipError_t bwd(const BwdArgs &a, int groups, void *ro
       switch (t.lanes * 16 + t.vecs) {
         case 1 * 16 + 1: CF_BWD_WAVE(1, 1, 2)
         case 2 * 16 + 1: CF_BWD_WAVE(2, 1, 2)
-        case 2 * 16 + 3: CF_BWD_WAVE(2, 3, 1)
         case 4 * 16 + 1: CF_BWD_WAVE(4, 1, 2)
         case 4 * 16 + 3: CF_BWD_WAVE(4, 3, 1)
         case 8 * 16 + 1: CF_BWD_WAVE(8, 1, 2)
