@@ -251,7 +251,9 @@ __device__ __forceinline__ void tile_product(TileAcc<G> &acc, char *lds, const c
     if (s + G::NS <= steps) wait_loads<(G::NS - 2) * 2 * T::LD>();
     else wait_loads<0>();
   };
-  constexpr int PH = G::KG == 1 ? 2 : 1, HR = T::TR / PH;  // phases of a k-step, rows of instruction tiles in one
+  // phases of a k-step, rows of instruction tiles in one: the fragments of a whole step where
+  // the registers hold them beside the accumulators
+  constexpr int PH = G::B == 256 ? 2 : 1, HR = T::TR / PH;
   static_assert(T::TR % PH == 0, "phases of equal rows");
   wait_next(-1);
   barrier();
