@@ -60,20 +60,32 @@ __global__ __launch_bounds__(256) void ns_prep_kernel(NsTable T, NsMomentum mom,
   for (long long e = beg + 4LL * threadIdx.x; e < end; e += 4LL * 256) {
     float x[4];
     const int k = (int)min(4LL, end - e);
-    if (DT == DT_F32 && k == 4) {
-      const float4 a = *reinterpret_cast<const float4 *>((const float *)g + M.off + e);
-      x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+    if (k == 4) {
+      if (DT == DT_F32) {
+        const float4 a = *reinterpret_cast<const float4 *>((const float *)g + M.off + e);
+        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+      } else {
+        const ushort4 a = *reinterpret_cast<const ushort4 *>((const uint16_t *)g + M.off + e);
+        x[0] = to_f32<DT_BF16>(a.x); x[1] = to_f32<DT_BF16>(a.y); x[2] = to_f32<DT_BF16>(a.z); x[3] = to_f32<DT_BF16>(a.w);
+      }
+      if constexpr (MOM) {
+        float4 v = *reinterpret_cast<const float4 *>(m + M.off + e);
+        x[0] = ns_momentum(mom, x[0], v.x);
+        x[1] = ns_momentum(mom, x[1], v.y);
+        x[2] = ns_momentum(mom, x[2], v.z);
+        x[3] = ns_momentum(mom, x[3], v.w);
+        *reinterpret_cast<float4 *>(m + M.off + e) = v;
+        *reinterpret_cast<float4 *>(u + e) = make_float4(x[0], x[1], x[2], x[3]);
+      }
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        x[i] = i < k ? to_f32<DT>(((const typename Store<DT>::T *)g)[M.off + e + i]) : 0.f;
-    }
-    if constexpr (MOM) {
-#pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if (i < k) {
-          x[i] = ns_momentum(mom, x[i], m[M.off + e + i]);
-          u[e + i] = x[i];
+        x[i] = i < k ? to_f32<DT>(((const typename Store<DT>::T *)g)[M.off + e + i]) : 0.f;
+        if constexpr (MOM) {
+          if (i < k) {
+            x[i] = ns_momentum(mom, x[i], m[M.off + e + i]);
+            u[e + i] = x[i];
+          }
         }
       }
     }
@@ -98,14 +110,18 @@ __global__ __launch_bounds__(256) void ns_split_kernel(NsTable T, double eps, fl
   const int cols = M.tall ? M.m : M.n, rlim = M.tall ? M.n : M.m;
   const int rr = M.tall ? n0 : m0, cc = M.tall ? m0 : n0;
   float x[16];
+  // (from an element that exists, whatever the lane: loads under a condition would wait one
+  // for the other, 15 us instead of 10 for 517 x 2051)
+  auto load = [&](const auto *p, auto value) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int r = r0 + 4 * i;
-    const long long e = (long long)(rr + r) * cols + cc + c;
-    x[i] = 0.f;
-    if (rr + r < rlim && cc + c < cols)
-      x[i] = M.ws_u >= 0 ? ((const float *)(ws + M.ws_u))[e] : to_f32<DT>(((const typename Store<DT>::T *)src)[M.off + e]);
-  }
+    for (int i = 0; i < 16; ++i)
+      x[i] = value(p[(long long)min(rr + r0 + 4 * i, rlim - 1) * cols + min(cc + c, cols - 1)]);
+  };
+  if (M.ws_u >= 0) load((const float *)(ws + M.ws_u), [](float v) { return v; });
+  else load((const typename Store<DT>::T *)src + M.off, [](auto v) { return to_f32<DT>(v); });
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    if (rr + r0 + 4 * i >= rlim || cc + c >= cols) x[i] = 0.f;
   const Scale sc = scale_of(ns_inv_norm(M, ws, eps, red), scale);
 #pragma unroll
   for (int i = 0; i < 16; ++i) tile[r0 + 4 * i][c] = x[i] * sc.s1 * sc.s2;
@@ -137,22 +153,22 @@ typedef __attribute__((address_space(3))) void lds_void_t;
 typedef const __attribute__((address_space(1))) void global_void_t;
 
 // A square tile of B columns: WR x WC waves of TR x TC matrix instructions each, NS
-// k-steps of both factors in LDS.  Small tiles have KG such groups of waves, each with
-// its own k-steps (group k the steps k, k + KG, ...) and loads; one group alone waits for
-// LDS and the barrier most of a step (64: 0.32 us a step, of which the matrix
-// instructions are 0.08).
+// turns of KS k-steps of both factors in LDS.  Small tiles have KG such groups of waves,
+// each with its own turns (group k the turns k, k + KG, ...) and loads; one group alone
+// waits for LDS and the barrier most of a step (64: 0.32 us a step, of which the matrix
+// instructions are 0.08; two groups 0.26, two k-steps a turn 0.22).
 template <int B_> struct Tile;
 template <> struct Tile<64> {
-  static constexpr int B = 64, WR = 2, WC = 2, NS = 4, KG = 2;
+  static constexpr int B = 64, WR = 2, WC = 2, NS = 2, KG = 2, KS = 2;
 };
 template <> struct Tile<128> {
-  static constexpr int B = 128, WR = 2, WC = 2, NS = 2, KG = 2;
+  static constexpr int B = 128, WR = 2, WC = 2, NS = 2, KG = 2, KS = 1;
 };
 template <> struct Tile<192> {
-  static constexpr int B = 192, WR = 2, WC = 4, NS = 3, KG = 1;
+  static constexpr int B = 192, WR = 2, WC = 4, NS = 3, KG = 1, KS = 1;
 };
 template <> struct Tile<256> {
-  static constexpr int B = 256, WR = 2, WC = 4, NS = 2, KG = 1;
+  static constexpr int B = 256, WR = 2, WC = 4, NS = 2, KG = 1, KS = 1;
 };
 constexpr int pow2_of(int n) { return n & -n; }
 // In a wave's part of the tile, instruction tile (ii, jj) has rows 4 g + q and columns r at
@@ -161,8 +177,9 @@ constexpr int pow2_of(int n) { return n & -n; }
 template <class G> struct TileGeo {
   static constexpr int NG = 64 * G::WR * G::WC, NT = NG * G::KG;  // threads of a group, of the workgroup
   static constexpr int TR = G::B / G::WR / 16, TC = G::B / G::WC / 16;
-  static constexpr int STAGE = 2 * G::B * 128;  // bytes of one k-step
+  static constexpr int STEP = 2 * G::B * 128, STAGE = G::KS * STEP;  // bytes of a k-step, of a turn
   static constexpr int LDS = G::NS * G::KG * STAGE;
+  static_assert(G::KS == 1 || G::NS == 2, "a turn of fewer k-steps has fewer loads to wait for");
   static constexpr int LD = G::B * 8 / NG;  // 16-byte loads a thread and factor
   static constexpr int VJ = pow2_of(TC);
   static constexpr int OROW = 16 * TR * 4 + 16;  // bytes of an output row of a wave in LDS
@@ -189,19 +206,24 @@ template <class G> struct Loader {
       bo[i] = (uint32_t)(min(T::tile_row(row, T::TC), rb - 1 - j0) * pair_row(ld)) + c * 16;
     }
   }
-  // the group's next k-step into `stage`
-  __device__ __forceinline__ void issue(char *stage) {
+  // the group's next turn of `have` k-steps into `stage`
+  __device__ __forceinline__ void issue(char *stage, int have) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x % T::NG >> 6);
 #pragma unroll
-    for (int i = 0; i < T::LD; ++i)
-      __builtin_amdgcn_global_load_lds((global_void_t *)(a + ao[i]), (lds_void_t *)(stage + (i * T::NG + wave * 64) * 16), 16,
-                                       0, 0);
+    for (int k = 0; k < G::KS; ++k) {
+      if (k >= have) break;
+      char *st = stage + k * T::STEP;
 #pragma unroll
-    for (int i = 0; i < T::LD; ++i)
-      __builtin_amdgcn_global_load_lds((global_void_t *)(b + bo[i]),
-                                       (lds_void_t *)(stage + G::B * 128 + (i * T::NG + wave * 64) * 16), 16, 0, 0);
-    a += 128 * G::KG;
-    b += 128 * G::KG;
+      for (int i = 0; i < T::LD; ++i)
+        __builtin_amdgcn_global_load_lds((global_void_t *)(a + k * 128 + ao[i]), (lds_void_t *)(st + (i * T::NG + wave * 64) * 16),
+                                         16, 0, 0);
+#pragma unroll
+      for (int i = 0; i < T::LD; ++i)
+        __builtin_amdgcn_global_load_lds((global_void_t *)(b + k * 128 + bo[i]),
+                                         (lds_void_t *)(st + G::B * 128 + (i * T::NG + wave * 64) * 16), 16, 0, 0);
+    }
+    a += 128 * G::KG * G::KS;
+    b += 128 * G::KG * G::KS;
   }
 };
 
@@ -225,12 +247,14 @@ __device__ __forceinline__ void tile_product(TileAcc<G> &acc, char *lds, const c
   for (int i = 0; i < T::TR; ++i)
 #pragma unroll
     for (int j = 0; j < T::TC; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  const int all = (k1 - k0) / kStep, steps = (all - group + G::KG - 1) / G::KG, turns = (all + G::KG - 1) / G::KG;
+  const int all = (k1 - k0) / kStep, sets = (all + G::KS - 1) / G::KS;  // k-steps, turns of all groups
+  const int steps = (sets - group + G::KG - 1) / G::KG, turns = (sets + G::KG - 1) / G::KG;
+  auto have = [&](int s) { return min(G::KS, all - (s * G::KG + group) * G::KS); };  // k-steps of the group's turn s
   char *ring = lds + group * G::NS * T::STAGE;
-  Loader<G> load(A, ra, i0, B, rb, j0, ld, k0 + group * kStep);
+  Loader<G> load(A, ra, i0, B, rb, j0, ld, k0 + group * G::KS * kStep);
 #pragma unroll
   for (int s = 0; s < G::NS - 1; ++s)
-    if (s < steps) load.issue(ring + s * T::STAGE);
+    if (s < steps) load.issue(ring + s * T::STAGE, have(s));
   // this lane's pieces of a fragment: (row r, hi g) and (row r, lo g)
   const int sw = (r >> 1) & 7;
   const int fh = r * 128 + ((g ^ sw) << 4), fl = r * 128 + (((4 + g) ^ sw) << 4);
@@ -262,22 +286,26 @@ __device__ __forceinline__ void tile_product(TileAcc<G> &acc, char *lds, const c
   for (int s = 0; s < turns; ++s) {
     // every wave has read all of the slot that the next loads overwrite: the reads of
     // both halves were over before the last barrier
-    if (s + G::NS - 1 < steps) load.issue(ring + (slot + G::NS - 1) % G::NS * T::STAGE);
+    if (s + G::NS - 1 < steps) load.issue(ring + (slot + G::NS - 1) % G::NS * T::STAGE, have(s + G::NS - 1));
     const char *st = ring + slot * T::STAGE;
-    f16x8_t bh[T::TC], bl[T::TC];
+    f16x8_t bh[G::KS][T::TC], bl[G::KS][T::TC];
 #pragma unroll
-    for (int j = 0; j < T::TC; ++j) {
-      bh[j] = *reinterpret_cast<const f16x8_t *>(st + brow + j * 2048 + fh);
-      bl[j] = *reinterpret_cast<const f16x8_t *>(st + brow + j * 2048 + fl);
-    }
+    for (int k = 0; k < G::KS; ++k)
+#pragma unroll
+      for (int j = 0; j < T::TC; ++j) {
+        bh[k][j] = *reinterpret_cast<const f16x8_t *>(st + k * T::STEP + brow + j * 2048 + fh);
+        bl[k][j] = *reinterpret_cast<const f16x8_t *>(st + k * T::STEP + brow + j * 2048 + fl);
+      }
 #pragma unroll
     for (int half = 0; half < PH; ++half) {
-      f16x8_t ah[HR], al[HR];
+      f16x8_t ah[G::KS][HR], al[G::KS][HR];
 #pragma unroll
-      for (int i = 0; i < HR; ++i) {
-        ah[i] = *reinterpret_cast<const f16x8_t *>(st + arow + (half * HR + i) * 2048 + fh);
-        al[i] = *reinterpret_cast<const f16x8_t *>(st + arow + (half * HR + i) * 2048 + fl);
-      }
+      for (int k = 0; k < G::KS; ++k)
+#pragma unroll
+        for (int i = 0; i < HR; ++i) {
+          ah[k][i] = *reinterpret_cast<const f16x8_t *>(st + k * T::STEP + arow + (half * HR + i) * 2048 + fh);
+          al[k][i] = *reinterpret_cast<const f16x8_t *>(st + k * T::STEP + arow + (half * HR + i) * 2048 + fl);
+        }
       wait_lds();
       // (one group: the early half reads the next k-step, all waves' loads of it, right
       // after the barrier that ends the later half's last load phase)
@@ -286,20 +314,24 @@ __device__ __forceinline__ void tile_product(TileAcc<G> &acc, char *lds, const c
       if (G::KG == 1 || s < steps) {  // (a group without a last step only keeps the barriers)
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int i = 0; i < HR; ++i)
+        for (int k = 0; k < G::KS; ++k) {
+          if (k > 0 && k >= have(s)) break;  // (the last turn's missing k-step)
 #pragma unroll
-          for (int j = 0; j < T::TC; ++j)
-            acc[half * HR + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[i], bl[j], acc[half * HR + i][j], 0, 0, 0);
+          for (int i = 0; i < HR; ++i)
 #pragma unroll
-        for (int i = 0; i < HR; ++i)
+            for (int j = 0; j < T::TC; ++j)
+              acc[half * HR + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[k][i], bl[k][j], acc[half * HR + i][j], 0, 0, 0);
 #pragma unroll
-          for (int j = 0; j < T::TC; ++j)
-            acc[half * HR + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al[i], bh[j], acc[half * HR + i][j], 0, 0, 0);
+          for (int i = 0; i < HR; ++i)
 #pragma unroll
-        for (int i = 0; i < HR; ++i)
+            for (int j = 0; j < T::TC; ++j)
+              acc[half * HR + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al[k][i], bh[k][j], acc[half * HR + i][j], 0, 0, 0);
 #pragma unroll
-          for (int j = 0; j < T::TC; ++j)
-            acc[half * HR + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[i], bh[j], acc[half * HR + i][j], 0, 0, 0);
+          for (int i = 0; i < HR; ++i)
+#pragma unroll
+            for (int j = 0; j < T::TC; ++j)
+              acc[half * HR + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[k][i], bh[k][j], acc[half * HR + i][j], 0, 0, 0);
+        }
         __builtin_amdgcn_s_setprio(0);
       }
       if (G::KG > 1) wait_next(s);  // (two groups: each reads its own loads)
@@ -426,7 +458,10 @@ __device__ __forceinline__ void store_tile(const TileAcc<G> &acc, char *lds, int
 //   APPLY  xt' = xt P, xn' its transpose
 //   FINAL  the output: o = xt P, or the parameter update with it
 // The m x m products commute and are symmetric: tiles of the upper triangle, stored
-// both ways.
+// both ways.  The matrix cores bound large ones: 4096 x 4096 takes 290 us a product
+// (256 tiles, 1.42 PFLOP/s of half-precision instructions) and 176 a triangle (192 tiles,
+// 1.25).  Small ones wait for their loads: 4.5 us for a launch, its first loads and its
+// stores, then 0.22 us a k-step of 64 tiles.
 template <int MODE, int TB, int DT>
 __global__ __launch_bounds__(TileGeo<Tile<TB>>::NT, 1) void ns_product_kernel(NsTable T, NsProduct p, void *out, uint16_t *v16,
                                                                               char *ws) {
@@ -631,14 +666,14 @@ namespace {
 // Time of a product of `tiles` tiles over `ksteps` k-steps, in us: rounds of a tile a
 // compute unit, each a launch's and tile's fixed share and its k-steps, which take 1.4
 // times as long on a full machine as on an empty one.  Measured on square matrices (tiles
-// of the triangle; m x m products of 64 / 128 / 192 / 256 in us): 512 8.2 / 13.6 / 28 / 34,
-// 1024 12.6 / 19.9 / 44 / 56, 1536 33 / 28 / 60 / 79, 2048 64 / 39 / 79 / 105,
-// 3200 - / 120 / 126 / 168, 4096 - / 242 / 187 / 223.
+// of the triangle; m x m products of 64 / 128 / 192 / 256 in us): 512 8.2 / 13 / 26 / 34,
+// 1024 11.8 / 19 / 39 / 56, 1536 31 / 29 / 53 / 81, 2048 62 / 39 / 69 / 106,
+// 3200 - / 123 / 113 / 170, 4096 - / 242 / 173 / 230.
 struct TileCost {
   int tile;
   double fixed, step;
 };
-constexpr TileCost kTileCost[] = {{64, 4.4, 0.25}, {128, 6.5, 0.42}, {192, 11.5, 1.0}, {256, 21.5, 1.45}};
+constexpr TileCost kTileCost[] = {{64, 4.5, 0.225}, {128, 6.5, 0.42}, {192, 11.5, 0.94}, {256, 21.5, 1.45}};
 double tile_time(const TileCost &c, long long tiles, long long ksteps) {
   const long long full = tiles / kNumCUs, rest = tiles % kNumCUs;
   double t = full * (c.fixed + 1.4 * c.step * ksteps);
@@ -678,7 +713,9 @@ size_t ns_plan(int count, const long long *off, const int *rows, const int *cols
       while (((long long)M.n + M.prow - 1) / M.prow > 512) M.prow *= 2;
       M.chunks = (M.n + M.prow - 1) / M.prow;
       // Workgroups of the long side: 256 rows at a time (128 of 128 columns), on at most
-      // two thirds of the compute units so that a call's other matrices run beside.
+      // two thirds of the compute units so that a call's other matrices run beside: on all
+      // of them 65536 x 128 takes 133 us instead of 150, but the 128^3 network's update 241
+      // instead of 197.
       const long long wgs = ((long long)M.n + (mt == 128 ? 127 : 255)) / (mt == 128 ? 128 : 256);
       M.slices = (int)(wgs < kNsSlices ? wgs : kNsSlices);
       const int tt = mt / 16;

@@ -12,9 +12,16 @@
 // The Gram matrix's upper tiles stay in accumulators; a workgroup's four waves add
 // theirs through LDS, the workgroups' sums are added in a fixed order.
 //
-// The m x m polynomials run in one workgroup a matrix.  Its waves own columns: for
-// a symmetric M and any product C = M B, a wave's columns of B are its own, so a
-// chain of products needs only M in LDS and no exchange between them.
+// The m x m polynomials run at the start of every launch that applies them, in each of
+// its workgroups.  Their waves own columns: for a symmetric M and any product C = M B, a
+// wave's columns of B are its own, so a chain of products needs only M in LDS and no
+// exchange between them.  That repeats the work (128 columns: 63 million operations, 13 us
+// at the matrix rate), but one workgroup's launch for it takes as long and its way through
+// memory longer: the 128^3 network's update took 220 us so and takes 197.
+//
+// What bounds it, 65536 x 128 (150 us of five steps): the norm's pass 9 us and the first
+// Gram matrix 12 at memory's rate; two products with their Gram matrices 46 each, 28 of
+// them the polynomial; the last product 25; the sums between them 5 each.
 //
 // Columns are handled in slots: slot 16 (4 u + c) + r is column 64 u + 4 r + c, so that
 // a lane's four tiles c hold four consecutive columns and rows load and store in
@@ -341,8 +348,8 @@ __device__ __forceinline__ void apply_gram_steps(Acc<MT> &acc, ApplyRows<MT> &x,
 // The same of 128 columns by pairs of waves: all 36 Gram tiles and the factors fill one
 // wave's registers and leave a SIMD one wave.  Two waves have the same rows; each
 // multiplies them by half of P, hands its columns' factors to the other through LDS, and
-// adds 18 tiles.  Then two waves share a SIMD and cover each other's waits (65536 rows:
-// 25 us with one, 18 with two).
+// adds 18 tiles.  Then two waves share a SIMD and cover each other's waits: 4.5 us for a
+// turn of four pairs, of which the matrix instructions are 2.8.
 struct PairAcc {
   f32x4_t own[10], cross[8];  // tiles inside the wave's half, tiles of both
 };
