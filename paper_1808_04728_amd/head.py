@@ -53,6 +53,15 @@ class FCHead:
         self.ws = torch.empty(max(ws, 16), dtype=torch.uint8, device=dev)
         self.x = None
 
+    def bind_params(self, params):
+        """Use the caller's tensors for the parameters and their gradients: one dict of w
+        (the head's dtype), b, dw and db (fp32) a layer, 16-byte aligned."""
+        for i, p in enumerate(params):
+            for k in ("w", "b", "dw", "db"):
+                own = getattr(self, k)
+                assert p[k].shape == own[i].shape and p[k].dtype == own[i].dtype and p[k].is_contiguous(), k
+                own[i] = p[k]
+
     def set_params(self, weights, biases, target):
         for i, (w, b) in enumerate(zip(weights, biases)):
             self.w[i].copy_(torch.as_tensor(w, dtype=torch.float32).to(self.w[i].dtype))

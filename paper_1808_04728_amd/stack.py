@@ -143,6 +143,16 @@ class ConvStack:
         self.opt_m = self.opt_s = self.opt_ws = None
         self.opt_t = 0
 
+    def bind_params(self, params):
+        """Use the caller's tensors for the parameters and their gradients: one dict of
+        w (the stack's dtype), w32 (fp32, may be w), b, dw and db (fp32) a layer, in the
+        shapes of the stack's own, 16-byte aligned.  Their update is then the caller's."""
+        for l, p in zip(self.L, params, strict=True):
+            for k in ("w", "w32", "b", "dw", "db"):
+                assert p[k].shape == l[k].shape and p[k].dtype == l[k].dtype and p[k].is_contiguous(), k
+                l[k] = p[k]
+        self.flat_param = self.flat_grad = self.flat_w16 = self.opt_m = self.opt_s = None
+
     def _alloc(self):
         dev, tdt, n = self.device, self.tdt, self.batch
         self._alloc_params()
@@ -252,6 +262,8 @@ class ConvStack:
         (Adam + LARC + linear decay, one group per tensor); hp is a
         binding.cf_adam_larc_hparams.  Writes the master values and, for a
         bf16 stack, the bf16 weights the next forward pass reads."""
+        if self.flat_param is None:
+            raise RuntimeError("the parameters are the caller's (bind_params)")
         if self.opt_m is None:
             self.opt_m = torch.zeros_like(self.flat_param)
             self.opt_s = torch.zeros_like(self.flat_param)
