@@ -156,8 +156,12 @@ typedef const __attribute__((address_space(1))) void global_void_t;
 // turns of KS k-steps of both factors in LDS.  Small tiles have KG such groups of waves,
 // each with its own turns (group k the turns k, k + KG, ...) and loads; one group alone
 // waits for LDS and the barrier most of a step (64: 0.32 us a step, of which the matrix
-// instructions are 0.08; two groups 0.26, two k-steps a turn 0.22).
+// instructions are 0.08; two groups 0.26, two k-steps a turn 0.22).  The smallest tile has
+// a wave a group and eight k-steps on their way: 0.1 us a step.
 template <int B_> struct Tile;
+template <> struct Tile<32> {
+  static constexpr int B = 32, WR = 1, WC = 1, NS = 2, KG = 8, KS = 1;
+};
 template <> struct Tile<64> {
   static constexpr int B = 64, WR = 2, WC = 2, NS = 2, KG = 2, KS = 2;
 };
@@ -342,19 +346,24 @@ __device__ __forceinline__ void tile_product(TileAcc<G> &acc, char *lds, const c
   if (!late) barrier();
   __syncthreads();  // the output goes through the LDS
   if constexpr (G::KG > 1) {
-    static_assert(G::KG == 2 && G::B * G::B * 4 <= T::LDS, "the second group's accumulators in LDS");
+    // the other groups' accumulators through the LDS, added in group order
+    static_assert((G::KG - 1) * G::B * G::B * 4 <= T::LDS, "their tiles in LDS");
     f32x4_t *part = reinterpret_cast<f32x4_t *>(lds);
+    constexpr int TILE = G::WR * G::WC * T::TR * T::TC * 64;
 #pragma unroll
     for (int i = 0; i < T::TR; ++i)
 #pragma unroll
       for (int j = 0; j < T::TC; ++j)
-        if (group == 1) part[((wave * T::TR + i) * T::TC + j) * 64 + lane] = acc[i][j];
+        if (group > 0) part[(group - 1) * TILE + ((wave * T::TR + i) * T::TC + j) * 64 + lane] = acc[i][j];
     __syncthreads();
+    if (group == 0) {
 #pragma unroll
-    for (int i = 0; i < T::TR; ++i)
+      for (int o = 0; o < G::KG - 1; ++o)
 #pragma unroll
-      for (int j = 0; j < T::TC; ++j)
-        if (group == 0) acc[i][j] += part[((wave * T::TR + i) * T::TC + j) * 64 + lane];
+        for (int i = 0; i < T::TR; ++i)
+#pragma unroll
+          for (int j = 0; j < T::TC; ++j) acc[i][j] += part[o * TILE + ((wave * T::TR + i) * T::TC + j) * 64 + lane];
+    }
     __syncthreads();
   }
 }
@@ -461,7 +470,7 @@ __device__ __forceinline__ void store_tile(const TileAcc<G> &acc, char *lds, int
 // both ways.  The matrix cores bound large ones: 4096 x 4096 takes 290 us a product
 // (256 tiles, 1.42 PFLOP/s of half-precision instructions) and 176 a triangle (192 tiles,
 // 1.25).  Small ones wait for their loads: 4.5 us for a launch, its first loads and its
-// stores, then 0.22 us a k-step of 64 tiles.
+// stores, then 0.1 us a k-step of 32 tiles and 0.22 of 64.
 template <int MODE, int TB, int DT>
 __global__ __launch_bounds__(TileGeo<Tile<TB>>::NT, 1) void ns_product_kernel(NsTable T, NsProduct p, void *out, uint16_t *v16,
                                                                               char *ws) {
@@ -666,14 +675,15 @@ namespace {
 // Time of a product of `tiles` tiles over `ksteps` k-steps, in us: rounds of a tile a
 // compute unit, each a launch's and tile's fixed share and its k-steps, which take 1.4
 // times as long on a full machine as on an empty one.  Measured on square matrices (tiles
-// of the triangle; m x m products of 64 / 128 / 192 / 256 in us): 512 8.2 / 13 / 26 / 34,
-// 1024 11.8 / 19 / 39 / 56, 1536 31 / 29 / 53 / 81, 2048 62 / 39 / 69 / 106,
-// 3200 - / 123 / 113 / 170, 4096 - / 242 / 173 / 230.
+// of the triangle; m x m products of 32 / 64 / 128 / 192 / 256 in us): 256 5.6 / 6.1 / 9.5,
+// 512 6.1 / 8.2 / 13 / 26 / 34, 640 7.2 / 8.8 / 15, 768 12.6 / 9.6 / 17, 1024 22 / 11.8 / 19 /
+// 39 / 56, 1536 45 / 31 / 29 / 53 / 81, 2048 - / 62 / 39 / 69 / 106, 3200 - / - / 123 / 113 /
+// 170, 4096 - / - / 242 / 173 / 230.
 struct TileCost {
   int tile;
   double fixed, step;
 };
-constexpr TileCost kTileCost[] = {{64, 4.5, 0.225}, {128, 6.5, 0.42}, {192, 11.5, 0.94}, {256, 21.5, 1.45}};
+constexpr TileCost kTileCost[] = {{32, 4.7, 0.095}, {64, 4.5, 0.225}, {128, 6.5, 0.42}, {192, 11.5, 0.94}, {256, 21.5, 1.45}};
 double tile_time(const TileCost &c, long long tiles, long long ksteps) {
   const long long full = tiles / kNumCUs, rest = tiles % kNumCUs;
   double t = full * (c.fixed + 1.4 * c.step * ksteps);
@@ -793,6 +803,7 @@ hipError_t launch_newton_schulz(const NsTable &T0, const NsSteps &S, int dtype, 
     if (used(192)) f(std::integral_constant<int, 192>{});
     if (used(128)) f(std::integral_constant<int, 128>{});
     if (used(64)) f(std::integral_constant<int, 64>{});
+    if (used(32)) f(std::integral_constant<int, 32>{});
   };
   auto product = [&](auto mode, auto dt, NsProduct p) {
     constexpr int MODE = decltype(mode)::value, DT = decltype(dt)::value;
