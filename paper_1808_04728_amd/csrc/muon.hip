@@ -383,11 +383,11 @@ __device__ __forceinline__ void triangle_tile(int b, int t, int *ti, int *tj) {
 // where a lane's part of the tile begins
 template <class G> struct Origin {
   int i, j;
-  __device__ __forceinline__ Origin(int ti, int tj) {
+  __device__ __forceinline__ Origin(int ti, int tj, int part) {
     using T = TileGeo<G>;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;  // (of the first group)
-    i = ti * G::B + wave / G::WC * T::TR * 16 + (lane >> 4) * 4 * T::TR;
-    j = tj * G::B + wave % G::WC * T::TC * 16 + (lane & 15) * T::TC;
+    const int lane = threadIdx.x & 63;
+    i = ti * G::B + part / G::WC * T::TR * 16 + (lane >> 4) * 4 * T::TR;
+    j = tj * G::B + part % G::WC * T::TC * 16 + (lane & 15) * T::TC;
   }
 };
 
@@ -401,14 +401,15 @@ template <class G> __device__ __forceinline__ float acc_at(const TileAcc<G> &acc
 // columns past jlim (multiples of 32) are not stored.  By rows sixteen lanes store 64
 // bytes in a piece as they are; by columns a lane has a whole line, and sixteen rows at
 // a time pass through the wave's part of the LDS so that eight lanes store a line
-// together (each its own line took 25 of a 256 tile's 42 us at 256 columns).
+// together (each its own line took 25 of a 256 tile's 42 us at 256 columns).  `part`: which
+// wave's part the accumulators are, that of the wave itself after a product.
 template <class G>
 __device__ __forceinline__ void store_tile(const TileAcc<G> &acc, char *lds, int ti, int tj, float scale, char *cols, int ldc,
-                                           char *rows, int ldr, int ilim, int jlim) {
+                                           char *rows, int ldr, int ilim, int jlim, int part) {
   using T = TileGeo<G>;
-  const Origin<G> at(ti, tj);
+  const Origin<G> at(ti, tj, part);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-  const int iw = ti * G::B + wave / G::WC * T::TR * 16, jw = tj * G::B + wave % G::WC * T::TC * 16;  // the wave's part
+  const int iw = ti * G::B + part / G::WC * T::TR * 16, jw = tj * G::B + part % G::WC * T::TC * 16;
   char *mine = lds + wave * 16 * T::OROW;
   f16x8_t hi[T::TR / 2][T::TC], lo[T::TR / 2][T::TC];
 #pragma unroll
@@ -509,9 +510,10 @@ __global__ __launch_bounds__(TileGeo<Tile<TB>>::NT, 1) void ns_product_kernel(Ns
   TileAcc<G> acc;
   tile_product<G>(acc, lds, A, ra, ti * TB, B, M.mp, tj * TB, ld, k0, k1);
   if (threadIdx.x >= TG::NG) return;
+  const int wave = threadIdx.x >> 6;
   char *o = ws + M.ws_sq + sq * p.out;
   if (MODE == NS_GRAM && M.slices == 1) {
-    store_tile<G>(acc, lds, ti, tj, p.unscale * p.scale, o, M.mp, ti != tj ? o : nullptr, M.mp, M.mp, M.mp);
+    store_tile<G>(acc, lds, ti, tj, p.unscale * p.scale, o, M.mp, ti != tj ? o : nullptr, M.mp, M.mp, M.mp, wave);
   } else if constexpr (MODE == NS_GRAM) {
     // accumulators as they are: [slice][tile][wave tile][lane]
     float4 *part = (float4 *)(ws + M.ws_part) + (long long)b * (TB * TB / 4) + (threadIdx.x >> 6) * TG::TR * TG::TC * 64 +
@@ -525,7 +527,7 @@ __global__ __launch_bounds__(TileGeo<Tile<TB>>::NT, 1) void ns_product_kernel(Ns
     float scale = p.unscale * p.scale;
     if constexpr (MODE == NS_POLY) {
       // H is symmetric: eight consecutive columns of its row j
-      const Origin<G> at(ti, tj);
+      const Origin<G> at(ti, tj, wave);
 #pragma unroll
       for (int jj = 0; jj < TG::TC; ++jj)
 #pragma unroll
@@ -543,11 +545,11 @@ __global__ __launch_bounds__(TileGeo<Tile<TB>>::NT, 1) void ns_product_kernel(Ns
         }
       scale = p.scale;
     }
-    store_tile<G>(acc, lds, ti, tj, scale, o, M.mp, ti != tj ? o : nullptr, M.mp, M.mp, M.mp);
+    store_tile<G>(acc, lds, ti, tj, scale, o, M.mp, ti != tj ? o : nullptr, M.mp, M.mp, M.mp, wave);
   } else if constexpr (MODE == NS_APPLY) {
-    store_tile<G>(acc, lds, ti, tj, p.unscale * p.scale, ws + M.ws_xn, M.np, ws + (p.a ? M.ws_xt : M.ws_xt2), M.mp, M.np, M.mp);
+    store_tile<G>(acc, lds, ti, tj, p.unscale * p.scale, ws + M.ws_xn, M.np, ws + (p.a ? M.ws_xt : M.ws_xt2), M.mp, M.np, M.mp, wave);
   } else {
-    const Origin<G> at(ti, tj);
+    const Origin<G> at(ti, tj, wave);
     const Out dst{out, v16, p.update, p.eta, p.decay, M.gain};
     if (M.tall) {
 #pragma unroll
@@ -575,35 +577,52 @@ __global__ __launch_bounds__(TileGeo<Tile<TB>>::NT, 1) void ns_product_kernel(Ns
   }
 }
 
-// H = sum of the slices' Gram matrices, in slice order
+// H = sum of the slices' Gram matrices: a workgroup takes what one wave of the product
+// had, its W waves every W-th slice each, and their sums are added in wave order.  (With
+// a workgroup a tile that went through all slices 65536 x 256, three tiles of 64 slices,
+// took 73 us, so 17.)  W: as many as the call's most slices, up to kSumWaves; a matrix of
+// fewer has a wave a slice whatever W is.
+template <int TB> constexpr int kSumWaves = TB == 256 ? 4 : 8;
+template <int TB> constexpr int sum_lds(int waves) {  // the other waves' sums, or the rows to be stored
+  using TG = TileGeo<Tile<TB>>;
+  const int sets = (waves - 1) * TG::TR * TG::TC * 1024, rows = 16 * TG::OROW;
+  return sets > rows ? sets : rows;
+}
 template <int TB>
-__global__ __launch_bounds__(TileGeo<Tile<TB>>::NG) void ns_gram_sum_kernel(NsTable T, int slot, float scale, char *ws) {
+__global__ __launch_bounds__(64 * kSumWaves<TB>) void ns_gram_sum_kernel(NsTable T, int slot, float scale, char *ws) {
   using G = Tile<TB>;
   using TG = TileGeo<G>;
-  __shared__ __attribute__((aligned(16))) char lds[16 * TG::OROW * G::WR * G::WC];
+  constexpr int N = TG::TR * TG::TC, PARTS = G::WR * G::WC;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const int W = blockDim.x >> 6;
   const int l = ns_find(T, blockIdx.x);
   const NsMat &M = T.mat[l];
-  const int tm = (M.mp + TB - 1) / TB, tri = tm * (tm + 1) / 2, b = blockIdx.x - T.first[l];
+  const int tm = (M.mp + TB - 1) / TB, tri = tm * (tm + 1) / 2, b = (blockIdx.x - T.first[l]) / PARTS;
+  const int part = (blockIdx.x - T.first[l]) % PARTS, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int ti, tj;
   triangle_tile(b, tm, &ti, &tj);
-  const float4 *part = (const float4 *)(ws + M.ws_part) + (long long)b * (TB * TB / 4) + (threadIdx.x >> 6) * TG::TR * TG::TC * 64 +
-                       (threadIdx.x & 63);
+  const f32x4_t *src = (const f32x4_t *)(ws + M.ws_part) + (long long)b * (TB * TB / 4) + part * N * 64 + lane;
   TileAcc<G> acc;
 #pragma unroll
-  for (int i = 0; i < TG::TR; ++i)
+  for (int i = 0; i < N; ++i) acc[i / TG::TC][i % TG::TC] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  for (int n = wave; n < M.slices; n += W) {
 #pragma unroll
-    for (int j = 0; j < TG::TC; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  for (int n = 0; n < M.slices; ++n) {
+    for (int i = 0; i < N; ++i) acc[i / TG::TC][i % TG::TC] += src[(long long)n * tri * (TB * TB / 4) + i * 64];
+  }
+  f32x4_t *sets = reinterpret_cast<f32x4_t *>(lds);
+  if (wave > 0) {
 #pragma unroll
-    for (int i = 0; i < TG::TR; ++i)
+    for (int i = 0; i < N; ++i) sets[((wave - 1) * N + i) * 64 + lane] = acc[i / TG::TC][i % TG::TC];
+  }
+  __syncthreads();
+  if (wave > 0) return;
+  for (int o = 0; o < min(W, M.slices) - 1; ++o) {
 #pragma unroll
-      for (int j = 0; j < TG::TC; ++j) {
-        const float4 a = part[(long long)n * tri * (TB * TB / 4) + (i * TG::TC + j) * 64];
-        acc[i][j] += f32x4_t{a.x, a.y, a.z, a.w};
-      }
+    for (int i = 0; i < N; ++i) acc[i / TG::TC][i % TG::TC] += sets[(o * N + i) * 64 + lane];
   }
   char *o = ws + M.ws_sq + (long long)M.mp * M.mp * 4 * slot;
-  store_tile<G>(acc, lds, ti, tj, scale, o, M.mp, ti != tj ? o : nullptr, M.mp, M.mp, M.mp);
+  store_tile<G>(acc, lds, ti, tj, scale, o, M.mp, ti != tj ? o : nullptr, M.mp, M.mp, M.mp, part);
 }
 
 }  // namespace
@@ -760,10 +779,12 @@ size_t ns_plan(int count, const long long *off, const int *rows, const int *cols
       if (sq < best_sq) best_sq = sq, M.tile_sq = c.tile;
       const double lng = tile_time(c, tiles(M.mp, c.tile) * tiles(M.np, c.tile), M.mp / kStep);
       if (lng < best_long) best_long = lng, M.tile_long = c.tile;
-      // the Gram product also in slices of the long side, whose sums another launch adds
+      // the Gram product also in slices of the long side, whose sums another launch adds (4 us,
+      // 8 TB/s, and 1.2 us for a turn of its waves: 64 slices of 3 tiles of 128 17 us, 25 of 10
+      // 10.8)
       for (long long s = 1; s <= 64 && (s == 1 || s * 8 <= ksteps); ++s) {
         const double bytes = 8.0 * s * triangle(c.tile) * c.tile * c.tile;  // written and read
-        const double gram = tile_time(c, triangle(c.tile) * s, (ksteps + s - 1) / s) + (s > 1 ? 5.0 + bytes / 4e6 : 0.0);
+        const double gram = tile_time(c, triangle(c.tile) * s, (ksteps + s - 1) / s) + (s > 1 ? 4.0 + bytes / 8e6 + 1.2 * ((s + 7) / 8) : 0.0);
         if (gram < best_gram) best_gram = gram, M.tile_gram = c.tile, M.slices = (int)s;
       }
     }
@@ -841,10 +862,13 @@ hipError_t launch_newton_schulz(const NsTable &T0, const NsSteps &S, int dtype, 
       constexpr int TB = decltype(tile)::value;
       nb = number(&T, [](const NsMat &M) {
         const long long t = (M.mp + TB - 1) / TB;
-        return M.tile_gram == TB && M.slices > 1 ? t * (t + 1) / 2 : 0LL;
+        return M.tile_gram == TB && M.slices > 1 ? t * (t + 1) / 2 * (Tile<TB>::WR * Tile<TB>::WC) : 0LL;
       });
+      int waves = 0;
+      for (int l = 0; l < T.count; ++l)
+        if (!T.mat[l].mt && T.mat[l].tile_gram == TB) waves = max(waves, min(T.mat[l].slices, kSumWaves<TB>));
       if (nb)
-        hipLaunchKernelGGL((ns_gram_sum_kernel<TB>), dim3(nb), dim3(TileGeo<Tile<TB>>::NG), 0, st, T, (int)SQ_H,
+        hipLaunchKernelGGL((ns_gram_sum_kernel<TB>), dim3(nb), dim3(64 * waves), sum_lds<TB>(waves), st, T, (int)SQ_H,
                            G.sh[0] / (G.sx * G.sx), ws);
     });
     square(Poly{}, SQ_H, SQ_H, SQ_Q, 1.f / (G.sh[0] * G.sh[0]), 1.f / G.sh[0], G.sq[0]);

@@ -92,6 +92,19 @@ def test_shapes(r, c, dt):
     check(run_ns([x], dt)[0], x, dt)
 
 
+@pytest.mark.parametrize("r,c", [(20000, 256), (200, 30011), (400, 12000), (9000, 900)])
+def test_gram_products_in_slices(r, c):
+    """Long sides whose Gram products are cut and summed, alone and beside a matrix of
+    few slices."""
+    x, y = matrix(r, c, "noise"), matrix(160, 700, "noise")
+    one = run_ns([x])[0]
+    check(one, x)
+    both = run_ns([x, y])
+    assert torch.equal(both[0], one)
+    assert torch.equal(both[1], run_ns([y])[0])
+    check(both[1], y)
+
+
 @pytest.mark.parametrize("kind", ["noise", "rank1"])
 @pytest.mark.parametrize("r,c", [(16, 27), (60, 200), (300, 128), (128, 128), (260, 400)])
 def test_spectra(r, c, kind):
