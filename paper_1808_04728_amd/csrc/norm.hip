@@ -1001,10 +1001,20 @@ size_t layernorm_bwd_workspace(long long rows, int c, int dtype) {
 
 hipError_t launch_layernorm_fwd(long long rows, int c, int dtype, const void *x, const float *gamma, const float *beta,
                                 float eps, void *y, float *mean, float *rstd, void *ws, hipStream_t st) {
-  const long long bytes = 2 * rows * c * (dtype == DT_BF16 ? 2 : 4);
-  const FwdArgs a{rows, c, eps, 1.0f / (float)c, x, gamma, beta, y, mean, rstd};
-  if (dtype == DT_BF16) return by_row<DT_BF16>(c, bytes, [&](auto row) { return fwd<DT_BF16, decltype(row)::value>(a, ws, st); });
-  return by_row<DT_F32>(c, bytes, [&](auto row) { return fwd<DT_F32, decltype(row)::value>(a, ws, st); });
+  const long long es = dtype == DT_BF16 ? 2 : 4, bytes = 2 * rows * c * es;
+  // a launch has fewer than 2^32 threads: rows of 2^32 values at a time, a thread for at
+  // least two (the chunks of longer rows lie along several grid dimensions)
+  const long long pieces = fwd_chunked(rows, c) ? 1 : (rows * c + (1LL << 32) - 1) >> 32, per = (rows + pieces - 1) / pieces;
+  for (long long r = 0; r < rows; r += per) {
+    const FwdArgs a{min(per, rows - r), c, eps, 1.0f / (float)c, (const char *)x + r * c * es, gamma, beta, (char *)y + r * c * es,
+                    mean + r, rstd + r};
+    const hipError_t e =
+        dtype == DT_BF16
+            ? by_row<DT_BF16>(c, bytes, [&](auto row) { return fwd<DT_BF16, decltype(row)::value>(a, ws, st); })
+            : by_row<DT_F32>(c, bytes, [&](auto row) { return fwd<DT_F32, decltype(row)::value>(a, ws, st); });
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 hipError_t launch_layernorm_bwd(long long rows, int c, int dtype, const void *dy, const void *x, const float *gamma,

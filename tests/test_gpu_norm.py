@@ -265,3 +265,33 @@ def test_offsets_past_32_bits():
     ry, _, rr = _fwd64(tail, gamma, beta)
     _close(x[-64:].double().cpu(), ry, max(float(ry.abs().max()), float((tail.double().abs().amax(1) * rr).max())), "bf16")
     assert torch.equal(x[5], beta.to(torch.bfloat16).cuda())
+
+
+@pytest.mark.parametrize("c", [4, 3])
+def test_more_rows_than_one_launch_takes(c):
+    """bf16 rows of 2^32 values and more in all, in place: rows around the places where
+    2^32 values and half of all end, and the last ones."""
+    rows = 2 ** 32 // c + 9
+    x = torch.empty(rows * c, dtype=torch.bfloat16, device="cuda").fill_(0.5)
+    at = sorted({0, 1, rows // 2 - 1, rows // 2, rows // 2 + 1, rows // 2 + 2, 2 ** 32 // c - 1, 2 ** 32 // c, rows - 2, rows - 1})
+    gen = torch.Generator().manual_seed(c)
+    vals = torch.randn((len(at), c), generator=gen).bfloat16()
+    for i, r in enumerate(at):
+        x[r * c:(r + 1) * c] = vals[i].cuda()
+    g = torch.rand(c, generator=gen) + 0.5
+    b = torch.randn(c, generator=gen)
+    mean = torch.full((rows,), 9.0, device="cuda")
+    rstd = torch.full((rows,), 9.0, device="cuda")
+    B.cf_layernorm_fwd(rows, c, "bf16", x, g.cuda(), b.cuda(), 1e-5, x, mean, rstd, None)
+    v = vals.double()
+    mu = v.mean(1, keepdim=True)
+    rs = 1.0 / torch.sqrt(((v - mu) ** 2).mean(1, keepdim=True) + 1e-5)
+    want = (v - mu) * rs * g.double() + b.double()
+    got = torch.stack([x[r * c:(r + 1) * c] for r in at]).double().cpu()
+    # one rounding to bf16 of values whose fp32 error is far below it
+    assert ((got - want).abs() <= 2.0 ** -8 * want.abs() + 1e-5).all()
+    assert float((mean[at].double().cpu() - mu[:, 0]).abs().max()) <= 1e-6
+    # the constant rows between: mean 0.5, y = beta
+    flat = torch.cat([mean[at[0] + 2:rows // 2 - 1], mean[rows // 2 + 3:2 ** 32 // c - 1]])
+    assert bool((flat == 0.5).all())
+    assert torch.equal(x[2 * c:3 * c].cpu(), b.bfloat16())
