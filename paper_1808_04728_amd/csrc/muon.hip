@@ -20,6 +20,7 @@
 
 #include <math.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "muon_common.h"
@@ -199,7 +200,7 @@ template <class G> struct TileGeo {
 template <class G> struct Loader {
   using T = TileGeo<G>;
   const char *a, *b;  // first row of the tile, this k-step
-  uint32_t ao[T::LD], bo[T::LD];
+  uint32_t ao[T::LD], bo[T::LD];  // (the plan takes only tiles whose rows they reach)
   __device__ __forceinline__ Loader(const char *A, int ra, int i0, const char *B, int rb, int j0, int ld, int k0) {
     a = A + i0 * pair_row(ld) + (long long)k0 * 4;
     b = B + j0 * pair_row(ld) + (long long)k0 * 4;
@@ -781,7 +782,9 @@ size_t ns_plan(int count, const long long *off, const int *rows, const int *cols
       if (lng < best_long) best_long = lng, M.tile_long = c.tile;
       // the Gram product also in slices of the long side, whose sums another launch adds (4 us,
       // 8 TB/s, and 1.2 us for a turn of its waves: 64 slices of 3 tiles of 128 17 us, 25 of 10
-      // 10.8)
+      // 10.8).  It reads rows of the long side, whose offsets from the tile's first have 32 bits
+      // (a tile of 64 fits at any length, one of 256 up to 4.2 million).
+      if ((std::min<long long>(c.tile, M.mp) - 1) * 4 * M.np + 128 > 1LL << 32) continue;
       for (long long s = 1; s <= 64 && (s == 1 || s * 8 <= ksteps); ++s) {
         const double bytes = 8.0 * s * triangle(c.tile) * c.tile * c.tile;  // written and read
         const double gram = tile_time(c, triangle(c.tile) * s, (ksteps + s - 1) / s) + (s > 1 ? 4.0 + bytes / 8e6 + 1.2 * ((s + 7) / 8) : 0.0);
