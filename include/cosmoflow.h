@@ -574,8 +574,8 @@ cf_status cf_layernorm_bwd(int64_t rows, int32_t c, int32_t dtype, const void *d
  * fp32 accumulators on the matrix cores); the Frobenius norm is summed in
  * fp64.  Entries of X_i below about 2^-39 count as zero (with eps far above
  * ||G||_F X_0 itself is that small).  Coefficients with which the iteration
- * can leave the range of those factors for some singular value in [0, 1] are
- * refused (CF_ERR_UNSUPPORTED).  A matrix with a NaN or an infinity becomes
+ * can leave the range of those factors for some singular value in [0, 1], or
+ * one a rounding above, are refused (CF_ERR_UNSUPPORTED).  A matrix with a NaN or an infinity becomes
  * all NaN; other matrices of the call are not affected.  A zero matrix gives
  * zeros (eps > 0).  Deterministic.
  * ------------------------------------------------------------------------ */

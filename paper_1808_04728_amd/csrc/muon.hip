@@ -648,37 +648,61 @@ template <class F> int number(NsTable *T, F blocks) {
 enum : int { SQ_H = 0, SQ_Q = 1, SQ_T = 2, SQ_Q1 = 3, SQ_P = 4, SQ_COUNT = 5 };
 }  // namespace
 
+namespace {
+double most(double x, double y) { return x > y ? x : y; }
+
+// The largest |f(h)| for 0 <= h <= top, f a polynomial whose derivative is a multiple of
+// d2 h^2 + d1 h + d0: at an end or at one of its roots.
+template <class F> double largest(double top, double d2, double d1, double d0, F f) {
+  double r = most(fabs(f(0.0)), fabs(f(top)));
+  auto at = [&](double h) {
+    if (h > 0.0 && h < top) r = most(fabs(f(h)), r);
+  };
+  if (d2 == 0.0) {
+    if (d1 != 0.0) at(-d0 / d1);
+  } else if (const double disc = d1 * d1 - 4.0 * d2 * d0; disc >= 0.0) {
+    const double t = -0.5 * (d1 + copysign(sqrt(disc), d1));
+    at(t / d2);
+    if (t != 0.0) at(d0 / t);
+  }
+  return r;
+}
+}  // namespace
+
+// The polynomial's largest values are where its derivatives vanish, not at sampled points: a
+// range narrower than their distance could grow unseen from pair to pair of steps.
 bool ns_scales(double a, double b, double c, int steps, NsSteps *S) {
   S->a = a;
   S->b = b;
   S->c = c;
   S->stages = (steps + 1) / 2;
-  // the largest power of two that keeps values up to `bound` and twice that below 2^16:
-  // room for rounding and for what lies between the points at which the bounds are taken
+  // (what stays below 1024 on [0, 1] has coefficients of at most 8 times that)
+  if (!(fabs(a) <= 8192.0 && fabs(b) <= 8192.0 && fabs(c) <= 8192.0)) return false;
+  // the largest power of two that keeps values up to `bound` and twice that below 2^16
   auto scale = [](double bound) {
     int e = 0;
     (void)frexp(32768.0 / (1.05 * (bound > 0.125 ? bound : 0.125)), &e);
     return (float)ldexp(1.0, e - 1 < 14 ? e - 1 : 14);
   };
-  auto most = [](double x, double y) { return x > y ? x : y; };
-  constexpr int N = 64;  // (every call pays for them: 8192 points took 100 us)
-  double sigma = 1.0;    // bound of the singular values
+  auto q = [=](double h) { return a + b * h + c * h * h; };
+  // of |q(s^2)|, |s^2 q(s^2)| and |s q(s^2)| for singular values s up to x
+  auto most_q = [&](double x) { return largest(x * x, 0.0, 2.0 * c, b, q); };
+  auto most_qh = [&](double x) { return largest(x * x, 3.0 * c, 2.0 * b, a, [&](double h) { return h * q(h); }); };
+  auto most_step = [&](double x) { return largest(x * x, 5.0 * c, 3.0 * b, a, [&](double h) { return sqrt(h) * q(h); }); };
+  // A singular value may be larger than its bound by the roundings of the norm and of a pair
+  // of steps; a polynomial that multiplies that from step to step is refused.
+  constexpr double kRound = 1.0 + 1.0 / 65536.0;
+  double sigma = kRound;  // bound of the singular values
   for (int s = 0; s < S->stages; ++s) {
     NsStage &G = S->stage[s];
     G = NsStage{};
     G.steps = 2 * s + 1 < steps ? 2 : 1;
     G.sx = scale(sigma);
-    double hb[2] = {sigma * sigma, 0.0}, qb[2] = {0.0, 0.0}, tb = 0.0, pb = 0.0, next = 0.0;
-    for (int i = 0; i <= N; ++i) {
-      const double x = sigma * i / N, h = x * x, q = fabs(a + b * h + c * h * h);
-      const double y = x * q, h1 = y * y, q1 = G.steps == 2 ? fabs(a + b * h1 + c * h1 * h1) : 1.0;
-      qb[0] = most(q, qb[0]);
-      tb = most(q * h, tb);
-      hb[1] = most(h1, hb[1]);
-      qb[1] = most(q1, qb[1]);
-      pb = most(q * q1, pb);
-      next = most(y * q1, next);
-    }
+    // the first step's values are all from 0 to `step`, the second's bounds those over them
+    const double step = most_step(sigma);
+    const double hb[2] = {sigma * sigma, step * step};
+    const double qb[2] = {most_q(sigma), G.steps == 2 ? most_q(step) : 1.0};
+    const double tb = most_qh(sigma), pb = qb[0] * qb[1], next = G.steps == 2 ? most_step(step) : step;
     if (!(qb[0] < 1024.0 && qb[1] < 1024.0 && pb < 16384.0 && tb < 1024.0 && hb[1] < 1024.0 && next < 32.0)) return false;
     for (int k = 0; k < 2; ++k) {
       G.sh[k] = scale(hb[k]);
@@ -686,7 +710,7 @@ bool ns_scales(double a, double b, double c, int steps, NsSteps *S) {
     }
     G.st = scale(tb);
     G.sp = scale(pb);
-    sigma = most(next, 0.125);
+    sigma = most(next, 0.125) * kRound;
   }
   return true;
 }
