@@ -452,7 +452,7 @@ __global__ __launch_bounds__(256) void norm_fwd_chunk_stats(FwdArgs a, int chunk
     for (int i = 0; i < NV; ++i) q += sq_dist_part<DT>(v[i], ((int)threadIdx.x + 256 * i) * V, k, pm);
     const float pq = block_sum<4>(q, red, 1);
     const float d = pm - mean, w = (float)k / (float)(have + k);
-    m2 += pq + d * d * (float)have * w;
+    m2 += pq + (have > 0 ? d * d * (float)have * w : 0.f);  // (the first d is the mean itself: its square may be infinite)
     mean += d * w;
     have += k;
   }

@@ -1,0 +1,55 @@
+"""Layer normalisation of rows whose values come near the end of fp32's range, where the
+formulas are finite: the same results from every kernel that may take a row.
+
+Tolerances: those of the other normalisation tests, 1e-5 of the largest value an output
+could have without cancellation, and for bf16 half a unit in the last of eight bits.  The
+rows' sums and the squares of the deviations are powers of two that fp32 holds exactly."""
+import pytest
+import torch
+
+from paper_1808_04728_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+TOL = 1e-5
+EPS = 1e-5
+
+
+def _t(dt):
+    return torch.bfloat16 if dt == "bf16" else torch.float32
+
+
+def _ws(n):
+    return torch.empty(max(n, 16), dtype=torch.uint8, device="cuda").fill_(0xff)  # NaN patterns
+
+
+def _fwd(x, gamma, beta, dt):
+    rows, c = x.shape
+    y, mean, rstd = torch.empty_like(x), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    B.cf_layernorm_fwd(rows, c, dt, x, gamma, beta, EPS, y, mean, rstd, _ws(B.cf_layernorm_fwd_workspace_size(rows, c, dt)))
+    return y.double(), mean.double(), rstd.double()
+
+
+# waves, workgroups, chunks of one piece and of many pieces
+@pytest.mark.parametrize("rows,c", [(4, 1024), (300, 32768), (3, 32768), (2, 131072), (2, 1 << 24)])
+def test_mean_whose_square_is_infinite(rows, c):
+    gen = torch.Generator(device="cuda").manual_seed(c)
+    gamma, beta = (torch.randn(c, generator=gen, device="cuda") for _ in range(2))
+    sign = torch.tensor([1.0, 1.0, -1.0, -1.0], device="cuda").repeat(c // 4)
+    base = torch.tensor([1.0, -1.0], device="cuda").repeat((rows + 1) // 2)[:rows, None] * 2.0 ** 67
+    y, mean, rstd = _fwd(base + 2.0 ** 50 * sign, gamma, beta, "f32")
+    assert torch.equal(mean, base[:, 0].double())
+    assert float((rstd * 2.0 ** 50 - 1).abs().max()) <= TOL
+    want = sign.double() * gamma.double() + beta.double()
+    assert float((y - want).abs().max()) <= TOL * float(want.abs().max())
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,c", [(5, 8), (4, 1024), (300, 32768), (3, 32768), (2, 131072), (2, 1 << 24)])
+def test_constant_rows_whose_square_is_infinite(rows, c, dt):
+    gen = torch.Generator(device="cuda").manual_seed(c)
+    gamma, beta = (torch.randn(c, generator=gen, device="cuda") for _ in range(2))
+    y, mean, rstd = _fwd(torch.full((rows, c), 2.0 ** 67, dtype=_t(dt), device="cuda"), gamma, beta, dt)
+    assert (mean == 2.0 ** 67).all()
+    assert float((rstd * EPS ** 0.5 - 1).abs().max()) <= TOL
+    assert torch.equal(y, beta.to(_t(dt)).double().expand(rows, c))
