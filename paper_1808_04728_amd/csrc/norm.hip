@@ -505,7 +505,8 @@ struct BwdArgs {
 };
 
 // adds a vector's share of the two sums over the row (of the elements that count; dy is
-// zero past the end) and of dgamma, dbeta
+// zero past the end, and so has to be xh, where mean rstd may be infinite though no value's
+// xh is: mean and rstd are zero for FULL vectors past the end) and of dgamma, dbeta
 template <int DT, int ROW>
 __device__ __forceinline__ void bwd_sums(const u32x4_t &xv, const u32x4_t &dv, const Place<DT, ROW> &at, int c, float mean,
                                          float rstd, const float (&ga)[Store<DT>::VEC], float &sg, float &sgx,
@@ -516,8 +517,9 @@ __device__ __forceinline__ void bwd_sums(const u32x4_t &xv, const u32x4_t &dv, c
   unpack<DT>(dv, d);
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const float xh = (x[i] - mean) * rstd;
-    float g = mul_rounded(d[i], ga[i]);
+    float xh = (x[i] - mean) * rstd;
+    if constexpr (ROW == SHORT) xh = at.has(i, c) ? xh : 0.f;
+    const float g = mul_rounded(d[i], ga[i]);
     dg[i] += d[i] * xh;
     db[i] += d[i];
     if constexpr (ROW == RAGGED) {
@@ -575,16 +577,20 @@ __global__ __launch_bounds__(256) void norm_bwd_wave(BwdArgs a) {
         xv[u][i] = load_vec<DT, ROW, ROW != RAGGED>((const S *)a.x + have * a.c, at, a.c, in);
         dv[u][i] = load_vec<DT, ROW, ROW != RAGGED>((const S *)a.dy + have * a.c, at, a.c, in);
       }
-      mean[u] = in ? a.mean[have] : 0.f;
-      rstd[u] = in ? a.rstd[have] : 0.f;
+      const bool use = in && (NV > 1 || Place<DT, ROW>(t, a.c).any());
+      mean[u] = use ? a.mean[have] : 0.f;
+      rstd[u] = use ? a.rstd[have] : 0.f;
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const long long r = rb + u * (256 / T) + threadIdx.x / T;
       float sg = 0.f, sgx = 0.f;
 #pragma unroll
-      for (int i = 0; i < NV; ++i)
-        bwd_sums<DT, ROW>(xv[u][i], dv[u][i], Place<DT, ROW>(t + T * i, a.c), a.c, mean[u], rstd[u], ga[i], sg, sgx, dg[i], db[i]);
+      for (int i = 0; i < NV; ++i) {
+        const Place<DT, ROW> at(t + T * i, a.c);
+        const bool use = NV == 1 || ROW == RAGGED || at.any();
+        bwd_sums<DT, ROW>(xv[u][i], dv[u][i], at, a.c, use ? mean[u] : 0.f, use ? rstd[u] : 0.f, ga[i], sg, sgx, dg[i], db[i]);
+      }
       const float mg = team_sum<T>(sg) * a.inv_c, mgx = team_sum<T>(sgx) * a.inv_c;
       if (r < a.rows) {
 #pragma unroll
@@ -650,7 +656,8 @@ template <int DT, int TH, int NV, int ROW> __global__ __launch_bounds__(TH) void
     for (int i = 0; i < NV; ++i) {
       const Place<DT, ROW> at(t + TH * i, a.c);
       if constexpr (!kKeep) load_f32<DT, ROW, false>(a.gamma, at, a.c, ga[0]);
-      bwd_sums<DT, ROW>(xv[i], dv[i], at, a.c, mean, rstd, ga[kKeep ? i : 0], sg, sgx, dg[i], db[i]);
+      const bool use = ROW == RAGGED || at.any();
+      bwd_sums<DT, ROW>(xv[i], dv[i], at, a.c, use ? mean : 0.f, use ? rstd : 0.f, ga[kKeep ? i : 0], sg, sgx, dg[i], db[i]);
     }
     sg = team_sum<64>(sg);
     sgx = team_sum<64>(sgx);
@@ -701,7 +708,8 @@ __global__ __launch_bounds__(256) void norm_bwd_chunk_sums(BwdArgs a, int chunk,
     float ga[V];
     const u32x4_t xv = load_part<DT, RAG>(x, e, n), dv = load_part<DT, RAG>(dy, e, n);
     load_f32_part<V>(a.gamma + beg, e, n, ga);
-    bwd_sums<DT, FULL>(xv, dv, Place<DT, FULL>(0, V), V, mean, rstd, ga, sg, sgx, unused0, unused1);
+    constexpr int PART = RAG ? SHORT : FULL;  // the last vector may end early
+    bwd_sums<DT, PART>(xv, dv, Place<DT, PART>(0, V), n - e, mean, rstd, ga, sg, sgx, unused0, unused1);
   }
   sg = block_sum<4>(sg, red, 0);
   sgx = block_sum<4>(sgx, red, 1);

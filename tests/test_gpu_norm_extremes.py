@@ -53,3 +53,27 @@ def test_constant_rows_whose_square_is_infinite(rows, c, dt):
     assert (mean == 2.0 ** 67).all()
     assert float((rstd * EPS ** 0.5 - 1).abs().max()) <= TOL
     assert torch.equal(y, beta.to(_t(dt)).double().expand(rows, c))
+
+
+# lanes, whole vectors and parts of vectors past the row's end, in each kernel: teams (of one,
+# two and three vectors a lane), rows below a vector, workgroups, chunks
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,c", [(70, 1), (70, 3), (70, 5), (70, 12), (70, 24), (70, 35), (9, 272), (9, 320), (5, 1544), (5, 3000),
+                                    (4, 9000), (3, 9001), (3, 20000), (3, 20001), (3, 40003)])
+def test_backward_of_rows_with_infinite_mean_times_rstd(rows, c, dt):
+    """Constant rows: xh = (x - mean) rstd is 0 for every value of the row, -mean rstd would
+    be infinite past its end."""
+    gen = torch.Generator(device="cuda").manual_seed(c)
+    gamma = torch.randn(c, generator=gen, device="cuda")
+    dy = torch.randn((rows, c), generator=gen, device="cuda").to(_t(dt))
+    x = torch.full((rows, c), 2.0 ** 121, dtype=_t(dt), device="cuda")
+    x[1::2] *= -1
+    mean, rstd = x[:, 0].float().contiguous(), torch.full((rows,), EPS ** -0.5, device="cuda")
+    dx, dg, db = torch.empty_like(x), torch.empty(c, device="cuda"), torch.empty(c, device="cuda")
+    B.cf_layernorm_bwd(rows, c, dt, dy, x, gamma, mean, rstd, dx, dg, db, _ws(B.cf_layernorm_bwd_workspace_size(rows, c, dt)))
+    g = dy.double() * gamma.double()
+    want = rstd.double()[:, None] * (g - g.mean(1, keepdim=True))
+    lim = TOL * float((rstd.double() * g.abs().amax(1)).max()) + (2.0 ** -8 * want.abs() if dt == "bf16" else 0.0)
+    assert ((dx.double() - want).abs() <= lim).all()
+    assert (dg == 0).all()
+    assert float((db.double() - dy.double().sum(0)).abs().max()) <= TOL * float(dy.double().abs().sum(0).max())
