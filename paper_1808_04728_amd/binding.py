@@ -222,6 +222,23 @@ def _ptr(t):
     return t.data_ptr()
 
 
+def check_params(own, params):
+    """ValueError unless params can stand in for own, the parameters of each layer (a dict of
+    tensors a layer): the same layers and names, shapes, dtypes and device, contiguous and
+    16-byte aligned."""
+    if len(params) != len(own):
+        raise ValueError(f"parameters of {len(params)} layers for {len(own)}")
+    for i, (o, p) in enumerate(zip(own, params)):
+        for k, t in o.items():
+            x = p.get(k)
+            if not isinstance(x, torch.Tensor):
+                raise ValueError(f"layer {i}, {k}: not a tensor")
+            if x.shape != t.shape or x.dtype != t.dtype or x.device != t.device:
+                raise ValueError(f"layer {i}, {k}: {tuple(x.shape)} {x.dtype} on {x.device}, not {tuple(t.shape)} {t.dtype} on {t.device}")
+            if not x.is_contiguous() or x.data_ptr() % 16:
+                raise ValueError(f"layer {i}, {k}: not contiguous or not 16-byte aligned")
+
+
 _raw_current = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 

@@ -55,12 +55,11 @@ class FCHead:
 
     def bind_params(self, params):
         """Use the caller's tensors for the parameters and their gradients: one dict of w
-        (the head's dtype), b, dw and db (fp32) a layer, 16-byte aligned."""
-        for i, p in enumerate(params):
-            for k in ("w", "b", "dw", "db"):
-                own = getattr(self, k)
-                assert p[k].shape == own[i].shape and p[k].dtype == own[i].dtype and p[k].is_contiguous(), k
-                own[i] = p[k]
+        (the head's dtype), b, dw and db (fp32) a layer, in the shapes of the head's own,
+        contiguous and 16-byte aligned (ValueError)."""
+        B.check_params([dict(w=w, b=b, dw=dw, db=db) for w, b, dw, db in zip(self.w, self.b, self.dw, self.db)], params)
+        for k in ("w", "b", "dw", "db"):
+            setattr(self, k, [p[k] for p in params])
 
     def set_params(self, weights, biases, target):
         for i, (w, b) in enumerate(zip(weights, biases)):

@@ -146,11 +146,12 @@ class ConvStack:
     def bind_params(self, params):
         """Use the caller's tensors for the parameters and their gradients: one dict of
         w (the stack's dtype), w32 (fp32, may be w), b, dw and db (fp32) a layer, in the
-        shapes of the stack's own, 16-byte aligned.  Their update is then the caller's."""
-        for l, p in zip(self.L, params, strict=True):
-            for k in ("w", "w32", "b", "dw", "db"):
-                assert p[k].shape == l[k].shape and p[k].dtype == l[k].dtype and p[k].is_contiguous(), k
-                l[k] = p[k]
+        shapes of the stack's own, contiguous and 16-byte aligned (ValueError).  Their
+        update is then the caller's."""
+        keys = ("w", "w32", "b", "dw", "db")
+        B.check_params([{k: l[k] for k in keys} for l in self.L], params)
+        for l, p in zip(self.L, params):
+            l.update((k, p[k]) for k in keys)
         self.flat_param = self.flat_grad = self.flat_w16 = self.opt_m = self.opt_s = None
 
     def _alloc(self):
