@@ -60,3 +60,19 @@ def test_offsets_in_a_tile_fit_32_bits(plan):
     for (r, c), (mp, np_, sq, lng, gram, slices) in zip(shapes, plan(shapes)):
         assert (min(gram, mp) - 1) * 4 * np_ + 112 < 1 << 32, (r, c, gram)
         assert (max(sq, lng) - 1) * 4 * mp + 112 < 1 << 32
+
+
+def test_every_tile_is_run(plan):
+    """The sizes of test_gpu_muon_tiles.py take each tile in each product, the Gram product's
+    whole and in slices, the long side's for tall and for wide matrices."""
+    import test_gpu_muon_tiles as tiles
+
+    shapes = tiles.SHAPES
+    plans = plan(shapes)
+    assert plans == plan(shapes, dt=1) == plan(shapes, momentum=True)
+    sides = {32, 64, 128, 192, 256}
+    assert {p[2] for p in plans} == sides
+    assert {p[3] for (r, c), p in zip(shapes, plans) if r < c} == sides
+    assert {p[3] for (r, c), p in zip(shapes, plans) if r > c} == sides
+    assert {p[4] for p in plans if p[5] == 1} == sides
+    assert {p[4] for p in plans if p[5] > 1} == sides
