@@ -115,3 +115,15 @@ def test_many_steps_give_orthonormal_rows(r, c):
     o = o.double()
     h = o @ o.t().contiguous() if r <= c else o.t().contiguous() @ o
     assert float((h - torch.eye(m, dtype=torch.float64, device="cuda")).abs().max()) <= 1e-5
+
+
+def test_largest_short_side():
+    """Offsets of a 16384 x 16384 matrix's products, 2^28 values of 4 bytes each."""
+    if torch.cuda.mem_get_info()[0] < 48 << 30:
+        pytest.skip("needs 48 GB of device memory")
+    m = 16384
+    x = matrix(m, m, 5)
+    mats = B.make_matrices([0], [m], [m])
+    o = torch.empty_like(x)
+    B.cf_newton_schulz(mats, "f32", B.make_ns_hparams(), x, o, workspace(B.cf_newton_schulz_workspace_size(mats, "f32"), 0xff))
+    close(o, ns64(x), TOL)
