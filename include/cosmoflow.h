@@ -604,8 +604,9 @@ size_t cf_newton_schulz_workspace_size(int32_t nmat, const cf_matrix *mats, int3
  * a matrix without rows or columns is skipped.  g and o: flat device arrays in
  * dtype; o may be g exactly, otherwise they must not overlap.  Elements of o
  * outside the matrices are not touched.  Sizes: shorter side up to 16384,
- * longer up to 2^24 (CF_ERR_UNSUPPORTED).  Matrices of one call run in the
- * same launches, 24 at a time. */
+ * longer up to 2^24 (CF_ERR_UNSUPPORTED).  Matrices of one call share
+ * launches, 24 at a time: those whose shorter side is up to 128, and the
+ * others by the tiles that they take. */
 cf_status cf_newton_schulz(int32_t nmat, const cf_matrix *mats, int32_t dtype, const cf_ns_hparams *hp,
                            const void *g, void *o, void *ws, size_t ws_bytes, void *stream);
 

@@ -15,8 +15,9 @@
 // the polynomial, |x_ij| <= ||X||_2) and lo above its smallest step; a product is
 // hi hi + hi lo + lo hi in fp32 accumulators, what is left out is 2^-24 of it.
 //
-// All groups of a call share their launches: a workgroup finds its matrix in the
-// table of its launch.
+// The groups of a call share launches: those of up to 128 columns or rows have the skinny
+// kernels', the others these, a launch for each size of tile; a workgroup finds its matrix
+// in the table of its launch.
 
 #include <math.h>
 

@@ -625,7 +625,7 @@ __device__ __forceinline__ void polynomial(const float *gram, int parts, const N
 
 // ---- kernels ----------------------------------------------------------------------
 
-// calls f.template run<MT>() for the matrix's width, MT <= MAX
+// CALL(MT) for the matrix's width mt, MT <= MAX
 #define CF_NS_WIDTH(MAX, mt, CALL)                        \
   {                                                       \
     if (MAX >= 128 && (mt) == 128) CALL(128)              \
@@ -835,7 +835,7 @@ __global__ __launch_bounds__(256) void skinny_gram_kernel(NsTable T, NsSteps S, 
 #undef CALL
 }
 
-// sums of many workgroups' Gram matrices: 64 columns of float4 by 4 phases a workgroup
+// sums of many workgroups' Gram matrices: 16 columns of float4 by 16 phases a workgroup
 __global__ __launch_bounds__(256) void skinny_sum_kernel(NsTable T, char *ws) {
   __shared__ float4 red[256];
   const int l = ns_find(T, blockIdx.x);

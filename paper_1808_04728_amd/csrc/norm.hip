@@ -6,9 +6,10 @@
 //   dx = rstd (g - sum(g) / c - xh sum(g xh) / c),  dgamma = sum_r dy xh,  dbeta = sum_r dy
 //
 // Both passes are bound by HBM (7 and 12 operations a value), so a value is
-// read once: a team of threads holds its row in registers (16-byte vectors as
-// they were loaded) between the sums over the row and the stores.  The variance
-// is the second pass over those registers, not a difference of moments.
+// read once, rows in chunks (below) apart: a team of threads holds its row in
+// registers (16-byte vectors as they were loaded) between the sums over the row and
+// the stores.  The variance is the second pass over those registers, not a
+// difference of moments.
 // Statistics, sums and the arithmetic are fp32 for both types; a bf16 output is
 // rounded once.
 //
@@ -17,7 +18,9 @@
 // exchange), then a wave with more vectors a lane, then a workgroup.  Rows that
 // no workgroup holds, and a few long rows that would leave most compute units
 // idle, are cut into chunks: a first launch leaves each chunk's statistics, the
-// second combines them in a fixed order and reads the chunk again.
+// second combines them in a fixed order and reads the chunk again (from HBM in tensors
+// larger than the last-level cache: 1024 bf16 rows of 2^18 465 us forward, 4096 of 65536
+// 555 us backward, 3.5 and 4.8 TB/s of those that move).
 //
 // Rows whose length is no multiple of a vector start at any element: their
 // vectors are loaded and stored at the elements' own alignment, and the last one is
@@ -343,7 +346,8 @@ __device__ __forceinline__ u32x4_t normalised(const u32x4_t &v, float mean, floa
 }
 
 // Teams of T lanes, NV vectors a lane, U rows a team, their loads all in flight.  Memory
-// bounds it: 2^24 bf16 rows of 16 177 us, 6.8 TB/s; 65536 fp32 rows of 1024 89 us, 6.0.
+// bounds it: 2^24 bf16 rows of 16 175 to 202 us on several cards, 6.0 to 6.9 TB/s; 65536 fp32
+// rows of 1024 90 us, 5.9.
 template <int DT, int T, int NV, int U, int ROW>
 __global__ __launch_bounds__(256) void norm_fwd_wave(FwdArgs a) {
   constexpr int V = Store<DT>::VEC;
@@ -548,7 +552,8 @@ __device__ __forceinline__ u32x4_t bwd_dx(const u32x4_t &xv, const u32x4_t &dv, 
 }
 
 // Teams of T lanes; every team walks rows and keeps its columns' sums.  2^24 bf16 rows of 16
-// 294 us, 6.2 TB/s; 65536 fp32 rows of 1024 148 us, 5.4.
+// 295 to 318 us on several cards, 5.5 to 5.9 TB/s; 65536 fp32 rows of 1024 139 to 150 us, 5.4 to
+// 5.8.
 template <int DT, int T, int NV, int U, int ROW>
 __global__ __launch_bounds__(256) void norm_bwd_wave(BwdArgs a) {
   constexpr int V = Store<DT>::VEC;
@@ -814,8 +819,9 @@ bool fwd_chunked(long long rows, int c) { return c > 65536 || (c > 16384 && rows
 // Backward: past what 1024 threads hold of x, dy and the column sums.
 bool bwd_chunked(int c) { return c > 16384; }
 
-// rows of a block of the column pass: a multiple of kColRows that leaves about four
-// workgroups a compute unit
+// Rows of a block of the column pass: a multiple of kColRows that leaves about four blocks a
+// compute unit over 256 vectors each.  (The launch's strips are of 64, a wave each: sixteen
+// workgroups a compute unit.)
 int column_rows(long long rows, int c, int V) {
   const long long strips = (c + 256LL * V - 1) / (256LL * V), want = (4LL * kNumCUs + strips - 1) / strips;
   const long long per = (rows + want - 1) / want;
