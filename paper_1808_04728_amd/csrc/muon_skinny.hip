@@ -17,9 +17,9 @@
 // wave's columns of B are its own, so a chain of products needs only M in LDS and no
 // exchange between them.  That repeats the work (128 columns: 63 million operations, 13 us
 // at the matrix rate), but one workgroup's launch for it takes as long and its way through
-// memory longer: the 128^3 network's update took 220 us so and takes 197.
+// memory longer: the 128^3 network's update took 220 us so and takes 177 to 197 on several cards.
 //
-// What bounds it, 65536 x 128 (150 us of five steps): the norm's pass 9 us and the first
+// What bounds it, 65536 x 128 (144 to 150 us of five steps on several cards): the norm's pass 9 us and the first
 // Gram matrix 12 at memory's rate; two products with their Gram matrices 46 each, 28 of
 // them the polynomial; the last product 25; the sums between them 5 each.
 //
