@@ -362,7 +362,7 @@ def _bits(q):
 def _scale(x):
     """The smallest power of two that brings a block's largest value to 448 or below."""
     f, e = torch.frexp(x.abs().amax(1, keepdim=True))  # f in [0.5, 1)
-    e = torch.clamp(e - 9 + (f > 0.875).int(), min=-126)
+    e = torch.where(f > 0, torch.clamp(e - 9 + (f > 0.875).int(), min=-126), -126)
     return torch.ldexp(torch.ones_like(f), e)
 
 
