@@ -643,6 +643,164 @@ size_t cf_muon_workspace_size(int32_t nmat, const cf_matrix *mats);
 cf_status cf_muon_step(int32_t nmat, const cf_matrix *mats, int64_t t, const cf_muon_hparams *hp, float *v,
                        const float *g, float *m, void *v16, void *ws, size_t ws_bytes, void *stream);
 
+/* ------------------------------------------------------------------------
+ * Activations of the operators below.  act(u), and its derivative act'(u):
+ *   CF_ACT_NONE   u
+ *   CF_ACT_LRELU  u > 0 ? u : alpha u          (the derivative at 0 is alpha)
+ *   CF_ACT_SILU   u / (1 + e^-u)
+ *   CF_ACT_GELU   u (1 + erf(u / sqrt 2)) / 2
+ * alpha is read by CF_ACT_LRELU alone and must be finite there.
+ * ------------------------------------------------------------------------ */
+typedef enum cf_act { CF_ACT_NONE = 0, CF_ACT_LRELU = 1, CF_ACT_SILU = 2, CF_ACT_GELU = 3 } cf_act;
+
+/* ------------------------------------------------------------------------
+ * Group normalisation and the activation behind it, for networks that
+ * normalise between their convolutions at any batch: the c channels of a
+ * sample are groups of c / groups consecutive ones, and a group's values at
+ * all vox = d*h*w voxels share their statistics.  With x [n][vox][c]:
+ *   mean, rstd [n][groups]: as in layer normalisation, over a sample's group
+ *   u = (x - mean) rstd gamma[ch] + beta[ch],   y = act(u)
+ * and, with du = dy act'(u), xh = (x - mean) rstd and E the mean over a
+ * sample's group,
+ *   dx = rstd (gamma du - E[gamma du] - xh E[gamma du xh])
+ *   dgamma[ch] = sum du xh,   dbeta[ch] = sum du   (over samples and voxels).
+ * groups = 1 normalises whole samples, groups = c each channel.
+ * x, y, dy, dx are in dtype; gamma, beta, mean, rstd, dgamma, dbeta fp32.
+ * Statistics and sums are fp32 or wider, the variance from distances to
+ * means.  The leaky ReLU's slope in the backward pass is that of the u that
+ * exact arithmetic on these inputs gives.  A NaN or an infinity stays in its sample's group (and,
+ * backward, in its channels' gradients) as the formulas have it.
+ * Sizes: n, vox >= 0, c >= 1 and a multiple of groups >= 1, vox < 2^31,
+ * n * c < 2^24, n * vox * c < 2^40.  n == 0 or vox == 0 is a no-op of the
+ * forward pass; the backward pass writes dgamma = dbeta = 0.  eps finite and
+ * >= 0.  All pointers 16-byte aligned; y may be x, and dx may be dy or x,
+ * exactly, otherwise outputs must not overlap inputs or each other
+ * (CF_ERR_ALIAS).  Deterministic: every sum has an order fixed by the sizes.
+ * ------------------------------------------------------------------------ */
+
+/* Bytes of device workspace cf_groupnorm_fwd needs (0 for invalid or empty
+ * sizes and where a group fits a workgroup; ws may then be NULL). */
+size_t cf_groupnorm_fwd_workspace_size(int32_t n, int64_t vox, int32_t c, int32_t groups, int32_t dtype);
+
+/* y, and mean and rstd [n][groups], which the backward pass reads. */
+cf_status cf_groupnorm_fwd(int32_t n, int64_t vox, int32_t c, int32_t groups, int32_t dtype, const void *x,
+                           const float *gamma, const float *beta, float eps, int32_t act, float alpha, void *y,
+                           float *mean, float *rstd, void *ws, size_t ws_bytes, void *stream);
+
+/* Bytes of device workspace cf_groupnorm_bwd needs (0 as above). */
+size_t cf_groupnorm_bwd_workspace_size(int32_t n, int64_t vox, int32_t c, int32_t groups, int32_t dtype);
+
+/* dx, dgamma [c] and dbeta [c] (overwritten, not accumulated) from dy, the
+ * forward pass's input x and its mean and rstd. */
+cf_status cf_groupnorm_bwd(int32_t n, int64_t vox, int32_t c, int32_t groups, int32_t dtype, const void *dy,
+                           const void *x, const float *gamma, const float *beta, const float *mean, const float *rstd,
+                           int32_t act, float alpha, void *dx, float *dgamma, float *dbeta, void *ws, size_t ws_bytes,
+                           void *stream);
+
+/* ------------------------------------------------------------------------
+ * Matrix products with bias, activation and residual in their epilogue, for
+ * layers of many rows: a voxel-wise (1^3) layer on the m = n*d*h*w voxels of
+ * an NDHWC tensor, or a fully-connected layer of a large batch (cf_fc_* are
+ * for the few rows of a head).  With W stored [k][n] as there:
+ *   forward            z = x W + bias,  y = act(z) + residual
+ *   backward data      dx = (dz W' + residual) act'(z)
+ *   backward weights   dW = x' dz,  db[j] = sum_i dz[i][j].
+ * In backward data, z is the pre-activation of the layer before (x = act(z)),
+ * so dx is that layer's dz, and residual a gradient that reaches x by another
+ * path (of a residual block: the block's own output gradient).
+ * x, W, z, y, dz, dx and residual are in dtype; bias, dW, db are fp32.
+ * Products and sums are fp32, with one rounding per output; y is computed
+ * from z before z's rounding.
+ * Sizes: m >= 0, 1 <= k, n <= 2^24, m * k, m * n, k * n < 2^40.  m == 0 is a
+ * no-op, but backward weights writes dW = 0 and db = 0.  All device pointers
+ * 16-byte aligned.  y may be the residual exactly, and dx the residual or z;
+ * otherwise outputs must not overlap inputs or each other (CF_ERR_ALIAS).
+ * Deterministic: every sum has an order fixed by the sizes.
+ * ------------------------------------------------------------------------ */
+
+/* Bytes of device workspace (0 for invalid sizes, or where none is needed;
+ * ws may then be NULL). */
+size_t cf_linear_fwd_workspace_size(int32_t m, int32_t k, int32_t n, int32_t dtype);
+size_t cf_linear_bwd_data_workspace_size(int32_t m, int32_t k, int32_t n, int32_t dtype);
+size_t cf_linear_bwd_weight_workspace_size(int32_t m, int32_t k, int32_t n, int32_t dtype);
+
+/* y [m][n], and z [m][n] unless NULL.  bias [n] and residual [m][n] may be
+ * NULL. */
+cf_status cf_linear_fwd(int32_t m, int32_t k, int32_t n, int32_t dtype, const void *x, const void *w, const float *bias,
+                        int32_t act, float alpha, const void *residual, void *y, void *z, void *ws, size_t ws_bytes,
+                        void *stream);
+
+/* dx [m][k].  residual [m][k] may be NULL; z [m][k] is read unless act is
+ * CF_ACT_NONE, and may be NULL then. */
+cf_status cf_linear_bwd_data(int32_t m, int32_t k, int32_t n, int32_t dtype, const void *dz, const void *w,
+                             const void *residual, const void *z, int32_t act, float alpha, void *dx, void *ws,
+                             size_t ws_bytes, void *stream);
+
+/* dW [k][n], and db [n] unless NULL (overwritten, not accumulated). */
+cf_status cf_linear_bwd_weight(int32_t m, int32_t k, int32_t n, int32_t dtype, const void *x, const void *dz, float *dw,
+                               float *db, void *ws, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
+ * AdamW: Adam with decoupled weight decay (Loshchilov and Hutter) over a list
+ * of tensors wherever they lie, as an alternative to cf_adam_larc_step for
+ * networks whose layers are normalised.  With k = t + 1 and eta_t as in
+ * cf_adam_larc_hparams:
+ *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
+ *   p = (1 - eta_t decay) p - eta_t / (1 - beta1^k) m / (sqrt(v / (1 - beta2^k)) + eps)
+ * in fp32, each operation rounded, in this order:
+ *   m: m beta1 + g (1 - beta1);  v: v beta2 + (g g)(1 - beta2);  r = sqrt(v);
+ *   p keep - (m / (r (1 / sqrt(1 - beta2^k)) + eps)) (eta_t / (1 - beta1^k)),
+ *   keep = 1 - eta_t decay
+ * with the scalars formed in fp64 (keep in fp32).
+ *
+ * Moments are fp32 (m_scale = v_scale = NULL), or 8 bits a value: bytes m and
+ * v hold e4m3 codes (IEEE-like, 4 exponent bits, largest 448, NaN 0x7f) of
+ * m / s and of sqrt(v) / s, where s is the scale of the value's block of
+ * CF_ADAMW_BLOCK consecutive values (the last may be shorter): m_scale[i /
+ * CF_ADAMW_BLOCK], the smallest power of two, at least 2^-126, that brings the
+ * block's largest finite value to 448 or below.  p takes its step from the
+ * moments before they are rounded.  Codes are rounded at random: value a
+ * between two codes goes up where the fraction of the distance in 20 bits,
+ * plus 16 random bits * 16, carries; m takes the low and v the high 16 of
+ *   h = mix(key + i 0x9E3779B9),  key = mix(mix(seed + t 0x9E3779B9) + l 0x9E3779B9)
+ * for value i of tensor l (mod 2^32), mix(h): h ^= h >> 16; h *= 0x6A09E667;
+ * h ^= h >> 15; h *= 0xBB67AE85; h ^= h >> 16.  A v that is not zero is not
+ * held as zero.  A NaN or an infinity becomes NaN and stays at its value; its
+ * block's scale is that of the finite ones.
+ * ------------------------------------------------------------------------ */
+#define CF_ADAMW_BLOCK 256
+
+/* One tensor of `count` values (0: skipped).  p fp32, updated; g in g_dtype;
+ * m and v as above, updated, zero bytes before the first update; m_scale and
+ * v_scale both NULL or both fp32 arrays of a value a block, updated, finite
+ * before the first update; p16: NULL, or bf16 that receives RNE(p).  Device
+ * pointers, 16-byte aligned (the scales, which may be parts of one array for
+ * many tensors, 4-byte aligned). */
+typedef struct cf_adamw_tensor {
+  float *p;
+  const void *g;
+  void *m, *v;
+  float *m_scale, *v_scale;
+  void *p16;
+  int64_t count;
+  float weight_decay; /* decay of this tensor, finite and >= 0 */
+  int32_t g_dtype;    /* a cf_dtype */
+} cf_adamw_tensor;
+
+typedef struct cf_adamw_hparams {
+  double eta0, eta_min; /* global rate, linear in t as in cf_adam_larc_hparams */
+  int64_t t_decay;      /* > 0 */
+  double beta1, beta2;  /* in [0, 1) */
+  double eps;           /* >= 0 */
+  uint32_t seed;        /* of the random bits of 8-bit moments */
+} cf_adamw_hparams;
+
+/* One update of every tensor at step t (the updates already applied).
+ * tensors: HOST array, at most 65536, counts below 2^40.  What a call writes must not overlap
+ * anything else it reads or writes (CF_ERR_ALIAS); tensors may share g. */
+cf_status cf_adamw_step(int32_t ntensors, const cf_adamw_tensor *tensors, int64_t t, const cf_adamw_hparams *hp,
+                        void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -44,6 +44,9 @@ EXPORTS = [
     "cf_conv3d_bwd", "cf_conv3d_bwd_deferred",
     "cf_layernorm_fwd_workspace_size", "cf_layernorm_fwd", "cf_layernorm_bwd_workspace_size", "cf_layernorm_bwd",
     "cf_newton_schulz_workspace_size", "cf_newton_schulz", "cf_muon_workspace_size", "cf_muon_step",
+    "cf_groupnorm_fwd_workspace_size", "cf_groupnorm_fwd", "cf_groupnorm_bwd_workspace_size", "cf_groupnorm_bwd",
+    "cf_linear_fwd_workspace_size", "cf_linear_fwd", "cf_linear_bwd_data_workspace_size", "cf_linear_bwd_data",
+    "cf_linear_bwd_weight_workspace_size", "cf_linear_bwd_weight", "cf_adamw_step",
 ]
 
 
@@ -123,6 +126,56 @@ def make_matrices(offsets, rows, cols):
     return (cf_matrix * len(offsets))(*[cf_matrix(int(o), int(r), int(c)) for o, r, c in zip(offsets, rows, cols)])
 
 
+CF_ACT_NONE, CF_ACT_LRELU, CF_ACT_SILU, CF_ACT_GELU = range(4)
+_ACTS = {"none": CF_ACT_NONE, "lrelu": CF_ACT_LRELU, "silu": CF_ACT_SILU, "gelu": CF_ACT_GELU}
+
+#: values that share a scale where AdamW's moments are held in 8 bits
+CF_ADAMW_BLOCK = 256
+
+
+class cf_adamw_tensor(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("p", "g", "m", "v", "m_scale", "v_scale", "p16")] + [
+        ("count", ctypes.c_int64), ("weight_decay", ctypes.c_float), ("g_dtype", ctypes.c_int32)]
+
+
+class cf_adamw_hparams(ctypes.Structure):
+    _fields_ = [("eta0", ctypes.c_double), ("eta_min", ctypes.c_double), ("t_decay", ctypes.c_int64),
+                ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("seed", ctypes.c_uint32)]
+
+
+def make_adamw_hparams(t_decay, eta0=1e-3, eta_min=1e-4, beta1=0.9, beta2=0.999, eps=1e-8, seed=0) -> cf_adamw_hparams:
+    return cf_adamw_hparams(eta0, eta_min, int(t_decay), beta1, beta2, eps, int(seed) & 0xFFFFFFFF)
+
+
+def make_adamw_tensors(tensors):
+    """Host array of cf_adamw_tensor from one dict a tensor: p (fp32), g (fp32 or bf16), m, v
+    (fp32, or a byte a value with m_scale and v_scale), p16 (bf16 copy of p), weight_decay;
+    all contiguous and on one device (ValueError).  The dicts' tensors have to live as long as
+    the array is used."""
+    out = (cf_adamw_tensor * max(len(tensors), 1))()
+    for l, (a, d) in enumerate(zip(out, tensors)):
+        p = d["p"]
+        n = p.numel()
+        eight = d.get("m_scale") is not None
+        blocks = -(-n // CF_ADAMW_BLOCK)
+        for name, size, types in (("p", n, (torch.float32,)), ("g", n, (torch.float32, torch.bfloat16)),
+                                  ("m", n, (torch.float8_e4m3fn, torch.uint8) if eight else (torch.float32,)),
+                                  ("v", n, (torch.float8_e4m3fn, torch.uint8) if eight else (torch.float32,)),
+                                  ("m_scale", blocks, (torch.float32,)), ("v_scale", blocks, (torch.float32,)),
+                                  ("p16", n, (torch.bfloat16,))):
+            x = d.get(name)
+            if x is None:
+                if name in ("p16", "m_scale", "v_scale"):
+                    continue
+                raise ValueError(f"tensor {l}, {name}: missing")
+            if x.numel() != size or x.dtype not in types or x.device != p.device or not x.is_contiguous():
+                raise ValueError(f"tensor {l}, {name}: {x.numel()} {x.dtype} on {x.device}, or not contiguous")
+            setattr(a, name, x.data_ptr())
+        a.count, a.weight_decay, a.g_dtype = n, float(d.get("weight_decay", 0.0)), dtype_code(d["g"].dtype)
+    return len(tensors), out
+
+
 _lib = None
 
 
@@ -187,6 +240,17 @@ def lib():
         "cf_muon_workspace_size": ([i32, ctypes.POINTER(cf_matrix)], sz),
         "cf_muon_step": ([i32, ctypes.POINTER(cf_matrix), i64, ctypes.POINTER(cf_muon_hparams), vp, vp, vp, vp, vp, sz, vp],
                          ctypes.c_int),
+        "cf_groupnorm_fwd_workspace_size": ([i32, i64, i32, i32, i32], sz),
+        "cf_groupnorm_fwd": ([i32, i64, i32, i32, i32, vp, vp, vp, f32, i32, f32, vp, vp, vp, vp, sz, vp], ctypes.c_int),
+        "cf_groupnorm_bwd_workspace_size": ([i32, i64, i32, i32, i32], sz),
+        "cf_groupnorm_bwd": ([i32, i64, i32, i32, i32] + [vp] * 6 + [i32, f32, vp, vp, vp, vp, sz, vp], ctypes.c_int),
+        "cf_linear_fwd_workspace_size": ([i32] * 4, sz),
+        "cf_linear_fwd": ([i32] * 4 + [vp, vp, vp, i32, f32, vp, vp, vp, vp, sz, vp], ctypes.c_int),
+        "cf_linear_bwd_data_workspace_size": ([i32] * 4, sz),
+        "cf_linear_bwd_data": ([i32] * 4 + [vp, vp, vp, vp, i32, f32, vp, vp, sz, vp], ctypes.c_int),
+        "cf_linear_bwd_weight_workspace_size": ([i32] * 4, sz),
+        "cf_linear_bwd_weight": ([i32] * 4 + [vp, vp, vp, vp, vp, sz, vp], ctypes.c_int),
+        "cf_adamw_step": ([i32, ctypes.POINTER(cf_adamw_tensor), i64, ctypes.POINTER(cf_adamw_hparams), vp], ctypes.c_int),
         "cf_adam_larc_workspace_size": ([i32, ctypes.POINTER(i64)], sz),
         "cf_adam_larc_step": ([i32, ctypes.POINTER(i64), i64, ctypes.POINTER(cf_adam_larc_hparams), vp, vp, vp, vp,
                                vp, vp, sz, vp], ctypes.c_int),
@@ -264,6 +328,15 @@ def dtype_code(dt) -> int:
     if dt in (torch.bfloat16, "bf16", CF_BF16):
         return CF_BF16
     raise ValueError(f"unsupported dtype {dt}")
+
+
+def act_code(act) -> int:
+    """Code of an activation's name (or code)."""
+    if act in _ACTS:
+        return _ACTS[act]
+    if act in _ACTS.values():
+        return int(act)
+    raise ValueError(f"unknown activation {act}")
 
 
 def make_desc(n, dhw, c_in, c_out, k, stride=1, pad="same", dtype=CF_F32) -> cf_conv3d_desc:
@@ -596,3 +669,71 @@ def cf_muon_step(mats, t, hp, v, g, m, v16, ws, ws_bytes=None, stream=None):
         ws_bytes = 0 if ws is None or isinstance(ws, int) else ws.numel() * ws.element_size()
     _check(lib().cf_muon_step(len(mats), mats, int(t), ctypes.byref(hp), _ptr(v), _ptr(g), _ptr(m), _ptr(v16), _ptr(ws),
                               ws_bytes, _stream(stream)))
+
+
+# ---- group normalisation ---------------------------------------------------------
+
+def _ws_bytes(ws, ws_bytes):
+    if ws_bytes is None:
+        return 0 if ws is None or isinstance(ws, int) else ws.numel() * ws.element_size()
+    return ws_bytes
+
+
+def cf_groupnorm_fwd_workspace_size(n, vox, c, groups, dtype) -> int:
+    return int(lib().cf_groupnorm_fwd_workspace_size(n, vox, c, groups, dtype_code(dtype)))
+
+
+def cf_groupnorm_fwd(n, vox, c, groups, dtype, x, gamma, beta, eps, act, alpha, y, mean, rstd, ws=None, ws_bytes=None,
+                     stream=None):
+    """act: "none", "lrelu", "silu" or "gelu" (or a CF_ACT_ code)."""
+    _check(lib().cf_groupnorm_fwd(n, vox, c, groups, dtype_code(dtype), _ptr(x), _ptr(gamma), _ptr(beta), float(eps),
+                                  act_code(act), float(alpha), _ptr(y), _ptr(mean), _ptr(rstd), _ptr(ws),
+                                  _ws_bytes(ws, ws_bytes), _stream(stream)))
+
+
+def cf_groupnorm_bwd_workspace_size(n, vox, c, groups, dtype) -> int:
+    return int(lib().cf_groupnorm_bwd_workspace_size(n, vox, c, groups, dtype_code(dtype)))
+
+
+def cf_groupnorm_bwd(n, vox, c, groups, dtype, dy, x, gamma, beta, mean, rstd, act, alpha, dx, dgamma, dbeta, ws,
+                     ws_bytes=None, stream=None):
+    _check(lib().cf_groupnorm_bwd(n, vox, c, groups, dtype_code(dtype), _ptr(dy), _ptr(x), _ptr(gamma), _ptr(beta),
+                                  _ptr(mean), _ptr(rstd), act_code(act), float(alpha), _ptr(dx), _ptr(dgamma),
+                                  _ptr(dbeta), _ptr(ws), _ws_bytes(ws, ws_bytes), _stream(stream)))
+
+
+# ---- matrix products with an epilogue ----------------------------------------------
+
+def cf_linear_fwd_workspace_size(m, k, n, dtype) -> int:
+    return int(lib().cf_linear_fwd_workspace_size(m, k, n, dtype_code(dtype)))
+
+
+def cf_linear_fwd(m, k, n, dtype, x, w, bias, act, alpha, residual, y, z=None, ws=None, ws_bytes=None, stream=None):
+    _check(lib().cf_linear_fwd(m, k, n, dtype_code(dtype), _ptr(x), _ptr(w), _ptr(bias), act_code(act), float(alpha),
+                               _ptr(residual), _ptr(y), _ptr(z), _ptr(ws), _ws_bytes(ws, ws_bytes), _stream(stream)))
+
+
+def cf_linear_bwd_data_workspace_size(m, k, n, dtype) -> int:
+    return int(lib().cf_linear_bwd_data_workspace_size(m, k, n, dtype_code(dtype)))
+
+
+def cf_linear_bwd_data(m, k, n, dtype, dz, w, residual, z, act, alpha, dx, ws=None, ws_bytes=None, stream=None):
+    _check(lib().cf_linear_bwd_data(m, k, n, dtype_code(dtype), _ptr(dz), _ptr(w), _ptr(residual), _ptr(z), act_code(act),
+                                    float(alpha), _ptr(dx), _ptr(ws), _ws_bytes(ws, ws_bytes), _stream(stream)))
+
+
+def cf_linear_bwd_weight_workspace_size(m, k, n, dtype) -> int:
+    return int(lib().cf_linear_bwd_weight_workspace_size(m, k, n, dtype_code(dtype)))
+
+
+def cf_linear_bwd_weight(m, k, n, dtype, x, dz, dw, db=None, ws=None, ws_bytes=None, stream=None):
+    _check(lib().cf_linear_bwd_weight(m, k, n, dtype_code(dtype), _ptr(x), _ptr(dz), _ptr(dw), _ptr(db), _ptr(ws),
+                                      _ws_bytes(ws, ws_bytes), _stream(stream)))
+
+
+# ---- AdamW -------------------------------------------------------------------------
+
+def cf_adamw_step(tensors, t, hp, stream=None):
+    """tensors: what make_adamw_tensors returns; hp: a cf_adamw_hparams (see make_adamw_hparams)."""
+    n, arr = tensors
+    _check(lib().cf_adamw_step(n, arr, int(t), ctypes.byref(hp), _stream(stream)))

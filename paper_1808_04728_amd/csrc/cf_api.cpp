@@ -8,6 +8,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdio>
 #include <cstdlib>
@@ -15,6 +16,7 @@
 #include <string>
 #include <vector>
 
+#include "activation.h"
 #include "cf_common.h"
 #include "cf_kernels.h"
 
@@ -1231,6 +1233,326 @@ cf_status cf_muon_step(int32_t nmat, const cf_matrix *mats, int64_t t, const cf_
     return finish(cf::launch_newton_schulz(T, S, cf::DT_F32, g, &mom, m, &up, v, (uint16_t *)v16, ws, st), st,
                   "cf_muon_step");
   });
+}
+
+}  // extern "C"
+
+// ---- group normalisation ----------------------------------------------------------
+
+namespace {
+cf_status act_check(int32_t act, float alpha, const char *who) {
+  if (act < CF_ACT_NONE || act > CF_ACT_GELU) return fail(CF_ERR_INVALID_ARG, std::string(who) + ": unknown activation");
+  if (act == CF_ACT_LRELU && !std::isfinite(alpha))
+    return fail(CF_ERR_INVALID_ARG, std::string(who) + ": alpha must be finite");
+  return CF_OK;
+}
+static_assert((int)CF_ACT_LRELU == (int)cf::ACT_LRELU && (int)CF_ACT_SILU == (int)cf::ACT_SILU &&
+                  (int)CF_ACT_GELU == (int)cf::ACT_GELU && (int)CF_ACT_NONE == (int)cf::ACT_NONE,
+              "activation codes");
+
+cf_status gn_check(int32_t n, int64_t vox, int32_t c, int32_t groups, int32_t dtype, const char *who) {
+  if (n < 0 || vox < 0) return fail(CF_ERR_INVALID_ARG, std::string(who) + ": n and vox must be >= 0");
+  if (c <= 0 || groups <= 0) return fail(CF_ERR_INVALID_ARG, std::string(who) + ": c and groups must be > 0");
+  if (c % groups != 0) return fail(CF_ERR_INVALID_ARG, std::string(who) + ": c is not a multiple of groups");
+  if (vox >= (1LL << 31)) return fail(CF_ERR_UNSUPPORTED, std::string(who) + ": more than 2^31 voxels a sample");
+  if ((int64_t)(n > 0 ? n : 1) * c >= (1LL << 24)) return fail(CF_ERR_UNSUPPORTED, std::string(who) + ": n * c too large");
+  if ((int64_t)n * c * vox >= (1LL << 40)) return fail(CF_ERR_UNSUPPORTED, std::string(who) + ": n * vox * c too large");
+  if (dtype != CF_F32 && dtype != CF_BF16) return fail(CF_ERR_INVALID_ARG, "unknown dtype");
+  return CF_OK;
+}
+
+// bytes of a workspace query: 0 for what `bad` rejects, the last error as it was
+template <class Bad, class Size> size_t workspace_query(Bad bad, Size size) {
+  const std::string keep = g_last_error;
+  const bool b = bad() != CF_OK;
+  g_last_error = keep;
+  return b ? 0 : size();
+}
+
+cf_status workspace_check(const void *ws, size_t ws_bytes, size_t need, const char *who) {
+  if (!need) return CF_OK;
+  if (!ws || ws_bytes < need) return fail(CF_ERR_WORKSPACE, std::string(who) + ": workspace missing or smaller than its size query returns");
+  if (!aligned16(ws)) return fail(CF_ERR_ALIGNMENT, "workspace not 16-byte aligned");
+  return CF_OK;
+}
+}  // namespace
+
+extern "C" {
+
+size_t cf_groupnorm_fwd_workspace_size(int32_t n, int64_t vox, int32_t c, int32_t groups, int32_t dtype) {
+  return workspace_query([&] { return gn_check(n, vox, c, groups, dtype, "groupnorm"); },
+                         [&] { return n == 0 || vox == 0 ? 0 : cf::groupnorm_fwd_workspace(n, vox, c, groups, kdt(dtype)); });
+}
+
+cf_status cf_groupnorm_fwd(int32_t n, int64_t vox, int32_t c, int32_t groups, int32_t dtype, const void *x,
+                           const float *gamma, const float *beta, float eps, int32_t act, float alpha, void *y,
+                           float *mean, float *rstd, void *ws, size_t ws_bytes, void *stream) {
+  const char *who = "groupnorm_fwd";
+  cf_status r = gn_check(n, vox, c, groups, dtype, who);
+  if (r != CF_OK || (r = act_check(act, alpha, who)) != CF_OK) return r;
+  if (!std::isfinite(eps) || eps < 0.f) return fail(CF_ERR_INVALID_ARG, "groupnorm_fwd: eps must be finite and >= 0");
+  if (n == 0 || vox == 0) return ok();
+  if ((r = check_ptrs({x, gamma, beta, y, mean, rstd})) != CF_OK) return r;
+  const size_t need = cf::groupnorm_fwd_workspace(n, vox, c, groups, kdt(dtype));
+  if ((r = workspace_check(ws, ws_bytes, need, who)) != CF_OK) return r;
+  const size_t nx = (size_t)n * vox * c * elem_size(dtype), nc = (size_t)c * 4, ng = (size_t)n * groups * 4;
+  if ((r = norm_alias({{x, nx}, {gamma, nc}, {beta, nc}}, {{y, nx}, {mean, ng}, {rstd, ng}, {ws, need}}, y, {x}, who)) != CF_OK)
+    return r;
+  hipStream_t st = (hipStream_t)stream;
+  return finish(cf::launch_groupnorm_fwd(n, vox, c, groups, kdt(dtype), x, gamma, beta, eps, act, alpha, y, mean, rstd, ws, st),
+                st, "cf_groupnorm_fwd");
+}
+
+size_t cf_groupnorm_bwd_workspace_size(int32_t n, int64_t vox, int32_t c, int32_t groups, int32_t dtype) {
+  return workspace_query([&] { return gn_check(n, vox, c, groups, dtype, "groupnorm"); },
+                         [&] { return n == 0 || vox == 0 ? 0 : cf::groupnorm_bwd_workspace(n, vox, c, groups, kdt(dtype)); });
+}
+
+cf_status cf_groupnorm_bwd(int32_t n, int64_t vox, int32_t c, int32_t groups, int32_t dtype, const void *dy,
+                           const void *x, const float *gamma, const float *beta, const float *mean, const float *rstd,
+                           int32_t act, float alpha, void *dx, float *dgamma, float *dbeta, void *ws, size_t ws_bytes,
+                           void *stream) {
+  const char *who = "groupnorm_bwd";
+  cf_status r = gn_check(n, vox, c, groups, dtype, who);
+  if (r != CF_OK || (r = act_check(act, alpha, who)) != CF_OK) return r;
+  hipStream_t st = (hipStream_t)stream;
+  const size_t nc = (size_t)c * 4;
+  if (n == 0 || vox == 0) {
+    if ((r = check_ptrs({dgamma, dbeta})) != CF_OK) return r;
+    if (overlap(dgamma, nc, dbeta, nc)) return fail(CF_ERR_ALIAS, "groupnorm_bwd: two outputs overlap");
+    hipError_t e = cf::launch_fill_zero(dgamma, c, st);
+    if (e == hipSuccess) e = cf::launch_fill_zero(dbeta, c, st);
+    return finish(e, st, "cf_groupnorm_bwd");
+  }
+  if ((r = check_ptrs({dy, x, gamma, beta, mean, rstd, dx, dgamma, dbeta})) != CF_OK) return r;
+  const size_t need = cf::groupnorm_bwd_workspace(n, vox, c, groups, kdt(dtype));
+  if ((r = workspace_check(ws, ws_bytes, need, who)) != CF_OK) return r;
+  const size_t nx = (size_t)n * vox * c * elem_size(dtype), ng = (size_t)n * groups * 4;
+  if ((r = norm_alias({{dy, nx}, {x, nx}, {gamma, nc}, {beta, nc}, {mean, ng}, {rstd, ng}},
+                      {{dx, nx}, {dgamma, nc}, {dbeta, nc}, {ws, need}}, dx, {dy, x}, who)) != CF_OK)
+    return r;
+  return finish(cf::launch_groupnorm_bwd(n, vox, c, groups, kdt(dtype), dy, x, gamma, beta, mean, rstd, act, alpha, dx,
+                                         dgamma, dbeta, ws, st),
+                st, "cf_groupnorm_bwd");
+}
+
+}  // extern "C"
+
+// ---- matrix products with an epilogue -----------------------------------------------
+
+namespace {
+cf_status linear_check(int32_t m, int32_t k, int32_t n, int32_t dtype, const char *who) {
+  if (m < 0) return fail(CF_ERR_INVALID_ARG, std::string(who) + ": m must be >= 0");
+  if (k <= 0 || n <= 0) return fail(CF_ERR_INVALID_ARG, std::string(who) + ": k and n must be > 0");
+  if (k > (1 << 24) || n > (1 << 24)) return fail(CF_ERR_UNSUPPORTED, std::string(who) + ": k or n past 2^24");
+  for (int64_t p : {(int64_t)m * k, (int64_t)m * n, (int64_t)k * n})
+    if (p >= (1LL << 40)) return fail(CF_ERR_UNSUPPORTED, std::string(who) + ": a matrix of 2^40 values or more");
+  if (dtype != CF_F32 && dtype != CF_BF16) return fail(CF_ERR_INVALID_ARG, "unknown dtype");
+  return CF_OK;
+}
+cf_status optional_ptr(const void *p, const char *who) {
+  return p && !aligned16(p) ? fail(CF_ERR_ALIGNMENT, std::string(who) + ": tensor pointer not 16-byte aligned") : CF_OK;
+}
+}  // namespace
+
+extern "C" {
+
+size_t cf_linear_fwd_workspace_size(int32_t m, int32_t k, int32_t n, int32_t dtype) {
+  return workspace_query([&] { return linear_check(m, k, n, dtype, "linear"); },
+                         [&] { return m == 0 ? 0 : cf::linear_fwd_workspace(m, k, n, kdt(dtype)); });
+}
+size_t cf_linear_bwd_data_workspace_size(int32_t m, int32_t k, int32_t n, int32_t dtype) {
+  return workspace_query([&] { return linear_check(m, k, n, dtype, "linear"); },
+                         [&] { return m == 0 ? 0 : cf::linear_bwd_data_workspace(m, k, n, kdt(dtype)); });
+}
+size_t cf_linear_bwd_weight_workspace_size(int32_t m, int32_t k, int32_t n, int32_t dtype) {
+  return workspace_query([&] { return linear_check(m, k, n, dtype, "linear"); },
+                         [&] { return m == 0 ? 0 : cf::linear_bwd_weight_workspace(m, k, n, kdt(dtype)); });
+}
+
+cf_status cf_linear_fwd(int32_t m, int32_t k, int32_t n, int32_t dtype, const void *x, const void *w, const float *bias,
+                        int32_t act, float alpha, const void *residual, void *y, void *z, void *ws, size_t ws_bytes,
+                        void *stream) {
+  const char *who = "linear_fwd";
+  cf_status r = linear_check(m, k, n, dtype, who);
+  if (r != CF_OK || (r = act_check(act, alpha, who)) != CF_OK) return r;
+  if (m == 0) return ok();
+  if ((r = check_ptrs({x, w, y})) != CF_OK) return r;
+  for (const void *p : {(const void *)bias, residual, (const void *)z})
+    if ((r = optional_ptr(p, who)) != CF_OK) return r;
+  const size_t need = cf::linear_fwd_workspace(m, k, n, kdt(dtype)), es = elem_size(dtype);
+  if ((r = workspace_check(ws, ws_bytes, need, who)) != CF_OK) return r;
+  const size_t ny = (size_t)m * n * es;
+  if ((r = norm_alias({{x, (size_t)m * k * es}, {w, (size_t)k * n * es}, {bias, (size_t)n * 4}, {residual, ny}},
+                      {{y, ny}, {z, ny}, {ws, need}}, y, {residual}, who)) != CF_OK)
+    return r;
+  hipStream_t st = (hipStream_t)stream;
+  const cf::LinearEpilogue e{bias, residual, z, nullptr, act, alpha};
+  return finish(cf::launch_linear_fwd(m, k, n, kdt(dtype), x, w, e, y, ws, st), st, "cf_linear_fwd");
+}
+
+cf_status cf_linear_bwd_data(int32_t m, int32_t k, int32_t n, int32_t dtype, const void *dz, const void *w,
+                             const void *residual, const void *z, int32_t act, float alpha, void *dx, void *ws,
+                             size_t ws_bytes, void *stream) {
+  const char *who = "linear_bwd_data";
+  cf_status r = linear_check(m, k, n, dtype, who);
+  if (r != CF_OK || (r = act_check(act, alpha, who)) != CF_OK) return r;
+  if (m == 0) return ok();
+  if ((r = check_ptrs({dz, w, dx})) != CF_OK) return r;
+  if (act != CF_ACT_NONE && !z) return fail(CF_ERR_INVALID_ARG, "linear_bwd_data: an activation needs z");
+  if (act == CF_ACT_NONE) z = nullptr;
+  for (const void *p : {residual, z})
+    if ((r = optional_ptr(p, who)) != CF_OK) return r;
+  const size_t need = cf::linear_bwd_data_workspace(m, k, n, kdt(dtype)), es = elem_size(dtype);
+  if ((r = workspace_check(ws, ws_bytes, need, who)) != CF_OK) return r;
+  const size_t nx = (size_t)m * k * es;
+  if ((r = norm_alias({{dz, (size_t)m * n * es}, {w, (size_t)k * n * es}, {residual, nx}, {z, nx}}, {{dx, nx}, {ws, need}}, dx,
+                      {residual, z}, who)) != CF_OK)
+    return r;
+  hipStream_t st = (hipStream_t)stream;
+  const cf::LinearEpilogue e{nullptr, residual, nullptr, z, act, alpha};
+  return finish(cf::launch_linear_bwd_data(m, k, n, kdt(dtype), dz, w, e, dx, ws, st), st, "cf_linear_bwd_data");
+}
+
+cf_status cf_linear_bwd_weight(int32_t m, int32_t k, int32_t n, int32_t dtype, const void *x, const void *dz, float *dw,
+                               float *db, void *ws, size_t ws_bytes, void *stream) {
+  const char *who = "linear_bwd_weight";
+  cf_status r = linear_check(m, k, n, dtype, who);
+  if (r != CF_OK) return r;
+  hipStream_t st = (hipStream_t)stream;
+  const size_t nw = (size_t)k * n * 4, nb = (size_t)n * 4;
+  if ((r = check_ptrs({dw})) != CF_OK || (r = optional_ptr(db, who)) != CF_OK) return r;
+  if (overlap(dw, nw, db, nb)) return fail(CF_ERR_ALIAS, "linear_bwd_weight: two outputs overlap");
+  if (m == 0) {
+    hipError_t e = cf::launch_fill_zero(dw, (long long)k * n, st);
+    if (e == hipSuccess && db) e = cf::launch_fill_zero(db, n, st);
+    return finish(e, st, "cf_linear_bwd_weight");
+  }
+  if ((r = check_ptrs({x, dz})) != CF_OK) return r;
+  const size_t need = cf::linear_bwd_weight_workspace(m, k, n, kdt(dtype)), es = elem_size(dtype);
+  if ((r = workspace_check(ws, ws_bytes, need, who)) != CF_OK) return r;
+  if ((r = norm_alias({{x, (size_t)m * k * es}, {dz, (size_t)m * n * es}}, {{dw, nw}, {db, nb}, {ws, need}}, nullptr, {},
+                      who)) != CF_OK)
+    return r;
+  return finish(cf::launch_linear_bwd_weight(m, k, n, kdt(dtype), x, dz, dw, db, ws, st), st, "cf_linear_bwd_weight");
+}
+
+}  // extern "C"
+
+// ---- AdamW ------------------------------------------------------------------------
+
+namespace {
+constexpr int32_t kMaxTensors = 1 << 16;
+constexpr int64_t kAdamwPiece = 1LL << 30;  // values of one table entry: a launch stays below 2^24 workgroups
+
+struct Extent {
+  uintptr_t beg, end;
+  bool written;
+};
+
+// whether something written overlaps anything else (the extents of each role are mostly
+// in ascending order already)
+bool any_overlap(std::vector<Extent> &v) {
+  std::sort(v.begin(), v.end(), [](const Extent &a, const Extent &b) { return a.beg < b.beg; });
+  uintptr_t read_end = 0, write_end = 0;
+  for (const Extent &e : v) {
+    if (e.beg < write_end || (e.written && e.beg < read_end)) return true;
+    uintptr_t &end = e.written ? write_end : read_end;
+    end = std::max(end, e.end);
+  }
+  return false;
+}
+
+cf_status adamw_check(int32_t ntensors, const cf_adamw_tensor *tensors) {
+  if (ntensors < 0) return fail(CF_ERR_INVALID_ARG, "adamw: ntensors must be >= 0");
+  if (ntensors > kMaxTensors) return fail(CF_ERR_UNSUPPORTED, "adamw: more than 65536 tensors");
+  if (ntensors > 0 && !tensors) return fail(CF_ERR_INVALID_ARG, "adamw: tensors is NULL");
+  std::vector<Extent> ext;
+  ext.reserve((size_t)ntensors * 7);
+  for (int32_t l = 0; l < ntensors; ++l) {
+    const cf_adamw_tensor &A = tensors[l];
+    if (A.count < 0 || A.count >= (1LL << 40)) return fail(CF_ERR_INVALID_ARG, "adamw: a count is negative or past 2^40");
+    if (A.g_dtype != CF_F32 && A.g_dtype != CF_BF16) return fail(CF_ERR_INVALID_ARG, "adamw: unknown g_dtype");
+    if (!std::isfinite(A.weight_decay) || A.weight_decay < 0.f)
+      return fail(CF_ERR_INVALID_ARG, "adamw: weight_decay must be finite and >= 0");
+    if (!A.m_scale != !A.v_scale) return fail(CF_ERR_INVALID_ARG, "adamw: m_scale and v_scale must both be given or both be NULL");
+    if (A.count == 0) continue;
+    cf_status r;
+    if ((r = check_ptrs({A.p, A.g, A.m, A.v})) != CF_OK) return r;
+    const size_t n = (size_t)A.count, state = A.m_scale ? n : 4 * n, scales = (n + CF_ADAMW_BLOCK - 1) / CF_ADAMW_BLOCK * 4;
+    auto add = [&](const void *p, size_t bytes, bool written) {
+      if (p) ext.push_back({(uintptr_t)p, (uintptr_t)p + bytes, written});
+    };
+    if ((r = optional_ptr(A.p16, "adamw")) != CF_OK) return r;
+    if (((uintptr_t)A.m_scale | (uintptr_t)A.v_scale) & 3u) return fail(CF_ERR_ALIGNMENT, "adamw: scales not 4-byte aligned");
+    add(A.p, 4 * n, true);
+    add(A.g, n * elem_size(A.g_dtype), false);
+    add(A.m, state, true);
+    add(A.v, state, true);
+    add(A.m_scale, scales, true);
+    add(A.v_scale, scales, true);
+    add(A.p16, 2 * n, true);
+  }
+  if (any_overlap(ext)) return fail(CF_ERR_ALIAS, "adamw: what is updated overlaps something else of the call");
+  return CF_OK;
+}
+}  // namespace
+
+extern "C" {
+
+cf_status cf_adamw_step(int32_t ntensors, const cf_adamw_tensor *tensors, int64_t t, const cf_adamw_hparams *hp,
+                        void *stream) {
+  if (!hp) return fail(CF_ERR_INVALID_ARG, "adamw: hp is NULL");
+  if (t < 0) return fail(CF_ERR_INVALID_ARG, "adamw: t must be >= 0");
+  if (hp->t_decay <= 0) return fail(CF_ERR_INVALID_ARG, "adamw: t_decay must be > 0");
+  for (double x : {hp->eta0, hp->eta_min, hp->beta1, hp->beta2, hp->eps})
+    if (!std::isfinite(x)) return fail(CF_ERR_INVALID_ARG, "adamw: hyperparameters must be finite");
+  if (hp->beta1 < 0.0 || hp->beta1 >= 1.0 || hp->beta2 < 0.0 || hp->beta2 >= 1.0)
+    return fail(CF_ERR_INVALID_ARG, "adamw: beta1 and beta2 must lie in [0, 1)");
+  if (hp->eps < 0.0) return fail(CF_ERR_INVALID_ARG, "adamw: eps must be >= 0");
+  cf_status r = adamw_check(ntensors, tensors);
+  if (r != CF_OK) return r;
+  const double tc = (double)(t < hp->t_decay ? t : hp->t_decay), k = (double)t + 1.0;
+  const double eta = (hp->eta0 - hp->eta_min) * (1.0 - tc / (double)hp->t_decay) + hp->eta_min;
+  const cf::AdamwStep step{(float)hp->beta1, (float)(1.0 - hp->beta1), (float)hp->beta2, (float)(1.0 - hp->beta2),
+                           (float)(1.0 / std::sqrt(1.0 - std::pow(hp->beta2, k))), (float)hp->eps,
+                           (float)(eta / (1.0 - std::pow(hp->beta1, k)))};
+  hipStream_t st = (hipStream_t)stream;
+  cf::AdamwTable T;
+  T.count = 0;
+  int64_t total = 0;
+  auto flush = [&] {
+    const hipError_t e = T.count ? cf::launch_adamw(T, step, st) : hipSuccess;
+    T.count = 0;
+    total = 0;
+    return finish(e, st, "cf_adamw_step");
+  };
+  for (int32_t l = 0; l < ntensors; ++l) {
+    const cf_adamw_tensor &A = tensors[l];
+    const int es = (int)elem_size(A.g_dtype), ss = A.m_scale ? 1 : 4;
+    const uint32_t key = cf::adamw_key(hp->seed, t, l);
+    const volatile float decayed = (float)eta * A.weight_decay;  // rounded by itself
+    for (int64_t at = 0; at < A.count; at += kAdamwPiece) {
+      const int64_t n = std::min(kAdamwPiece, A.count - at);
+      if (T.count == cf::kAdamwTable || total + n > 4 * kAdamwPiece)
+        if ((r = flush()) != CF_OK) return r;
+      cf::AdamwTensor &B = T.t[T.count++];
+      total += n;
+      B.p = A.p + at;
+      B.g = (const char *)A.g + at * es;
+      B.m = (char *)A.m + at * ss;
+      B.v = (char *)A.v + at * ss;
+      B.ms = A.m_scale ? A.m_scale + at / CF_ADAMW_BLOCK : nullptr;
+      B.vs = A.v_scale ? A.v_scale + at / CF_ADAMW_BLOCK : nullptr;
+      B.p16 = A.p16 ? (uint16_t *)A.p16 + at : nullptr;
+      B.count = n;
+      B.key = key + (uint32_t)at * 0x9E3779B9u;
+      B.keep = 1.f - decayed;
+      B.first = 0;
+      B.g16 = A.g_dtype == CF_BF16;
+    }
+  }
+  return flush();
 }
 
 }  // extern "C"

@@ -314,6 +314,63 @@ hipError_t launch_ns_skinny(const NsTable &T, const NsSteps &S, int dtype, const
 hipError_t launch_newton_schulz(const NsTable &T, const NsSteps &S, int dtype, const void *g, const NsMomentum *mom,
                                 float *m, const NsUpdate *up, void *out, uint16_t *v16, void *ws, hipStream_t st);
 
+// AdamW over a list of tensors (adamw.hip).  A table holds the tensors of one launch and
+// is passed by value as a kernel argument.
+constexpr int kAdamwTable = 44;
+struct AdamwTensor {
+  float *p;
+  const void *g;
+  void *m, *v;
+  float *ms, *vs;  // scales of 8-bit moments; null: fp32 moments
+  uint16_t *p16;
+  long long count;
+  uint32_t key;  // of its random bits
+  float keep;    // 1 - eta * decay
+  int first;     // first workgroup (set by launch_adamw)
+  int g16;
+};
+struct AdamwTable {
+  int count;
+  AdamwTensor t[kAdamwTable];
+};
+struct AdamwStep {
+  float b1, c1, b2, c2, root, eps, lr;
+};
+uint32_t adamw_key(uint32_t seed, long long t, int tensor);
+// tensors of at least one value, 2^32 in all at most
+hipError_t launch_adamw(AdamwTable &T, const AdamwStep &h, hipStream_t st);
+
+// Group normalisation with its activation (groupnorm.hip) of n samples of vox voxels of c
+// channels; act as in activation.h.
+size_t groupnorm_fwd_workspace(int n, long long vox, int c, int groups, int dtype);
+size_t groupnorm_bwd_workspace(int n, long long vox, int c, int groups, int dtype);
+hipError_t launch_groupnorm_fwd(int n, long long vox, int c, int groups, int dtype, const void *x, const float *gamma,
+                                const float *beta, float eps, int act, float alpha, void *y, float *mean, float *rstd,
+                                void *ws, hipStream_t st);
+hipError_t launch_groupnorm_bwd(int n, long long vox, int c, int groups, int dtype, const void *dy, const void *x,
+                                const float *gamma, const float *beta, const float *mean, const float *rstd, int act,
+                                float alpha, void *dx, float *dgamma, float *dbeta, void *ws, hipStream_t st);
+
+// Matrix products with an epilogue (linear.hip): rows x[M][K], W[K][N].
+struct LinearEpilogue {
+  const float *bias;     // [N], may be null
+  const void *residual;  // [M][N] of the output, may be null
+  void *z;               // out: the pre-activation, may be null
+  const void *zin;       // the pre-activation whose slope multiplies the output
+  int act;
+  float alpha;
+};
+size_t linear_fwd_workspace(long long M, int K, int N, int dtype);
+size_t linear_bwd_data_workspace(long long M, int K, int N, int dtype);
+size_t linear_bwd_weight_workspace(long long M, int K, int N, int dtype);
+hipError_t launch_linear_fwd(long long M, int K, int N, int dtype, const void *x, const void *w, const LinearEpilogue &e,
+                             void *y, void *ws, hipStream_t st);
+hipError_t launch_linear_bwd_data(long long M, int K, int N, int dtype, const void *dz, const void *w,
+                                  const LinearEpilogue &e, void *dx, void *ws, hipStream_t st);
+// db may be null
+hipError_t launch_linear_bwd_weight(long long M, int K, int N, int dtype, const void *x, const void *dz, float *dw,
+                                    float *db, void *ws, hipStream_t st);
+
 // Fully-connected layers (fc.hip): rows x[M][K], W[K][N], z[M][N].
 size_t fc_fwd_workspace(int M, int K, int N);
 hipError_t launch_fc_fwd(int M, int K, int N, int dtype, const void *x, const void *w, void *y, void *ws,

@@ -1,0 +1,255 @@
+// linear.hip -- matrix products with bias, activation and residual in their epilogue, and
+// their gradients (gfx950).
+//
+//   forward        z = x W + b,  y = act(z) + r           x [M][K], W [K][N]
+//   backward data  dx = (dz W' + r) act'(z)               z: of the layer before
+//   backward weights  dW = x' dz,  db = sum of dz's rows
+//
+// All three are C[i][j] = sum_l A(i, l) B(l, j) with the sum's axis innermost in memory or
+// not: forward has A by rows of l and B by columns, backward data both by rows of l,
+// backward weights neither.
+
+#include <algorithm>
+
+#include "activation.h"
+#include "cf_common.h"
+#include "cf_kernels.h"
+
+namespace cf {
+namespace {
+
+constexpr int kThreads = 256;
+
+// Which operand has the sum's axis innermost.
+enum : int { FORM_FWD = 0, FORM_DATA = 1, FORM_WEIGHT = 2 };
+template <int FORM> struct Form;
+template <> struct Form<FORM_FWD> { static constexpr bool AK = true, BK = false; };
+template <> struct Form<FORM_DATA> { static constexpr bool AK = true, BK = true; };
+template <> struct Form<FORM_WEIGHT> { static constexpr bool AK = false, BK = false; };
+
+// The product's sizes: C [M][N], the sum over L.
+struct Sizes {
+  long long M, L;
+  int N;
+  int tn;           // tiles along N
+  long long tiles;  // of the output
+  int slices;       // of the sum: each a part of the launch, joined by a second one
+  long long per;    // terms of a slice
+};
+
+// A grid's x dimension holds fewer than 2^32 threads: tiles past 2^22 go on in y.
+dim3 tile_grid(long long tiles) {
+  const long long x = std::min(tiles, 1LL << 22);
+  return dim3((unsigned)x, (unsigned)((tiles + x - 1) / x));
+}
+__device__ __forceinline__ long long tile_index() { return (long long)blockIdx.y * gridDim.x + blockIdx.x; }
+
+// one value of the output, C[i][j] = v
+template <int DT, int FORM, int ACT>
+__device__ __forceinline__ void put(const LinearEpilogue &E, void *out, long long i, int j, int N, float v) {
+  typedef typename Store<DT>::T T;
+  const long long at = i * N + j;
+  if constexpr (FORM == FORM_WEIGHT) {
+    ((float *)out)[at] = v;
+  } else if constexpr (FORM == FORM_FWD) {
+    if (E.bias) v += E.bias[j];
+    if (E.z) ((T *)E.z)[at] = from_f32<DT>(v);
+    v = act<ACT>(v, E.alpha);
+    if (E.residual) v += to_f32<DT>(((const T *)E.residual)[at]);
+    ((T *)out)[at] = from_f32<DT>(v);
+  } else {
+    if (E.residual) v += to_f32<DT>(((const T *)E.residual)[at]);
+    if constexpr (ACT != ACT_NONE) v *= act_slope<ACT>(to_f32<DT>(((const T *)E.zin)[at]), E.alpha);
+    ((T *)out)[at] = from_f32<DT>(v);
+  }
+}
+
+// Any sizes and alignment: tiles of 64 x 64, four waves of 32 x 32, both factors element by
+// element into LDS with the sum's axis innermost.
+template <int DT, int FORM, int ACT>
+__global__ __launch_bounds__(kThreads) void any_kernel(Sizes S, const void *A_, const void *B_, LinearEpilogue E, void *out,
+                                                       float *part) {
+  typedef typename Store<DT>::T T;
+  constexpr int TB = 64, KS = DT == DT_BF16 ? 32 : 16, LD = KS + (DT == DT_BF16 ? 8 : 4);
+  __shared__ __attribute__((aligned(16))) T la[TB * LD], lb[TB * LD];
+  const T *A = (const T *)A_, *B = (const T *)B_;
+  const long long index = tile_index(), tile = index % S.tiles, slice = index / S.tiles;
+  if (slice >= S.slices) return;
+  const long long i0 = tile / S.tn * TB;
+  const int j0 = (int)(tile % S.tn) * TB;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, g = lane >> 4;
+  const int wi = (wave >> 1) * 32, wj = (wave & 1) * 32;
+  f32x4_t acc[2][2];
+#pragma unroll
+  for (int a = 0; a < 2; ++a)
+#pragma unroll
+    for (int b = 0; b < 2; ++b) acc[a][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  const long long l1 = min((slice + 1) * S.per, S.L);
+  for (long long l0 = slice * S.per; l0 < l1; l0 += KS) {
+#pragma unroll
+    for (int q = 0; q < TB * KS / kThreads; ++q) {
+      const int id = q * kThreads + tid;
+      {
+        const int i = Form<FORM>::AK ? id / KS : id % TB, l = Form<FORM>::AK ? id % KS : id / TB;
+        const bool in = i0 + i < S.M && l0 + l < l1;
+        la[i * LD + l] = in ? A[Form<FORM>::AK ? (i0 + i) * S.L + l0 + l : (l0 + l) * S.M + i0 + i] : (T)0;
+      }
+      {
+        const int j = Form<FORM>::BK ? id / KS : id % TB, l = Form<FORM>::BK ? id % KS : id / TB;
+        const bool in = j0 + j < S.N && l0 + l < l1;
+        lb[j * LD + l] = in ? B[Form<FORM>::BK ? (j0 + j) * S.L + l0 + l : (l0 + l) * S.N + j0 + j] : (T)0;
+      }
+    }
+    __syncthreads();
+    if constexpr (DT == DT_BF16) {
+      bf16x8_t a[2], b[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        a[t] = *reinterpret_cast<const bf16x8_t *>(la + (wi + 16 * t + r) * LD + 8 * g);
+        b[t] = *reinterpret_cast<const bf16x8_t *>(lb + (wj + 16 * t + r) * LD + 8 * g);
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[t], b[u], acc[t][u], 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int k = 0; k < KS; k += 4) {
+        float a[2], b[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          a[t] = la[(wi + 16 * t + r) * LD + k + g];
+          b[t] = lb[(wj + 16 * t + r) * LD + k + g];
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[t], b[u], acc[t][u], 0, 0, 0);
+      }
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const long long i = i0 + wi + 16 * t + 4 * g + e;
+        const int j = j0 + wj + 16 * u + r;
+        if (i >= S.M || j >= S.N) continue;
+        if (S.slices > 1) part[(slice * S.M + i) * S.N + j] = acc[t][u][e];
+        else put<DT, FORM, ACT>(E, out, i, j, S.N, acc[t][u][e]);
+      }
+}
+
+// The slices' sum, in slice order, and the epilogue.
+template <int DT, int FORM, int ACT>
+__global__ __launch_bounds__(kThreads) void join_kernel(long long M, int N, int slices, const float *part, LinearEpilogue E,
+                                                        void *out) {
+  const long long n = M * N, at = tile_index() * kThreads + threadIdx.x;
+  if (at >= n) return;
+  float v = part[at];
+  for (int s = 1; s < slices; ++s) v += part[s * n + at];
+  put<DT, FORM, ACT>(E, out, at / N, (int)(at % N), N, v);
+}
+
+// part[slice][N] = sums of the slice's rows of dz
+template <int DT>
+__global__ __launch_bounds__(kThreads) void colsum_kernel(long long M, int N, long long per, const void *dz_, float *part) {
+  __shared__ float red[kThreads];
+  const int tiles = (N + 63) / 64;
+  const long long s = blockIdx.x / tiles;
+  const int j = (int)(blockIdx.x % tiles) * 64 + (threadIdx.x & 63), ph = threadIdx.x >> 6;
+  const typename Store<DT>::T *dz = (const typename Store<DT>::T *)dz_;
+  float a = 0.f;
+  if (j < N)
+    for (long long i = s * per + ph; i < min((s + 1) * per, M); i += 4) a += to_f32<DT>(dz[i * N + j]);
+  red[threadIdx.x] = a;
+  __syncthreads();
+  if (ph == 0 && j < N)
+    part[s * N + j] = (red[threadIdx.x] + red[threadIdx.x + 64]) + (red[threadIdx.x + 128] + red[threadIdx.x + 192]);
+}
+
+int colsum_slices(long long M, int N) {
+  const long long tiles = (N + 63) / 64;
+  return (int)std::max(1LL, std::min((M + 63) / 64, 1024 / tiles));
+}
+
+constexpr int kCUs = 256;
+constexpr long long kChain = 65536;  // most terms of one fp32 sum, where the partial sums' size allows
+
+// Slices of the sum: where the output's tiles leave compute units idle, as many as fill
+// them twice (each of at least 256 terms), and none of more than kChain terms while the
+// partial sums stay below 2^28 values.
+int slices_of(long long M, int N, long long L) {
+  const long long tiles = (M + 63) / 64 * ((N + 63) / 64), out = M * N;
+  const long long fill = std::min(2 * kCUs / tiles, L / 256);
+  const long long chain = std::min((L + kChain - 1) / kChain, (1LL << 28) / out);
+  return (int)std::max(1LL, std::max(fill, chain));
+}
+size_t slices_bytes(long long M, int N, long long L) {
+  const int s = slices_of(M, N, L);
+  return s > 1 ? ((size_t)s * M * N * 4 + 15) / 16 * 16 : 0;
+}
+
+template <int FORM>
+hipError_t product(long long M, int N, long long L, int dtype, const void *A, const void *B, const LinearEpilogue &E, void *out,
+                   void *ws, hipStream_t st) {
+  const int tn = (N + 63) / 64, slices = slices_of(M, N, L);
+  const long long per = ((L + slices - 1) / slices + 31) / 32 * 32;
+  const Sizes S{M, L, N, tn, (M + 63) / 64 * tn, slices, per};
+  const dim3 grid = tile_grid(S.tiles * slices), block(kThreads);
+  float *part = (float *)ws;
+  with_act(E.act, [&](auto a) {
+    constexpr int ACT = FORM == FORM_WEIGHT ? (int)ACT_NONE : decltype(a)::value;
+    if (dtype == DT_BF16) hipLaunchKernelGGL((any_kernel<DT_BF16, FORM, ACT>), grid, block, 0, st, S, A, B, E, out, part);
+    else hipLaunchKernelGGL((any_kernel<DT_F32, FORM, ACT>), grid, block, 0, st, S, A, B, E, out, part);
+    if (slices > 1 && FORM != FORM_WEIGHT) {
+      const dim3 all = tile_grid((M * N + kThreads - 1) / kThreads);
+      if (dtype == DT_BF16)
+        hipLaunchKernelGGL((join_kernel<DT_BF16, FORM, ACT>), all, block, 0, st, M, N, slices, (const float *)part, E, out);
+      else hipLaunchKernelGGL((join_kernel<DT_F32, FORM, ACT>), all, block, 0, st, M, N, slices, (const float *)part, E, out);
+    }
+  });
+  const hipError_t r = hipGetLastError();
+  if (r != hipSuccess || slices == 1 || FORM != FORM_WEIGHT) return r;
+  // (slices of more than one have fewer than 2^28 values in all, or fill 512 tiles of 4096)
+  return launch_sum_rows(part, (float *)out, slices, (int)(M * N), st);
+}
+
+}  // namespace
+
+size_t linear_fwd_workspace(long long M, int K, int N, int) { return slices_bytes(M, N, K); }
+size_t linear_bwd_data_workspace(long long M, int K, int N, int) { return slices_bytes(M, K, N); }
+// (the column sums come after the product, in the same place)
+size_t linear_bwd_weight_workspace(long long M, int K, int N, int) {
+  const size_t sums = ((size_t)colsum_slices(M, N) * N * 4 + 15) / 16 * 16;
+  return std::max(sums, slices_bytes(K, N, M));
+}
+
+hipError_t launch_linear_fwd(long long M, int K, int N, int dtype, const void *x, const void *w, const LinearEpilogue &e,
+                             void *y, void *ws, hipStream_t st) {
+  return product<FORM_FWD>(M, N, K, dtype, x, w, e, y, ws, st);
+}
+
+hipError_t launch_linear_bwd_data(long long M, int K, int N, int dtype, const void *dz, const void *w,
+                                  const LinearEpilogue &e, void *dx, void *ws, hipStream_t st) {
+  return product<FORM_DATA>(M, K, N, dtype, dz, w, e, dx, ws, st);
+}
+
+hipError_t launch_linear_bwd_weight(long long M, int K, int N, int dtype, const void *x, const void *dz, float *dw, float *db,
+                                    void *ws, hipStream_t st) {
+  const LinearEpilogue none{nullptr, nullptr, nullptr, nullptr, ACT_NONE, 0.f};
+  hipError_t r = product<FORM_WEIGHT>(K, N, M, dtype, x, dz, none, dw, ws, st);
+  if (r != hipSuccess || !db) return r;
+  const int slices = colsum_slices(M, N);
+  const long long per = (M + slices - 1) / slices;
+  const dim3 grid((unsigned)((long long)slices * ((N + 63) / 64)));
+  if (dtype == DT_BF16) hipLaunchKernelGGL((colsum_kernel<DT_BF16>), grid, dim3(kThreads), 0, st, M, N, per, dz, (float *)ws);
+  else hipLaunchKernelGGL((colsum_kernel<DT_F32>), grid, dim3(kThreads), 0, st, M, N, per, dz, (float *)ws);
+  if ((r = hipGetLastError()) != hipSuccess) return r;
+  return launch_sum_rows((const float *)ws, db, slices, N, st);
+}
+
+}  // namespace cf
