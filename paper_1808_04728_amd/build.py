@@ -38,6 +38,7 @@ EXTRA = {
     "conv_smallc4.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "conv_f32.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "conv_f32_wgrad.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "linear_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "muon.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "muon_skinny.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
 }

@@ -9,40 +9,12 @@
 // not: forward has A by rows of l and B by columns, backward data both by rows of l,
 // backward weights neither.
 
-#include <algorithm>
-
-#include "activation.h"
-#include "cf_common.h"
-#include "cf_kernels.h"
+#include "linear.h"
 
 namespace cf {
 namespace {
 
 constexpr int kThreads = 256;
-
-// Which operand has the sum's axis innermost.
-enum : int { FORM_FWD = 0, FORM_DATA = 1, FORM_WEIGHT = 2 };
-template <int FORM> struct Form;
-template <> struct Form<FORM_FWD> { static constexpr bool AK = true, BK = false; };
-template <> struct Form<FORM_DATA> { static constexpr bool AK = true, BK = true; };
-template <> struct Form<FORM_WEIGHT> { static constexpr bool AK = false, BK = false; };
-
-// The product's sizes: C [M][N], the sum over L.
-struct Sizes {
-  long long M, L;
-  int N;
-  int tn;           // tiles along N
-  long long tiles;  // of the output
-  int slices;       // of the sum: each a part of the launch, joined by a second one
-  long long per;    // terms of a slice
-};
-
-// A grid's x dimension holds fewer than 2^32 threads: tiles past 2^22 go on in y.
-dim3 tile_grid(long long tiles) {
-  const long long x = std::min(tiles, 1LL << 22);
-  return dim3((unsigned)x, (unsigned)((tiles + x - 1) / x));
-}
-__device__ __forceinline__ long long tile_index() { return (long long)blockIdx.y * gridDim.x + blockIdx.x; }
 
 // one value of the output, C[i][j] = v
 template <int DT, int FORM, int ACT>
@@ -67,13 +39,13 @@ __device__ __forceinline__ void put(const LinearEpilogue &E, void *out, long lon
 // Any sizes and alignment: tiles of 64 x 64, four waves of 32 x 32, both factors element by
 // element into LDS with the sum's axis innermost.
 template <int DT, int FORM, int ACT>
-__global__ __launch_bounds__(kThreads) void any_kernel(Sizes S, const void *A_, const void *B_, LinearEpilogue E, void *out,
+__global__ __launch_bounds__(kThreads) void any_kernel(LinearPlan S, const void *A_, const void *B_, LinearEpilogue E, void *out,
                                                        float *part) {
   typedef typename Store<DT>::T T;
   constexpr int TB = 64, KS = DT == DT_BF16 ? 32 : 16, LD = KS + (DT == DT_BF16 ? 8 : 4);
   __shared__ __attribute__((aligned(16))) T la[TB * LD], lb[TB * LD];
   const T *A = (const T *)A_, *B = (const T *)B_;
-  const long long index = tile_index(), tile = index % S.tiles, slice = index / S.tiles;
+  const long long index = long_index(), tiles = (long long)S.tm * S.tn, tile = index % tiles, slice = index / tiles;
   if (slice >= S.slices) return;
   const long long i0 = tile / S.tn * TB;
   const int j0 = (int)(tile % S.tn) * TB;
@@ -147,7 +119,7 @@ __global__ __launch_bounds__(kThreads) void any_kernel(Sizes S, const void *A_, 
 template <int DT, int FORM, int ACT>
 __global__ __launch_bounds__(kThreads) void join_kernel(long long M, int N, int slices, const float *part, LinearEpilogue E,
                                                         void *out) {
-  const long long n = M * N, at = tile_index() * kThreads + threadIdx.x;
+  const long long n = M * N, at = long_index() * kThreads + threadIdx.x;
   if (at >= n) return;
   float v = part[at];
   for (int s = 1; s < slices; ++s) v += part[s * n + at];
@@ -176,9 +148,6 @@ int colsum_slices(long long M, int N) {
   return (int)std::max(1LL, std::min((M + 63) / 64, 1024 / tiles));
 }
 
-constexpr int kCUs = 256;
-constexpr long long kChain = 65536;  // most terms of one fp32 sum, where the partial sums' size allows
-
 // Slices of the sum: where the output's tiles leave compute units idle, as many as fill
 // them twice (each of at least 256 terms), and none of more than kChain terms while the
 // partial sums stay below 2^28 values.
@@ -188,44 +157,52 @@ int slices_of(long long M, int N, long long L) {
   const long long chain = std::min((L + kChain - 1) / kChain, (1LL << 28) / out);
   return (int)std::max(1LL, std::max(fill, chain));
 }
-size_t slices_bytes(long long M, int N, long long L) {
-  const int s = slices_of(M, N, L);
-  return s > 1 ? ((size_t)s * M * N * 4 + 15) / 16 * 16 : 0;
+// form, and the output's rows and columns and the sum's terms
+LinearPlan plan_of(int form, long long M, int N, long long L, int dtype) {
+  LinearPlan p;
+  if (dtype == DT_BF16 && linear_bf16_plan(form, M, N, L, &p)) return p;
+  const int slices = slices_of(M, N, L);
+  const long long per = ((L + slices - 1) / slices + 31) / 32 * 32;
+  return LinearPlan{M, L, N, LIN_ANY, (int)((M + 63) / 64), (N + 63) / 64, (int)((L + per - 1) / per), per};
+}
+size_t slices_bytes(const LinearPlan &p) {
+  return p.slices > 1 ? ((size_t)p.slices * p.M * p.N * 4 + 15) / 16 * 16 : 0;
 }
 
 template <int FORM>
 hipError_t product(long long M, int N, long long L, int dtype, const void *A, const void *B, const LinearEpilogue &E, void *out,
                    void *ws, hipStream_t st) {
-  const int tn = (N + 63) / 64, slices = slices_of(M, N, L);
-  const long long per = ((L + slices - 1) / slices + 31) / 32 * 32;
-  const Sizes S{M, L, N, tn, (M + 63) / 64 * tn, slices, per};
-  const dim3 grid = tile_grid(S.tiles * slices), block(kThreads);
+  const LinearPlan p = plan_of(FORM, M, N, L, dtype);
   float *part = (float *)ws;
+  if (p.kernel != LIN_ANY) return launch_linear_bf16(FORM, p, A, B, E, out, part, st);
+  const dim3 grid = long_grid((long long)p.tm * p.tn * p.slices), block(kThreads);
   with_act(E.act, [&](auto a) {
     constexpr int ACT = FORM == FORM_WEIGHT ? (int)ACT_NONE : decltype(a)::value;
-    if (dtype == DT_BF16) hipLaunchKernelGGL((any_kernel<DT_BF16, FORM, ACT>), grid, block, 0, st, S, A, B, E, out, part);
-    else hipLaunchKernelGGL((any_kernel<DT_F32, FORM, ACT>), grid, block, 0, st, S, A, B, E, out, part);
-    if (slices > 1 && FORM != FORM_WEIGHT) {
-      const dim3 all = tile_grid((M * N + kThreads - 1) / kThreads);
+    if (dtype == DT_BF16) hipLaunchKernelGGL((any_kernel<DT_BF16, FORM, ACT>), grid, block, 0, st, p, A, B, E, out, part);
+    else hipLaunchKernelGGL((any_kernel<DT_F32, FORM, ACT>), grid, block, 0, st, p, A, B, E, out, part);
+    if (p.slices > 1 && FORM != FORM_WEIGHT) {
+      const dim3 all = long_grid((M * N + kThreads - 1) / kThreads);
       if (dtype == DT_BF16)
-        hipLaunchKernelGGL((join_kernel<DT_BF16, FORM, ACT>), all, block, 0, st, M, N, slices, (const float *)part, E, out);
-      else hipLaunchKernelGGL((join_kernel<DT_F32, FORM, ACT>), all, block, 0, st, M, N, slices, (const float *)part, E, out);
+        hipLaunchKernelGGL((join_kernel<DT_BF16, FORM, ACT>), all, block, 0, st, M, N, p.slices, (const float *)part, E, out);
+      else hipLaunchKernelGGL((join_kernel<DT_F32, FORM, ACT>), all, block, 0, st, M, N, p.slices, (const float *)part, E, out);
     }
   });
   const hipError_t r = hipGetLastError();
-  if (r != hipSuccess || slices == 1 || FORM != FORM_WEIGHT) return r;
+  if (r != hipSuccess || p.slices == 1 || FORM != FORM_WEIGHT) return r;
   // (slices of more than one have fewer than 2^28 values in all, or fill 512 tiles of 4096)
-  return launch_sum_rows(part, (float *)out, slices, (int)(M * N), st);
+  return launch_sum_rows(part, (float *)out, p.slices, (int)(M * N), st);
 }
 
 }  // namespace
 
-size_t linear_fwd_workspace(long long M, int K, int N, int) { return slices_bytes(M, N, K); }
-size_t linear_bwd_data_workspace(long long M, int K, int N, int) { return slices_bytes(M, K, N); }
+size_t linear_fwd_workspace(long long M, int K, int N, int dtype) { return slices_bytes(plan_of(FORM_FWD, M, N, K, dtype)); }
+size_t linear_bwd_data_workspace(long long M, int K, int N, int dtype) {
+  return slices_bytes(plan_of(FORM_DATA, M, K, N, dtype));
+}
 // (the column sums come after the product, in the same place)
-size_t linear_bwd_weight_workspace(long long M, int K, int N, int) {
+size_t linear_bwd_weight_workspace(long long M, int K, int N, int dtype) {
   const size_t sums = ((size_t)colsum_slices(M, N) * N * 4 + 15) / 16 * 16;
-  return std::max(sums, slices_bytes(K, N, M));
+  return std::max(sums, slices_bytes(plan_of(FORM_WEIGHT, K, N, M, dtype)));
 }
 
 hipError_t launch_linear_fwd(long long M, int K, int N, int dtype, const void *x, const void *w, const LinearEpilogue &e,

@@ -1,0 +1,471 @@
+// linear_bf16.hip -- bf16 matrix products on tiles of up to 256 x 256 (gfx950).
+//
+// C[i][j] = sum_l A(i, l) B(l, j).  A workgroup's step brings BK terms of its tile's rows of
+// both factors into LDS, 16 bytes a lane straight from memory (buffer loads to LDS, whose
+// range check gives zeros past a tensor's end).  A factor with the sum's axis innermost lies
+// there by rows of BK terms and is read 8 terms a lane; one with the sum's axis outermost
+// lies as it is in memory, by terms, 64 columns a line, and is read with the transposing
+// loads.  Both orders are swizzled so that the reads of a fragment touch all banks.
+//
+// The matrix instructions take B's columns as their rows: a lane's four results are then
+// four neighbours of a row of C, and exchanging registers between the four lanes of a row
+// leaves each with sixteen, so the epilogue reads and writes 16 bytes a lane.
+
+#include "linear.h"
+
+namespace cf {
+namespace {
+
+typedef short v4i16_t __attribute__((ext_vector_type(4)));
+typedef short v8i16_t __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) v4i16_t lds_v4i16_t;
+typedef __attribute__((address_space(3))) void lds_void_t;
+
+// A tile: WM x WN waves of TM x TN instruction tiles of 16 x 16; NS steps of BK terms in LDS.
+// PAIRED: two halves of eight waves take turns at LDS and the matrix units.
+template <int KERNEL> struct Tile;
+template <> struct Tile<LIN_256> {
+  static constexpr int BM = 256, BN = 256, WM = 2, WN = 4, BK = 64, NS = 2;
+  static constexpr bool PAIRED = true;
+};
+template <> struct Tile<LIN_128> {
+  static constexpr int BM = 128, BN = 128, WM = 2, WN = 2, BK = 32, NS = 4;
+  static constexpr bool PAIRED = false;
+};
+template <> struct Tile<LIN_64> {
+  static constexpr int BM = 64, BN = 64, WM = 4, WN = 1, BK = 64, NS = 3;
+  static constexpr bool PAIRED = false;
+};
+
+constexpr uint32_t kOut = 0x80000000u;  // past every buffer: the load gives zeros
+
+// The rows r0 .. r0 + ROWS - 1 of a factor, a step of BK terms at a time.  KC: the sum's axis
+// is innermost.
+template <bool KC, int ROWS, int BK, int NT> struct Loader {
+  static constexpr int BYTES = ROWS * BK * 2, N = BYTES / 16 / NT;
+  static_assert(BYTES % (16 * NT) == 0, "whole loads");
+  const char *base;
+  long long left;     // bytes from base to the factor's end
+  long long advance;  // bytes of a step
+  uint32_t off[N];
+  int term[N];  // KC: the first term of the lane's piece
+  __device__ __forceinline__ Loader(const uint16_t *p, long long rows, long long terms, int r0, long long k0) {
+    const long long ld = KC ? terms : rows;
+    const long long at = KC ? r0 * ld + k0 : k0 * ld + r0;
+    base = (const char *)(p + at);
+    left = (rows * terms - at) * 2;
+    advance = KC ? BK * 2 : BK * ld * 2;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int id = i * NT + threadIdx.x;
+      if constexpr (KC) {
+        const int row = id / (BK / 8), piece = id % (BK / 8);
+        const int c = piece ^ (BK == 64 ? (row >> 1) & 7 : (row >> 2) & 3);
+        off[i] = (uint32_t)(row * (ld * 2)) + c * 16;
+        term[i] = c * 8;
+      } else {
+        const int sub = id / (BK * 8), row = id / 8 % BK, piece = id & 7;
+        const int c = ((piece >> 1) ^ (((row >> 1) & 1) | (((row >> 3) & 1) << 1))) * 2 + (piece & 1);
+        off[i] = (uint32_t)(row * (ld * 2)) + sub * 128 + c * 16;
+        term[i] = 0;
+      }
+    }
+  }
+  // the next step's `terms` (BK or, at the sum's end, fewer) into the stage
+  __device__ __forceinline__ void issue(unsigned char *stage, long long terms) {
+    const uint32_t records = (uint32_t)max(0LL, min(left, 0x7ffffff0LL));
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void *)base, (short)0, records, 0x00020000);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      uint32_t o = off[i];
+      if constexpr (KC) {
+        if (terms < BK) o = term[i] < terms ? o : kOut;
+        asm volatile("" : "+v"(o));  // a select, not two predicated copies of the load
+      }
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t *)(stage + (i * NT + wave * 64) * 16), 16, o, 0, 0, 0);
+    }
+    base += advance;
+    left -= advance;
+  }
+};
+
+// A lane's place in the fragments of 16 rows and 32 terms.
+template <bool KC, int BK> struct Reader {
+  int lane_off, swz;
+  __device__ __forceinline__ Reader() {
+    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    if constexpr (KC) {
+      lane_off = r * BK * 2;
+      swz = BK == 64 ? (r >> 1) & 7 : (r >> 2) & 3;
+    } else {
+      lane_off = (8 * g + (r >> 2)) * 128 + (r & 3) * 8;
+      swz = ((r >> 3) & 1) | ((g & 1) << 1);
+    }
+  }
+  // rows 16 t .. of the stage, terms 32 k ..
+  __device__ __forceinline__ bf16x8_t frag(const unsigned char *stage, int t, int k) const {
+    if constexpr (KC) {
+      const int g = (threadIdx.x & 63) >> 4;
+      return *reinterpret_cast<const bf16x8_t *>(stage + lane_off + t * 16 * BK * 2 + (((4 * k + g) ^ swz) << 4));
+    } else {
+      const unsigned char *p = stage + (t >> 2) * (BK * 128) + k * 32 * 128 + lane_off + (((t & 3) ^ swz) << 5);
+      const v4i16_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t *)p);
+      const v4i16_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t *)(p + 512));
+      const v8i16_t v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      return __builtin_bit_cast(bf16x8_t, v);
+    }
+  }
+};
+
+// waits until at most N of the wave's loads are in flight
+template <int N> __device__ __forceinline__ void wait_loads() {
+  __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | ((N >> 4) << 14));
+}
+__device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xc07f); }  // lgkmcnt(0)
+__device__ __forceinline__ void barrier() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_barrier" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+template <int N> struct Stage {
+  static constexpr int v = N;
+};
+
+// Four registers of four lanes (those 16 apart) transposed: register k of lane g gets
+// register g of lane k.
+__device__ __forceinline__ void transpose4(float &a, float &b, float &c, float &d) {
+  auto swap32 = [](float &x, float &y) {
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+    x = __uint_as_float(s[0]);
+    y = __uint_as_float(s[1]);
+  };
+  auto swap16 = [](float &x, float &y) {
+    const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+    x = __uint_as_float(s[0]);
+    y = __uint_as_float(s[1]);
+  };
+  swap32(a, c);
+  swap32(b, d);
+  swap16(a, b);
+  swap16(c, d);
+}
+
+// eight bf16 of a row, of which k exist (a multiple of 8 or none)
+__device__ __forceinline__ void load8(const uint16_t *p, float (&x)[8]) {
+  const u32x4_t a = *reinterpret_cast<const u32x4_t *>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(a[i] << 16);
+    x[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void store8(uint16_t *p, const float (&x)[8]) { *reinterpret_cast<u32x4_t *>(p) = pack_bf16x8(x); }
+__device__ __forceinline__ void store8(float *p, const float (&x)[8]) {
+  reinterpret_cast<float4 *>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+  reinterpret_cast<float4 *>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+}
+
+// eight neighbouring outputs
+template <int FORM, int ACT>
+__device__ __forceinline__ void put8(const LinearEpilogue &E, const float (&bias)[8], void *out, long long at, float (&v)[8]) {
+  if constexpr (FORM == FORM_WEIGHT) {
+    store8((float *)out + at, v);
+  } else if constexpr (FORM == FORM_FWD) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] += bias[q];
+    if (E.z) store8((uint16_t *)E.z + at, v);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = act<ACT>(v[q], E.alpha);
+    if (E.residual) {
+      float r[8];
+      load8((const uint16_t *)E.residual + at, r);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] += r[q];
+    }
+    store8((uint16_t *)out + at, v);
+  } else {
+    float r[8];
+    if (E.residual) {
+      load8((const uint16_t *)E.residual + at, r);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] += r[q];
+    }
+    if constexpr (ACT != ACT_NONE) {
+      load8((const uint16_t *)E.zin + at, r);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] *= act_slope<ACT>(r[q], E.alpha);
+    }
+    store8((uint16_t *)out + at, v);
+  }
+}
+
+template <int FORM>
+__device__ __forceinline__ void load_bias(const LinearEpilogue &E, int j, int N, float (&b)[8]) {
+#pragma unroll
+  for (int q = 0; q < 8; ++q) b[q] = 0.f;
+  if (FORM == FORM_FWD && E.bias && j < N) {
+    const float4 u = *reinterpret_cast<const float4 *>(E.bias + j), v = *reinterpret_cast<const float4 *>(E.bias + j + 4);
+    b[0] = u.x; b[1] = u.y; b[2] = u.z; b[3] = u.w;
+    b[4] = v.x; b[5] = v.y; b[6] = v.z; b[7] = v.w;
+  }
+}
+
+template <class C> constexpr int threads_of() { return 64 * C::WM * C::WN; }
+
+template <int KERNEL, int FORM, int ACT>
+__global__ __launch_bounds__(threads_of<Tile<KERNEL>>(), Tile<KERNEL>::PAIRED ? 2 : 1) void product_kernel(
+    LinearPlan p, long long per_xcd, const uint16_t *A, const uint16_t *B, LinearEpilogue E, void *out, float *part) {
+  using C = Tile<KERNEL>;
+  constexpr int NT = threads_of<C>(), TM = C::BM / C::WM / 16, TN = C::BN / C::WN / 16, KK = C::BK / 32;
+  static_assert(TN == 4, "a lane's row of the epilogue is sixteen columns");
+  constexpr int AB = C::BM * C::BK * 2, BB = C::BN * C::BK * 2;
+  // every stage in arrays of its own: the compiler then knows which loads a read waits for
+  __shared__ __attribute__((aligned(16))) unsigned char a0[AB], b0[BB], a1[AB], b1[BB];
+  __shared__ __attribute__((aligned(16))) unsigned char a2[C::NS > 2 ? AB : 16], b2[C::NS > 2 ? BB : 16];
+  __shared__ __attribute__((aligned(16))) unsigned char a3[C::NS > 3 ? AB : 16], b3[C::NS > 3 ? BB : 16];
+
+  // the workgroups of an XCD (every eighth) take neighbouring tiles, eight tiles down before
+  // one across: 32 at a time read 8 + 4 tiles' factors through its L2
+  const long long index = long_index(), job = (index & 7) * per_xcd + (index >> 3);
+  const long long tiles = (long long)p.tm * p.tn;
+  if (job >= tiles * p.slices) return;
+  const long long slice = job / tiles;
+  const int t = (int)(job % tiles), group = t / (8 * p.tn), in = t % (8 * p.tn), high = min(8, p.tm - 8 * group);
+  const int ti = 8 * group + in % high, tj = in / high;
+  const int j0 = tj * C::BN;
+  const int i0 = ti * C::BM;
+  const long long k0 = slice * p.per, k1 = min(k0 + p.per, p.L);
+  const int steps = k1 > k0 ? (int)((k1 - k0 + C::BK - 1) / C::BK) : 0;
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / C::WN, wn = wave % C::WN;
+  Loader<Form<FORM>::AK, C::BM, C::BK, NT> la(A, p.M, p.L, i0, k0);
+  Loader<Form<FORM>::BK, C::BN, C::BK, NT> lb(B, p.N, p.L, j0, k0);
+  const Reader<Form<FORM>::AK, C::BK> ra;
+  const Reader<Form<FORM>::BK, C::BK> rb;
+  constexpr int LOADS = decltype(la)::N + decltype(lb)::N;
+  auto stage_a = [&](auto s) -> unsigned char * {
+    constexpr int S = decltype(s)::v;
+    if constexpr (S == 0) return a0;
+    else if constexpr (S == 1) return a1;
+    else if constexpr (S == 2) return a2;
+    else return a3;
+  };
+  auto stage_b = [&](auto s) -> unsigned char * {
+    constexpr int S = decltype(s)::v;
+    if constexpr (S == 0) return b0;
+    else if constexpr (S == 1) return b1;
+    else if constexpr (S == 2) return b2;
+    else return b3;
+  };
+  long long rest = p.L - k0;  // terms from the next step to load on
+  auto issue = [&](auto s) {
+    la.issue(stage_a(s), rest);
+    lb.issue(stage_b(s), rest);
+    rest -= C::BK;
+  };
+
+  f32x4_t acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+
+  if constexpr (C::PAIRED) {
+    static_assert(NT == 512 && C::NS == 2, "two waves a SIMD, two stages");
+    // Two halves of the waves, the later one a phase behind: while the matrix instructions
+    // of one run, the fragments of the other come from LDS.  A barrier ends every phase.
+    // (Waves w and w + 4 share a SIMD.)
+    const bool late = wave >= 4;
+    if (steps > 0) {
+      issue(Stage<0>{});
+      wait_loads<0>();
+    }
+    barrier();
+    if (late) barrier();
+    auto step = [&](auto st, int s) {
+      constexpr int S = decltype(st)::v;
+      // every wave has read all of the other stage: the reads of both halves were over
+      // before the last barrier
+      if (s + 1 < steps) issue(Stage<1 - S>{});
+#pragma unroll
+      for (int k = 0; k < KK; ++k) {
+        bf16x8_t fb[TN], fa[TM];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) fb[j] = rb.frag(stage_b(st), wn * TN + j, k);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) fa[i] = ra.frag(stage_a(st), wm * TM + i, k);
+        wait_lds();
+        if (k == KK - 1) wait_loads<0>();  // the next step's, before its first reader's barrier
+        barrier();
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
+        __builtin_amdgcn_s_setprio(0);
+        barrier();
+      }
+    };
+    for (int s = 0; s < steps; s += 2) {
+      step(Stage<0>{}, s);
+      if (s + 1 < steps) step(Stage<1>{}, s + 1);
+    }
+    if (!late) barrier();
+  } else {
+    // NS - 1 steps ahead; a step waits for its own loads, and its barrier also ends the
+    // reads of the stage that the next loads overwrite
+    constexpr int AHEAD = C::NS - 1;
+    auto first = [&](auto st) {
+      if (decltype(st)::v < steps) issue(st);
+    };
+    first(Stage<0>{});
+    first(Stage<1>{});
+    if constexpr (AHEAD > 2) first(Stage<2>{});
+    auto step = [&](auto st, int s) {
+      constexpr int S = decltype(st)::v;
+      if (s + AHEAD <= steps) wait_loads<(AHEAD - 1) * LOADS>();
+      else wait_loads<0>();
+      wait_lds();
+      barrier();
+      if (s + AHEAD < steps) issue(Stage<(S + AHEAD) % C::NS>{});
+#pragma unroll
+      for (int k = 0; k < KK; ++k) {
+        bf16x8_t fb[TN], fa[TM];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) fb[j] = rb.frag(stage_b(st), wn * TN + j, k);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) fa[i] = ra.frag(stage_a(st), wm * TM + i, k);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
+      }
+    };
+    for (int s = 0; s < steps; s += C::NS) {
+      step(Stage<0>{}, s);
+      if (s + 1 < steps) step(Stage<1>{}, s + 1);
+      if (s + 2 < steps) step(Stage<2>{}, s + 2);
+      if constexpr (C::NS > 3) {
+        if (s + 3 < steps) step(Stage<3>{}, s + 3);
+      }
+    }
+  }
+
+  // lane (r, g) gets row r of each instruction tile, columns 16 g .. 16 g + 15 of the wave's 64
+  const int r = lane & 15, g = lane >> 4;
+  const int j = j0 + wn * 64 + 16 * g;
+  float bias[2][8];
+  load_bias<FORM>(E, j, p.N, bias[0]);
+  load_bias<FORM>(E, j + 8, p.N, bias[1]);
+  const bool whole = p.slices == 1;
+  const float none[8] = {};
+#pragma unroll
+  for (int ii = 0; ii < TM; ++ii) {
+    float row[16];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) row[4 * k + e] = acc[ii][k][e];
+      transpose4(row[e], row[4 + e], row[8 + e], row[12 + e]);
+    }
+    const long long i = (long long)i0 + (wm * TM + ii) * 16 + r;
+    if (i >= p.M) continue;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (j + 8 * h >= p.N) continue;
+      float v[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] = row[8 * h + q];
+      if (whole) put8<FORM, ACT>(E, bias[h], out, i * p.N + j + 8 * h, v);
+      else put8<FORM_WEIGHT, ACT_NONE>(E, none, part, (slice * p.M + i) * p.N + j + 8 * h, v);
+    }
+  }
+}
+
+// the slices' sum, in slice order, and the epilogue; eight outputs a thread
+template <int FORM, int ACT>
+__global__ __launch_bounds__(256) void join8_kernel(LinearPlan p, const float *part, LinearEpilogue E, void *out) {
+  const long long n = p.M * p.N, at = (long_index() * 256 + threadIdx.x) * 8;
+  if (at >= n) return;
+  float v[8];
+  for (int s = 0; s < p.slices; ++s) {
+    const float4 a = *reinterpret_cast<const float4 *>(part + s * n + at), b = *reinterpret_cast<const float4 *>(part + s * n + at + 4);
+    const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = s ? v[q] + x[q] : x[q];
+  }
+  float bias[8];
+  load_bias<FORM>(E, (int)(at % p.N), p.N, bias);
+  put8<FORM, ACT>(E, bias, out, at, v);
+}
+
+struct Cost {
+  int kernel, bm, bn, bk;
+  double fixed, step;  // us of a tile, and of 64 terms of it
+};
+constexpr Cost kCost[] = {{LIN_256, 256, 256, 64, 8.0, 0.90}, {LIN_128, 128, 128, 32, 5.0, 0.50}, {LIN_64, 64, 64, 64, 3.0, 0.25}};
+
+}  // namespace
+
+bool linear_bf16_plan(int form, long long M, int N, long long L, LinearPlan *p) {
+  // rows of whole 16-byte pieces, and 32-bit offsets inside a tile's rows
+  const long long la = form == FORM_WEIGHT ? M : L, lb = form == FORM_DATA ? L : N;
+  if (la % 8 || lb % 8 || N % 8 || la >= (1LL << 22) || lb >= (1LL << 22)) return false;
+  if (M >= (1LL << 31) - 256) return false;
+  double best = 1e30;
+  for (const Cost &c : kCost) {
+    const long long tm = (M + c.bm - 1) / c.bm, tn = (N + c.bn - 1) / c.bn, tiles = tm * tn, steps = (L + 63) / 64;
+    const long long chain = std::max(1LL, std::min((L + kChain - 1) / kChain, (1LL << 28) / (M * N)));
+    for (long long s = 1; s <= 64; s = s < 4 ? s + 1 : s * 2) {
+      const long long slices = std::max(s, chain);
+      if (s > 1 && (steps / s < 4 || slices * M * N > (1LL << 28) || tiles * s > 4 * kCUs)) break;
+      const long long jobs = tiles * slices, rounds = (jobs + kCUs - 1) / kCUs;
+      double t = rounds * (c.fixed + c.step * ((steps + slices - 1) / slices));
+      if (slices > 1) t += 3.0 + slices * (double)M * N * 8 / 4e6;
+      if (t < best) {
+        best = t;
+        const long long per = ((L + slices - 1) / slices + 63) / 64 * 64;
+        *p = LinearPlan{M, L, N, c.kernel, (int)tm, (int)tn, (int)((L + per - 1) / per), per};
+      }
+    }
+  }
+  return true;
+}
+
+namespace {
+template <int FORM>
+hipError_t launch_form(const LinearPlan &p, const uint16_t *A, const uint16_t *B, const LinearEpilogue &E, void *out, float *part,
+                       hipStream_t st) {
+  const long long per_xcd = ((long long)p.tm * p.tn * p.slices + 7) / 8;
+  with_act(E.act, [&](auto a) {
+    constexpr int ACT = FORM == FORM_WEIGHT ? (int)ACT_NONE : decltype(a)::value;
+    auto run = [&](auto k) {
+      constexpr int KERNEL = decltype(k)::value;
+      hipLaunchKernelGGL((product_kernel<KERNEL, FORM, ACT>), long_grid(8 * per_xcd), dim3(threads_of<Tile<KERNEL>>()), 0, st, p,
+                         per_xcd, A, B, E, out, part);
+    };
+    if (p.kernel == LIN_256) run(std::integral_constant<int, LIN_256>{});
+    else if (p.kernel == LIN_128) run(std::integral_constant<int, LIN_128>{});
+    else run(std::integral_constant<int, LIN_64>{});
+    if (p.slices > 1 && FORM != FORM_WEIGHT)
+      hipLaunchKernelGGL((join8_kernel<FORM, ACT>), long_grid((p.M * p.N / 8 + 255) / 256), dim3(256), 0, st, p,
+                         (const float *)part, E, out);
+  });
+  const hipError_t r = hipGetLastError();
+  if (r != hipSuccess || p.slices == 1 || FORM != FORM_WEIGHT) return r;
+  return launch_sum_rows(part, (float *)out, p.slices, (int)(p.M * p.N), st);
+}
+}  // namespace
+
+hipError_t launch_linear_bf16(int form, const LinearPlan &p, const void *A, const void *B, const LinearEpilogue &E, void *out,
+                              float *part, hipStream_t st) {
+  const uint16_t *a = (const uint16_t *)A, *b = (const uint16_t *)B;
+  if (form == FORM_FWD) return launch_form<FORM_FWD>(p, a, b, E, out, part, st);
+  if (form == FORM_DATA) return launch_form<FORM_DATA>(p, a, b, E, out, part, st);
+  return launch_form<FORM_WEIGHT>(p, a, b, E, out, part, st);
+}
+
+}  // namespace cf

@@ -23,7 +23,7 @@ ACTS = ["none", "lrelu", "silu", "gelu"]
 SHAPES = [(1, 1, 1), (1, 7, 3), (3, 1, 5), (5, 8, 1), (64, 128, 512), (63, 65, 67), (64, 64, 64), (65, 32, 129), (128, 256, 128),
           (257, 100, 255), (256, 512, 256), (1, 4096, 1000), (1000, 3, 1000), (33, 1000, 8), (300, 520, 260), (129, 2048, 64),
           (1331, 130, 517), (512, 192, 1024), (2048, 64, 72), (96, 4104, 40), (7, 16, 8192), (4100, 40, 24), (40, 24, 4100),
-          (16384, 16, 16), (20000, 5, 3)]
+          (16384, 16, 16), (20000, 5, 3), (4096, 1024, 1024), (4104, 264, 4088), (520, 4200, 4104), (8192, 72, 4096)]
 
 
 def _t(dt):
