@@ -24,11 +24,32 @@ __device__ __forceinline__ float fast_exp(float x) {
 
 __device__ __forceinline__ float sigmoid(float u) { return __builtin_amdgcn_rcpf(1.f + fast_exp(-u)); }
 
+// Phi(-t) e^(t^2 / 2) for t >= 0, Phi the normal distribution function: a polynomial in
+// 1 / (1 + t / 4), fitted to the function so that u Phi(u) is within 2^-21.9 |u| and Phi(u)
+// + u phi(u) within 2^-21.9.  (erff costs three times as much: the epilogue of 32768 x 1024 x
+// 4096 took 113 us with it.)
+__device__ __forceinline__ float normal_tail(float t) {
+  const float s = __builtin_amdgcn_rcpf(__builtin_fmaf(0.25f, t, 1.f));
+  float q = -0.0978302136f;
+  q = __builtin_fmaf(q, s, 0.371543974f);
+  q = __builtin_fmaf(q, s, -0.327021211f);
+  q = __builtin_fmaf(q, s, 0.346005082f);
+  q = __builtin_fmaf(q, s, -0.0157256275f);
+  q = __builtin_fmaf(q, s, 0.126760602f);
+  q = __builtin_fmaf(q, s, 0.0960564613f);
+  return __builtin_fmaf(q, s, 0.000210965038f);
+}
+// e^(-u^2 / 2)
+__device__ __forceinline__ float bell(float u) { return __builtin_amdgcn_exp2f(u * u * -0.721347520f); }
+
 // act(u)
 template <int ACT> __device__ __forceinline__ float act(float u, float alpha) {
   if constexpr (ACT == ACT_LRELU) return u > 0.f ? u : alpha * u;
   if constexpr (ACT == ACT_SILU) return u * sigmoid(u);
-  if constexpr (ACT == ACT_GELU) return 0.5f * u * (1.f + erff(u * 0.707106781f));
+  if constexpr (ACT == ACT_GELU) {
+    const float q = bell(u) * normal_tail(fabsf(u));
+    return u * (u >= 0.f ? 1.f - q : q);
+  }
   return u;
 }
 
@@ -39,8 +60,10 @@ template <int ACT> __device__ __forceinline__ float act_slope(float u, float alp
     const float s = sigmoid(u);
     return s * (1.f + u * (1.f - s));
   }
-  if constexpr (ACT == ACT_GELU)
-    return 0.5f * (1.f + erff(u * 0.707106781f)) + u * (fast_exp(-0.5f * u * u) * 0.398942280f);
+  if constexpr (ACT == ACT_GELU) {
+    const float e = bell(u), q = e * normal_tail(fabsf(u));
+    return (u >= 0.f ? 1.f - q : q) + u * (e * 0.398942280f);
+  }
   return 1.f;
 }
 

@@ -143,9 +143,52 @@ __global__ __launch_bounds__(kThreads) void colsum_kernel(long long M, int N, lo
     part[s * N + j] = (red[threadIdx.x] + red[threadIdx.x + 64]) + (red[threadIdx.x + 128] + red[threadIdx.x + 192]);
 }
 
-int colsum_slices(long long M, int N) {
-  const long long tiles = (N + 63) / 64;
-  return (int)std::max(1LL, std::min((M + 63) / 64, 1024 / tiles));
+// The same for rows of whole 16-byte pieces: 32 pieces of a row by 8 rows a workgroup, four
+// rows of a thread on their way.
+template <int DT>
+__global__ __launch_bounds__(kThreads) void colsum_vec_kernel(long long M, int N, long long per, const void *dz_, float *part) {
+  constexpr int V = Store<DT>::VEC;
+  __shared__ float red[8][32 * V + 1];
+  const int pieces = N / V, tiles = (pieces + 31) / 32;
+  const long long s = blockIdx.x / tiles;
+  const int q = (int)(blockIdx.x % tiles) * 32 + (threadIdx.x & 31), ph = threadIdx.x >> 5;
+  const typename Store<DT>::T *dz = (const typename Store<DT>::T *)dz_;
+  float a[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) a[i] = 0.f;
+  if (q < pieces) {
+    const long long end = min((s + 1) * per, M);
+    long long i = s * per + ph;
+    for (; i + 24 < end; i += 32) {
+      Vec16<DT> v[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[u].u = ld16<false>(dz + (i + 8 * u) * N + q * V);
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int k = 0; k < V; ++k) a[k] += to_f32<DT>(v[u].e[k]);
+    }
+    for (; i < end; i += 8) {
+      Vec16<DT> v;
+      v.u = ld16<false>(dz + i * N + q * V);
+#pragma unroll
+      for (int k = 0; k < V; ++k) a[k] += to_f32<DT>(v.e[k]);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < V; ++k) red[ph][(threadIdx.x & 31) * V + k] = a[k];
+  __syncthreads();
+  for (int c = threadIdx.x; c < 32 * V; c += kThreads) {
+    const int j = (int)(blockIdx.x % tiles) * 32 * V + c;
+    if (j < N)
+      part[s * N + j] = ((red[0][c] + red[1][c]) + (red[2][c] + red[3][c])) + ((red[4][c] + red[5][c]) + (red[6][c] + red[7][c]));
+  }
+}
+
+bool colsum_vec(int N, int dtype) { return N % (dtype == DT_BF16 ? 8 : 4) == 0; }
+int colsum_tiles(int N, int dtype) { return colsum_vec(N, dtype) ? (N + (dtype == DT_BF16 ? 255 : 127)) / (dtype == DT_BF16 ? 256 : 128) : (N + 63) / 64; }
+int colsum_slices(long long M, int N, int dtype) {
+  return (int)std::max(1LL, std::min<long long>((M + 63) / 64, 1024 / colsum_tiles(N, dtype)));
 }
 
 // Slices of the sum: where the output's tiles leave compute units idle, as many as fill
@@ -201,7 +244,7 @@ size_t linear_bwd_data_workspace(long long M, int K, int N, int dtype) {
 }
 // (the column sums come after the product, in the same place)
 size_t linear_bwd_weight_workspace(long long M, int K, int N, int dtype) {
-  const size_t sums = ((size_t)colsum_slices(M, N) * N * 4 + 15) / 16 * 16;
+  const size_t sums = ((size_t)colsum_slices(M, N, dtype) * N * 4 + 15) / 16 * 16;
   return std::max(sums, slices_bytes(plan_of(FORM_WEIGHT, K, N, M, dtype)));
 }
 
@@ -220,11 +263,17 @@ hipError_t launch_linear_bwd_weight(long long M, int K, int N, int dtype, const 
   const LinearEpilogue none{nullptr, nullptr, nullptr, nullptr, ACT_NONE, 0.f};
   hipError_t r = product<FORM_WEIGHT>(K, N, M, dtype, x, dz, none, dw, ws, st);
   if (r != hipSuccess || !db) return r;
-  const int slices = colsum_slices(M, N);
+  const int slices = colsum_slices(M, N, dtype);
   const long long per = (M + slices - 1) / slices;
-  const dim3 grid((unsigned)((long long)slices * ((N + 63) / 64)));
-  if (dtype == DT_BF16) hipLaunchKernelGGL((colsum_kernel<DT_BF16>), grid, dim3(kThreads), 0, st, M, N, per, dz, (float *)ws);
-  else hipLaunchKernelGGL((colsum_kernel<DT_F32>), grid, dim3(kThreads), 0, st, M, N, per, dz, (float *)ws);
+  const dim3 grid((unsigned)((long long)slices * colsum_tiles(N, dtype))), block(kThreads);
+  float *part = (float *)ws;
+  auto run = [&](auto dt) {
+    constexpr int DT = decltype(dt)::value;
+    if (colsum_vec(N, dtype)) hipLaunchKernelGGL((colsum_vec_kernel<DT>), grid, block, 0, st, M, N, per, dz, part);
+    else hipLaunchKernelGGL((colsum_kernel<DT>), grid, block, 0, st, M, N, per, dz, part);
+  };
+  if (dtype == DT_BF16) run(std::integral_constant<int, DT_BF16>{});
+  else run(std::integral_constant<int, DT_F32>{});
   if ((r = hipGetLastError()) != hipSuccess) return r;
   return launch_sum_rows((const float *)ws, db, slices, N, st);
 }

@@ -21,73 +21,65 @@ typedef short v8i16_t __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) v4i16_t lds_v4i16_t;
 typedef __attribute__((address_space(3))) void lds_void_t;
 
-// A tile: WM x WN waves of TM x TN instruction tiles of 16 x 16; NS steps of BK terms in LDS.
-// PAIRED: two halves of eight waves take turns at LDS and the matrix units.
+// A tile: WM x WN waves of TM x TN instruction tiles of 16 x 16; NS steps of 64 terms in LDS.
 template <int KERNEL> struct Tile;
 template <> struct Tile<LIN_256> {
-  static constexpr int BM = 256, BN = 256, WM = 2, WN = 4, BK = 64, NS = 2;
-  static constexpr bool PAIRED = true;
+  static constexpr int BM = 256, BN = 256, WM = 2, WN = 4, BK = 64, NS = 2, WAVES = 2;
 };
 template <> struct Tile<LIN_128> {
-  static constexpr int BM = 128, BN = 128, WM = 2, WN = 2, BK = 32, NS = 4;
-  static constexpr bool PAIRED = false;
+  static constexpr int BM = 128, BN = 128, WM = 2, WN = 2, BK = 64, NS = 2, WAVES = 2;
 };
 template <> struct Tile<LIN_64> {
-  static constexpr int BM = 64, BN = 64, WM = 4, WN = 1, BK = 64, NS = 3;
-  static constexpr bool PAIRED = false;
+  static constexpr int BM = 64, BN = 64, WM = 4, WN = 1, BK = 64, NS = 3, WAVES = 3;
 };
 
 constexpr uint32_t kOut = 0x80000000u;  // past every buffer: the load gives zeros
 
 // The rows r0 .. r0 + ROWS - 1 of a factor, a step of BK terms at a time.  KC: the sum's axis
-// is innermost.
+// is innermost.  Pieces past the rows' or the sum's end read as zeros: their offset is out of
+// the buffer's range.
 template <bool KC, int ROWS, int BK, int NT> struct Loader {
   static constexpr int BYTES = ROWS * BK * 2, N = BYTES / 16 / NT;
   static_assert(BYTES % (16 * NT) == 0, "whole loads");
+  static_assert(KC ? NT / (BK / 8) % 16 == 0 : NT / 8 % BK == 0 || BK % (NT / 8) == 0, "a lane's pieces share their terms");
+  static constexpr bool SPLIT = !KC && NT / 8 < BK;  // a lane's pieces are of two or more terms
   const char *base;
-  long long left;     // bytes from base to the factor's end
   long long advance;  // bytes of a step
   uint32_t off[N];
-  int term[N];  // KC: the first term of the lane's piece
+  int term;  // the lane's first piece's (first) term of a step
   __device__ __forceinline__ Loader(const uint16_t *p, long long rows, long long terms, int r0, long long k0) {
     const long long ld = KC ? terms : rows;
-    const long long at = KC ? r0 * ld + k0 : k0 * ld + r0;
-    base = (const char *)(p + at);
-    left = (rows * terms - at) * 2;
+    base = (const char *)(p + (KC ? r0 * ld + k0 : k0 * ld + r0));
     advance = KC ? BK * 2 : BK * ld * 2;
+    const long long have = rows - r0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int id = i * NT + threadIdx.x;
       if constexpr (KC) {
         const int row = id / (BK / 8), piece = id % (BK / 8);
         const int c = piece ^ (BK == 64 ? (row >> 1) & 7 : (row >> 2) & 3);
-        off[i] = (uint32_t)(row * (ld * 2)) + c * 16;
-        term[i] = c * 8;
+        off[i] = row < have ? (uint32_t)(row * (ld * 2)) + c * 16 : kOut;
+        if (i == 0) term = c * 8;
       } else {
         const int sub = id / (BK * 8), row = id / 8 % BK, piece = id & 7;
         const int c = ((piece >> 1) ^ (((row >> 1) & 1) | (((row >> 3) & 1) << 1))) * 2 + (piece & 1);
-        off[i] = (uint32_t)(row * (ld * 2)) + sub * 128 + c * 16;
-        term[i] = 0;
+        off[i] = sub * 64 + c * 8 < have ? (uint32_t)(row * (ld * 2)) + sub * 128 + c * 16 : kOut;
+        if (i == 0) term = row;
       }
     }
   }
-  // the next step's `terms` (BK or, at the sum's end, fewer) into the stage
-  __device__ __forceinline__ void issue(unsigned char *stage, long long terms) {
-    const uint32_t records = (uint32_t)max(0LL, min(left, 0x7ffffff0LL));
-    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void *)base, (short)0, records, 0x00020000);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      uint32_t o = off[i];
-      if constexpr (KC) {
-        if (terms < BK) o = term[i] < terms ? o : kOut;
-        asm volatile("" : "+v"(o));  // a select, not two predicated copies of the load
-      }
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t *)(stage + (i * NT + wave * 64) * 16), 16, o, 0, 0, 0);
-    }
-    base += advance;
-    left -= advance;
+  // Load i of the next step to `stage` (bytes from the LDS's start); `rest` terms are left.
+  // Written out because the compiler, which cannot tell the stages apart in the transposing
+  // reads, would wait for every load before each of them; the waits are the kernel's own.
+  __device__ __forceinline__ void load(int i, int wave, uint32_t stage, int rest) const {
+    const uint32_t o = term + (SPLIT ? i * (NT / 8) % BK : 0) < rest ? off[i] : kOut;
+    const u32x4_t r = {(uint32_t)(uintptr_t)base, (uint32_t)((uintptr_t)base >> 32) & 0xffffu, 0x7ffffff0u, 0x00020000u};
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 :
+                 : "s"(stage + (uint32_t)(i * NT + wave * 64) * 16), "v"(o), "s"(r)
+                 : "memory");
   }
+  __device__ __forceinline__ void next() { base += advance; }
 };
 
 // A lane's place in the fragments of 16 rows and 32 terms.
@@ -118,10 +110,8 @@ template <bool KC, int BK> struct Reader {
   }
 };
 
-// waits until at most N of the wave's loads are in flight
-template <int N> __device__ __forceinline__ void wait_loads() {
-  __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | ((N >> 4) << 14));
-}
+// waits until at most N of the wave's loads are in flight, and for its LDS reads
+template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
 __device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xc07f); }  // lgkmcnt(0)
 __device__ __forceinline__ void barrier() {
   __builtin_amdgcn_sched_barrier(0);
@@ -215,16 +205,13 @@ __device__ __forceinline__ void load_bias(const LinearEpilogue &E, int j, int N,
 template <class C> constexpr int threads_of() { return 64 * C::WM * C::WN; }
 
 template <int KERNEL, int FORM, int ACT>
-__global__ __launch_bounds__(threads_of<Tile<KERNEL>>(), Tile<KERNEL>::PAIRED ? 2 : 1) void product_kernel(
+__global__ __launch_bounds__(threads_of<Tile<KERNEL>>(), Tile<KERNEL>::WAVES) void product_kernel(
     LinearPlan p, long long per_xcd, const uint16_t *A, const uint16_t *B, LinearEpilogue E, void *out, float *part) {
   using C = Tile<KERNEL>;
-  constexpr int NT = threads_of<C>(), TM = C::BM / C::WM / 16, TN = C::BN / C::WN / 16, KK = C::BK / 32;
-  static_assert(TN == 4, "a lane's row of the epilogue is sixteen columns");
-  constexpr int AB = C::BM * C::BK * 2, BB = C::BN * C::BK * 2;
-  // every stage in arrays of its own: the compiler then knows which loads a read waits for
-  __shared__ __attribute__((aligned(16))) unsigned char a0[AB], b0[BB], a1[AB], b1[BB];
-  __shared__ __attribute__((aligned(16))) unsigned char a2[C::NS > 2 ? AB : 16], b2[C::NS > 2 ? BB : 16];
-  __shared__ __attribute__((aligned(16))) unsigned char a3[C::NS > 3 ? AB : 16], b3[C::NS > 3 ? BB : 16];
+  constexpr int NT = threads_of<C>(), BK = C::BK, KK = BK / 32, TM = C::BM / C::WM / 16, TN = C::BN / C::WN / 16;
+  static_assert(TN % 4 == 0, "a lane's row of the epilogue is sixteen columns of 64");
+  constexpr int AB = C::BM * BK * 2, STAGE = AB + C::BN * BK * 2;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[C::NS * STAGE];
 
   // the workgroups of an XCD (every eighth) take neighbouring tiles, eight tiles down before
   // one across: 32 at a time read 8 + 4 tiles' factors through its L2
@@ -237,34 +224,26 @@ __global__ __launch_bounds__(threads_of<Tile<KERNEL>>(), Tile<KERNEL>::PAIRED ? 
   const int j0 = tj * C::BN;
   const int i0 = ti * C::BM;
   const long long k0 = slice * p.per, k1 = min(k0 + p.per, p.L);
-  const int steps = k1 > k0 ? (int)((k1 - k0 + C::BK - 1) / C::BK) : 0;
+  const int steps = k1 > k0 ? (int)((k1 - k0 + BK - 1) / BK) : 0;
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / C::WN, wn = wave % C::WN;
-  Loader<Form<FORM>::AK, C::BM, C::BK, NT> la(A, p.M, p.L, i0, k0);
-  Loader<Form<FORM>::BK, C::BN, C::BK, NT> lb(B, p.N, p.L, j0, k0);
-  const Reader<Form<FORM>::AK, C::BK> ra;
-  const Reader<Form<FORM>::BK, C::BK> rb;
+  Loader<Form<FORM>::AK, C::BM, BK, NT> la(A, p.M, p.L, i0, k0);
+  Loader<Form<FORM>::BK, C::BN, BK, NT> lb(B, p.N, p.L, j0, k0);
+  const Reader<Form<FORM>::AK, BK> ra;
+  const Reader<Form<FORM>::BK, BK> rb;
   constexpr int LOADS = decltype(la)::N + decltype(lb)::N;
-  auto stage_a = [&](auto s) -> unsigned char * {
-    constexpr int S = decltype(s)::v;
-    if constexpr (S == 0) return a0;
-    else if constexpr (S == 1) return a1;
-    else if constexpr (S == 2) return a2;
-    else return a3;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void_t *)lds;
+  int rest = (int)(p.L - k0);  // terms from the next step to load on
+  constexpr int NA = decltype(la)::N;
+  auto load = [&](int q, int stage) {  // load q of the next step
+    if (q < NA) la.load(q, wave, lds0 + stage * STAGE, rest);
+    else lb.load(q - NA, wave, lds0 + stage * STAGE + AB, rest);
   };
-  auto stage_b = [&](auto s) -> unsigned char * {
-    constexpr int S = decltype(s)::v;
-    if constexpr (S == 0) return b0;
-    else if constexpr (S == 1) return b1;
-    else if constexpr (S == 2) return b2;
-    else return b3;
-  };
-  long long rest = p.L - k0;  // terms from the next step to load on
-  auto issue = [&](auto s) {
-    la.issue(stage_a(s), rest);
-    lb.issue(stage_b(s), rest);
-    rest -= C::BK;
+  auto next = [&] {
+    la.next();
+    lb.next();
+    rest -= BK;
   };
 
   f32x4_t acc[TM][TN];
@@ -273,114 +252,89 @@ __global__ __launch_bounds__(threads_of<Tile<KERNEL>>(), Tile<KERNEL>::PAIRED ? 
 #pragma unroll
     for (int j = 0; j < TN; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
-  if constexpr (C::PAIRED) {
-    static_assert(NT == 512 && C::NS == 2, "two waves a SIMD, two stages");
-    // Two halves of the waves, the later one a phase behind: while the matrix instructions
-    // of one run, the fragments of the other come from LDS.  A barrier ends every phase.
-    // (Waves w and w + 4 share a SIMD.)
-    const bool late = wave >= 4;
-    if (steps > 0) {
-      issue(Stage<0>{});
-      wait_loads<0>();
+  // While the matrix instructions of 32 terms run, the fragments of the next 32 come from
+  // LDS; one barrier a step, in front of its last 32 terms: by then every wave has read all
+  // of the step's stage, which the loads of the step NS further overwrite, and has waited for
+  // its own loads of the next.  (Steps past the end load zeros.)
+  bf16x8_t fb[2][TN], fa[2][TM];
+  auto read = [&](int f, int q, const unsigned char *stage, int k) {  // fragment q of the 32 terms k
+    if (q < TN) fb[f][q] = rb.frag(stage + AB, wn * TN + q, k);
+    else fa[f][q - TN] = ra.frag(stage, wm * TM + q - TN, k);
+  };
+  // The matrix instructions of fragments f, the reads of the others and `loads` loads between
+  // them: a load's issue takes its wave sixteen cycles and more, in front of all matrix
+  // instructions a third of their time.
+  constexpr int EARLY = TM > 2 ? TM - 2 : TM;  // the reads are under way this many rows before the end
+  auto half = [&](int f, const unsigned char *rs, int k, auto loads, int ls) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+#pragma unroll
+      for (int q = i * (TM + TN) / EARLY; q < (i + 1) * (TM + TN) / EARLY && q < TM + TN; ++q) read(1 - f, q, rs, k);
+#pragma unroll
+      for (int q = i * decltype(loads)::v / TM; q < (i + 1) * decltype(loads)::v / TM; ++q) load(q, ls);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[f][j], fa[f][i], acc[i][j], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    barrier();
-    if (late) barrier();
-    auto step = [&](auto st, int s) {
-      constexpr int S = decltype(st)::v;
-      // every wave has read all of the other stage: the reads of both halves were over
-      // before the last barrier
-      if (s + 1 < steps) issue(Stage<1 - S>{});
+  };
 #pragma unroll
-      for (int k = 0; k < KK; ++k) {
-        bf16x8_t fb[TN], fa[TM];
+  for (int n = 0; n < C::NS; ++n) {
 #pragma unroll
-        for (int j = 0; j < TN; ++j) fb[j] = rb.frag(stage_b(st), wn * TN + j, k);
-#pragma unroll
-        for (int i = 0; i < TM; ++i) fa[i] = ra.frag(stage_a(st), wm * TM + i, k);
-        wait_lds();
-        if (k == KK - 1) wait_loads<0>();  // the next step's, before its first reader's barrier
-        barrier();
-        __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-          for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
-        __builtin_amdgcn_s_setprio(0);
-        barrier();
-      }
-    };
-    for (int s = 0; s < steps; s += 2) {
-      step(Stage<0>{}, s);
-      if (s + 1 < steps) step(Stage<1>{}, s + 1);
-    }
-    if (!late) barrier();
-  } else {
-    // NS - 1 steps ahead; a step waits for its own loads, and its barrier also ends the
-    // reads of the stage that the next loads overwrite
-    constexpr int AHEAD = C::NS - 1;
-    auto first = [&](auto st) {
-      if (decltype(st)::v < steps) issue(st);
-    };
-    first(Stage<0>{});
-    first(Stage<1>{});
-    if constexpr (AHEAD > 2) first(Stage<2>{});
-    auto step = [&](auto st, int s) {
-      constexpr int S = decltype(st)::v;
-      if (s + AHEAD <= steps) wait_loads<(AHEAD - 1) * LOADS>();
-      else wait_loads<0>();
-      wait_lds();
-      barrier();
-      if (s + AHEAD < steps) issue(Stage<(S + AHEAD) % C::NS>{});
-#pragma unroll
-      for (int k = 0; k < KK; ++k) {
-        bf16x8_t fb[TN], fa[TM];
-#pragma unroll
-        for (int j = 0; j < TN; ++j) fb[j] = rb.frag(stage_b(st), wn * TN + j, k);
-#pragma unroll
-        for (int i = 0; i < TM; ++i) fa[i] = ra.frag(stage_a(st), wm * TM + i, k);
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-          for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
-      }
-    };
-    for (int s = 0; s < steps; s += C::NS) {
-      step(Stage<0>{}, s);
-      if (s + 1 < steps) step(Stage<1>{}, s + 1);
-      if (s + 2 < steps) step(Stage<2>{}, s + 2);
-      if constexpr (C::NS > 3) {
-        if (s + 3 < steps) step(Stage<3>{}, s + 3);
-      }
-    }
+    for (int q = 0; q < LOADS; ++q) load(q, n);
+    next();
   }
+  wait_loads<(C::NS - 1) * LOADS>();
+  barrier();
+#pragma unroll
+  for (int q = 0; q < TM + TN; ++q) read(0, q, lds, 0);
+  int slot = 0;
+  auto step = [&](int first) {  // first: which fragments the step begins with
+    const int after = slot + 1 == C::NS ? 0 : slot + 1;
+    if constexpr (KK == 2) half(first, lds + slot * STAGE, 1, Stage<0>{}, 0);
+    wait_lds();
+    wait_loads<(C::NS - 2) * LOADS>();
+    barrier();
+    half(KK == 2 ? 1 - first : first, lds + after * STAGE, 0, Stage<LOADS>{}, slot);
+    next();
+    slot = after;
+  };
+  for (int s = 0; s < steps; s += 3 - KK) {
+    step(0);
+    if constexpr (KK == 1) step(1);
+  }
+  wait_loads<0>();  // no load outlives the workgroup
 
   // lane (r, g) gets row r of each instruction tile, columns 16 g .. 16 g + 15 of the wave's 64
   const int r = lane & 15, g = lane >> 4;
-  const int j = j0 + wn * 64 + 16 * g;
-  float bias[2][8];
-  load_bias<FORM>(E, j, p.N, bias[0]);
-  load_bias<FORM>(E, j + 8, p.N, bias[1]);
   const bool whole = p.slices == 1;
   const float none[8] = {};
 #pragma unroll
-  for (int ii = 0; ii < TM; ++ii) {
-    float row[16];
+  for (int jj = 0; jj < TN; jj += 4) {
+    const int j = j0 + (wn * TN + jj) * 16 + 16 * g;
+    float bias[2][8];
+    load_bias<FORM>(E, j, p.N, bias[0]);
+    load_bias<FORM>(E, j + 8, p.N, bias[1]);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+    for (int ii = 0; ii < TM; ++ii) {
+      float row[16];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) row[4 * k + e] = acc[ii][k][e];
-      transpose4(row[e], row[4 + e], row[8 + e], row[12 + e]);
-    }
-    const long long i = (long long)i0 + (wm * TM + ii) * 16 + r;
-    if (i >= p.M) continue;
+      for (int e = 0; e < 4; ++e) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if (j + 8 * h >= p.N) continue;
-      float v[8];
+        for (int k = 0; k < 4; ++k) row[4 * k + e] = acc[ii][jj + k][e];
+        transpose4(row[e], row[4 + e], row[8 + e], row[12 + e]);
+      }
+      const long long i = (long long)i0 + (wm * TM + ii) * 16 + r;
+      if (i >= p.M) continue;
 #pragma unroll
-      for (int q = 0; q < 8; ++q) v[q] = row[8 * h + q];
-      if (whole) put8<FORM, ACT>(E, bias[h], out, i * p.N + j + 8 * h, v);
-      else put8<FORM_WEIGHT, ACT_NONE>(E, none, part, (slice * p.M + i) * p.N + j + 8 * h, v);
+      for (int h = 0; h < 2; ++h) {
+        if (j + 8 * h >= p.N) continue;
+        float v[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] = row[8 * h + q];
+        if (whole) put8<FORM, ACT>(E, bias[h], out, i * p.N + j + 8 * h, v);
+        else put8<FORM_WEIGHT, ACT_NONE>(E, none, part, (slice * p.M + i) * p.N + j + 8 * h, v);
+      }
     }
   }
 }
