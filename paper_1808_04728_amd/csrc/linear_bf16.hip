@@ -38,11 +38,13 @@ constexpr uint32_t kOut = 0x80000000u;  // past every buffer: the load gives zer
 // The rows r0 .. r0 + ROWS - 1 of a factor, a step of BK terms at a time.  KC: the sum's axis
 // is innermost.  Pieces past the rows' or the sum's end read as zeros: their offset is out of
 // the buffer's range.
-template <bool KC, int ROWS, int BK, int NT> struct Loader {
+template <bool KC, bool COLS, int ROWS, int BK, int NT> struct Loader {
   static constexpr int BYTES = ROWS * BK * 2, N = BYTES / 16 / NT;
   static_assert(BYTES % (16 * NT) == 0, "whole loads");
-  static_assert(KC ? NT / (BK / 8) % 16 == 0 : NT / 8 % BK == 0 || BK % (NT / 8) == 0, "a lane's pieces share their terms");
-  static constexpr bool SPLIT = !KC && NT / 8 < BK;  // a lane's pieces are of two or more terms
+  static_assert(BK == 64, "lines of 128 bytes");
+  static_assert(NT / 8 % 64 == 0 || NT / 8 == 32, "a lane's pieces are of one term, or of two in turn");
+  // bit 5 of a lane's term (of its odd pieces) where a load is 32 rows
+  static constexpr int FLIP = NT / 8 == 32 && (!KC || COLS) ? 32 : 0;
   const char *base;
   long long advance;  // bytes of a step
   uint32_t off[N];
@@ -57,12 +59,12 @@ template <bool KC, int ROWS, int BK, int NT> struct Loader {
       const int id = i * NT + threadIdx.x;
       if constexpr (KC) {
         const int row = id / (BK / 8), piece = id % (BK / 8);
-        const int c = piece ^ (BK == 64 ? (row >> 1) & 7 : (row >> 2) & 3);
+        const int c = piece ^ (COLS ? ((row >> 1) & 3) | ((row >> 5) & 1) << 2 : (row >> 1) & 7);
         off[i] = row < have ? (uint32_t)(row * (ld * 2)) + c * 16 : kOut;
         if (i == 0) term = c * 8;
       } else {
         const int sub = id / (BK * 8), row = id / 8 % BK, piece = id & 7;
-        const int c = ((piece >> 1) ^ (((row >> 1) & 1) | (((row >> 3) & 1) << 1))) * 2 + (piece & 1);
+        const int x = ((row >> 1) & 1) | (((row >> 3) & 1) << 1), c = piece ^ (COLS ? x : 2 * x);
         off[i] = sub * 64 + c * 8 < have ? (uint32_t)(row * (ld * 2)) + sub * 128 + c * 16 : kOut;
         if (i == 0) term = row;
       }
@@ -72,7 +74,7 @@ template <bool KC, int ROWS, int BK, int NT> struct Loader {
   // Written out because the compiler, which cannot tell the stages apart in the transposing
   // reads, would wait for every load before each of them; the waits are the kernel's own.
   __device__ __forceinline__ void load(int i, int wave, uint32_t stage, int rest) const {
-    const uint32_t o = term + (SPLIT ? i * (NT / 8) % BK : 0) < rest ? off[i] : kOut;
+    const uint32_t o = (term ^ (i % 2 * FLIP)) < rest ? off[i] : kOut;
     const u32x4_t r = {(uint32_t)(uintptr_t)base, (uint32_t)((uintptr_t)base >> 32) & 0xffffu, 0x7ffffff0u, 0x00020000u};
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                  :
@@ -82,26 +84,30 @@ template <bool KC, int ROWS, int BK, int NT> struct Loader {
   __device__ __forceinline__ void next() { base += advance; }
 };
 
-// A lane's place in the fragments of 16 rows and 32 terms.
-template <bool KC, int BK> struct Reader {
+// A lane's place in the fragments of 16 rows and 32 terms.  Fragment t of A has rows 16 t + r;
+// fragment t of B (COLS) has, of every 64 columns, 8 t' + r (r < 8) and 32 + 8 t' + r - 8, t' =
+// t % 4: after the epilogue's exchange a lane then has twice eight columns, and four lanes
+// eight by eight 64 neighbouring bytes of a row of C.
+template <bool KC, bool COLS, int BK> struct Reader {
   int lane_off, swz;
   __device__ __forceinline__ Reader() {
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     if constexpr (KC) {
-      lane_off = r * BK * 2;
-      swz = BK == 64 ? (r >> 1) & 7 : (r >> 2) & 3;
+      const int row = COLS ? (r & 7) + 32 * (r >> 3) : r;
+      lane_off = row * BK * 2;
+      swz = COLS ? ((r >> 1) & 3) | (r >> 3) << 2 : (r >> 1) & 7;
     } else {
-      lane_off = (8 * g + (r >> 2)) * 128 + (r & 3) * 8;
+      lane_off = (8 * g + (r >> 2)) * 128 + (COLS ? (r & 1) * 8 + (r & 2) * 32 : (r & 3) * 8);
       swz = ((r >> 3) & 1) | ((g & 1) << 1);
     }
   }
-  // rows 16 t .. of the stage, terms 32 k ..
+  // fragment t of the stage, terms 32 k ..
   __device__ __forceinline__ bf16x8_t frag(const unsigned char *stage, int t, int k) const {
     if constexpr (KC) {
-      const int g = (threadIdx.x & 63) >> 4;
-      return *reinterpret_cast<const bf16x8_t *>(stage + lane_off + t * 16 * BK * 2 + (((4 * k + g) ^ swz) << 4));
+      const int g = (threadIdx.x & 63) >> 4, row = COLS ? t / 4 * 64 + t % 4 * 8 : t * 16;
+      return *reinterpret_cast<const bf16x8_t *>(stage + lane_off + row * BK * 2 + (((4 * k + g) ^ swz) << 4));
     } else {
-      const unsigned char *p = stage + (t >> 2) * (BK * 128) + k * 32 * 128 + lane_off + (((t & 3) ^ swz) << 5);
+      const unsigned char *p = stage + (t >> 2) * (BK * 128) + k * 32 * 128 + lane_off + (((t & 3) ^ swz) << (COLS ? 4 : 5));
       const v4i16_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t *)p);
       const v4i16_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t *)(p + 512));
       const v8i16_t v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
@@ -228,10 +234,10 @@ __global__ __launch_bounds__(threads_of<Tile<KERNEL>>(), Tile<KERNEL>::WAVES) vo
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / C::WN, wn = wave % C::WN;
-  Loader<Form<FORM>::AK, C::BM, BK, NT> la(A, p.M, p.L, i0, k0);
-  Loader<Form<FORM>::BK, C::BN, BK, NT> lb(B, p.N, p.L, j0, k0);
-  const Reader<Form<FORM>::AK, BK> ra;
-  const Reader<Form<FORM>::BK, BK> rb;
+  Loader<Form<FORM>::AK, false, C::BM, BK, NT> la(A, p.M, p.L, i0, k0);
+  Loader<Form<FORM>::BK, true, C::BN, BK, NT> lb(B, p.N, p.L, j0, k0);
+  const Reader<Form<FORM>::AK, false, BK> ra;
+  const Reader<Form<FORM>::BK, true, BK> rb;
   constexpr int LOADS = decltype(la)::N + decltype(lb)::N;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void_t *)lds;
   int rest = (int)(p.L - k0);  // terms from the next step to load on
@@ -305,16 +311,16 @@ __global__ __launch_bounds__(threads_of<Tile<KERNEL>>(), Tile<KERNEL>::WAVES) vo
   }
   wait_loads<0>();  // no load outlives the workgroup
 
-  // lane (r, g) gets row r of each instruction tile, columns 16 g .. 16 g + 15 of the wave's 64
+  // lane (r, g) gets row r of each instruction tile, columns 8 g .. 8 g + 7 and 32 + 8 g .. of 64
   const int r = lane & 15, g = lane >> 4;
   const bool whole = p.slices == 1;
   const float none[8] = {};
 #pragma unroll
   for (int jj = 0; jj < TN; jj += 4) {
-    const int j = j0 + (wn * TN + jj) * 16 + 16 * g;
+    const int j = j0 + (wn * TN + jj) * 16 + 8 * g;
     float bias[2][8];
     load_bias<FORM>(E, j, p.N, bias[0]);
-    load_bias<FORM>(E, j + 8, p.N, bias[1]);
+    load_bias<FORM>(E, j + 32, p.N, bias[1]);
 #pragma unroll
     for (int ii = 0; ii < TM; ++ii) {
       float row[16];
@@ -328,12 +334,12 @@ __global__ __launch_bounds__(threads_of<Tile<KERNEL>>(), Tile<KERNEL>::WAVES) vo
       if (i >= p.M) continue;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        if (j + 8 * h >= p.N) continue;
+        if (j + 32 * h >= p.N) continue;
         float v[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) v[q] = row[8 * h + q];
-        if (whole) put8<FORM, ACT>(E, bias[h], out, i * p.N + j + 8 * h, v);
-        else put8<FORM_WEIGHT, ACT_NONE>(E, none, part, (slice * p.M + i) * p.N + j + 8 * h, v);
+        if (whole) put8<FORM, ACT>(E, bias[h], out, i * p.N + j + 32 * h, v);
+        else put8<FORM_WEIGHT, ACT_NONE>(E, none, part, (slice * p.M + i) * p.N + j + 32 * h, v);
       }
     }
   }
