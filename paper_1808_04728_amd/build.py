@@ -39,6 +39,7 @@ EXTRA = {
     "conv_f32.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "conv_f32_wgrad.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "linear_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "linear_f32.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "muon.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "muon_skinny.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
 }

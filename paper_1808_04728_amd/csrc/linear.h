@@ -44,4 +44,139 @@ bool linear_bf16_plan(int form, long long M, int N, long long L, LinearPlan *p);
 hipError_t launch_linear_bf16(int form, const LinearPlan &p, const void *A, const void *B, const LinearEpilogue &E, void *out,
                               float *part, hipStream_t st);
 
+// The fp32 kernels (linear_f32.hip): any sizes whose rows 32-bit offsets reach.
+bool linear_f32_plan(int form, long long M, int N, long long L, LinearPlan *p);
+hipError_t launch_linear_f32(int form, const LinearPlan &p, const void *A, const void *B, const LinearEpilogue &E, void *out,
+                             float *part, hipStream_t st);
+
+// ---- device helpers -----------------------------------------------------------------
+
+typedef __attribute__((address_space(3))) void lds_void_t;
+
+constexpr uint32_t kOut = 0x80000000u;  // past every buffer: the load gives zeros
+
+// The exchange of the 16-byte pieces of 128-byte rows in LDS: the sixteen rows of a fragment
+// at one piece touch all banks.  Rows of a fragment: 16 t + r, or (COLS), of every 64, 8 t + r
+// (r < 8) and 32 + 8 t + r - 8: after the epilogue's exchange a lane then has twice eight
+// columns, and four lanes eight by eight 64 neighbouring values of a row of C.
+template <bool COLS> __device__ __forceinline__ int swizzle(int row) {
+  return COLS ? ((row >> 1) & 3) | ((row >> 5) & 1) << 2 : (row >> 1) & 7;
+}
+
+// waits until at most N of the wave's loads are in flight, and for its LDS reads
+template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
+__device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xc07f); }  // lgkmcnt(0)
+__device__ __forceinline__ void barrier() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_barrier" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// Four registers of four lanes (those 16 apart) transposed: register k of lane g gets
+// register g of lane k.
+__device__ __forceinline__ void transpose4(float &a, float &b, float &c, float &d) {
+  auto swap32 = [](float &x, float &y) {
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+    x = __uint_as_float(s[0]);
+    y = __uint_as_float(s[1]);
+  };
+  auto swap16 = [](float &x, float &y) {
+    const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+    x = __uint_as_float(s[0]);
+    y = __uint_as_float(s[1]);
+  };
+  swap32(a, c);
+  swap32(b, d);
+  swap16(a, b);
+  swap16(c, d);
+}
+
+// Eight neighbouring values of a row, of which n exist.  bf16 rows are whole 16-byte pieces;
+// fp32 ones start anywhere.
+typedef uint32_t u32x4e4_t __attribute__((ext_vector_type(4), aligned(4)));
+__device__ __forceinline__ void load8(const uint16_t *p, int, float (&x)[8]) {
+  const u32x4_t a = *reinterpret_cast<const u32x4_t *>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(a[i] << 16);
+    x[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void load8(const float *p, int n, float (&x)[8]) {
+  if (n >= 8) {
+    const u32x4_t a = reinterpret_cast<const u32x4e4_t *>(p)[0], b = reinterpret_cast<const u32x4e4_t *>(p)[1];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[i] = __uint_as_float(a[i]);
+      x[4 + i] = __uint_as_float(b[i]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = i < n ? p[i] : 0.f;
+  }
+}
+__device__ __forceinline__ void store8(uint16_t *p, int, const float (&x)[8]) { *reinterpret_cast<u32x4_t *>(p) = pack_bf16x8(x); }
+__device__ __forceinline__ void store8(float *p, int n, const float (&x)[8]) {
+  if (n >= 8) {
+    u32x4_t a, b;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      a[i] = __float_as_uint(x[i]);
+      b[i] = __float_as_uint(x[4 + i]);
+    }
+    reinterpret_cast<u32x4e4_t *>(p)[0] = a;
+    reinterpret_cast<u32x4e4_t *>(p)[1] = b;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) p[i] = x[i];
+  }
+}
+
+// eight neighbouring outputs
+template <int DT, int FORM, int ACT>
+__device__ __forceinline__ void put8(const LinearEpilogue &E, const float (&bias)[8], void *out, long long at, int n,
+                                     float (&v)[8]) {
+  typedef typename Store<DT>::T T;
+  if constexpr (FORM == FORM_WEIGHT) {
+    store8((float *)out + at, n, v);
+  } else if constexpr (FORM == FORM_FWD) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] += bias[q];
+    if (E.z) store8((T *)E.z + at, n, v);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = act<ACT>(v[q], E.alpha);
+    if (E.residual) {
+      float r[8];
+      load8((const T *)E.residual + at, n, r);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] += r[q];
+    }
+    store8((T *)out + at, n, v);
+  } else {
+    float r[8];
+    if (E.residual) {
+      load8((const T *)E.residual + at, n, r);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] += r[q];
+    }
+    if constexpr (ACT != ACT_NONE) {
+      load8((const T *)E.zin + at, n, r);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] *= act_slope<ACT>(r[q], E.alpha);
+    }
+    store8((T *)out + at, n, v);
+  }
+}
+
+// the bias of columns j .. j + 7 (a multiple of 8)
+template <int FORM>
+__device__ __forceinline__ void load_bias(const LinearEpilogue &E, int j, int N, float (&b)[8]) {
+  if (FORM == FORM_FWD && E.bias) load8(E.bias + j, N - j, b);
+  else {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) b[q] = 0.f;
+  }
+}
+
 }  // namespace cf

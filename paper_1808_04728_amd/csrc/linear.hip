@@ -203,7 +203,7 @@ int slices_of(long long M, int N, long long L) {
 // form, and the output's rows and columns and the sum's terms
 LinearPlan plan_of(int form, long long M, int N, long long L, int dtype) {
   LinearPlan p;
-  if (dtype == DT_BF16 && linear_bf16_plan(form, M, N, L, &p)) return p;
+  if (dtype == DT_BF16 ? linear_bf16_plan(form, M, N, L, &p) : linear_f32_plan(form, M, N, L, &p)) return p;
   const int slices = slices_of(M, N, L);
   const long long per = ((L + slices - 1) / slices + 31) / 32 * 32;
   return LinearPlan{M, L, N, LIN_ANY, (int)((M + 63) / 64), (N + 63) / 64, (int)((L + per - 1) / per), per};
@@ -217,11 +217,16 @@ hipError_t product(long long M, int N, long long L, int dtype, const void *A, co
                    void *ws, hipStream_t st) {
   const LinearPlan p = plan_of(FORM, M, N, L, dtype);
   float *part = (float *)ws;
-  if (p.kernel != LIN_ANY) return launch_linear_bf16(FORM, p, A, B, E, out, part, st);
+  if (p.kernel != LIN_ANY && dtype == DT_BF16) return launch_linear_bf16(FORM, p, A, B, E, out, part, st);
+  if (p.kernel != LIN_ANY) {
+    const hipError_t r = launch_linear_f32(FORM, p, A, B, E, out, part, st);
+    if (r != hipSuccess) return r;
+  }
   const dim3 grid = long_grid((long long)p.tm * p.tn * p.slices), block(kThreads);
   with_act(E.act, [&](auto a) {
     constexpr int ACT = FORM == FORM_WEIGHT ? (int)ACT_NONE : decltype(a)::value;
-    if (dtype == DT_BF16) hipLaunchKernelGGL((any_kernel<DT_BF16, FORM, ACT>), grid, block, 0, st, p, A, B, E, out, part);
+    if (p.kernel != LIN_ANY) {
+    } else if (dtype == DT_BF16) hipLaunchKernelGGL((any_kernel<DT_BF16, FORM, ACT>), grid, block, 0, st, p, A, B, E, out, part);
     else hipLaunchKernelGGL((any_kernel<DT_F32, FORM, ACT>), grid, block, 0, st, p, A, B, E, out, part);
     if (p.slices > 1 && FORM != FORM_WEIGHT) {
       const dim3 all = long_grid((M * N + kThreads - 1) / kThreads);

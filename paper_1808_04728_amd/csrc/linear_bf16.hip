@@ -19,29 +19,27 @@ namespace {
 typedef short v4i16_t __attribute__((ext_vector_type(4)));
 typedef short v8i16_t __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) v4i16_t lds_v4i16_t;
-typedef __attribute__((address_space(3))) void lds_void_t;
 
 // A tile: WM x WN waves of TM x TN instruction tiles of 16 x 16; NS steps of 64 terms in LDS.
 template <int KERNEL> struct Tile;
 template <> struct Tile<LIN_256> {
-  static constexpr int BM = 256, BN = 256, WM = 2, WN = 4, BK = 64, NS = 2, WAVES = 2;
+  static constexpr int BM = 256, BN = 256, WM = 2, WN = 4, NS = 2, WAVES = 2;
 };
 template <> struct Tile<LIN_128> {
-  static constexpr int BM = 128, BN = 128, WM = 2, WN = 2, BK = 64, NS = 2, WAVES = 2;
+  static constexpr int BM = 128, BN = 128, WM = 2, WN = 2, NS = 2, WAVES = 2;
 };
 template <> struct Tile<LIN_64> {
-  static constexpr int BM = 64, BN = 64, WM = 4, WN = 1, BK = 64, NS = 3, WAVES = 3;
+  static constexpr int BM = 64, BN = 64, WM = 4, WN = 1, NS = 3, WAVES = 3;
 };
 
-constexpr uint32_t kOut = 0x80000000u;  // past every buffer: the load gives zeros
+constexpr int BK = 64, KK = BK / 32;
 
 // The rows r0 .. r0 + ROWS - 1 of a factor, a step of BK terms at a time.  KC: the sum's axis
 // is innermost.  Pieces past the rows' or the sum's end read as zeros: their offset is out of
 // the buffer's range.
-template <bool KC, bool COLS, int ROWS, int BK, int NT> struct Loader {
+template <bool KC, bool COLS, int ROWS, int NT> struct Loader {
   static constexpr int BYTES = ROWS * BK * 2, N = BYTES / 16 / NT;
   static_assert(BYTES % (16 * NT) == 0, "whole loads");
-  static_assert(BK == 64, "lines of 128 bytes");
   static_assert(NT / 8 % 64 == 0 || NT / 8 == 32, "a lane's pieces are of one term, or of two in turn");
   // bit 5 of a lane's term (of its odd pieces) where a load is 32 rows
   static constexpr int FLIP = NT / 8 == 32 && (!KC || COLS) ? 32 : 0;
@@ -59,7 +57,7 @@ template <bool KC, bool COLS, int ROWS, int BK, int NT> struct Loader {
       const int id = i * NT + threadIdx.x;
       if constexpr (KC) {
         const int row = id / (BK / 8), piece = id % (BK / 8);
-        const int c = piece ^ (COLS ? ((row >> 1) & 3) | ((row >> 5) & 1) << 2 : (row >> 1) & 7);
+        const int c = piece ^ swizzle<COLS>(row);
         off[i] = row < have ? (uint32_t)(row * (ld * 2)) + c * 16 : kOut;
         if (i == 0) term = c * 8;
       } else {
@@ -88,14 +86,14 @@ template <bool KC, bool COLS, int ROWS, int BK, int NT> struct Loader {
 // fragment t of B (COLS) has, of every 64 columns, 8 t' + r (r < 8) and 32 + 8 t' + r - 8, t' =
 // t % 4: after the epilogue's exchange a lane then has twice eight columns, and four lanes
 // eight by eight 64 neighbouring bytes of a row of C.
-template <bool KC, bool COLS, int BK> struct Reader {
+template <bool KC, bool COLS> struct Reader {
   int lane_off, swz;
   __device__ __forceinline__ Reader() {
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     if constexpr (KC) {
       const int row = COLS ? (r & 7) + 32 * (r >> 3) : r;
       lane_off = row * BK * 2;
-      swz = COLS ? ((r >> 1) & 3) | (r >> 3) << 2 : (r >> 1) & 7;
+      swz = swizzle<COLS>(row);
     } else {
       lane_off = (8 * g + (r >> 2)) * 128 + (COLS ? (r & 1) * 8 + (r & 2) * 32 : (r & 3) * 8);
       swz = ((r >> 3) & 1) | ((g & 1) << 1);
@@ -116,105 +114,13 @@ template <bool KC, bool COLS, int BK> struct Reader {
   }
 };
 
-// waits until at most N of the wave's loads are in flight, and for its LDS reads
-template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
-__device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xc07f); }  // lgkmcnt(0)
-__device__ __forceinline__ void barrier() {
-  __builtin_amdgcn_sched_barrier(0);
-  asm volatile("s_barrier" ::: "memory");
-  __builtin_amdgcn_sched_barrier(0);
-}
-
-template <int N> struct Stage {
-  static constexpr int v = N;
-};
-
-// Four registers of four lanes (those 16 apart) transposed: register k of lane g gets
-// register g of lane k.
-__device__ __forceinline__ void transpose4(float &a, float &b, float &c, float &d) {
-  auto swap32 = [](float &x, float &y) {
-    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false);
-    x = __uint_as_float(s[0]);
-    y = __uint_as_float(s[1]);
-  };
-  auto swap16 = [](float &x, float &y) {
-    const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false, false);
-    x = __uint_as_float(s[0]);
-    y = __uint_as_float(s[1]);
-  };
-  swap32(a, c);
-  swap32(b, d);
-  swap16(a, b);
-  swap16(c, d);
-}
-
-// eight bf16 of a row, of which k exist (a multiple of 8 or none)
-__device__ __forceinline__ void load8(const uint16_t *p, float (&x)[8]) {
-  const u32x4_t a = *reinterpret_cast<const u32x4_t *>(p);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(a[i] << 16);
-    x[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
-  }
-}
-__device__ __forceinline__ void store8(uint16_t *p, const float (&x)[8]) { *reinterpret_cast<u32x4_t *>(p) = pack_bf16x8(x); }
-__device__ __forceinline__ void store8(float *p, const float (&x)[8]) {
-  reinterpret_cast<float4 *>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
-  reinterpret_cast<float4 *>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
-}
-
-// eight neighbouring outputs
-template <int FORM, int ACT>
-__device__ __forceinline__ void put8(const LinearEpilogue &E, const float (&bias)[8], void *out, long long at, float (&v)[8]) {
-  if constexpr (FORM == FORM_WEIGHT) {
-    store8((float *)out + at, v);
-  } else if constexpr (FORM == FORM_FWD) {
-#pragma unroll
-    for (int q = 0; q < 8; ++q) v[q] += bias[q];
-    if (E.z) store8((uint16_t *)E.z + at, v);
-#pragma unroll
-    for (int q = 0; q < 8; ++q) v[q] = act<ACT>(v[q], E.alpha);
-    if (E.residual) {
-      float r[8];
-      load8((const uint16_t *)E.residual + at, r);
-#pragma unroll
-      for (int q = 0; q < 8; ++q) v[q] += r[q];
-    }
-    store8((uint16_t *)out + at, v);
-  } else {
-    float r[8];
-    if (E.residual) {
-      load8((const uint16_t *)E.residual + at, r);
-#pragma unroll
-      for (int q = 0; q < 8; ++q) v[q] += r[q];
-    }
-    if constexpr (ACT != ACT_NONE) {
-      load8((const uint16_t *)E.zin + at, r);
-#pragma unroll
-      for (int q = 0; q < 8; ++q) v[q] *= act_slope<ACT>(r[q], E.alpha);
-    }
-    store8((uint16_t *)out + at, v);
-  }
-}
-
-template <int FORM>
-__device__ __forceinline__ void load_bias(const LinearEpilogue &E, int j, int N, float (&b)[8]) {
-#pragma unroll
-  for (int q = 0; q < 8; ++q) b[q] = 0.f;
-  if (FORM == FORM_FWD && E.bias && j < N) {
-    const float4 u = *reinterpret_cast<const float4 *>(E.bias + j), v = *reinterpret_cast<const float4 *>(E.bias + j + 4);
-    b[0] = u.x; b[1] = u.y; b[2] = u.z; b[3] = u.w;
-    b[4] = v.x; b[5] = v.y; b[6] = v.z; b[7] = v.w;
-  }
-}
-
 template <class C> constexpr int threads_of() { return 64 * C::WM * C::WN; }
 
 template <int KERNEL, int FORM, int ACT>
 __global__ __launch_bounds__(threads_of<Tile<KERNEL>>(), Tile<KERNEL>::WAVES) void product_kernel(
     LinearPlan p, long long per_xcd, const uint16_t *A, const uint16_t *B, LinearEpilogue E, void *out, float *part) {
   using C = Tile<KERNEL>;
-  constexpr int NT = threads_of<C>(), BK = C::BK, KK = BK / 32, TM = C::BM / C::WM / 16, TN = C::BN / C::WN / 16;
+  constexpr int NT = threads_of<C>(), TM = C::BM / C::WM / 16, TN = C::BN / C::WN / 16;
   static_assert(TN % 4 == 0, "a lane's row of the epilogue is sixteen columns of 64");
   constexpr int AB = C::BM * BK * 2, STAGE = AB + C::BN * BK * 2;
   __shared__ __attribute__((aligned(16))) unsigned char lds[C::NS * STAGE];
@@ -234,10 +140,10 @@ __global__ __launch_bounds__(threads_of<Tile<KERNEL>>(), Tile<KERNEL>::WAVES) vo
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / C::WN, wn = wave % C::WN;
-  Loader<Form<FORM>::AK, false, C::BM, BK, NT> la(A, p.M, p.L, i0, k0);
-  Loader<Form<FORM>::BK, true, C::BN, BK, NT> lb(B, p.N, p.L, j0, k0);
-  const Reader<Form<FORM>::AK, false, BK> ra;
-  const Reader<Form<FORM>::BK, true, BK> rb;
+  Loader<Form<FORM>::AK, false, C::BM, NT> la(A, p.M, p.L, i0, k0);
+  Loader<Form<FORM>::BK, true, C::BN, NT> lb(B, p.N, p.L, j0, k0);
+  const Reader<Form<FORM>::AK, false> ra;
+  const Reader<Form<FORM>::BK, true> rb;
   constexpr int LOADS = decltype(la)::N + decltype(lb)::N;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void_t *)lds;
   int rest = (int)(p.L - k0);  // terms from the next step to load on
@@ -277,7 +183,7 @@ __global__ __launch_bounds__(threads_of<Tile<KERNEL>>(), Tile<KERNEL>::WAVES) vo
 #pragma unroll
       for (int q = i * (TM + TN) / EARLY; q < (i + 1) * (TM + TN) / EARLY && q < TM + TN; ++q) read(1 - f, q, rs, k);
 #pragma unroll
-      for (int q = i * decltype(loads)::v / TM; q < (i + 1) * decltype(loads)::v / TM; ++q) load(q, ls);
+      for (int q = i * decltype(loads)::value / TM; q < (i + 1) * decltype(loads)::value / TM; ++q) load(q, ls);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[f][j], fa[f][i], acc[i][j], 0, 0, 0);
@@ -295,19 +201,15 @@ __global__ __launch_bounds__(threads_of<Tile<KERNEL>>(), Tile<KERNEL>::WAVES) vo
 #pragma unroll
   for (int q = 0; q < TM + TN; ++q) read(0, q, lds, 0);
   int slot = 0;
-  auto step = [&](int first) {  // first: which fragments the step begins with
+  for (int s = 0; s < steps; ++s) {
     const int after = slot + 1 == C::NS ? 0 : slot + 1;
-    if constexpr (KK == 2) half(first, lds + slot * STAGE, 1, Stage<0>{}, 0);
+    half(0, lds + slot * STAGE, 1, std::integral_constant<int, 0>{}, 0);
     wait_lds();
     wait_loads<(C::NS - 2) * LOADS>();
     barrier();
-    half(KK == 2 ? 1 - first : first, lds + after * STAGE, 0, Stage<LOADS>{}, slot);
+    half(1, lds + after * STAGE, 0, std::integral_constant<int, LOADS>{}, slot);
     next();
     slot = after;
-  };
-  for (int s = 0; s < steps; s += 3 - KK) {
-    step(0);
-    if constexpr (KK == 1) step(1);
   }
   wait_loads<0>();  // no load outlives the workgroup
 
@@ -338,8 +240,8 @@ __global__ __launch_bounds__(threads_of<Tile<KERNEL>>(), Tile<KERNEL>::WAVES) vo
         float v[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) v[q] = row[8 * h + q];
-        if (whole) put8<FORM, ACT>(E, bias[h], out, i * p.N + j + 32 * h, v);
-        else put8<FORM_WEIGHT, ACT_NONE>(E, none, part, (slice * p.M + i) * p.N + j + 32 * h, v);
+        if (whole) put8<DT_BF16, FORM, ACT>(E, bias[h], out, i * p.N + j + 32 * h, 8, v);
+        else put8<DT_BF16, FORM_WEIGHT, ACT_NONE>(E, none, part, (slice * p.M + i) * p.N + j + 32 * h, 8, v);
       }
     }
   }
@@ -359,7 +261,7 @@ __global__ __launch_bounds__(256) void join8_kernel(LinearPlan p, const float *p
   }
   float bias[8];
   load_bias<FORM>(E, (int)(at % p.N), p.N, bias);
-  put8<FORM, ACT>(E, bias, out, at, v);
+  put8<DT_BF16, FORM, ACT>(E, bias, out, at, 8, v);
 }
 
 struct Cost {

@@ -1,0 +1,285 @@
+// linear_f32.hip -- fp32 matrix products on tiles of 128 and 64 (gfx950).
+//
+// As the bf16 kernels' tiles, with the fp32 matrix instructions (16 x 16 x 4: a sixteenth of
+// the bf16 rate, so the matrix units are busy eight times as long for the same bytes).  Rows
+// may start on any element and end anywhere: every lane loads single values, for which the
+// matrix instructions leave time enough, and values past a row's or the sum's end read as
+// zeros.  A step is 32 terms.  A factor with the sum's axis innermost lies in LDS by rows of
+// 32 terms and is read four terms a lane; one with the sum's axis outermost lies by terms and
+// is read value by value, a lane's four terms the same four as the other factor's.
+
+#include "linear.h"
+
+namespace cf {
+namespace {
+
+// A tile: WM x WN waves of TM x TN instruction tiles of 16 x 16; NS steps in LDS.
+template <int KERNEL> struct Tile;
+template <> struct Tile<LIN_128> {
+  static constexpr int B = 128, WM = 2, WN = 2, NS = 2, WAVES = 2;
+};
+template <> struct Tile<LIN_64> {
+  static constexpr int B = 64, WM = 4, WN = 1, NS = 3, WAVES = 3;
+};
+constexpr int BK = 32, NT = 256;
+
+// The rows r0 .. r0 + ROWS - 1 of a factor, a step of BK terms at a time; NT lanes load a value
+// each.  KC: the sum's axis is innermost.  Otherwise the columns of term k are exchanged by 16
+// (COLS: by 8) with k / 4, so that the four lanes of a column that read four terms apart
+// touch different banks.
+template <bool COLS> constexpr int kExchange = COLS ? 8 : 16;
+template <bool KC, bool COLS, int ROWS> struct Loader {
+  static constexpr int N = ROWS * BK / NT;
+  const char *base;
+  long long advance, row_bytes;
+  uint32_t off[KC ? 2 : 4];  // of the lane's value, by what the exchange has for a load
+  int term[KC ? 2 : 1], row;  // of load 0; not KC: row is the column in LDS
+  int have;
+  __device__ __forceinline__ Loader(const float *p, long long rows, long long terms, int r0, long long k0) {
+    const long long ld = KC ? terms : rows;
+    base = (const char *)(p + (KC ? r0 * ld + k0 : k0 * ld + r0));
+    row_bytes = ld * 4;
+    advance = KC ? BK * 4 : BK * row_bytes;
+    have = (int)min(rows - r0, (long long)ROWS);
+    if constexpr (KC) {
+      // load i has rows 8 i ..: bit 2 of their exchange is bit 0 of i, with COLS bit 2
+      row = threadIdx.x >> 5;
+      const int d = threadIdx.x & 31;
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        term[b] = ((d >> 2) ^ (row >> 1 | b << 2)) * 4 + (d & 3);
+        off[b] = (uint32_t)(row * row_bytes) + term[b] * 4;
+      }
+    } else {
+      term[0] = threadIdx.x / ROWS;
+      row = threadIdx.x % ROWS;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) off[e] = (uint32_t)(term[0] * row_bytes) + (row ^ e * kExchange<COLS>) * 4;
+    }
+  }
+  // Load i of the next step to `stage` (bytes from the LDS's start); `rest` terms are left.
+  // (Written out, with the kernel's own waits, as in the bf16 kernels.)
+  __device__ __forceinline__ void load(int i, int wave, uint32_t stage, int rest) const {
+    uint32_t o;
+    const char *b;
+    if constexpr (KC) {
+      const int e = COLS ? (i >> 2) & 1 : i & 1;
+      o = row + 8 * i < have && term[e] < rest ? off[e] : kOut;
+      b = base + 8 * i * row_bytes;
+    } else {
+      constexpr int PER = NT / ROWS;  // terms of a load
+      const int k = i * PER, e = (k >> 2) & 3;
+      o = (row ^ e * kExchange<COLS>) < have && term[0] + k < rest ? off[e] : kOut;
+      b = base + k * row_bytes;
+    }
+    const u32x4_t r = {(uint32_t)(uintptr_t)b, (uint32_t)((uintptr_t)b >> 32) & 0xffffu, 0x7ffffff0u, 0x00020000u};
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+                 :
+                 : "s"(stage + (uint32_t)(i * NT + wave * 64) * 4), "v"(o), "s"(r)
+                 : "memory");
+  }
+  __device__ __forceinline__ void next() { base += advance; }
+};
+
+// A lane's place in the fragments of 16 rows (see swizzle) and 16 terms: its terms 4 g .. 4 g + 3.
+template <bool KC, bool COLS, int ROWS> struct Reader {
+  int lane_off, swz;
+  __device__ __forceinline__ Reader() {
+    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int row = COLS ? (r & 7) + 32 * (r >> 3) : r;
+    lane_off = KC ? row * BK * 4 : 4 * g * ROWS * 4 + row * 4;
+    swz = KC ? swizzle<COLS>(row) : g;
+  }
+  // fragment t of the stage, terms 16 k ..
+  __device__ __forceinline__ f32x4_t frag(const unsigned char *stage, int t, int k) const {
+    if constexpr (KC) {
+      const int g = (threadIdx.x & 63) >> 4, row = COLS ? t / 4 * 64 + t % 4 * 8 : t * 16;
+      return *reinterpret_cast<const f32x4_t *>(stage + lane_off + row * BK * 4 + (((4 * k + g) ^ swz) << 4));
+    } else {
+      const unsigned char *p = stage + lane_off + (t / 4 * 64 + ((t % 4) ^ swz) * kExchange<COLS>) * 4 + 16 * k * ROWS * 4;
+      f32x4_t v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const float *>(p + e * ROWS * 4);
+      return v;
+    }
+  }
+};
+
+template <int KERNEL, int FORM, int ACT>
+__global__ __launch_bounds__(NT, Tile<KERNEL>::WAVES) void product_kernel(LinearPlan p, long long per_xcd, const float *A,
+                                                                          const float *B, LinearEpilogue E, void *out,
+                                                                          float *part) {
+  using C = Tile<KERNEL>;
+  constexpr int TM = C::B / C::WM / 16, TN = C::B / C::WN / 16, AB = C::B * BK * 4, STAGE = 2 * AB;
+  static_assert(TN == 4 && 64 * C::WM * C::WN == NT, "a lane's row of the epilogue is sixteen columns of 64");
+  __shared__ __attribute__((aligned(16))) unsigned char lds[C::NS * STAGE];
+
+  // (the order of tiles of the bf16 kernels)
+  const long long index = long_index(), job = (index & 7) * per_xcd + (index >> 3);
+  const long long tiles = (long long)p.tm * p.tn;
+  if (job >= tiles * p.slices) return;
+  const long long slice = job / tiles, t = job % tiles, group = t / (8 * p.tn), in = t % (8 * p.tn);
+  const int high = (int)min(8LL, p.tm - 8 * group);
+  const int i0 = (int)(8 * group + in % high) * C::B, j0 = (int)(in / high) * C::B;
+  const long long k0 = slice * p.per, k1 = min(k0 + p.per, p.L);
+  const int steps = k1 > k0 ? (int)((k1 - k0 + BK - 1) / BK) : 0;
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / C::WN, wn = wave % C::WN;
+  Loader<Form<FORM>::AK, false, C::B> la(A, p.M, p.L, i0, k0);
+  Loader<Form<FORM>::BK, true, C::B> lb(B, p.N, p.L, j0, k0);
+  const Reader<Form<FORM>::AK, false, C::B> ra;
+  const Reader<Form<FORM>::BK, true, C::B> rb;
+  constexpr int NA = decltype(la)::N, LOADS = NA + decltype(lb)::N;
+  static_assert((C::NS - 1) * LOADS < 64, "loads that a wait can leave in flight");
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void_t *)lds;
+  int rest = (int)(p.L - k0);  // terms from the next step to load on
+  auto load = [&](int q, int stage) {  // load q of the next step
+    if (q < NA) la.load(q, wave, lds0 + stage * STAGE, rest);
+    else lb.load(q - NA, wave, lds0 + stage * STAGE + AB, rest);
+  };
+  auto next = [&] {
+    la.next();
+    lb.next();
+    rest -= BK;
+  };
+
+  f32x4_t acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+
+  // As in the bf16 kernels: the fragments of the next 16 terms are read, and the step NS
+  // further is loaded, between the matrix instructions of these; one barrier a step.
+  f32x4_t fb[2][TN], fa[2][TM];
+  auto read = [&](int f, int q, const unsigned char *stage, int k) {
+    if (q < TN) fb[f][q] = rb.frag(stage + AB, wn * TN + q, k);
+    else fa[f][q - TN] = ra.frag(stage, wm * TM + q - TN, k);
+  };
+  auto half = [&](int f, const unsigned char *rs, int k, auto loads, int ls) {
+    constexpr int GROUPS = 4 * TM, FIRST = 3 * TM;  // reads go out in the first groups
+#pragma unroll
+    for (int n = 0; n < GROUPS; ++n) {
+#pragma unroll
+      for (int q = n * (TM + TN) / FIRST; q < (n + 1) * (TM + TN) / FIRST && q < TM + TN; ++q) read(1 - f, q, rs, k);
+#pragma unroll
+      for (int q = n * decltype(loads)::value / GROUPS; q < (n + 1) * decltype(loads)::value / GROUPS; ++q) load(q, ls);
+      __builtin_amdgcn_sched_barrier(0);
+      const int i = n / 4, e = n % 4;
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[f][j][e], fa[f][i][e], acc[i][j], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+#pragma unroll
+  for (int n = 0; n < C::NS; ++n) {
+#pragma unroll
+    for (int q = 0; q < LOADS; ++q) load(q, n);
+    next();
+  }
+  wait_loads<(C::NS - 1) * LOADS>();
+  barrier();
+#pragma unroll
+  for (int q = 0; q < TM + TN; ++q) read(0, q, lds, 0);
+  int slot = 0;
+  for (int s = 0; s < steps; ++s) {
+    const int after = slot + 1 == C::NS ? 0 : slot + 1;
+    half(0, lds + slot * STAGE, 1, std::integral_constant<int, 0>{}, 0);
+    wait_lds();
+    wait_loads<(C::NS - 2) * LOADS>();
+    barrier();
+    half(1, lds + after * STAGE, 0, std::integral_constant<int, LOADS>{}, slot);
+    next();
+    slot = after;
+  }
+  wait_loads<0>();  // no load outlives the workgroup
+
+  // lane (r, g) gets row r of each instruction tile, columns 8 g .. 8 g + 7 and 32 + 8 g .. of 64
+  const int r = lane & 15, g = lane >> 4, j = j0 + wn * 64 + 8 * g;
+  const bool whole = p.slices == 1;
+  const float none[8] = {};
+  float bias[2][8];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) load_bias<FORM>(E, j + 32 * h, p.N, bias[h]);
+#pragma unroll
+  for (int ii = 0; ii < TM; ++ii) {
+    float row[16];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) row[4 * k + e] = acc[ii][k][e];
+      transpose4(row[e], row[4 + e], row[8 + e], row[12 + e]);
+    }
+    const long long i = (long long)i0 + (wm * TM + ii) * 16 + r;
+    if (i >= p.M) continue;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int n = p.N - j - 32 * h;
+      if (n <= 0) continue;
+      float v[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] = row[8 * h + q];
+      if (whole) put8<DT_F32, FORM, ACT>(E, bias[h], out, i * p.N + j + 32 * h, n, v);
+      else put8<DT_F32, FORM_WEIGHT, ACT_NONE>(E, none, part, (slice * p.M + i) * p.N + j + 32 * h, n, v);
+    }
+  }
+}
+
+struct Cost {
+  int kernel, b;
+  double fixed, step;  // us of a tile, and of 32 terms of it
+};
+constexpr Cost kCost[] = {{LIN_128, 128, 6.0, 2.3}, {LIN_64, 64, 3.0, 0.65}};
+
+}  // namespace
+
+bool linear_f32_plan(int form, long long M, int N, long long L, LinearPlan *p) {
+  // 32-bit offsets inside a tile's rows, and its first row's and column's numbers
+  const long long la = form == FORM_WEIGHT ? M : L, lb = form == FORM_DATA ? L : N;
+  if (la >= (1LL << 22) || lb >= (1LL << 22) || M >= (1LL << 31) - 256) return false;
+  double best = 1e30;
+  for (const Cost &c : kCost) {
+    const long long tm = (M + c.b - 1) / c.b, tn = (N + c.b - 1) / c.b, tiles = tm * tn, steps = (L + BK - 1) / BK;
+    const long long chain = std::max(1LL, std::min((L + kChain - 1) / kChain, (1LL << 28) / (M * N)));
+    for (long long s = 1; s <= 64; s = s < 4 ? s + 1 : s * 2) {
+      const long long slices = std::max(s, chain);
+      if (s > 1 && (steps / s < 4 || slices * M * N > (1LL << 28) || tiles * s > 8 * kCUs)) break;
+      const long long rounds = (tiles * slices + kCUs - 1) / kCUs;
+      double t = rounds * (c.fixed + c.step * ((steps + slices - 1) / slices));
+      if (slices > 1) t += 3.0 + slices * (double)M * N * 8 / 4e6;
+      if (t < best) {
+        best = t;
+        const long long per = ((L + slices - 1) / slices + BK - 1) / BK * BK;
+        *p = LinearPlan{M, L, N, c.kernel, (int)tm, (int)tn, (int)((L + per - 1) / per), per};
+      }
+    }
+  }
+  return true;
+}
+
+namespace {
+template <int FORM>
+hipError_t launch_form(const LinearPlan &p, const float *A, const float *B, const LinearEpilogue &E, void *out, float *part,
+                       hipStream_t st) {
+  const long long per_xcd = ((long long)p.tm * p.tn * p.slices + 7) / 8;
+  with_act(E.act, [&](auto a) {
+    constexpr int ACT = FORM == FORM_WEIGHT ? (int)ACT_NONE : decltype(a)::value;
+    const dim3 grid = long_grid(8 * per_xcd), block(NT);
+    if (p.kernel == LIN_128)
+      hipLaunchKernelGGL((product_kernel<LIN_128, FORM, ACT>), grid, block, 0, st, p, per_xcd, A, B, E, out, part);
+    else hipLaunchKernelGGL((product_kernel<LIN_64, FORM, ACT>), grid, block, 0, st, p, per_xcd, A, B, E, out, part);
+  });
+  return hipGetLastError();
+}
+}  // namespace
+
+hipError_t launch_linear_f32(int form, const LinearPlan &p, const void *A, const void *B, const LinearEpilogue &E, void *out,
+                             float *part, hipStream_t st) {
+  const float *a = (const float *)A, *b = (const float *)B;
+  if (form == FORM_FWD) return launch_form<FORM_FWD>(p, a, b, E, out, part, st);
+  if (form == FORM_DATA) return launch_form<FORM_DATA>(p, a, b, E, out, part, st);
+  return launch_form<FORM_WEIGHT>(p, a, b, E, out, part, st);
+}
+
+}  // namespace cf
