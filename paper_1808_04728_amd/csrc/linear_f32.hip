@@ -2,9 +2,9 @@
 //
 // As the bf16 kernels' tiles, with the fp32 matrix instructions (16 x 16 x 4: a sixteenth of
 // the bf16 rate, so the matrix units are busy eight times as long for the same bytes).  Rows
-// may start on any element and end anywhere: every lane loads single values, for which the
-// matrix instructions leave time enough, and values past a row's or the sum's end read as
-// zeros.  A step is 32 terms.  A factor with the sum's axis innermost lies in LDS by rows of
+// may start on any element and end anywhere: then every lane loads single values, for which
+// the matrix instructions leave time enough, and 16 bytes where all rows are whole 16-byte
+// pieces.  What is past a row's or the sum's end reads as zeros.  A step is 32 terms.  A factor with the sum's axis innermost lies in LDS by rows of
 // 32 terms and is read four terms a lane; one with the sum's axis outermost lies by terms and
 // is read value by value, a lane's four terms the same four as the other factor's.
 
@@ -23,60 +23,51 @@ template <> struct Tile<LIN_64> {
 };
 constexpr int BK = 32, NT = 256;
 
-// The rows r0 .. r0 + ROWS - 1 of a factor, a step of BK terms at a time; NT lanes load a value
+// The rows r0 .. r0 + ROWS - 1 of a factor, a step of BK terms at a time; NT lanes load V values
 // each.  KC: the sum's axis is innermost.  Otherwise the columns of term k are exchanged by 16
 // (COLS: by 8) with k / 4, so that the four lanes of a column that read four terms apart
 // touch different banks.
 template <bool COLS> constexpr int kExchange = COLS ? 8 : 16;
-template <bool KC, bool COLS, int ROWS> struct Loader {
-  static constexpr int N = ROWS * BK / NT;
+template <bool KC, bool COLS, int ROWS, int V> struct Loader {
+  static constexpr int N = ROWS * BK / (NT * V), LINE = (KC ? BK : ROWS) / V;  // loads; lanes of a line in LDS
   const char *base;
-  long long advance, row_bytes;
-  uint32_t off[KC ? 2 : 4];  // of the lane's value, by what the exchange has for a load
-  int term[KC ? 2 : 1], row;  // of load 0; not KC: row is the column in LDS
-  int have;
+  long long advance;  // bytes of a step
+  uint32_t off[N];
+  int term[2];  // the lane's (first) term: in loads of kind 0 and 1, or (not KC) of load 0
   __device__ __forceinline__ Loader(const float *p, long long rows, long long terms, int r0, long long k0) {
     const long long ld = KC ? terms : rows;
     base = (const char *)(p + (KC ? r0 * ld + k0 : k0 * ld + r0));
-    row_bytes = ld * 4;
-    advance = KC ? BK * 4 : BK * row_bytes;
-    have = (int)min(rows - r0, (long long)ROWS);
-    if constexpr (KC) {
-      // load i has rows 8 i ..: bit 2 of their exchange is bit 0 of i, with COLS bit 2
-      row = threadIdx.x >> 5;
-      const int d = threadIdx.x & 31;
+    advance = (KC ? 1 : ld) * BK * 4;
+    const long long have = rows - r0;
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        term[b] = ((d >> 2) ^ (row >> 1 | b << 2)) * 4 + (d & 3);
-        off[b] = (uint32_t)(row * row_bytes) + term[b] * 4;
+    for (int i = 0; i < N; ++i) {
+      const int line = (i * NT + threadIdx.x) / LINE, at = threadIdx.x % LINE * V;
+      if constexpr (KC) {
+        const int k = ((at >> 2) ^ swizzle<COLS>(line)) * 4 + (at & 3);
+        off[i] = line < have ? (uint32_t)(line * ld * 4) + k * 4 : kOut;
+        term[kind(i)] = k;
+      } else {
+        const int c = at ^ ((line >> 2) & 3) * kExchange<COLS>;
+        off[i] = c < have ? (uint32_t)(line * ld * 4) + c * 4 : kOut;
+        if (i == 0) term[0] = term[1] = line;
       }
-    } else {
-      term[0] = threadIdx.x / ROWS;
-      row = threadIdx.x % ROWS;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) off[e] = (uint32_t)(term[0] * row_bytes) + (row ^ e * kExchange<COLS>) * 4;
     }
+  }
+  // KC: what load i's lines have in their exchange beyond those of load 0 or 1
+  static constexpr int kind(int i) {
+    constexpr int PER = NT / LINE;  // lines of a load: 8 or 32
+    return COLS ? (i * PER >> 5) & 1 : (i * PER >> 3) & 1;
   }
   // Load i of the next step to `stage` (bytes from the LDS's start); `rest` terms are left.
   // (Written out, with the kernel's own waits, as in the bf16 kernels.)
   __device__ __forceinline__ void load(int i, int wave, uint32_t stage, int rest) const {
-    uint32_t o;
-    const char *b;
-    if constexpr (KC) {
-      const int e = COLS ? (i >> 2) & 1 : i & 1;
-      o = row + 8 * i < have && term[e] < rest ? off[e] : kOut;
-      b = base + 8 * i * row_bytes;
-    } else {
-      constexpr int PER = NT / ROWS;  // terms of a load
-      const int k = i * PER, e = (k >> 2) & 3;
-      o = (row ^ e * kExchange<COLS>) < have && term[0] + k < rest ? off[e] : kOut;
-      b = base + k * row_bytes;
-    }
-    const u32x4_t r = {(uint32_t)(uintptr_t)b, (uint32_t)((uintptr_t)b >> 32) & 0xffffu, 0x7ffffff0u, 0x00020000u};
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
-                 :
-                 : "s"(stage + (uint32_t)(i * NT + wave * 64) * 4), "v"(o), "s"(r)
-                 : "memory");
+    const uint32_t o = (KC ? term[kind(i)] < rest : term[0] < rest - i * (NT / LINE)) ? off[i] : kOut;
+    const u32x4_t r = {(uint32_t)(uintptr_t)base, (uint32_t)((uintptr_t)base >> 32) & 0xffffu, 0x7ffffff0u, 0x00020000u};
+    const uint32_t to = stage + (uint32_t)(i * NT + wave * 64) * 4 * V;
+    if constexpr (V == 4)
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(to), "v"(o), "s"(r) : "memory");
+    else
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" : : "s"(to), "v"(o), "s"(r) : "memory");
   }
   __device__ __forceinline__ void next() { base += advance; }
 };
@@ -105,7 +96,7 @@ template <bool KC, bool COLS, int ROWS> struct Reader {
   }
 };
 
-template <int KERNEL, int FORM, int ACT>
+template <int KERNEL, int FORM, int ACT, int V>
 __global__ __launch_bounds__(NT, Tile<KERNEL>::WAVES) void product_kernel(LinearPlan p, long long per_xcd, const float *A,
                                                                           const float *B, LinearEpilogue E, void *out,
                                                                           float *part) {
@@ -126,8 +117,8 @@ __global__ __launch_bounds__(NT, Tile<KERNEL>::WAVES) void product_kernel(Linear
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / C::WN, wn = wave % C::WN;
-  Loader<Form<FORM>::AK, false, C::B> la(A, p.M, p.L, i0, k0);
-  Loader<Form<FORM>::BK, true, C::B> lb(B, p.N, p.L, j0, k0);
+  Loader<Form<FORM>::AK, false, C::B, V> la(A, p.M, p.L, i0, k0);
+  Loader<Form<FORM>::BK, true, C::B, V> lb(B, p.N, p.L, j0, k0);
   const Reader<Form<FORM>::AK, false, C::B> ra;
   const Reader<Form<FORM>::BK, true, C::B> rb;
   constexpr int NA = decltype(la)::N, LOADS = NA + decltype(lb)::N;
@@ -226,6 +217,11 @@ __global__ __launch_bounds__(NT, Tile<KERNEL>::WAVES) void product_kernel(Linear
   }
 }
 
+// of the rows of A or B as they lie in memory
+long long row_length(int form, bool a, long long M, int N, long long L) {
+  return a ? (form == FORM_WEIGHT ? M : L) : form == FORM_DATA ? L : N;
+}
+
 struct Cost {
   int kernel, b;
   double fixed, step;  // us of a tile, and of 32 terms of it
@@ -236,7 +232,7 @@ constexpr Cost kCost[] = {{LIN_128, 128, 6.0, 2.3}, {LIN_64, 64, 3.0, 0.65}};
 
 bool linear_f32_plan(int form, long long M, int N, long long L, LinearPlan *p) {
   // 32-bit offsets inside a tile's rows, and its first row's and column's numbers
-  const long long la = form == FORM_WEIGHT ? M : L, lb = form == FORM_DATA ? L : N;
+  const long long la = row_length(form, true, M, N, L), lb = row_length(form, false, M, N, L);
   if (la >= (1LL << 22) || lb >= (1LL << 22) || M >= (1LL << 31) - 256) return false;
   double best = 1e30;
   for (const Cost &c : kCost) {
@@ -266,9 +262,17 @@ hipError_t launch_form(const LinearPlan &p, const float *A, const float *B, cons
   with_act(E.act, [&](auto a) {
     constexpr int ACT = FORM == FORM_WEIGHT ? (int)ACT_NONE : decltype(a)::value;
     const dim3 grid = long_grid(8 * per_xcd), block(NT);
-    if (p.kernel == LIN_128)
-      hipLaunchKernelGGL((product_kernel<LIN_128, FORM, ACT>), grid, block, 0, st, p, per_xcd, A, B, E, out, part);
-    else hipLaunchKernelGGL((product_kernel<LIN_64, FORM, ACT>), grid, block, 0, st, p, per_xcd, A, B, E, out, part);
+    auto run = [&](auto k, auto v) {
+      hipLaunchKernelGGL((product_kernel<decltype(k)::value, FORM, ACT, decltype(v)::value>), grid, block, 0, st, p, per_xcd, A, B,
+                         E, out, part);
+    };
+    constexpr std::integral_constant<int, LIN_128> big;
+    constexpr std::integral_constant<int, LIN_64> small;
+    constexpr std::integral_constant<int, 4> pieces;
+    constexpr std::integral_constant<int, 1> values;
+    const bool whole = row_length(FORM, true, p.M, p.N, p.L) % 4 == 0 && row_length(FORM, false, p.M, p.N, p.L) % 4 == 0;
+    if (p.kernel == LIN_128) whole ? run(big, pieces) : run(big, values);
+    else whole ? run(small, pieces) : run(small, values);
   });
   return hipGetLastError();
 }
