@@ -28,6 +28,10 @@ struct LinearPlan {
   int tm, tn;
   int slices;
   long long per;
+  // row lengths of A and B as the kernel reads them, and (bf16) whether they are copies in
+  // the workspace, of rows of whole 16-byte pieces
+  long long lda, ldb;
+  int copy_a, copy_b;
 };
 enum : int { LIN_ANY = 0, LIN_256 = 1, LIN_128 = 2, LIN_64 = 3 };
 
@@ -38,8 +42,16 @@ inline dim3 long_grid(long long n) {
 }
 __device__ __forceinline__ long long long_index() { return (long long)blockIdx.y * gridDim.x + blockIdx.x; }
 
-// The bf16 kernels (linear_bf16.hip): rows of whole 16-byte pieces.  part: the slices' sums
-// [slices][M][N] where there are several.
+// Rows and row length of a factor as it lies in memory.
+inline long long row_length(int form, bool a, long long M, int N, long long L) {
+  return a ? (form == FORM_WEIGHT ? M : L) : form == FORM_DATA ? L : N;
+}
+inline long long row_count(int form, bool a, long long M, int N, long long L) {
+  return a ? (form == FORM_WEIGHT ? L : M) : form == FORM_DATA ? N : L;
+}
+
+// The bf16 kernels (linear_bf16.hip).  part: the slices' sums [slices][M][N] where there are
+// several.
 bool linear_bf16_plan(int form, long long M, int N, long long L, LinearPlan *p);
 hipError_t launch_linear_bf16(int form, const LinearPlan &p, const void *A, const void *B, const LinearEpilogue &E, void *out,
                               float *part, hipStream_t st);
@@ -91,15 +103,20 @@ __device__ __forceinline__ void transpose4(float &a, float &b, float &c, float &
   swap16(c, d);
 }
 
-// Eight neighbouring values of a row, of which n exist.  bf16 rows are whole 16-byte pieces;
-// fp32 ones start anywhere.
+// Eight neighbouring values of a row, of which n exist; rows start anywhere.
 typedef uint32_t u32x4e4_t __attribute__((ext_vector_type(4), aligned(4)));
-__device__ __forceinline__ void load8(const uint16_t *p, int, float (&x)[8]) {
-  const u32x4_t a = *reinterpret_cast<const u32x4_t *>(p);
+typedef uint32_t u32x4e2_t __attribute__((ext_vector_type(4), aligned(2)));
+__device__ __forceinline__ void load8(const uint16_t *p, int n, float (&x)[8]) {
+  if (n >= 8) {
+    const u32x4_t a = *reinterpret_cast<const u32x4e2_t *>(p);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(a[i] << 16);
-    x[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(a[i] << 16);
+      x[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = i < n ? bf2f(p[i]) : 0.f;
   }
 }
 __device__ __forceinline__ void load8(const float *p, int n, float (&x)[8]) {
@@ -115,7 +132,15 @@ __device__ __forceinline__ void load8(const float *p, int n, float (&x)[8]) {
     for (int i = 0; i < 8; ++i) x[i] = i < n ? p[i] : 0.f;
   }
 }
-__device__ __forceinline__ void store8(uint16_t *p, int, const float (&x)[8]) { *reinterpret_cast<u32x4_t *>(p) = pack_bf16x8(x); }
+__device__ __forceinline__ void store8(uint16_t *p, int n, const float (&x)[8]) {
+  if (n >= 8) {
+    *reinterpret_cast<u32x4e2_t *>(p) = pack_bf16x8(x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) p[i] = f2bf(x[i]);
+  }
+}
 __device__ __forceinline__ void store8(float *p, int n, const float (&x)[8]) {
   if (n >= 8) {
     u32x4_t a, b;

@@ -126,6 +126,23 @@ __global__ __launch_bounds__(kThreads) void join_kernel(long long M, int N, int 
   put<DT, FORM, ACT>(E, out, at / N, (int)(at % N), N, v);
 }
 
+// The same for rows of whole 16-byte pieces of bf16: eight outputs a thread.
+template <int FORM, int ACT>
+__global__ __launch_bounds__(kThreads) void join8_kernel(LinearPlan p, const float *part, LinearEpilogue E, void *out) {
+  const long long n = p.M * p.N, at = (long_index() * kThreads + threadIdx.x) * 8;
+  if (at >= n) return;
+  float v[8];
+  for (int s = 0; s < p.slices; ++s) {
+    const float4 a = *reinterpret_cast<const float4 *>(part + s * n + at), b = *reinterpret_cast<const float4 *>(part + s * n + at + 4);
+    const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = s ? v[q] + x[q] : x[q];
+  }
+  float bias[8];
+  load_bias<FORM>(E, (int)(at % p.N), p.N, bias);
+  put8<DT_BF16, FORM, ACT>(E, bias, out, at, 8, v);
+}
+
 // part[slice][N] = sums of the slice's rows of dz
 template <int DT>
 __global__ __launch_bounds__(kThreads) void colsum_kernel(long long M, int N, long long per, const void *dz_, float *part) {
@@ -206,10 +223,35 @@ LinearPlan plan_of(int form, long long M, int N, long long L, int dtype) {
   if (dtype == DT_BF16 ? linear_bf16_plan(form, M, N, L, &p) : linear_f32_plan(form, M, N, L, &p)) return p;
   const int slices = slices_of(M, N, L);
   const long long per = ((L + slices - 1) / slices + 31) / 32 * 32;
-  return LinearPlan{M, L, N, LIN_ANY, (int)((M + 63) / 64), (N + 63) / 64, (int)((L + per - 1) / per), per};
+  return LinearPlan{M, L, N, LIN_ANY, (int)((M + 63) / 64), (N + 63) / 64, (int)((L + per - 1) / per), per, 0, 0, 0, 0};
 }
+// the workspace holds the slices' sums, then the copies of A and of B
 size_t slices_bytes(const LinearPlan &p) {
   return p.slices > 1 ? ((size_t)p.slices * p.M * p.N * 4 + 15) / 16 * 16 : 0;
+}
+size_t copy_bytes(int form, bool a, const LinearPlan &p) {
+  return (a ? p.copy_a : p.copy_b) ? (size_t)row_count(form, a, p.M, p.N, p.L) * (a ? p.lda : p.ldb) * 2 : 0;
+}
+size_t plan_bytes(int form, const LinearPlan &p) {
+  return slices_bytes(p) + copy_bytes(form, true, p) + copy_bytes(form, false, p);
+}
+
+// rows of n values to rows of ld, a multiple of 8, the rest zeros; a thread a piece of eight
+__global__ __launch_bounds__(kThreads) void pad_rows_kernel(long long rows, int n, int ld, const uint16_t *in, uint16_t *out) {
+  const long long id = long_index() * kThreads + threadIdx.x, row = id / (ld / 8);
+  if (row >= rows) return;
+  const int c = (int)(id % (ld / 8)) * 8;
+  const uint16_t *p = in + row * n + c;
+  u32x4_t v;
+  if (c + 8 <= n) {
+    v = *reinterpret_cast<const u32x4e2_t *>(p);
+  } else {
+    uint32_t h[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) h[i] = c + i < n ? p[i] : 0u;
+    v = u32x4_t{h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16};
+  }
+  *reinterpret_cast<u32x4_t *>(out + row * ld + c) = v;
 }
 
 template <int FORM>
@@ -217,8 +259,20 @@ hipError_t product(long long M, int N, long long L, int dtype, const void *A, co
                    void *ws, hipStream_t st) {
   const LinearPlan p = plan_of(FORM, M, N, L, dtype);
   float *part = (float *)ws;
-  if (p.kernel != LIN_ANY && dtype == DT_BF16) return launch_linear_bf16(FORM, p, A, B, E, out, part, st);
-  if (p.kernel != LIN_ANY) {
+  auto padded = [&](bool a, const void *src, char *dst) -> const void * {
+    if (!copy_bytes(FORM, a, p)) return src;
+    const long long rows = row_count(FORM, a, M, N, L), ld = a ? p.lda : p.ldb;
+    hipLaunchKernelGGL(pad_rows_kernel, long_grid((rows * (ld / 8) + kThreads - 1) / kThreads), dim3(kThreads), 0, st, rows,
+                       (int)row_length(FORM, a, M, N, L), (int)ld, (const uint16_t *)src, (uint16_t *)dst);
+    return dst;
+  };
+  char *copies = (char *)ws + slices_bytes(p);
+  A = padded(true, A, copies);
+  B = padded(false, B, copies + copy_bytes(FORM, true, p));
+  if (p.kernel != LIN_ANY && dtype == DT_BF16) {
+    const hipError_t r = launch_linear_bf16(FORM, p, A, B, E, out, part, st);
+    if (r != hipSuccess) return r;
+  } else if (p.kernel != LIN_ANY) {
     const hipError_t r = launch_linear_f32(FORM, p, A, B, E, out, part, st);
     if (r != hipSuccess) return r;
   }
@@ -228,7 +282,10 @@ hipError_t product(long long M, int N, long long L, int dtype, const void *A, co
     if (p.kernel != LIN_ANY) {
     } else if (dtype == DT_BF16) hipLaunchKernelGGL((any_kernel<DT_BF16, FORM, ACT>), grid, block, 0, st, p, A, B, E, out, part);
     else hipLaunchKernelGGL((any_kernel<DT_F32, FORM, ACT>), grid, block, 0, st, p, A, B, E, out, part);
-    if (p.slices > 1 && FORM != FORM_WEIGHT) {
+    if (p.slices > 1 && FORM != FORM_WEIGHT && p.kernel != LIN_ANY && dtype == DT_BF16 && N % 8 == 0) {
+      hipLaunchKernelGGL((join8_kernel<FORM, ACT>), long_grid((M * N / 8 + kThreads - 1) / kThreads), block, 0, st, p,
+                         (const float *)part, E, out);
+    } else if (p.slices > 1 && FORM != FORM_WEIGHT) {
       const dim3 all = long_grid((M * N + kThreads - 1) / kThreads);
       if (dtype == DT_BF16)
         hipLaunchKernelGGL((join_kernel<DT_BF16, FORM, ACT>), all, block, 0, st, M, N, p.slices, (const float *)part, E, out);
@@ -243,14 +300,14 @@ hipError_t product(long long M, int N, long long L, int dtype, const void *A, co
 
 }  // namespace
 
-size_t linear_fwd_workspace(long long M, int K, int N, int dtype) { return slices_bytes(plan_of(FORM_FWD, M, N, K, dtype)); }
+size_t linear_fwd_workspace(long long M, int K, int N, int dtype) { return plan_bytes(FORM_FWD, plan_of(FORM_FWD, M, N, K, dtype)); }
 size_t linear_bwd_data_workspace(long long M, int K, int N, int dtype) {
-  return slices_bytes(plan_of(FORM_DATA, M, K, N, dtype));
+  return plan_bytes(FORM_DATA, plan_of(FORM_DATA, M, K, N, dtype));
 }
 // (the column sums come after the product, in the same place)
 size_t linear_bwd_weight_workspace(long long M, int K, int N, int dtype) {
   const size_t sums = ((size_t)colsum_slices(M, N, dtype) * N * 4 + 15) / 16 * 16;
-  return std::max(sums, slices_bytes(plan_of(FORM_WEIGHT, K, N, M, dtype)));
+  return std::max(sums, plan_bytes(FORM_WEIGHT, plan_of(FORM_WEIGHT, K, N, M, dtype)));
 }
 
 hipError_t launch_linear_fwd(long long M, int K, int N, int dtype, const void *x, const void *w, const LinearEpilogue &e,

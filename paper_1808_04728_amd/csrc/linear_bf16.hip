@@ -47,8 +47,7 @@ template <bool KC, bool COLS, int ROWS, int NT> struct Loader {
   long long advance;  // bytes of a step
   uint32_t off[N];
   int term;  // the lane's first piece's (first) term of a step
-  __device__ __forceinline__ Loader(const uint16_t *p, long long rows, long long terms, int r0, long long k0) {
-    const long long ld = KC ? terms : rows;
+  __device__ __forceinline__ Loader(const uint16_t *p, long long rows, long long ld, int r0, long long k0) {
     base = (const char *)(p + (KC ? r0 * ld + k0 : k0 * ld + r0));
     advance = KC ? BK * 2 : BK * ld * 2;
     const long long have = rows - r0;
@@ -140,8 +139,8 @@ __global__ __launch_bounds__(threads_of<Tile<KERNEL>>(), Tile<KERNEL>::WAVES) vo
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / C::WN, wn = wave % C::WN;
-  Loader<Form<FORM>::AK, false, C::BM, NT> la(A, p.M, p.L, i0, k0);
-  Loader<Form<FORM>::BK, true, C::BN, NT> lb(B, p.N, p.L, j0, k0);
+  Loader<Form<FORM>::AK, false, C::BM, NT> la(A, p.M, p.lda, i0, k0);
+  Loader<Form<FORM>::BK, true, C::BN, NT> lb(B, p.N, p.ldb, j0, k0);
   const Reader<Form<FORM>::AK, false> ra;
   const Reader<Form<FORM>::BK, true> rb;
   constexpr int LOADS = decltype(la)::N + decltype(lb)::N;
@@ -221,8 +220,8 @@ __global__ __launch_bounds__(threads_of<Tile<KERNEL>>(), Tile<KERNEL>::WAVES) vo
   for (int jj = 0; jj < TN; jj += 4) {
     const int j = j0 + (wn * TN + jj) * 16 + 8 * g;
     float bias[2][8];
-    load_bias<FORM>(E, j, p.N, bias[0]);
-    load_bias<FORM>(E, j + 32, p.N, bias[1]);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) load_bias<FORM>(E, j + 32 * h, p.N, bias[h]);
 #pragma unroll
     for (int ii = 0; ii < TM; ++ii) {
       float row[16];
@@ -236,32 +235,16 @@ __global__ __launch_bounds__(threads_of<Tile<KERNEL>>(), Tile<KERNEL>::WAVES) vo
       if (i >= p.M) continue;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        if (j + 32 * h >= p.N) continue;
+        const int n = p.N - j - 32 * h;
+        if (n <= 0) continue;
         float v[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) v[q] = row[8 * h + q];
-        if (whole) put8<DT_BF16, FORM, ACT>(E, bias[h], out, i * p.N + j + 32 * h, 8, v);
-        else put8<DT_BF16, FORM_WEIGHT, ACT_NONE>(E, none, part, (slice * p.M + i) * p.N + j + 32 * h, 8, v);
+        if (whole) put8<DT_BF16, FORM, ACT>(E, bias[h], out, i * p.N + j + 32 * h, n, v);
+        else put8<DT_BF16, FORM_WEIGHT, ACT_NONE>(E, none, part, (slice * p.M + i) * p.N + j + 32 * h, n, v);
       }
     }
   }
-}
-
-// the slices' sum, in slice order, and the epilogue; eight outputs a thread
-template <int FORM, int ACT>
-__global__ __launch_bounds__(256) void join8_kernel(LinearPlan p, const float *part, LinearEpilogue E, void *out) {
-  const long long n = p.M * p.N, at = (long_index() * 256 + threadIdx.x) * 8;
-  if (at >= n) return;
-  float v[8];
-  for (int s = 0; s < p.slices; ++s) {
-    const float4 a = *reinterpret_cast<const float4 *>(part + s * n + at), b = *reinterpret_cast<const float4 *>(part + s * n + at + 4);
-    const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-    for (int q = 0; q < 8; ++q) v[q] = s ? v[q] + x[q] : x[q];
-  }
-  float bias[8];
-  load_bias<FORM>(E, (int)(at % p.N), p.N, bias);
-  put8<DT_BF16, FORM, ACT>(E, bias, out, at, 8, v);
 }
 
 struct Cost {
@@ -273,10 +256,11 @@ constexpr Cost kCost[] = {{LIN_256, 256, 256, 64, 8.0, 0.90}, {LIN_128, 128, 128
 }  // namespace
 
 bool linear_bf16_plan(int form, long long M, int N, long long L, LinearPlan *p) {
-  // rows of whole 16-byte pieces, and 32-bit offsets inside a tile's rows
-  const long long la = form == FORM_WEIGHT ? M : L, lb = form == FORM_DATA ? L : N;
-  if (la % 8 || lb % 8 || N % 8 || la >= (1LL << 22) || lb >= (1LL << 22)) return false;
-  if (M >= (1LL << 31) - 256) return false;
+  // 32-bit offsets inside a tile's rows, and its first row's and column's numbers.  Rows that
+  // are not whole 16-byte pieces are copied to such ones first: a copy of both factors costs
+  // what it reads and writes, and a kernel that loaded them value by value ten times as much.
+  const long long la = row_length(form, true, M, N, L), lb = row_length(form, false, M, N, L);
+  if (la >= (1LL << 22) || lb >= (1LL << 22) || M >= (1LL << 31) - 256) return false;
   double best = 1e30;
   for (const Cost &c : kCost) {
     const long long tm = (M + c.bm - 1) / c.bm, tn = (N + c.bn - 1) / c.bn, tiles = tm * tn, steps = (L + 63) / 64;
@@ -290,7 +274,8 @@ bool linear_bf16_plan(int form, long long M, int N, long long L, LinearPlan *p) 
       if (t < best) {
         best = t;
         const long long per = ((L + slices - 1) / slices + 63) / 64 * 64;
-        *p = LinearPlan{M, L, N, c.kernel, (int)tm, (int)tn, (int)((L + per - 1) / per), per};
+        *p = LinearPlan{M, L, N, c.kernel, (int)tm, (int)tn, (int)((L + per - 1) / per), per,
+                       (la + 7) / 8 * 8, (lb + 7) / 8 * 8, la % 8 != 0, lb % 8 != 0};
       }
     }
   }
@@ -312,13 +297,8 @@ hipError_t launch_form(const LinearPlan &p, const uint16_t *A, const uint16_t *B
     if (p.kernel == LIN_256) run(std::integral_constant<int, LIN_256>{});
     else if (p.kernel == LIN_128) run(std::integral_constant<int, LIN_128>{});
     else run(std::integral_constant<int, LIN_64>{});
-    if (p.slices > 1 && FORM != FORM_WEIGHT)
-      hipLaunchKernelGGL((join8_kernel<FORM, ACT>), long_grid((p.M * p.N / 8 + 255) / 256), dim3(256), 0, st, p,
-                         (const float *)part, E, out);
   });
-  const hipError_t r = hipGetLastError();
-  if (r != hipSuccess || p.slices == 1 || FORM != FORM_WEIGHT) return r;
-  return launch_sum_rows(part, (float *)out, p.slices, (int)(p.M * p.N), st);
+  return hipGetLastError();
 }
 }  // namespace
 

@@ -217,11 +217,6 @@ __global__ __launch_bounds__(NT, Tile<KERNEL>::WAVES) void product_kernel(Linear
   }
 }
 
-// of the rows of A or B as they lie in memory
-long long row_length(int form, bool a, long long M, int N, long long L) {
-  return a ? (form == FORM_WEIGHT ? M : L) : form == FORM_DATA ? L : N;
-}
-
 struct Cost {
   int kernel, b;
   double fixed, step;  // us of a tile, and of 32 terms of it
@@ -247,7 +242,7 @@ bool linear_f32_plan(int form, long long M, int N, long long L, LinearPlan *p) {
       if (t < best) {
         best = t;
         const long long per = ((L + slices - 1) / slices + BK - 1) / BK * BK;
-        *p = LinearPlan{M, L, N, c.kernel, (int)tm, (int)tn, (int)((L + per - 1) / per), per};
+        *p = LinearPlan{M, L, N, c.kernel, (int)tm, (int)tn, (int)((L + per - 1) / per), per, la, lb, 0, 0};
       }
     }
   }
@@ -270,7 +265,7 @@ hipError_t launch_form(const LinearPlan &p, const float *A, const float *B, cons
     constexpr std::integral_constant<int, LIN_64> small;
     constexpr std::integral_constant<int, 4> pieces;
     constexpr std::integral_constant<int, 1> values;
-    const bool whole = row_length(FORM, true, p.M, p.N, p.L) % 4 == 0 && row_length(FORM, false, p.M, p.N, p.L) % 4 == 0;
+    const bool whole = p.lda % 4 == 0 && p.ldb % 4 == 0;
     if (p.kernel == LIN_128) whole ? run(big, pieces) : run(big, values);
     else whole ? run(small, pieces) : run(small, values);
   });
