@@ -255,9 +255,10 @@ __global__ __launch_bounds__(kThreads) void pad_rows_kernel(long long rows, int 
 }
 
 template <int FORM>
-hipError_t product(long long M, int N, long long L, int dtype, const void *A, const void *B, const LinearEpilogue &E, void *out,
+hipError_t product(const LinearPlan &p, int dtype, const void *A, const void *B, const LinearEpilogue &E, void *out, float *db,
                    void *ws, hipStream_t st) {
-  const LinearPlan p = plan_of(FORM, M, N, L, dtype);
+  const long long M = p.M, L = p.L;
+  const int N = p.N;
   float *part = (float *)ws;
   auto padded = [&](bool a, const void *src, char *dst) -> const void * {
     if (!copy_bytes(FORM, a, p)) return src;
@@ -270,10 +271,10 @@ hipError_t product(long long M, int N, long long L, int dtype, const void *A, co
   A = padded(true, A, copies);
   B = padded(false, B, copies + copy_bytes(FORM, true, p));
   if (p.kernel != LIN_ANY && dtype == DT_BF16) {
-    const hipError_t r = launch_linear_bf16(FORM, p, A, B, E, out, part, st);
+    const hipError_t r = launch_linear_bf16(FORM, p, A, B, E, out, part, db, st);
     if (r != hipSuccess) return r;
   } else if (p.kernel != LIN_ANY) {
-    const hipError_t r = launch_linear_f32(FORM, p, A, B, E, out, part, st);
+    const hipError_t r = launch_linear_f32(FORM, p, A, B, E, out, part, db, st);
     if (r != hipSuccess) return r;
   }
   const dim3 grid = long_grid((long long)p.tm * p.tn * p.slices), block(kThreads);
@@ -292,10 +293,7 @@ hipError_t product(long long M, int N, long long L, int dtype, const void *A, co
       else hipLaunchKernelGGL((join_kernel<DT_F32, FORM, ACT>), all, block, 0, st, M, N, p.slices, (const float *)part, E, out);
     }
   });
-  const hipError_t r = hipGetLastError();
-  if (r != hipSuccess || p.slices == 1 || FORM != FORM_WEIGHT) return r;
-  // (slices of more than one have fewer than 2^28 values in all, or fill 512 tiles of 4096)
-  return launch_sum_rows(part, (float *)out, p.slices, (int)(M * N), st);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -304,40 +302,51 @@ size_t linear_fwd_workspace(long long M, int K, int N, int dtype) { return plan_
 size_t linear_bwd_data_workspace(long long M, int K, int N, int dtype) {
   return plan_bytes(FORM_DATA, plan_of(FORM_DATA, M, K, N, dtype));
 }
-// (the column sums come after the product, in the same place)
+// the rows of column sums that a bias gradient is joined from, behind the product's workspace
+int db_rows(const LinearPlan &p, long long M, int N, int dtype) {
+  return p.kernel == LIN_ANY ? colsum_slices(M, N, dtype) : p.slices * db_turns(p);
+}
 size_t linear_bwd_weight_workspace(long long M, int K, int N, int dtype) {
-  const size_t sums = ((size_t)colsum_slices(M, N, dtype) * N * 4 + 15) / 16 * 16;
-  return std::max(sums, plan_bytes(FORM_WEIGHT, plan_of(FORM_WEIGHT, K, N, M, dtype)));
+  const LinearPlan p = plan_of(FORM_WEIGHT, K, N, M, dtype);
+  return plan_bytes(FORM_WEIGHT, p) + ((size_t)db_rows(p, M, N, dtype) * N * 4 + 15) / 16 * 16;
 }
 
 hipError_t launch_linear_fwd(long long M, int K, int N, int dtype, const void *x, const void *w, const LinearEpilogue &e,
                              void *y, void *ws, hipStream_t st) {
-  return product<FORM_FWD>(M, N, K, dtype, x, w, e, y, ws, st);
+  return product<FORM_FWD>(plan_of(FORM_FWD, M, N, K, dtype), dtype, x, w, e, y, nullptr, ws, st);
 }
 
 hipError_t launch_linear_bwd_data(long long M, int K, int N, int dtype, const void *dz, const void *w,
                                   const LinearEpilogue &e, void *dx, void *ws, hipStream_t st) {
-  return product<FORM_DATA>(M, K, N, dtype, dz, w, e, dx, ws, st);
+  return product<FORM_DATA>(plan_of(FORM_DATA, M, K, N, dtype), dtype, dz, w, e, dx, nullptr, ws, st);
 }
 
 hipError_t launch_linear_bwd_weight(long long M, int K, int N, int dtype, const void *x, const void *dz, float *dw, float *db,
                                     void *ws, hipStream_t st) {
   const LinearEpilogue none{nullptr, nullptr, nullptr, nullptr, ACT_NONE, 0.f};
-  hipError_t r = product<FORM_WEIGHT>(K, N, M, dtype, x, dz, none, dw, ws, st);
-  if (r != hipSuccess || !db) return r;
-  const int slices = colsum_slices(M, N, dtype);
-  const long long per = (M + slices - 1) / slices;
-  const dim3 grid((unsigned)((long long)slices * colsum_tiles(N, dtype))), block(kThreads);
-  float *part = (float *)ws;
-  auto run = [&](auto dt) {
-    constexpr int DT = decltype(dt)::value;
-    if (colsum_vec(N, dtype)) hipLaunchKernelGGL((colsum_vec_kernel<DT>), grid, block, 0, st, M, N, per, dz, part);
-    else hipLaunchKernelGGL((colsum_kernel<DT>), grid, block, 0, st, M, N, per, dz, part);
-  };
-  if (dtype == DT_BF16) run(std::integral_constant<int, DT_BF16>{});
-  else run(std::integral_constant<int, DT_F32>{});
-  if ((r = hipGetLastError()) != hipSuccess) return r;
-  return launch_sum_rows((const float *)ws, db, slices, N, st);
+  const LinearPlan p = plan_of(FORM_WEIGHT, K, N, M, dtype);
+  const int rows = db_rows(p, M, N, dtype);
+  float *sums = (float *)((char *)ws + plan_bytes(FORM_WEIGHT, p));
+  hipError_t r = product<FORM_WEIGHT>(p, dtype, x, dz, none, dw, !db || p.kernel == LIN_ANY ? nullptr : rows == 1 ? db : sums, ws, st);
+  if (r != hipSuccess) return r;
+  if (db && p.kernel == LIN_ANY) {
+    const long long per = (M + rows - 1) / rows;
+    const dim3 grid((unsigned)((long long)rows * colsum_tiles(N, dtype))), block(kThreads);
+    auto run = [&](auto dt) {
+      constexpr int DT = decltype(dt)::value;
+      if (colsum_vec(N, dtype)) hipLaunchKernelGGL((colsum_vec_kernel<DT>), grid, block, 0, st, M, N, per, dz, sums);
+      else hipLaunchKernelGGL((colsum_kernel<DT>), grid, block, 0, st, M, N, per, dz, sums);
+    };
+    if (dtype == DT_BF16) run(std::integral_constant<int, DT_BF16>{});
+    else run(std::integral_constant<int, DT_F32>{});
+    if ((r = hipGetLastError()) != hipSuccess) return r;
+  }
+  // (slices of more than one have fewer than 2^28 values in all, or fill 512 tiles of 4096)
+  SumJob jobs[2];
+  int n = 0;
+  if (p.slices > 1) jobs[n++] = SumJob{(const float *)ws, dw, p.slices, (int)((long long)K * N)};
+  if (db && (rows > 1 || p.kernel == LIN_ANY)) jobs[n++] = SumJob{sums, db, rows, N};
+  return n ? launch_sum_batch(jobs, n, st) : hipSuccess;
 }
 
 }  // namespace cf

@@ -117,7 +117,8 @@ template <class C> constexpr int threads_of() { return 64 * C::WM * C::WN; }
 
 template <int KERNEL, int FORM, int ACT>
 __global__ __launch_bounds__(threads_of<Tile<KERNEL>>(), Tile<KERNEL>::WAVES) void product_kernel(
-    LinearPlan p, long long per_xcd, const uint16_t *A, const uint16_t *B, LinearEpilogue E, void *out, float *part) {
+    LinearPlan p, long long per_xcd, const uint16_t *A, const uint16_t *B, LinearEpilogue E, void *out, float *part,
+    float *db) {
   using C = Tile<KERNEL>;
   constexpr int NT = threads_of<C>(), TM = C::BM / C::WM / 16, TN = C::BN / C::WN / 16;
   static_assert(TN % 4 == 0, "a lane's row of the epilogue is sixteen columns of 64");
@@ -176,7 +177,20 @@ __global__ __launch_bounds__(threads_of<Tile<KERNEL>>(), Tile<KERNEL>::WAVES) vo
   // them: a load's issue takes its wave sixteen cycles and more, in front of all matrix
   // instructions a third of their time.
   constexpr int EARLY = TM > 2 ? TM - 2 : TM;  // the reads are under way this many rows before the end
+  const int turns = FORM == FORM_WEIGHT ? db_turns(p) : 0;
+  const bool sum_db = FORM == FORM_WEIGHT && db && wm == 0 && ti < turns;
+  ColumnSums<TN> sums(sum_db, ti, turns);
   auto half = [&](int f, const unsigned char *rs, int k, auto loads, int ls) {
+    if constexpr (FORM == FORM_WEIGHT) {
+      if (sums.mine) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+          const u32x4_t b = __builtin_bit_cast(u32x4_t, fb[f][j]);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) sums.s[j] += __uint_as_float(b[q] << 16) + __uint_as_float(b[q] & 0xffff0000u);
+        }
+      }
+    }
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
 #pragma unroll
@@ -209,8 +223,10 @@ __global__ __launch_bounds__(threads_of<Tile<KERNEL>>(), Tile<KERNEL>::WAVES) vo
     half(1, lds + after * STAGE, 0, std::integral_constant<int, LOADS>{}, slot);
     next();
     slot = after;
+    if constexpr (FORM == FORM_WEIGHT) sums.next_step();
   }
   wait_loads<0>();  // no load outlives the workgroup
+  if (sum_db) sums.store(db + (slice * turns + ti) * p.N, j0 + wn * 64, p.N);
 
   // lane (r, g) gets row r of each instruction tile, columns 8 g .. 8 g + 7 and 32 + 8 g .. of 64
   const int r = lane & 15, g = lane >> 4;
@@ -285,14 +301,14 @@ bool linear_bf16_plan(int form, long long M, int N, long long L, LinearPlan *p) 
 namespace {
 template <int FORM>
 hipError_t launch_form(const LinearPlan &p, const uint16_t *A, const uint16_t *B, const LinearEpilogue &E, void *out, float *part,
-                       hipStream_t st) {
+                       float *db, hipStream_t st) {
   const long long per_xcd = ((long long)p.tm * p.tn * p.slices + 7) / 8;
   with_act(E.act, [&](auto a) {
     constexpr int ACT = FORM == FORM_WEIGHT ? (int)ACT_NONE : decltype(a)::value;
     auto run = [&](auto k) {
       constexpr int KERNEL = decltype(k)::value;
       hipLaunchKernelGGL((product_kernel<KERNEL, FORM, ACT>), long_grid(8 * per_xcd), dim3(threads_of<Tile<KERNEL>>()), 0, st, p,
-                         per_xcd, A, B, E, out, part);
+                         per_xcd, A, B, E, out, part, db);
     };
     if (p.kernel == LIN_256) run(std::integral_constant<int, LIN_256>{});
     else if (p.kernel == LIN_128) run(std::integral_constant<int, LIN_128>{});
@@ -303,11 +319,11 @@ hipError_t launch_form(const LinearPlan &p, const uint16_t *A, const uint16_t *B
 }  // namespace
 
 hipError_t launch_linear_bf16(int form, const LinearPlan &p, const void *A, const void *B, const LinearEpilogue &E, void *out,
-                              float *part, hipStream_t st) {
+                              float *part, float *db, hipStream_t st) {
   const uint16_t *a = (const uint16_t *)A, *b = (const uint16_t *)B;
-  if (form == FORM_FWD) return launch_form<FORM_FWD>(p, a, b, E, out, part, st);
-  if (form == FORM_DATA) return launch_form<FORM_DATA>(p, a, b, E, out, part, st);
-  return launch_form<FORM_WEIGHT>(p, a, b, E, out, part, st);
+  if (form == FORM_FWD) return launch_form<FORM_FWD>(p, a, b, E, out, part, db, st);
+  if (form == FORM_DATA) return launch_form<FORM_DATA>(p, a, b, E, out, part, db, st);
+  return launch_form<FORM_WEIGHT>(p, a, b, E, out, part, db, st);
 }
 
 }  // namespace cf

@@ -99,7 +99,7 @@ template <bool KC, bool COLS, int ROWS> struct Reader {
 template <int KERNEL, int FORM, int ACT, int V>
 __global__ __launch_bounds__(NT, Tile<KERNEL>::WAVES) void product_kernel(LinearPlan p, long long per_xcd, const float *A,
                                                                           const float *B, LinearEpilogue E, void *out,
-                                                                          float *part) {
+                                                                          float *part, float *db) {
   using C = Tile<KERNEL>;
   constexpr int TM = C::B / C::WM / 16, TN = C::B / C::WN / 16, AB = C::B * BK * 4, STAGE = 2 * AB;
   static_assert(TN == 4 && 64 * C::WM * C::WN == NT, "a lane's row of the epilogue is sixteen columns of 64");
@@ -148,7 +148,17 @@ __global__ __launch_bounds__(NT, Tile<KERNEL>::WAVES) void product_kernel(Linear
     if (q < TN) fb[f][q] = rb.frag(stage + AB, wn * TN + q, k);
     else fa[f][q - TN] = ra.frag(stage, wm * TM + q - TN, k);
   };
+  const int ti = i0 / C::B;
+  const int turns = FORM == FORM_WEIGHT ? db_turns(p) : 0;
+  const bool sum_db = FORM == FORM_WEIGHT && db && wm == 0 && ti < turns;
+  ColumnSums<TN> sums(sum_db, ti, turns);
   auto half = [&](int f, const unsigned char *rs, int k, auto loads, int ls) {
+    if constexpr (FORM == FORM_WEIGHT) {
+      if (sums.mine) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j) sums.s[j] += (fb[f][j][0] + fb[f][j][1]) + (fb[f][j][2] + fb[f][j][3]);
+      }
+    }
     constexpr int GROUPS = 4 * TM, FIRST = 3 * TM;  // reads go out in the first groups
 #pragma unroll
     for (int n = 0; n < GROUPS; ++n) {
@@ -183,8 +193,10 @@ __global__ __launch_bounds__(NT, Tile<KERNEL>::WAVES) void product_kernel(Linear
     half(1, lds + after * STAGE, 0, std::integral_constant<int, LOADS>{}, slot);
     next();
     slot = after;
+    if constexpr (FORM == FORM_WEIGHT) sums.next_step();
   }
   wait_loads<0>();  // no load outlives the workgroup
+  if (sum_db) sums.store(db + (slice * turns + ti) * p.N, j0 + wn * 64, p.N);
 
   // lane (r, g) gets row r of each instruction tile, columns 8 g .. 8 g + 7 and 32 + 8 g .. of 64
   const int r = lane & 15, g = lane >> 4, j = j0 + wn * 64 + 8 * g;
@@ -252,14 +264,14 @@ bool linear_f32_plan(int form, long long M, int N, long long L, LinearPlan *p) {
 namespace {
 template <int FORM>
 hipError_t launch_form(const LinearPlan &p, const float *A, const float *B, const LinearEpilogue &E, void *out, float *part,
-                       hipStream_t st) {
+                       float *db, hipStream_t st) {
   const long long per_xcd = ((long long)p.tm * p.tn * p.slices + 7) / 8;
   with_act(E.act, [&](auto a) {
     constexpr int ACT = FORM == FORM_WEIGHT ? (int)ACT_NONE : decltype(a)::value;
     const dim3 grid = long_grid(8 * per_xcd), block(NT);
     auto run = [&](auto k, auto v) {
       hipLaunchKernelGGL((product_kernel<decltype(k)::value, FORM, ACT, decltype(v)::value>), grid, block, 0, st, p, per_xcd, A, B,
-                         E, out, part);
+                         E, out, part, db);
     };
     constexpr std::integral_constant<int, LIN_128> big;
     constexpr std::integral_constant<int, LIN_64> small;
@@ -274,11 +286,11 @@ hipError_t launch_form(const LinearPlan &p, const float *A, const float *B, cons
 }  // namespace
 
 hipError_t launch_linear_f32(int form, const LinearPlan &p, const void *A, const void *B, const LinearEpilogue &E, void *out,
-                             float *part, hipStream_t st) {
+                             float *part, float *db, hipStream_t st) {
   const float *a = (const float *)A, *b = (const float *)B;
-  if (form == FORM_FWD) return launch_form<FORM_FWD>(p, a, b, E, out, part, st);
-  if (form == FORM_DATA) return launch_form<FORM_DATA>(p, a, b, E, out, part, st);
-  return launch_form<FORM_WEIGHT>(p, a, b, E, out, part, st);
+  if (form == FORM_FWD) return launch_form<FORM_FWD>(p, a, b, E, out, part, db, st);
+  if (form == FORM_DATA) return launch_form<FORM_DATA>(p, a, b, E, out, part, db, st);
+  return launch_form<FORM_WEIGHT>(p, a, b, E, out, part, db, st);
 }
 
 }  // namespace cf
