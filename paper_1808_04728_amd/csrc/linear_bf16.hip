@@ -263,11 +263,19 @@ __global__ __launch_bounds__(threads_of<Tile<KERNEL>>(), Tile<KERNEL>::WAVES) vo
   }
 }
 
+// What a launch takes: `fixed` us of a workgroup and, of each 64 terms, `alone` and, the more
+// of the `at_once` workgroups that the card holds there are, up to `shared` more.  Measured,
+// us: 64 x 64 outputs of 1024 terms 22.8, 12.4, 8.0 with tiles of 256, 128, 64; 1024^3 25.4,
+// 13.2, 8.5; 1536^3 35.1, 20.4, 17.5; 8192 x 1024 of 1024 terms 30.9, 23.3, 32.5; 2048^3 44.6,
+// 28.4, 30.4; 4096 x 4096 of 1024 36.4, 43.4, 64.7.  Cut sums: 64 x 512 of 4096 with tiles of
+// 64 in 1, 4, 8, 16 slices 20.7, 12.1, 11.1, 12.0; 512 x 512 of 8192 37.7, 17.9, 18.3, 22.3;
+// 1024^3 in 1 and 2 slices 8.5 and 14.3.
 struct Cost {
-  int kernel, bm, bn, bk;
-  double fixed, step;  // us of a tile, and of 64 terms of it
+  int kernel, b, at_once;
+  double fixed, alone, shared;
 };
-constexpr Cost kCost[] = {{LIN_256, 256, 256, 64, 8.0, 0.90}, {LIN_128, 128, 128, 32, 5.0, 0.50}, {LIN_64, 64, 64, 64, 3.0, 0.25}};
+constexpr Cost kCost[] = {
+    {LIN_256, 256, kCUs, 6.0, 1.05, 0.50}, {LIN_128, 128, 2 * kCUs, 3.0, 0.55, 0.45}, {LIN_64, 64, 3 * kCUs, 1.5, 0.26, 0.34}};
 
 }  // namespace
 
@@ -279,14 +287,16 @@ bool linear_bf16_plan(int form, long long M, int N, long long L, LinearPlan *p) 
   if (la >= (1LL << 22) || lb >= (1LL << 22) || M >= (1LL << 31) - 256) return false;
   double best = 1e30;
   for (const Cost &c : kCost) {
-    const long long tm = (M + c.bm - 1) / c.bm, tn = (N + c.bn - 1) / c.bn, tiles = tm * tn, steps = (L + 63) / 64;
+    const long long tm = (M + c.b - 1) / c.b, tn = (N + c.b - 1) / c.b, tiles = tm * tn, steps = (L + 63) / 64;
     const long long chain = std::max(1LL, std::min((L + kChain - 1) / kChain, (1LL << 28) / (M * N)));
     for (long long s = 1; s <= 64; s = s < 4 ? s + 1 : s * 2) {
       const long long slices = std::max(s, chain);
       if (s > 1 && (steps / s < 4 || slices * M * N > (1LL << 28) || tiles * s > 4 * kCUs)) break;
-      const long long jobs = tiles * slices, rounds = (jobs + kCUs - 1) / kCUs;
-      double t = rounds * (c.fixed + c.step * ((steps + slices - 1) / slices));
-      if (slices > 1) t += 3.0 + slices * (double)M * N * 8 / 4e6;
+      const double full = (double)(tiles * slices) / c.at_once, step = c.alone + c.shared * std::min(1.0, full);
+      // (one workgroup a CU goes in whole rounds, several make room for the next one by one)
+      const double rounds = c.at_once == kCUs ? std::ceil(full) : std::max(1.0, full);
+      double t = rounds * (c.fixed + step * ((steps + slices - 1) / slices));
+      if (slices > 1) t += 3.5 + 0.15 * slices + slices * (double)M * N * 8 / 4e6;
       if (t < best) {
         best = t;
         const long long per = ((L + slices - 1) / slices + 63) / 64 * 64;

@@ -229,11 +229,17 @@ __global__ __launch_bounds__(NT, Tile<KERNEL>::WAVES) void product_kernel(Linear
   }
 }
 
+// What a launch takes: `fixed` us and, of each 32 terms, `step` us for the first workgroup on a
+// CU and `more` for each further one: the matrix pipes are shared.  Measured, us: 64 x 64
+// outputs of 1024 terms 69.9 and 24.4 with tiles of 128 and 64; 512^3 37.9, 14.4; 1024^3 69.8,
+// 25.8; 2048 x 1024 of 512 39.1, 23.7; 2048^3 139, 145; 4096 x 4096 of 1024 256, 280.  Cut
+// sums: 64 x 512 of 4096 with tiles of 64 in 1, 4, 8, 16, 32 slices 86, 27.5, 18.3, 15.6, 17.1;
+// 512 x 512 of 8192 169, 51.4, 47.2, 49.0, 54.9; 1024^3 in 1 and 2 slices 25.8 and 30.0.
 struct Cost {
   int kernel, b;
-  double fixed, step;  // us of a tile, and of 32 terms of it
+  double fixed, step, more;
 };
-constexpr Cost kCost[] = {{LIN_128, 128, 6.0, 2.3}, {LIN_64, 64, 3.0, 0.65}};
+constexpr Cost kCost[] = {{LIN_128, 128, 2.0, 2.05, 1.95}, {LIN_64, 64, 1.5, 0.65, 0.53}};
 
 }  // namespace
 
@@ -249,8 +255,8 @@ bool linear_f32_plan(int form, long long M, int N, long long L, LinearPlan *p) {
       const long long slices = std::max(s, chain);
       if (s > 1 && (steps / s < 4 || slices * M * N > (1LL << 28) || tiles * s > 8 * kCUs)) break;
       const long long rounds = (tiles * slices + kCUs - 1) / kCUs;
-      double t = rounds * (c.fixed + c.step * ((steps + slices - 1) / slices));
-      if (slices > 1) t += 3.0 + slices * (double)M * N * 8 / 4e6;
+      double t = c.fixed + (c.step + (rounds - 1) * c.more) * ((steps + slices - 1) / slices);
+      if (slices > 1) t += 3.5 + 0.15 * slices + slices * (double)M * N * 8 / 4e6;
       if (t < best) {
         best = t;
         const long long per = ((L + slices - 1) / slices + BK - 1) / BK * BK;
