@@ -1,16 +1,19 @@
-"""The whole network as it trains: convolution stack, layer normalisation of its
-output, fully-connected head, and one update of all parameters.
+"""The whole network as it trains: convolution stack, a block over the channels of each
+voxel if asked for, normalisation of its output, fully-connected head, and one update of
+all parameters.
 
-  forward   stack -> layer normalisation -> head -> loss
-  backward  head -> layer normalisation -> stack
-  update    matrices (convolution and fully-connected weights): momentum with
-            orthogonalised steps, one cf_muon_step call; vectors (biases, the
-            normalisation's gamma and beta): Adam + LARC, one cf_adam_larc_step call
+  forward   stack -> [mixer] -> normalisation -> head -> loss
+  backward  head -> normalisation -> [mixer] -> stack
+  update    "muon": matrices (the weights) take momentum with orthogonalised steps, one
+            cf_muon_step call; vectors (biases, the normalisations' gamma and beta) Adam +
+            LARC, one cf_adam_larc_step call
+            "adamw", "adamw8": one cf_adamw_step call for all of them, its two moments in
+            fp32 or in a byte a value; matrices decay, vectors do not
 
 The normalisation runs over a sample's whole output (``norm="sample"``: batch rows of
-d*h*w*c values) or over the channels of each voxel (``norm="voxel"``: batch*d*h*w
-rows of c).  The head then sees inputs of one scale whatever the updates do to the
-convolutions.
+d*h*w*c values), over the channels of each voxel (``norm="voxel"``: batch*d*h*w rows of
+c) or over groups of channels of a sample (``norm="group"``).  The head then sees inputs
+of one scale whatever the updates do to the convolutions.
 
 All parameters live in flat buffers, matrices first and vectors after them, each on
 a multiple of 16 elements: fp32 values, fp32 gradients, and for a bf16 network the
@@ -21,6 +24,7 @@ bf16 weights that the products read.
 from __future__ import annotations
 
 import argparse
+import math
 import time
 
 import numpy as np
@@ -29,6 +33,7 @@ import torch
 from . import binding as B
 from . import inputs
 from .head import FCHead
+from .mixer import ChannelMixer
 from .stack import ConvStack
 
 NORM_EPS = 1e-5
@@ -44,29 +49,46 @@ def layout(sizes):
 
 class Network:
     def __init__(self, layers, size, batch, widths=inputs.HEAD_WIDTHS, dtype="f32", norm="sample", alpha=0.01,
-                 device="cuda"):
-        if norm not in ("sample", "voxel"):
+                 device="cuda", groups=8, mixer=0, optimizer="muon", weight_decay=0.01):
+        """groups: of norm="group".  mixer: hidden values of the block over a voxel's channels
+        (0: no such block).  weight_decay: of the matrices, with "adamw" and "adamw8"."""
+        if norm not in ("sample", "voxel", "group"):
             raise ValueError(f"norm: {norm}")
-        self.dtype = dtype
+        if optimizer not in ("muon", "adamw", "adamw8"):
+            raise ValueError(f"optimizer: {optimizer}")
+        self.dtype, self.norm, self.groups, self.optimizer = dtype, norm, groups, optimizer
         self.stack = ConvStack(layers, size, batch, dtype=dtype, alpha=alpha, device=device)
         out = self.stack.output()
-        features = out.numel() // batch
-        self.rows, self.c = (batch, features) if norm == "sample" else (out.numel() // out.shape[-1], out.shape[-1])
+        features, channels = out.numel() // batch, out.shape[-1]
+        if norm == "group" and (groups < 1 or channels % groups):
+            raise ValueError(f"groups: {groups} of {channels} channels")
+        self.vox = features // channels
+        self.rows, self.c = (batch, features) if norm == "sample" else (out.numel() // channels, channels)
         self.head = FCHead(batch, features, widths, dtype=dtype, alpha=alpha, device=device)
-        self._alloc_params(device)
+        self.mixer = ChannelMixer(batch * self.vox, channels, mixer, dtype=dtype, device=device) if mixer else None
+        self._alloc_params(device, weight_decay)
         self.y = torch.empty((batch, features), dtype=out.dtype, device=device)
         self.dout = torch.empty_like(out)
-        self.mean = torch.empty(self.rows, dtype=torch.float32, device=device)
+        self.mean = torch.empty(batch * groups if norm == "group" else self.rows, dtype=torch.float32, device=device)
         self.rstd = torch.empty_like(self.mean)
-        nws = max(16, B.cf_layernorm_fwd_workspace_size(self.rows, self.c, dtype),
-                  B.cf_layernorm_bwd_workspace_size(self.rows, self.c, dtype), B.cf_muon_workspace_size(self.mats),
-                  B.cf_adam_larc_workspace_size(self.vec_offsets))
+        if norm == "group":
+            shape = (batch, self.vox, self.c, groups, dtype)
+            nws = max(16, B.cf_groupnorm_fwd_workspace_size(*shape), B.cf_groupnorm_bwd_workspace_size(*shape))
+        else:
+            nws = max(16, B.cf_layernorm_fwd_workspace_size(self.rows, self.c, dtype),
+                      B.cf_layernorm_bwd_workspace_size(self.rows, self.c, dtype))
+        if optimizer == "muon":
+            nws = max(nws, B.cf_muon_workspace_size(self.mats), B.cf_adam_larc_workspace_size(self.vec_offsets))
         self.ws = torch.empty(nws, dtype=torch.uint8, device=device)
         self.t = 0
 
-    def _alloc_params(self, device):
-        shapes = [tuple(l["w32"].shape) for l in self.stack.L] + [tuple(w.shape) for w in self.head.w]
-        vectors = [l["b"].numel() for l in self.stack.L] + [b.numel() for b in self.head.b] + [self.c, self.c]
+    def _alloc_params(self, device, weight_decay):
+        convs, mixed = self.stack.L, self.mixer.w if self.mixer else []
+        normed = [i for i, l in enumerate(convs) if l["groups"]]
+        shapes = [tuple(l["w32"].shape) for l in convs] + [tuple(w.shape) for w in [*self.head.w, *mixed]]
+        vectors = [l["b"].numel() for l in convs] + [b.numel() for b in self.head.b]
+        vectors += [b.numel() for b in self.mixer.b] if self.mixer else []
+        vectors += [self.c, self.c] + [convs[i]["gamma"].numel() for i in normed]
         off = layout([int(np.prod(s)) for s in shapes] + vectors)
         nm = len(shapes)
         self.vec0 = off[nm]
@@ -75,8 +97,6 @@ class Network:
         self.mats = B.make_matrices(off[:nm], [int(np.prod(s[:-1])) for s in shapes], [s[-1] for s in shapes])
         self.param = torch.zeros(off[-1], dtype=torch.float32, device=device)
         self.grad = torch.zeros_like(self.param)
-        self.momentum = torch.zeros_like(self.param)  # of matrices, and Adam's first moment
-        self.second = torch.zeros(off[-1] - self.vec0, dtype=torch.float32, device=device)
         self.w16 = torch.zeros(self.vec0, dtype=torch.bfloat16, device=device) if self.dtype == "bf16" else None
 
         def view(buf, i):
@@ -85,25 +105,58 @@ class Network:
 
         ps = [dict(w=view(self.w16 if self.w16 is not None else self.param, i), w32=view(self.param, i),
                    b=view(self.param, nm + i), dw=view(self.grad, i), db=view(self.grad, nm + i)) for i in range(nm)]
-        nl = len(self.stack.L)
+        nl, nh = len(convs), len(self.head.w)
+        for j, i in enumerate(normed):
+            ps[i].update(gamma=view(self.param, 2 * nm + 2 + j), dgamma=view(self.grad, 2 * nm + 2 + j))
+            ps[i]["gamma"].fill_(1.0)
         self.stack.bind_params(ps[:nl])
-        self.head.bind_params(ps[nl:])
-        self._head_params = ps[nl:]
+        self.head.bind_params(ps[nl:nl + nh])
+        if self.mixer:
+            self.mixer.bind_params(ps[nl + nh:])
+        self._head_params, self._mixer_params = ps[nl:nl + nh], ps[nl + nh:]
         self.gamma, self.beta = view(self.param, 2 * nm), view(self.param, 2 * nm + 1)
         self.dgamma, self.dbeta = view(self.grad, 2 * nm), view(self.grad, 2 * nm + 1)
         self.gamma.fill_(1.0)
+        if self.optimizer == "muon":
+            self.momentum = torch.zeros_like(self.param)  # of matrices, and Adam's first moment
+            self.second = torch.zeros(off[-1] - self.vec0, dtype=torch.float32, device=device)
+            self.state = [self.momentum, self.second]
+            return
+        count = len(off) - 1
+        if self.optimizer == "adamw":
+            self.state = [torch.zeros_like(self.param) for _ in range(2)]
+            moments = [dict(m=view(self.state[0], i), v=view(self.state[1], i)) for i in range(count)]
+        else:
+            self.state = [torch.zeros(off[-1], dtype=torch.uint8, device=device) for _ in range(2)]
+            blocks = [-(-int(np.prod(n)) // B.CF_ADAMW_BLOCK) for n in shapes + vectors]
+            at = np.cumsum([0] + blocks)
+            self.state += [torch.zeros(int(at[-1]), dtype=torch.float32, device=device) for _ in range(2)]
+            moments = [dict(m=view(self.state[0], i), v=view(self.state[1], i), m_scale=self.state[2][at[i]:at[i + 1]],
+                            v_scale=self.state[3][at[i]:at[i + 1]]) for i in range(count)]
+        self.tensors = B.make_adamw_tensors(
+            [dict(p=view(self.param, i), g=view(self.grad, i),
+                  p16=view(self.w16, i) if self.w16 is not None and i < nm else None,
+                  weight_decay=weight_decay if i < nm else 0.0, **moments[i]) for i in range(count)])
 
-    def set_params(self, conv_weights, conv_biases, fc_weights, fc_biases, target):
+    def set_params(self, conv_weights, conv_biases, fc_weights, fc_biases, target, mixer=None):
         """Weights are rounded to the network's dtype, their fp32 values hold exactly those;
-        gamma = 1, beta = 0; resets the optimizer state."""
+        gamma = 1, beta = 0; resets the optimizer state.  mixer: its (weights, biases); by
+        default He-normal first and zero second weights: the block starts as the identity."""
         self.stack.set_params(conv_weights, conv_biases)
         self.head.set_params(fc_weights, fc_biases, target)
-        for p in self._head_params:
+        if self.mixer:
+            c, h = self.mixer.c, self.mixer.hidden
+            self.mixer.set_params(*(mixer if mixer is not None else (
+                [inputs.normal((c, h), 4000, (2.0 / c) ** 0.5), np.zeros((h, c), np.float32)],
+                [np.zeros(h, np.float32), np.zeros(c, np.float32)])))
+        elif mixer is not None:
+            raise ValueError("mixer: the network has none")
+        for p in self._head_params + self._mixer_params:
             p["w32"].copy_(p["w"].float())
         self.gamma.fill_(1.0)
         self.beta.zero_()
-        self.momentum.zero_()
-        self.second.zero_()
+        for s in self.state:
+            s.zero_()
         self.t = 0
 
     def step(self, stream=None):
@@ -111,22 +164,42 @@ class Network:
         fills every gradient; returns the device loss tensor (one fp32 in element 0)."""
         s = B.raw_stream(stream)
         x = self.stack.forward(stream)
-        B.cf_layernorm_fwd(self.rows, self.c, self.dtype, x, self.gamma, self.beta, NORM_EPS, self.y, self.mean,
-                           self.rstd, self.ws, stream=s)
+        if self.mixer:
+            x = self.mixer.forward(x, s)
+        if self.norm == "group":
+            shape = (self.head.m, self.vox, self.c, self.groups, self.dtype)
+            B.cf_groupnorm_fwd(*shape, x, self.gamma, self.beta, NORM_EPS, "none", 0.0, self.y, self.mean, self.rstd,
+                               self.ws, stream=s)
+        else:
+            B.cf_layernorm_fwd(self.rows, self.c, self.dtype, x, self.gamma, self.beta, NORM_EPS, self.y, self.mean,
+                               self.rstd, self.ws, stream=s)
         dy = self.head.step(self.y, stream)
-        B.cf_layernorm_bwd(self.rows, self.c, self.dtype, dy, x, self.gamma, self.mean, self.rstd, self.dout,
-                           self.dgamma, self.dbeta, self.ws, stream=s)
-        self.stack.backward(self.dout, stream)
+        if self.norm == "group":
+            B.cf_groupnorm_bwd(*shape, dy, x, self.gamma, self.beta, self.mean, self.rstd, "none", 0.0, self.dout,
+                               self.dgamma, self.dbeta, self.ws, stream=s)
+        else:
+            B.cf_layernorm_bwd(self.rows, self.c, self.dtype, dy, x, self.gamma, self.mean, self.rstd, self.dout,
+                               self.dgamma, self.dbeta, self.ws, stream=s)
+        dout = self.mixer.backward(self.dout, s) if self.mixer else self.dout
+        self.stack.backward(dout, stream)
         return self.head.loss
 
-    def update(self, hp_matrices, hp_vectors, stream=None):
-        """One update of all parameters from the gradients of the last step
-        (binding.make_muon_hparams, binding.make_hparams)."""
+    def update(self, hp_matrices, hp_vectors=None, stream=None):
+        """One update of all parameters from the gradients of the last step: with "muon"
+        binding.make_muon_hparams and binding.make_hparams, else binding.make_adamw_hparams
+        alone."""
+        muon = self.optimizer == "muon"
+        if isinstance(hp_matrices, B.cf_muon_hparams) != muon or (hp_vectors is not None) != muon:
+            raise ValueError(f"hyperparameters of another optimizer than {self.optimizer}")
         s = B.raw_stream(stream)
-        B.cf_muon_step(self.mats, self.t, hp_matrices, self.param, self.grad, self.momentum, self.w16, self.ws, stream=s)
-        v = self.vec0
-        B.cf_adam_larc_step(self.vec_offsets, self.t, hp_vectors, self.param[v:], self.grad[v:], self.momentum[v:],
-                            self.second, None, self.ws, stream=s)
+        if muon:
+            B.cf_muon_step(self.mats, self.t, hp_matrices, self.param, self.grad, self.momentum, self.w16, self.ws,
+                           stream=s)
+            v = self.vec0
+            B.cf_adam_larc_step(self.vec_offsets, self.t, hp_vectors, self.param[v:], self.grad[v:], self.momentum[v:],
+                                self.second, None, self.ws, stream=s)
+        else:
+            B.cf_adamw_step(self.tensors, self.t, hp_matrices, stream=s)
         self.t += 1
 
 
@@ -150,19 +223,29 @@ def main(argv=None):
     ap.add_argument("--batch", type=int, default=4)
     ap.add_argument("--steps", type=int, default=50)
     ap.add_argument("--dtype", choices=("f32", "bf16"), default="bf16")
-    ap.add_argument("--norm", choices=("sample", "voxel"), default="sample")
-    ap.add_argument("--rate", type=float, default=0.002, help="first rate of the matrices")
+    ap.add_argument("--norm", choices=("sample", "voxel", "group"), default="sample")
+    ap.add_argument("--groups", type=int, default=8, help="of --norm group and --conv-norm")
+    ap.add_argument("--conv-norm", choices=("lrelu", "silu", "gelu"), help="group normalisation and this activation in every convolution layer")
+    ap.add_argument("--mixer", type=int, default=0, help="hidden values of a block over each voxel's channels")
+    ap.add_argument("--optimizer", choices=("muon", "adamw", "adamw8"), default="muon")
+    ap.add_argument("--rate", type=float, default=0.002, help="first rate of the matrices, or of all parameters")
     a = ap.parse_args(argv)
     layers = inputs.stack_layers()
-    net = Network(layers, a.size, a.batch, dtype=a.dtype, norm=a.norm)
+    if a.conv_norm:
+        layers = [dict(l, norm=math.gcd(l["cout"], a.groups), act=a.conv_norm) for l in layers]
+    net = Network(layers, a.size, a.batch, dtype=a.dtype, norm=a.norm, groups=a.groups, mixer=a.mixer,
+                  optimizer=a.optimizer)
     x, *params = synthetic(a.size, a.batch, layers=layers, features=net.head.dims[0])
     net.stack.set_input(x)
     net.set_params(*params)
-    hm, hv = B.make_muon_hparams(a.steps, eta0=a.rate, eta_min=a.rate / 20), B.make_hparams(a.steps)
+    if a.optimizer == "muon":
+        hp = B.make_muon_hparams(a.steps, eta0=a.rate, eta_min=a.rate / 20), B.make_hparams(a.steps)
+    else:
+        hp = (B.make_adamw_hparams(a.steps, eta0=a.rate, eta_min=a.rate / 20),)
     t0 = None
     for i in range(a.steps):
         loss = net.step()
-        net.update(hm, hv)
+        net.update(*hp)
         if i == 0 or (i + 1) % 10 == 0 or i + 1 == a.steps:
             print(f"step {i + 1}: loss {float(loss[0]):.6f}", flush=True)
         if i == 0:

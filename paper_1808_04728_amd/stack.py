@@ -8,6 +8,11 @@ backward pass over the network's convolution part, Section III-A):
                          -> weight grad -> data grad (skipped for layer 1,
                             whose input needs no gradient)
 
+A layer whose spec has ``norm`` (a number of groups that divides its channels) runs
+group normalisation in place of bias + leaky ReLU: y = act(gamma x^ + b), with ``act``
+of the spec ("lrelu" with the stack's alpha, "silu", "gelu" or "none").  Its biases are
+the normalisation's beta, and gamma is one more parameter group behind them.
+
 PyTorch only allocates device memory and supplies the stream; every step is
 one call of ``binding`` (a HIP kernel).  Buffers are allocated once, so a
 step launches kernels and nothing else.
@@ -24,6 +29,10 @@ from __future__ import annotations
 import torch
 
 from . import binding as B
+
+
+#: added to a group's variance
+GROUP_NORM_EPS = 1e-5
 
 
 def _t(dtype):
@@ -96,8 +105,14 @@ class ConvStack:
                                spec.get("pad", "same"), dtype)
             od = B.cf_conv3d_out_shape(desc)
             pdhw = tuple(t // 2 for t in od) if spec["pool"] else od
+            groups, act = spec.get("norm") or 0, spec.get("act", "lrelu")
+            if groups < 0 or groups and spec["cout"] % groups:
+                raise ValueError(f"layer {i}: {groups} groups of {spec['cout']} channels")
+            B.act_code(act)
+            if act != "lrelu" and not groups:
+                raise ValueError(f"layer {i}: activation {act} without a normalisation")
             self.L.append(dict(spec=spec, desc=desc, in_dhw=dhw, out_dhw=od, pool_dhw=pdhw,
-                               nvox=batch * od[0] * od[1] * od[2]))
+                               nvox=batch * od[0] * od[1] * od[2], groups=groups, act=act))
             dhw = pdhw
         self.out_dhw = dhw
         if overlap_wgrad is None:
@@ -114,7 +129,8 @@ class ConvStack:
         off, shapes = [0], []
         for l in self.L:
             s = l["spec"]
-            for shape in (((s["k"],) * 3 + (s["cin"], s["cout"])), (s["cout"],)):
+            l["first"] = len(shapes)  # its first group
+            for shape in [(s["k"],) * 3 + (s["cin"], s["cout"])] + [(s["cout"],)] * (2 if l["groups"] else 1):
                 n = 1
                 for t in shape:
                     n *= t
@@ -134,24 +150,29 @@ class ConvStack:
                 n *= t
             return buf[off[g]:off[g] + n].view(shape)
 
-        for i, l in enumerate(self.L):
-            l["w"] = view(wsrc, 2 * i)
-            l["w32"] = view(self.flat_param, 2 * i)
-            l["b"] = view(self.flat_param, 2 * i + 1)
-            l["dw"] = view(self.flat_grad, 2 * i)
-            l["db"] = view(self.flat_grad, 2 * i + 1)
+        for l in self.L:
+            i = l["first"]
+            l["w"] = view(wsrc, i)
+            l["w32"] = view(self.flat_param, i)
+            l["b"] = view(self.flat_param, i + 1)
+            l["dw"] = view(self.flat_grad, i)
+            l["db"] = view(self.flat_grad, i + 1)
+            if l["groups"]:
+                l["gamma"] = view(self.flat_param, i + 2)
+                l["dgamma"] = view(self.flat_grad, i + 2)
+                l["gamma"].fill_(1.0)
         self.opt_m = self.opt_s = self.opt_ws = None
         self.opt_t = 0
 
     def bind_params(self, params):
         """Use the caller's tensors for the parameters and their gradients: one dict of
-        w (the stack's dtype), w32 (fp32, may be w), b, dw and db (fp32) a layer, in the
-        shapes of the stack's own, contiguous and 16-byte aligned (ValueError).  Their
-        update is then the caller's."""
-        keys = ("w", "w32", "b", "dw", "db")
-        B.check_params([{k: l[k] for k in keys} for l in self.L], params)
-        for l, p in zip(self.L, params):
-            l.update((k, p[k]) for k in keys)
+        w (the stack's dtype), w32 (fp32, may be w), b, dw and db (fp32; with a normalisation
+        gamma and dgamma too) a layer, in the shapes of the stack's own, contiguous and
+        16-byte aligned (ValueError).  Their update is then the caller's."""
+        own = [{k: l[k] for k in ("w", "w32", "b", "dw", "db", "gamma", "dgamma") if k in l} for l in self.L]
+        B.check_params(own, params)
+        for l, o, p in zip(self.L, own, params):
+            l.update((k, p[k]) for k in o)
         self.flat_param = self.flat_grad = self.flat_w16 = self.opt_m = self.opt_s = None
 
     def _alloc(self):
@@ -167,7 +188,7 @@ class ConvStack:
             both = B.FUSED_FWD | B.FUSED_BWD_WEIGHT
             # a layer whose data gradient is needed also needs a fused backward-data, or a
             # backward-weights that stores dz for the unfused backward-data
-            fz = self.fused and (self.fused_from <= 0 or i < self.fused_from)
+            fz = self.fused and (self.fused_from <= 0 or i < self.fused_from) and not l["groups"]
             l["fused"] = bool(fz and (sup & both) == both and
                               (not needs_dgrad or sup & (B.FUSED_BWD_DATA | B.FUSED_BWD_WEIGHT_DZ)))
             # otherwise conv + bias + leaky ReLU may still share one kernel (y written once)
@@ -225,7 +246,14 @@ class ConvStack:
                 continue
             l["dz"] = torch.empty_like(l["z"])
             wsw = B.cf_conv3d_bwd_weight_workspace_size(l["desc"])
-            wsb = B.cf_bias_lrelu_bwd_workspace_size(l["nvox"], s["cout"])
+            if l["groups"]:
+                l["u"] = torch.empty_like(l["z"])  # the convolution's output; z holds y
+                l["mean"] = torch.empty((n, l["groups"]), dtype=torch.float32, device=dev)
+                l["rstd"] = torch.empty_like(l["mean"])
+                shape = (n, l["nvox"] // n, s["cout"], l["groups"], self.dtype)
+                wsb = max(B.cf_groupnorm_fwd_workspace_size(*shape), B.cf_groupnorm_bwd_workspace_size(*shape))
+            else:
+                wsb = B.cf_bias_lrelu_bwd_workspace_size(l["nvox"], s["cout"])
             l["ws_w"] = torch.empty(max(wsw, 16), dtype=torch.uint8, device=dev)
             l["ws_b"] = torch.empty(max(wsb, 16), dtype=torch.uint8, device=dev)
         for i in range(1, len(self.L)):
@@ -244,12 +272,14 @@ class ConvStack:
 
     def set_params(self, weights, biases):
         """Weights are rounded to the stack's dtype; the fp32 master copy holds
-        exactly those values.  Resets the optimizer state."""
+        exactly those values; gamma = 1.  Resets the optimizer state."""
         for l, w, b in zip(self.L, weights, biases):
             l["w"].copy_(torch.as_tensor(w).to(self.tdt))
             if l["w32"].data_ptr() != l["w"].data_ptr():
                 l["w32"].copy_(l["w"].float())
             l["b"].copy_(torch.as_tensor(b).float())
+            if l["groups"]:
+                l["gamma"].fill_(1.0)
         self.reset_optimizer()
 
     def reset_optimizer(self):
@@ -314,7 +344,12 @@ class ConvStack:
                   B.CF_FUSE_POOL2, l["p"], l["mask"], stream)
                 h = l["p"]
                 continue
-            if l["fused_act"]:
+            if l["groups"]:
+                c(f"L{i+1}.conv_fwd", B.cf_conv3d_fwd, l["desc"], h, l["w"], l["u"], stream)
+                c(f"L{i+1}.groupnorm_fwd", B.cf_groupnorm_fwd, self.batch, l["nvox"] // self.batch, s["cout"],
+                  l["groups"], self.dtype, l["u"], l["gamma"], l["b"], GROUP_NORM_EPS, l["act"], self.alpha, l["z"],
+                  l["mean"], l["rstd"], l["ws_b"], None, stream)
+            elif l["fused_act"]:
                 c(f"L{i+1}.conv_bias_lrelu_fwd", B.cf_conv3d_fwd_fused, l["desc"], h, l["w"], l["b"], self.alpha, 0,
                   l["z"], None, stream)
             else:
@@ -458,7 +493,11 @@ class ConvStack:
             else:
                 dy = g
             # the weight gradient goes to the side stream where that pays
-            if d:
+            if l["groups"]:
+                c(f"L{i+1}.groupnorm_bwd", B.cf_groupnorm_bwd, self.batch, l["nvox"] // self.batch, s["cout"],
+                  l["groups"], self.dtype, dy, l["u"], l["gamma"], l["b"], l["mean"], l["rstd"], l["act"], self.alpha,
+                  l["dz"], l["dgamma"], l["db"], l["ws_b"], None, stream)
+            elif d:
                 pend += c(f"L{i+1}.bias_lrelu_bwd", B.cf_bias_lrelu_bwd_deferred, l["nvox"], s["cout"], self.dtype,
                           dy, l["z"], self.alpha, l["dz"], l["db"], l["ws_b"], None, stream)
             else:
@@ -548,7 +587,7 @@ class ConvStack:
                 "conv_bias_lrelu_fwd": xb + wb + zb,
                 "conv_fwd": xb + wb + zb, "conv_bwd_data": zb + wb + xb,
                 "conv_bwd_weight": xb + zb + wb // es * 4, "bias_lrelu_fwd": 2 * zb,
-                "bias_lrelu_bwd": 3 * zb, "avgpool_fwd": zb + pb, "avgpool_bwd": zb + pb,
+                "bias_lrelu_bwd": 3 * zb, "groupnorm_fwd": 2 * zb, "groupnorm_bwd": 3 * zb, "avgpool_fwd": zb + pb, "avgpool_bwd": zb + pb,
                 "pool_lrelu_bwd": pb + mb + zb}[op]
 
     # ------------------------------------------------------------------
