@@ -139,32 +139,37 @@ template <int TN> struct ColumnSums {
 // Eight neighbouring values of a row, of which n exist; rows start anywhere.
 typedef uint32_t u32x4e4_t __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t u32x4e2_t __attribute__((ext_vector_type(4), aligned(2)));
-__device__ __forceinline__ void load8(const uint16_t *p, int n, float (&x)[8]) {
-  if (n >= 8) {
-    const u32x4_t a = *reinterpret_cast<const u32x4e2_t *>(p);
+template <int DT> struct Eight;
+template <> struct Eight<DT_BF16> {
+  u32x4_t a;
+  __device__ __forceinline__ void load(const uint16_t *p, int n) {
+    if (n >= 8) {
+      a = *reinterpret_cast<const u32x4e2_t *>(p);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(a[i] << 16);
-      x[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
+      for (int i = 0; i < 4; ++i) a[i] = (2 * i < n ? p[2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)p[2 * i + 1] << 16 : 0u);
     }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = i < n ? bf2f(p[i]) : 0.f;
   }
-}
-__device__ __forceinline__ void load8(const float *p, int n, float (&x)[8]) {
-  if (n >= 8) {
-    const u32x4_t a = reinterpret_cast<const u32x4e4_t *>(p)[0], b = reinterpret_cast<const u32x4e4_t *>(p)[1];
+  __device__ __forceinline__ float operator[](int i) const {
+    return __uint_as_float(i % 2 ? a[i / 2] & 0xffff0000u : a[i / 2] << 16);
+  }
+};
+template <> struct Eight<DT_F32> {
+  u32x4_t a, b;
+  __device__ __forceinline__ void load(const float *p, int n) {
+    if (n >= 8) {
+      a = reinterpret_cast<const u32x4e4_t *>(p)[0];
+      b = reinterpret_cast<const u32x4e4_t *>(p)[1];
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[i] = __uint_as_float(a[i]);
-      x[4 + i] = __uint_as_float(b[i]);
+      for (int i = 0; i < 4; ++i) {
+        a[i] = i < n ? __float_as_uint(p[i]) : 0u;
+        b[i] = 4 + i < n ? __float_as_uint(p[4 + i]) : 0u;
+      }
     }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = i < n ? p[i] : 0.f;
   }
-}
+  __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(i < 4 ? a[i % 4] : b[i % 4]); }
+};
 __device__ __forceinline__ void store8(uint16_t *p, int n, const float (&x)[8]) {
   if (n >= 8) {
     *reinterpret_cast<u32x4e2_t *>(p) = pack_bf16x8(x);
@@ -191,10 +196,41 @@ __device__ __forceinline__ void store8(float *p, int n, const float (&x)[8]) {
   }
 }
 
-// eight neighbouring outputs
+// What an epilogue reads of the outputs' shape.  All of a wave's such loads go out in front
+// of its first store: behind a store, which may have changed what they read, each would wait
+// for memory by itself (data gradient of 32768 x 4096 x 1024 with GELU 373 us -> 300).  Where
+// both a slope and a residual are read, the residual's loads wait.
 template <int DT, int FORM, int ACT>
+__device__ __forceinline__ void fetch8(const LinearEpilogue &E, long long at, int n, Eight<DT> &x) {
+  typedef typename Store<DT>::T T;
+  if constexpr (FORM == FORM_DATA && ACT != ACT_NONE) x.load((const T *)E.zin + at, n);
+  else if (FORM != FORM_WEIGHT && E.residual) x.load((const T *)E.residual + at, n);
+}
+
+// Slopes of all bf16 values of sizes from 2^-16 to 32 (nearer 0 and further out they change
+// by less than 2^-16 of themselves), a value's at 4 times its bits, negative ones 16384
+// bytes on: the epilogue of a 256 x 256 tile looks 65536 of them up, four times as fast as it
+// computes them.
+struct SlopeTable {
+  static constexpr int LO = 0x3780, HI = 0x4200, BYTES = 16384 + (HI - LO + 1) * 4;
+  template <int ACT> static __device__ __forceinline__ void fill(unsigned char *t, float alpha) {
+    for (int i = threadIdx.x; i < 2 * (HI - LO + 1); i += blockDim.x) {
+      const int half = i > HI - LO, a = half ? i - (HI - LO + 1) : i;
+      *reinterpret_cast<float *>(t + half * 16384 + a * 4) = act_slope<ACT>(__uint_as_float((uint32_t)(LO + a + half * 0x8000) << 16), alpha);
+    }
+  }
+  // value i of x (a NaN or an infinity gives NaN, as the formula does)
+  static __device__ __forceinline__ float at(const unsigned char *t, const Eight<DT_BF16> &x, int i) {
+    const uint32_t b = i % 2 ? x.a[i / 2] >> 14 : x.a[i / 2] << 2;
+    const uint32_t a = min(max(b & 0x1fffcu, LO * 4u), HI * 4u) | (b >> 3 & 0x4000u);
+    return __builtin_fmaf(x[i], 0.f, *reinterpret_cast<const float *>(t + (int)a - LO * 4));
+  }
+};
+
+// eight neighbouring outputs; x: what fetch8 read for them; TABLE: slopes from `table`
+template <int DT, int FORM, int ACT, bool TABLE = false>
 __device__ __forceinline__ void put8(const LinearEpilogue &E, const float (&bias)[8], void *out, long long at, int n,
-                                     float (&v)[8]) {
+                                     const Eight<DT> &x, float (&v)[8], const unsigned char *table = nullptr) {
   typedef typename Store<DT>::T T;
   if constexpr (FORM == FORM_WEIGHT) {
     store8((float *)out + at, n, v);
@@ -205,23 +241,23 @@ __device__ __forceinline__ void put8(const LinearEpilogue &E, const float (&bias
 #pragma unroll
     for (int q = 0; q < 8; ++q) v[q] = act<ACT>(v[q], E.alpha);
     if (E.residual) {
-      float r[8];
-      load8((const T *)E.residual + at, n, r);
 #pragma unroll
-      for (int q = 0; q < 8; ++q) v[q] += r[q];
+      for (int q = 0; q < 8; ++q) v[q] += x[q];
     }
     store8((T *)out + at, n, v);
   } else {
-    float r[8];
     if (E.residual) {
-      load8((const T *)E.residual + at, n, r);
+      Eight<DT> r = x;
+      if constexpr (ACT != ACT_NONE) r.load((const T *)E.residual + at, n);
 #pragma unroll
       for (int q = 0; q < 8; ++q) v[q] += r[q];
     }
     if constexpr (ACT != ACT_NONE) {
-      load8((const T *)E.zin + at, n, r);
 #pragma unroll
-      for (int q = 0; q < 8; ++q) v[q] *= act_slope<ACT>(r[q], E.alpha);
+      for (int q = 0; q < 8; ++q) {
+        if constexpr (TABLE) v[q] *= SlopeTable::at(table, x, q);
+        else v[q] *= act_slope<ACT>(x[q], E.alpha);
+      }
     }
     store8((T *)out + at, n, v);
   }
@@ -230,11 +266,10 @@ __device__ __forceinline__ void put8(const LinearEpilogue &E, const float (&bias
 // the bias of columns j .. j + 7 (a multiple of 8)
 template <int FORM>
 __device__ __forceinline__ void load_bias(const LinearEpilogue &E, int j, int N, float (&b)[8]) {
-  if (FORM == FORM_FWD && E.bias) load8(E.bias + j, N - j, b);
-  else {
+  Eight<DT_F32> x{};
+  if (FORM == FORM_FWD && E.bias) x.load(E.bias + j, N - j);
 #pragma unroll
-    for (int q = 0; q < 8; ++q) b[q] = 0.f;
-  }
+  for (int q = 0; q < 8; ++q) b[q] = x[q];
 }
 
 }  // namespace cf

@@ -131,6 +131,8 @@ template <int FORM, int ACT>
 __global__ __launch_bounds__(kThreads) void join8_kernel(LinearPlan p, const float *part, LinearEpilogue E, void *out) {
   const long long n = p.M * p.N, at = (long_index() * kThreads + threadIdx.x) * 8;
   if (at >= n) return;
+  Eight<DT_BF16> in;
+  fetch8<DT_BF16, FORM, ACT>(E, at, 8, in);
   float v[8];
   for (int s = 0; s < p.slices; ++s) {
     const float4 a = *reinterpret_cast<const float4 *>(part + s * n + at), b = *reinterpret_cast<const float4 *>(part + s * n + at + 4);
@@ -140,7 +142,7 @@ __global__ __launch_bounds__(kThreads) void join8_kernel(LinearPlan p, const flo
   }
   float bias[8];
   load_bias<FORM>(E, (int)(at % p.N), p.N, bias);
-  put8<DT_BF16, FORM, ACT>(E, bias, out, at, 8, v);
+  put8<DT_BF16, FORM, ACT>(E, bias, out, at, 8, in, v);
 }
 
 // part[slice][N] = sums of the slice's rows of dz

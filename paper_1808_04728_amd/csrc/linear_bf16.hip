@@ -123,7 +123,9 @@ __global__ __launch_bounds__(threads_of<Tile<KERNEL>>(), Tile<KERNEL>::WAVES) vo
   constexpr int NT = threads_of<C>(), TM = C::BM / C::WM / 16, TN = C::BN / C::WN / 16;
   static_assert(TN % 4 == 0, "a lane's row of the epilogue is sixteen columns of 64");
   constexpr int AB = C::BM * BK * 2, STAGE = AB + C::BN * BK * 2;
-  __shared__ __attribute__((aligned(16))) unsigned char lds[C::NS * STAGE];
+  // (the large tile leaves 32 KB free)
+  constexpr bool TABLE = KERNEL == LIN_256 && FORM == FORM_DATA && (ACT == ACT_SILU || ACT == ACT_GELU);
+  __shared__ __attribute__((aligned(16))) unsigned char lds[C::NS * STAGE + (TABLE ? SlopeTable::BYTES : 0)];
 
   // the workgroups of an XCD (every eighth) take neighbouring tiles, eight tiles down before
   // one across: 32 at a time read 8 + 4 tiles' factors through its L2
@@ -209,6 +211,7 @@ __global__ __launch_bounds__(threads_of<Tile<KERNEL>>(), Tile<KERNEL>::WAVES) vo
     for (int q = 0; q < LOADS; ++q) load(q, n);
     next();
   }
+  if constexpr (TABLE) SlopeTable::fill<ACT>(lds + C::NS * STAGE, E.alpha);  // (a step's barrier is in front of its use)
   wait_loads<(C::NS - 1) * LOADS>();
   barrier();
 #pragma unroll
@@ -238,6 +241,18 @@ __global__ __launch_bounds__(threads_of<Tile<KERNEL>>(), Tile<KERNEL>::WAVES) vo
     float bias[2][8];
 #pragma unroll
     for (int h = 0; h < 2; ++h) load_bias<FORM>(E, j + 32 * h, p.N, bias[h]);
+    Eight<DT_BF16> ahead[TM][2];
+    if (whole) {
+#pragma unroll
+      for (int ii = 0; ii < TM; ++ii) {
+        const long long i = (long long)i0 + (wm * TM + ii) * 16 + r;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int n = p.N - j - 32 * h;
+          if (i < p.M && n > 0) fetch8<DT_BF16, FORM, ACT>(E, i * p.N + j + 32 * h, n, ahead[ii][h]);
+        }
+      }
+    }
 #pragma unroll
     for (int ii = 0; ii < TM; ++ii) {
       float row[16];
@@ -256,8 +271,8 @@ __global__ __launch_bounds__(threads_of<Tile<KERNEL>>(), Tile<KERNEL>::WAVES) vo
         float v[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) v[q] = row[8 * h + q];
-        if (whole) put8<DT_BF16, FORM, ACT>(E, bias[h], out, i * p.N + j + 32 * h, n, v);
-        else put8<DT_BF16, FORM_WEIGHT, ACT_NONE>(E, none, part, (slice * p.M + i) * p.N + j + 32 * h, n, v);
+        if (whole) put8<DT_BF16, FORM, ACT, TABLE>(E, bias[h], out, i * p.N + j + 32 * h, n, ahead[ii][h], v, lds + C::NS * STAGE);
+        else put8<DT_BF16, FORM_WEIGHT, ACT_NONE>(E, none, part, (slice * p.M + i) * p.N + j + 32 * h, n, ahead[ii][h], v);
       }
     }
   }

@@ -205,6 +205,18 @@ __global__ __launch_bounds__(NT, Tile<KERNEL>::WAVES) void product_kernel(Linear
   float bias[2][8];
 #pragma unroll
   for (int h = 0; h < 2; ++h) load_bias<FORM>(E, j + 32 * h, p.N, bias[h]);
+  Eight<DT_F32> ahead[TM][2];
+  if (whole) {
+#pragma unroll
+    for (int ii = 0; ii < TM; ++ii) {
+      const long long i = (long long)i0 + (wm * TM + ii) * 16 + r;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int n = p.N - j - 32 * h;
+        if (i < p.M && n > 0) fetch8<DT_F32, FORM, ACT>(E, i * p.N + j + 32 * h, n, ahead[ii][h]);
+      }
+    }
+  }
 #pragma unroll
   for (int ii = 0; ii < TM; ++ii) {
     float row[16];
@@ -223,8 +235,8 @@ __global__ __launch_bounds__(NT, Tile<KERNEL>::WAVES) void product_kernel(Linear
       float v[8];
 #pragma unroll
       for (int q = 0; q < 8; ++q) v[q] = row[8 * h + q];
-      if (whole) put8<DT_F32, FORM, ACT>(E, bias[h], out, i * p.N + j + 32 * h, n, v);
-      else put8<DT_F32, FORM_WEIGHT, ACT_NONE>(E, none, part, (slice * p.M + i) * p.N + j + 32 * h, n, v);
+      if (whole) put8<DT_F32, FORM, ACT>(E, bias[h], out, i * p.N + j + 32 * h, n, ahead[ii][h], v);
+      else put8<DT_F32, FORM_WEIGHT, ACT_NONE>(E, none, part, (slice * p.M + i) * p.N + j + 32 * h, n, ahead[ii][h], v);
     }
   }
 }
