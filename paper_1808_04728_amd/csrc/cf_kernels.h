@@ -359,6 +359,7 @@ struct LinearEpilogue {
   const void *zin;       // the pre-activation whose slope multiplies the output
   int act;
   float alpha;
+  bool stream = false;  // the launch sets it: the output passes the last-level cache by
 };
 size_t linear_fwd_workspace(long long M, int K, int N, int dtype);
 size_t linear_bwd_data_workspace(long long M, int K, int N, int dtype);

@@ -257,10 +257,11 @@ __global__ __launch_bounds__(kThreads) void pad_rows_kernel(long long rows, int 
 }
 
 template <int FORM>
-hipError_t product(const LinearPlan &p, int dtype, const void *A, const void *B, const LinearEpilogue &E, void *out, float *db,
+hipError_t product(const LinearPlan &p, int dtype, const void *A, const void *B, LinearEpilogue E, void *out, float *db,
                    void *ws, hipStream_t st) {
   const long long M = p.M, L = p.L;
   const int N = p.N;
+  E.stream = dtype == DT_BF16 && M * N * 2 >= kStreamBytes / 2;
   float *part = (float *)ws;
   auto padded = [&](bool a, const void *src, char *dst) -> const void * {
     if (!copy_bytes(FORM, a, p)) return src;
