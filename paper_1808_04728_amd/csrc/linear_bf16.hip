@@ -124,8 +124,9 @@ __global__ __launch_bounds__(threads_of<Tile<KERNEL>>(), Tile<KERNEL>::WAVES) vo
   static_assert(TN % 4 == 0, "a lane's row of the epilogue is sixteen columns of 64");
   constexpr int AB = C::BM * BK * 2, STAGE = AB + C::BN * BK * 2;
   // (the large tile leaves 32 KB free)
-  constexpr bool TABLE = KERNEL == LIN_256 && FORM == FORM_DATA && (ACT == ACT_SILU || ACT == ACT_GELU);
-  __shared__ __attribute__((aligned(16))) unsigned char lds[C::NS * STAGE + (TABLE ? SlopeTable::BYTES : 0)];
+  constexpr bool PHI = KERNEL == LIN_256 && FORM == FORM_FWD && ACT == ACT_GELU;
+  constexpr bool SLOPES = KERNEL == LIN_256 && FORM == FORM_DATA && (ACT == ACT_SILU || ACT == ACT_GELU);
+  __shared__ __attribute__((aligned(16))) unsigned char lds[C::NS * STAGE + (SLOPES ? SlopeTable::BYTES : PHI ? PhiTable::BYTES : 0)];
 
   // the workgroups of an XCD (every eighth) take neighbouring tiles, eight tiles down before
   // one across: 32 at a time read 8 + 4 tiles' factors through its L2
@@ -211,7 +212,9 @@ __global__ __launch_bounds__(threads_of<Tile<KERNEL>>(), Tile<KERNEL>::WAVES) vo
     for (int q = 0; q < LOADS; ++q) load(q, n);
     next();
   }
-  if constexpr (TABLE) SlopeTable::fill<ACT>(lds + C::NS * STAGE, E.alpha);  // (a step's barrier is in front of its use)
+  // (a step's barrier is in front of the tables' use)
+  if constexpr (SLOPES) SlopeTable::fill<ACT>(lds + C::NS * STAGE, E.alpha);
+  if constexpr (PHI) PhiTable::fill(lds + C::NS * STAGE);
   wait_loads<(C::NS - 1) * LOADS>();
   barrier();
 #pragma unroll
@@ -271,7 +274,7 @@ __global__ __launch_bounds__(threads_of<Tile<KERNEL>>(), Tile<KERNEL>::WAVES) vo
         float v[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) v[q] = row[8 * h + q];
-        if (whole) put8<DT_BF16, FORM, ACT, TABLE>(E, bias[h], out, i * p.N + j + 32 * h, n, ahead[ii][h], v, lds + C::NS * STAGE);
+        if (whole) put8<DT_BF16, FORM, ACT, SLOPES || PHI>(E, bias[h], out, i * p.N + j + 32 * h, n, ahead[ii][h], v, lds + C::NS * STAGE);
         else put8<DT_BF16, FORM_WEIGHT, ACT_NONE>(E, none, part, (slice * p.M + i) * p.N + j + 32 * h, n, ahead[ii][h], v);
       }
     }

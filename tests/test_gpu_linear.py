@@ -299,3 +299,55 @@ def test_past_32_bits(dt):
     B.cf_linear_bwd_weight(m, k, n, dt, x, y, dw, None, _ws(B.cf_linear_bwd_weight_workspace_size(m, k, n, dt)))
     ref = sum(x[i:i + (1 << 22)].double().t().contiguous() @ y[i:i + (1 << 22)].double() for i in range(0, m, 1 << 22))
     assert float((dw.double() - ref).abs().max()) <= 2.0 ** -20 * float(ref.abs().max())
+
+
+# 4096 x 4096 outputs of 64 terms are one round of the large tiles, whose epilogues look
+# activations and slopes up.  Terms that are zeros, or one that is 1, leave the epilogue alone:
+# its value to 2^-14 of itself and 2^-21 |u|, or its slope to 2^-16, and half a step of bf16.
+@pytest.mark.parametrize("part", range(4))
+def test_gelu_of_large_tiles(part):
+    m = n = 4096
+    u = torch.linspace(-10, 10, 4 * n, dtype=torch.float64)[part::4].float()
+    u[:8] = torch.tensor([0.0, -0.0, 40.0, -40.0, 1e30, -1e30, math.inf, math.nan])
+    x, w = torch.zeros(m, 64, device="cuda").bfloat16(), torch.ones(64, n, device="cuda").bfloat16()
+    y = torch.full((m, n), 7.0, device="cuda").bfloat16()
+    z = torch.empty_like(y)
+    ws = torch.empty(max(16, B.cf_linear_fwd_workspace_size(m, 64, n, "bf16")), dtype=torch.uint8, device="cuda")
+    B.cf_linear_fwd(m, 64, n, "bf16", x, w, u.cuda(), "gelu", 0.0, None, y, z, ws)
+    assert torch.equal(y[:1].expand(m, n)[:, :7], y[:, :7]) and torch.equal(y[:1, 8:].expand(m, n - 8), y[:, 8:])
+    got, d = y[m // 2].double().cpu(), u.double()
+    assert got[6] == math.inf and math.isnan(got[7]) and bool(torch.isnan(y[:, 7]).all())
+    want = d * 0.5 * torch.erfc(-d / math.sqrt(2))
+    want[5] = 0.0
+    keep = torch.ones(n, dtype=torch.bool)
+    keep[6:8] = False
+    err, bound = (got - want).abs(), (2.0 ** -8 + 2.0 ** -14) * want.abs() + 2.0 ** -21 * d.abs().clamp(max=8.0)
+    assert bool((err <= bound)[keep].all()), float((err / bound)[keep].max())
+    assert torch.equal(z[5].cpu()[keep], u.bfloat16()[keep])
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_slopes_of_large_tiles(act):
+    m = k = 4096
+    bits = torch.arange(65536, dtype=torch.int32).to(torch.int16)
+    z = bits.view(torch.bfloat16).repeat(m * k // 65536).view(m, k).cuda()
+    dz, w = torch.zeros(m, 64, device="cuda").bfloat16(), torch.zeros(k, 64, device="cuda").bfloat16()
+    dz[:, 0] = 1
+    w[:, 0] = 1
+    dx = torch.full((m, k), 7.0, device="cuda").bfloat16()
+    ws = torch.empty(max(16, B.cf_linear_bwd_data_workspace_size(m, k, 64, "bf16")), dtype=torch.uint8, device="cuda")
+    B.cf_linear_bwd_data(m, k, 64, "bf16", dz, w, None, z, act, 0.0, dx, ws)
+    rows = dx.view(-1, 65536).view(torch.int16)
+    assert torch.equal(rows, rows[:1].expand_as(rows))
+    got, u = dx.view(-1)[:65536].double().cpu(), bits.view(torch.bfloat16).double()
+    assert bool(torch.isnan(got[torch.isnan(u)]).all())
+    fin = torch.isfinite(u)
+    got, u = got[fin], u[fin]
+    if act == "gelu":
+        want = 0.5 * torch.erfc(-u / math.sqrt(2)) + u * torch.exp(-u * u / 2) / math.sqrt(2 * math.pi)
+    else:
+        s = torch.sigmoid(u)
+        want = s * (1 + u * torch.sigmoid(-u))
+    want = torch.where(u.abs() > 1e4, (u > 0).double(), want)
+    err, bound = (got - want).abs(), 2.0 ** -8 * want.abs() + 2.0 ** -16
+    assert bool((err <= bound).all()), float((err / bound).max())
