@@ -351,3 +351,68 @@ def test_slopes_of_large_tiles(act):
     want = torch.where(u.abs() > 1e4, (u > 0).double(), want)
     err, bound = (got - want).abs(), 2.0 ** -8 * want.abs() + 2.0 ** -16
     assert bool((err <= bound).all()), float((err / bound).max())
+
+
+# Outputs in both directions that take the tiles of 256, 128 and 64, whole and ragged; the
+# formulas in float64 on the GPU.
+LARGE = [(4096, 64, 4096, "bf16"), (4090, 72, 4104, "bf16"), (3901, 35, 4099, "bf16"), (4096, 128, 2048, "bf16"),
+         (4001, 130, 2101, "bf16"), (1536, 64, 1536, "bf16"), (2048, 96, 2048, "f32"), (4001, 70, 2051, "f32"),
+         (1024, 40, 1021, "f32")]
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("rows,terms,cols,dt", LARGE)
+def test_epilogues_of_all_tiles(rows, terms, cols, dt, act):
+    g = torch.Generator(device="cuda").manual_seed(rows + terms)
+
+    def real(shape, s=1.0, t=None):
+        return (s * torch.randn(shape, generator=g, device="cuda")).to(_t(t or dt))
+
+    x, w, b, r, zin = real((rows, terms)), real((terms, cols), terms ** -0.5), real((cols,), 1.0, "f32"), real((rows, cols)), real((rows, cols), 3.0)
+    s64, sabs = x.double() @ w.double(), x.double().abs() @ w.double().abs()
+    step = 2.0 ** -8 if dt == "bf16" else 2.0 ** -24
+
+    def check(got, ref, lim):
+        err, lim = (got.double() - ref).abs(), lim + step * ref.abs()
+        assert bool((err <= lim).all()), float((err / lim).max())
+
+    for res in (None, r):
+        y, z = torch.full((rows, cols), math.nan, device="cuda", dtype=_t(dt)), torch.full((rows, cols), math.nan, device="cuda", dtype=_t(dt))
+        B.cf_linear_fwd(rows, terms, cols, dt, x, w, b, act, ALPHA, res, y, z, _ws(B.cf_linear_fwd_workspace_size(rows, terms, cols, dt)))
+        z64 = s64 + b.double()
+        e = (terms + 8) * 2.0 ** -23 * (sabs + b.double().abs())
+        check(z, z64, e)
+        y64 = _curve(z64, act)[0] + (0.0 if res is None else res.double())
+        # (the large tiles' GELU: 2^-20 z^2 of itself more, at most where the step of bf16 is 2^-8)
+        table = 2.0 ** -14 * _curve(z64, act)[0].abs() if act == "gelu" and dt == "bf16" else 0.0
+        check(y, y64, 1.13 * e + 2.0 ** -21 * z64.abs() + 2.0 ** -23 * y64.abs() + table)
+        # the same numbers as a data gradient: dx = (x w^T ..) with w given as [cols][terms]
+        dx = torch.full((rows, cols), math.nan, device="cuda", dtype=_t(dt))
+        B.cf_linear_bwd_data(rows, cols, terms, dt, x, w.t().contiguous(), res, None if act == "none" else zin, act, ALPHA, dx,
+                             _ws(B.cf_linear_bwd_data_workspace_size(rows, cols, terms, dt)))
+        d64 = s64 + (0.0 if res is None else res.double())
+        e = (terms + 8) * 2.0 ** -23 * (sabs + (0.0 if res is None else res.double().abs()))
+        check(dx, d64 * _curve(zin.double(), act)[1], 1.13 * e + (2.0 ** -20 + (2.0 ** -15 if dt == "bf16" else 0.0)) * d64.abs())
+    if act == "none":
+        dw, db = torch.full((rows, cols), math.nan, device="cuda"), torch.full((cols,), math.nan, device="cuda")
+        xt = x.t().contiguous()
+        B.cf_linear_bwd_weight(terms, rows, cols, dt, xt, w, dw, db, _ws(B.cf_linear_bwd_weight_workspace_size(terms, rows, cols, dt)))
+        step = 2.0 ** -24
+        check(dw, s64, (terms + 8) * 2.0 ** -23 * sabs)
+        check(db, w.double().sum(0), (terms + 8) * 2.0 ** -23 * w.double().abs().sum(0))
+
+
+def test_other_stream_and_its_tensors():
+    """Calls on a stream of their own, behind the work that fills their inputs there."""
+    side = torch.cuda.Stream()
+    m, k, n = 1100, 264, 520
+    with torch.cuda.stream(side):
+        x, w = torch.zeros(m, k, device="cuda").bfloat16(), torch.zeros(k, n, device="cuda").bfloat16()
+        for _ in range(20):
+            x += 0.125
+            w += 0.0625
+        y = torch.empty(m, n, device="cuda").bfloat16()
+        B.cf_linear_fwd(m, k, n, "bf16", x, w, None, "none", 0.0, None, y, None,
+                        _ws(B.cf_linear_fwd_workspace_size(m, k, n, "bf16")))
+    side.synchronize()
+    assert torch.equal(y, torch.full_like(y, 2.5 * 1.25 * k))
