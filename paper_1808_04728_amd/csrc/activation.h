@@ -10,16 +10,16 @@ namespace cf {
 
 enum : int { ACT_NONE = 0, ACT_LRELU = 1, ACT_SILU = 2, ACT_GELU = 3 };
 
-// e^x to about an ulp, x clamped to where it neither over- nor underflows before infinity
-// and zero (a NaN counts as the lower bound: callers multiply by x itself).  x log2 e is
-// rounded to t; what that left out, r, comes back as a factor e^(r ln 2) = 1 + r ln 2.
+// e^x to about an ulp: infinite from 88.73 on, 0 far below (a NaN counts as -120: callers
+// multiply by x itself).  x log2 e is rounded to t; what that left out, r, comes back as a
+// factor e^(r ln 2) = 1 + r ln 2.  (A factor, not a sum of e and e r ln 2: where e is infinite
+// and r is below zero that has no value.  x is clamped so that r is finite.)
 __device__ __forceinline__ float fast_exp(float x) {
   constexpr float L = 1.44269504f, L_LO = 1.92596303e-8f;  // log2 e = L + L_LO
   x = fminf(fmaxf(x, -120.f), 120.f);
   const float t = x * L;
   const float r = __builtin_fmaf(x, L_LO, __builtin_fmaf(x, L, -t));
-  const float e = __builtin_amdgcn_exp2f(t);
-  return __builtin_fmaf(e, r * 0.693147181f, e);
+  return __builtin_amdgcn_exp2f(t) * __builtin_fmaf(r, 0.693147181f, 1.f);
 }
 
 __device__ __forceinline__ float sigmoid(float u) { return __builtin_amdgcn_rcpf(1.f + fast_exp(-u)); }
