@@ -108,13 +108,14 @@ __device__ __forceinline__ int row_count(const Walk &w, int s, int r, int ch) {
   return (int)max(0LL, (len - (r * w.c + ch) + w.width - 1) / w.width);
 }
 
-// mean and sum of squared distances of na and nb values joined
+// mean and sum of squared distances of na and nb values joined (d is multiplied by the weight
+// first: joined to no values it is the mean itself, whose square may be infinite)
 template <class T> __device__ __forceinline__ void join(T &mean, T &m2, T &na, T mb, T m2b, T nb) {
   const T n = na + nb;
   if (nb == (T)0) return;
   const T d = mb - mean, f = nb / n;
   mean += d * f;
-  m2 += m2b + d * d * (na * f);
+  m2 += m2b + d * (d * (na * f));
   na = n;
 }
 
@@ -173,7 +174,7 @@ __global__ __launch_bounds__(BT) void gn_stats_kernel(Walk w, const void *x_, fl
         for (int u = 0; u < kUnroll; ++u) q += (v[u][j] - mb) * (v[u][j] - mb);
         const float d = mb - mean[j];
         mean[j] += d * f;
-        m2[j] += q + d * d * g;
+        m2[j] += q + d * (d * g);
       }
     }
     u32x4_t raw[kUnroll - 1];
