@@ -673,6 +673,13 @@ def cf_muon_step(mats, t, hp, v, g, m, v16, ws, ws_bytes=None, stream=None):
 
 # ---- group normalisation ---------------------------------------------------------
 
+def _sizes32(*sizes):
+    """ValueError unless each fits the 32 bits of its C argument (ctypes would pass the low ones)."""
+    for s in sizes:
+        if not -0x80000000 <= s < 0x80000000:
+            raise ValueError(f"a size of {s}: past 32 bits")
+
+
 def _ws_bytes(ws, ws_bytes):
     if ws_bytes is None:
         return 0 if ws is None or isinstance(ws, int) else ws.numel() * ws.element_size()
@@ -680,23 +687,27 @@ def _ws_bytes(ws, ws_bytes):
 
 
 def cf_groupnorm_fwd_workspace_size(n, vox, c, groups, dtype) -> int:
+    _sizes32(n, c, groups)
     return int(lib().cf_groupnorm_fwd_workspace_size(n, vox, c, groups, dtype_code(dtype)))
 
 
 def cf_groupnorm_fwd(n, vox, c, groups, dtype, x, gamma, beta, eps, act, alpha, y, mean, rstd, ws=None, ws_bytes=None,
                      stream=None):
     """act: "none", "lrelu", "silu" or "gelu" (or a CF_ACT_ code)."""
+    _sizes32(n, c, groups)
     _check(lib().cf_groupnorm_fwd(n, vox, c, groups, dtype_code(dtype), _ptr(x), _ptr(gamma), _ptr(beta), float(eps),
                                   act_code(act), float(alpha), _ptr(y), _ptr(mean), _ptr(rstd), _ptr(ws),
                                   _ws_bytes(ws, ws_bytes), _stream(stream)))
 
 
 def cf_groupnorm_bwd_workspace_size(n, vox, c, groups, dtype) -> int:
+    _sizes32(n, c, groups)
     return int(lib().cf_groupnorm_bwd_workspace_size(n, vox, c, groups, dtype_code(dtype)))
 
 
 def cf_groupnorm_bwd(n, vox, c, groups, dtype, dy, x, gamma, beta, mean, rstd, act, alpha, dx, dgamma, dbeta, ws,
                      ws_bytes=None, stream=None):
+    _sizes32(n, c, groups)
     _check(lib().cf_groupnorm_bwd(n, vox, c, groups, dtype_code(dtype), _ptr(dy), _ptr(x), _ptr(gamma), _ptr(beta),
                                   _ptr(mean), _ptr(rstd), act_code(act), float(alpha), _ptr(dx), _ptr(dgamma),
                                   _ptr(dbeta), _ptr(ws), _ws_bytes(ws, ws_bytes), _stream(stream)))
@@ -705,28 +716,34 @@ def cf_groupnorm_bwd(n, vox, c, groups, dtype, dy, x, gamma, beta, mean, rstd, a
 # ---- matrix products with an epilogue ----------------------------------------------
 
 def cf_linear_fwd_workspace_size(m, k, n, dtype) -> int:
+    _sizes32(m, k, n)
     return int(lib().cf_linear_fwd_workspace_size(m, k, n, dtype_code(dtype)))
 
 
 def cf_linear_fwd(m, k, n, dtype, x, w, bias, act, alpha, residual, y, z=None, ws=None, ws_bytes=None, stream=None):
+    _sizes32(m, k, n)
     _check(lib().cf_linear_fwd(m, k, n, dtype_code(dtype), _ptr(x), _ptr(w), _ptr(bias), act_code(act), float(alpha),
                                _ptr(residual), _ptr(y), _ptr(z), _ptr(ws), _ws_bytes(ws, ws_bytes), _stream(stream)))
 
 
 def cf_linear_bwd_data_workspace_size(m, k, n, dtype) -> int:
+    _sizes32(m, k, n)
     return int(lib().cf_linear_bwd_data_workspace_size(m, k, n, dtype_code(dtype)))
 
 
 def cf_linear_bwd_data(m, k, n, dtype, dz, w, residual, z, act, alpha, dx, ws=None, ws_bytes=None, stream=None):
+    _sizes32(m, k, n)
     _check(lib().cf_linear_bwd_data(m, k, n, dtype_code(dtype), _ptr(dz), _ptr(w), _ptr(residual), _ptr(z), act_code(act),
                                     float(alpha), _ptr(dx), _ptr(ws), _ws_bytes(ws, ws_bytes), _stream(stream)))
 
 
 def cf_linear_bwd_weight_workspace_size(m, k, n, dtype) -> int:
+    _sizes32(m, k, n)
     return int(lib().cf_linear_bwd_weight_workspace_size(m, k, n, dtype_code(dtype)))
 
 
 def cf_linear_bwd_weight(m, k, n, dtype, x, dz, dw, db=None, ws=None, ws_bytes=None, stream=None):
+    _sizes32(m, k, n)
     _check(lib().cf_linear_bwd_weight(m, k, n, dtype_code(dtype), _ptr(x), _ptr(dz), _ptr(dw), _ptr(db), _ptr(ws),
                                       _ws_bytes(ws, ws_bytes), _stream(stream)))
 
