@@ -154,6 +154,7 @@ def make_adamw_tensors(tensors):
     all contiguous and on one device (ValueError).  The dicts' tensors have to live as long as
     the array is used."""
     out = (cf_adamw_tensor * max(len(tensors), 1))()
+    device = tensors[0]["p"].device if tensors else None
     for l, (a, d) in enumerate(zip(out, tensors)):
         p = d["p"]
         n = p.numel()
@@ -169,7 +170,7 @@ def make_adamw_tensors(tensors):
                 if name in ("p16", "m_scale", "v_scale"):
                     continue
                 raise ValueError(f"tensor {l}, {name}: missing")
-            if x.numel() != size or x.dtype not in types or x.device != p.device or not x.is_contiguous():
+            if x.numel() != size or x.dtype not in types or x.device != device or not x.is_contiguous():
                 raise ValueError(f"tensor {l}, {name}: {x.numel()} {x.dtype} on {x.device}, or not contiguous")
             setattr(a, name, x.data_ptr())
         a.count, a.weight_decay, a.g_dtype = n, float(d.get("weight_decay", 0.0)), dtype_code(d["g"].dtype)
