@@ -667,7 +667,8 @@ typedef enum cf_act { CF_ACT_NONE = 0, CF_ACT_LRELU = 1, CF_ACT_SILU = 2, CF_ACT
  * groups = 1 normalises whole samples, groups = c each channel.
  * x, y, dy, dx are in dtype; gamma, beta, mean, rstd, dgamma, dbeta fp32.
  * Statistics and sums are fp32 or wider, the variance from distances to
- * means.  The leaky ReLU's slope in the backward pass is that of the u that
+ * means; a group's sum of |x| and of squared distances, and backward rstd^2,
+ * have to be in fp32's range.  The leaky ReLU's slope in the backward pass is that of the u that
  * exact arithmetic on these inputs gives.  A NaN or an infinity stays in its sample's group (and,
  * backward, in its channels' gradients) as the formulas have it.
  * Sizes: n, vox >= 0, c >= 1 and a multiple of groups >= 1, vox < 2^31,

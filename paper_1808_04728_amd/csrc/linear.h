@@ -234,8 +234,10 @@ struct SlopeTable {
 };
 
 // The normal distribution function from -8 to 8 in steps of 1/256: value and difference, in
-// between a straight line, off by at most 2^-20 u^2 of itself (an output's rounding to bf16 is
-// 2^-8); below -8 it is 0.  GELU of 32768 x 1024 x 4096 by formula 295 us, from here 268.
+// between a straight line, off by an eighth of the step's square of its curvature |u| phi(u):
+// below 2^-21, and for u < 0 below 2^-19 (u^2 + 1) of itself (2^-13 of itself at -8, where it is
+// 6e-16, 2^-14.9 and less from -4 on; an output's rounding to bf16 is 2^-8); below -8 it is 0.
+// GELU of 32768 x 1024 x 4096 by formula 295 us, from here 268.
 struct PhiTable {
   static constexpr int N = 4096, BYTES = N * 8;
   static __device__ __forceinline__ void fill(unsigned char *t) {
